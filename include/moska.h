@@ -448,6 +448,137 @@ int moska_decode_step_fp8_host(const uint16_t* q_host, uint16_t* q_dev, const fl
                                const moska_shape* shape, void* ws, size_t ws_bytes, moska_stream stream,
                                moska_stream side_stream, moska_profiler* prof);
 
+/* ---- a paged private store ------------------------------------------------------------------------
+ * The private contexts of Section III-A in a pool of pages: a request's tokens live in the pages that
+ * its row of the page table names, so a context grows a token at a time without moving.  Two storage
+ * formats (n_pages, page_size and the table are the caller's; a page holds all KV heads):
+ *
+ *   MOSKA_KV_BF16  k_pages, v_pages bf16 [n_pages][page_size][Hkv][D]   (16-byte aligned)
+ *   MOSKA_KV_FP4   k_pages uint8 [n_pages][Hkv][page_size / 16][18 D]   (16-byte aligned), v_pages
+ *                  not read.  Keys and values as E2M1 codes (the 4-bit type of the tensor cores:
+ *                  0, .5, 1, 1.5, 2, 3, 4, 6 and their negatives) with one f16 scale per (token, KV
+ *                  head, 32 dimensions): value = scale * e2m1(code), 4.5 bits an element.
+ *
+ * A block of 16 tokens of one KV head in the 4-bit format is 18 D bytes; token t of the block
+ * (0..15), dimension d, an even dimension in the low half of its byte and d + 1 in the high half:
+ *   keys          t (D/2) + ((d % 32) / 8) (D/8) + (d / 32) 4 + (d % 8) / 2
+ *   values        8 D + (t/2) D + (x ^ s) (D/8) + (t % 2) (D/16) + (d % (D/8)) / 2,  x = d / (D/8),
+ *                 s = 2 ((t/2) % 4) for D = 128, 4 ((t/4) % 2) for D = 64
+ *   key scales    16 D + 2 (t (D/32) + d / 32)          (bytes; little-endian f16)
+ *   value scales  17 D + 2 ((d / 32) 16 + t)
+ * which is the order the attention kernel's lanes read: whole 16-byte (8-byte at D = 64) pieces,
+ * eight different bank groups a quarter warp, without a shuffle.
+ *
+ * Context token t of request r is row t % page_size of page page_table[r][t / page_size].  Entries
+ * behind the last page that a context reaches are not read.  A page index outside [0, n_pages), a
+ * context longer than max_pages pages or a negative length raise MOSKA_ERR_INVALID_ARG in the device
+ * status word: attention then reads page 0 (the pages that the row has, an empty context), appended
+ * and gathered rows are left out, and the results of that call are not valid.  Two requests may share pages that only one
+ * call at a time writes.
+ */
+enum { MOSKA_KV_BF16 = 0, MOSKA_KV_FP4 = 1 };
+
+typedef struct moska_paged_kv {
+    int32_t format;            /* MOSKA_KV_BF16 or MOSKA_KV_FP4                                    */
+    int32_t page_size;         /* tokens per page: a power of two, 16..32768                       */
+    int32_t n_pages;           /* pages in the pool, >= 1                                          */
+    int32_t max_pages;         /* entries in a row of the page table, >= 1                         */
+    void* k_pages;             /* keys, or the 4-bit pool (keys and values)                        */
+    void* v_pages;             /* values; MOSKA_KV_FP4: not read, may be NULL                      */
+    const int32_t* page_table; /* int32 [B / q_len, or n_requests][max_pages]                      */
+    const int32_t* kv_len;     /* int32 [same]: context tokens, those that an append call of this
+                                  step writes included; 0 = no context                             */
+} moska_paged_kv;
+
+/* Bytes of one pool tensor: of k_pages and of v_pages each (bf16), or of the one 4-bit pool. 0 if a
+ * field is out of range.  Host only, pure. */
+size_t moska_paged_pool_bytes(int32_t format, int32_t n_pages, int32_t page_size, int32_t Hkv, int32_t D);
+
+/* A reasonable n_unique_splits for the 4-bit store (for bf16 pages: moska_default_unique_splits). */
+int moska_default_unique_splits_fp4(int32_t B, int32_t Hkv, int32_t max_len);
+
+/*
+ * Appends new tokens to a paged store, with the position rotation applied on the way.  For every new
+ * row: its key is rotated and written, its value is written, its queries are rotated into q_out.
+ *   q, k, v     bf16, row i at q + i q_stride ([Hq][D] dense inside a row), k + i k_stride, v + i
+ *               v_stride ([Hkv][D]); strides in elements, multiples of 8, >= the row; pointers
+ *               16-byte aligned: the three may be columns of one projection's output.  q and q_out
+ *               may both be NULL (keys and values only).
+ *   positions   int32 [B], the rotation's position of row i, in [0, n_positions); a row outside is left
+ *               out and raises MOSKA_ERR_INVALID_ARG in the device status word
+ *   cos_sin     float [n_positions][rot_dim]: cos of the rot_dim / 2 angles, then their sin (16-byte
+ *               aligned)
+ *   rot_dim     leading dimensions that are rotated: a multiple of 16 up to D; 0 = no rotation
+ *               (positions and cos_sin are not read, the queries are copied)
+ *   interleaved 0: dimension p is paired with p + rot_dim / 2; 1: 2p with 2p + 1
+ *   row_start   NULL: shape->B rows, shape->q_len (0 or 1 = one) for each of n_requests = B / q_len
+ *               requests, in order.  Else int32 [n_requests + 1], ascending: request r has rows
+ *               row_start[r] .. row_start[r+1] - 1; rows from row_start[n_requests] to B are padding.
+ *   q_out       bf16 [B][Hq][D] (16-byte aligned), not overlapping q
+ * With n_r rows, row i of request r becomes context token kv_len[r] - n_r + i: kv_len counts the
+ * tokens after the call.  Where that is negative the row is padding.  For padding rows nothing is
+ * written, q_out included.  The rotation is (a, b) -> (a cos - b sin, b cos + a sin) in fp32, each
+ * product and sum rounded, the result rounded once to bf16, or to 4 bits: scale = f16(max|x| / 6) (at
+ * most 10912), code = the E2M1 value nearest to x / scale, ties to the even code.  A NaN or an
+ * infinity makes its 32 dimensions NaN.  Rows of one call must be different tokens; nothing outside
+ * them is changed.  shape: B, Hq, Hkv, D and q_len are read.
+ */
+int moska_kv_append_paged(const uint16_t* q, int64_t q_stride, const uint16_t* k, int64_t k_stride,
+                          const uint16_t* v, int64_t v_stride, const int32_t* positions,
+                          const float* cos_sin, int32_t n_positions, int32_t rot_dim,
+                          int32_t interleaved, const int32_t* row_start, int32_t n_requests,
+                          uint16_t* q_out, const moska_paged_kv* kv, const moska_shape* shape,
+                          moska_stream stream);
+
+/*
+ * Reads the last rows of paged contexts back as bf16 (for the 4-bit format: the values that the codes
+ * stand for, rounded to bf16), for instance to make a private context a chunk of the shared store.
+ * Rows and requests as in moska_kv_append_paged: row i of request r is context token kv_len[r] - n_r
+ * + i (kv->kv_len may be another array than the store's own lengths, to read an earlier range).
+ * Padding rows are left as they were.
+ *   k_out, v_out  bf16 [B][Hkv][D]   (16-byte aligned)
+ */
+int moska_kv_gather_paged(const int32_t* row_start, int32_t n_requests, uint16_t* k_out, uint16_t* v_out,
+                          const moska_paged_kv* kv, const moska_shape* shape, moska_stream stream);
+
+/*
+ * Unique KV Attention over a paged private store: the same partial results and slots as
+ * moska_unique_attn.  4-bit format: Q (scaled by a power of two per row) and the codes multiply
+ * exactly in f16 with fp32 accumulation, scales and softmax are fp32, values are widened to f16
+ * (code * scale) and P is rounded to f16.  With q_len > 1: q_len * G <= 16, and D = 128 for bf16.
+ *   softmax_scale  finite, > 0
+ */
+int moska_unique_attn_paged(const uint16_t* q, const moska_paged_kv* kv, float* o_part, float* lse_part,
+                            float softmax_scale, const moska_shape* shape, moska_stream stream);
+
+/*
+ * Attention of requests that have a paged private context and no shared store: the final rows,
+ * without a separate merge.
+ *   out      bf16  [B][Hq][D]   (16-byte aligned); a row without context is 0
+ *   lse_out  float [B][Hq]      may be NULL; -inf for such a row
+ *   ws       moska_paged_attn_workspace_bytes(shape) bytes, 256-byte aligned; calls that share it
+ *            must not overlap.  Not read or written (may be NULL) with n_unique_splits = 1.
+ * shape: B, Hq, Hkv, D, q_len and n_unique_splits are read.
+ */
+int moska_paged_attn(const uint16_t* q, const moska_paged_kv* kv, uint16_t* out, float* lse_out,
+                     float softmax_scale, const moska_shape* shape, void* ws, size_t ws_bytes,
+                     moska_stream stream);
+size_t moska_paged_attn_workspace_bytes(const moska_shape* shape);
+
+/*
+ * moska_decode_step with a paged private store.  The shared store is bf16 (k_shared, v_shared bf16,
+ * both scales NULL) or FP8 (E4M3 codes with k_scale_shared and v_scale_shared, as for
+ * moska_shared_attn_fp8, D = 128).  Same schedule, buffers, outputs and error behaviour (summaries
+ * NULL selects dense mode).
+ */
+int moska_decode_step_paged(const uint16_t* q, const float* summaries, const void* k_shared,
+                            const void* v_shared, const float* k_scale_shared, const float* v_scale_shared,
+                            const moska_paged_kv* kv, int32_t* topk_idx, int32_t* seg_offsets,
+                            int32_t* seg_entries, float* o_part, float* lse_part, uint16_t* out,
+                            float* lse_out, float softmax_scale, const moska_shape* shape, void* ws,
+                            size_t ws_bytes, moska_stream stream, moska_stream side_stream,
+                            moska_profiler* prof);
+
 #ifdef __cplusplus
 }
 #endif

@@ -30,6 +30,14 @@ class MoskaShape(ctypes.Structure):
                [("unique_tokens", ctypes.c_int64), ("q_len", ctypes.c_int32)]
 
 
+class MoskaPagedKv(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("format", "page_size", "n_pages", "max_pages")] + \
+               [(n, ctypes.c_void_p) for n in ("k_pages", "v_pages", "page_table", "kv_len")]
+
+
+KV_BF16, KV_FP4 = 0, 1
+
+
 class MoskaError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -41,6 +49,7 @@ ERR_CORRUPT = -6
 
 _vp, _sz, _f, _i = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_float, ctypes.c_int
 _sp = ctypes.POINTER(MoskaShape)
+_kvp, _i64 = ctypes.POINTER(MoskaPagedKv), ctypes.c_int64
 
 EXPORTS = {
     "moska_version": (_i, []),
@@ -68,6 +77,15 @@ EXPORTS = {
     "moska_decode_step_fp8": (_i, [_vp] * 19 + [_f, _sp, _vp, _sz, _vp, _vp, _vp]),
     "moska_decode_step_host": (_i, [_vp] * 16 + [_f, _sp, _vp, _sz, _vp, _vp, _vp]),
     "moska_decode_step_fp8_host": (_i, [_vp] * 20 + [_f, _sp, _vp, _sz, _vp, _vp, _vp]),
+    "moska_paged_pool_bytes": (_sz, [ctypes.c_int32] * 5),
+    "moska_default_unique_splits_fp4": (_i, [ctypes.c_int32] * 3),
+    "moska_kv_append_paged": (_i, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp] + [ctypes.c_int32] * 3 +
+                              [_vp, ctypes.c_int32, _vp, _kvp, _sp, _vp]),
+    "moska_kv_gather_paged": (_i, [_vp, ctypes.c_int32, _vp, _vp, _kvp, _sp, _vp]),
+    "moska_unique_attn_paged": (_i, [_vp, _kvp, _vp, _vp, _f, _sp, _vp]),
+    "moska_paged_attn": (_i, [_vp, _kvp, _vp, _vp, _f, _sp, _vp, _sz, _vp]),
+    "moska_paged_attn_workspace_bytes": (_sz, [_sp]),
+    "moska_decode_step_paged": (_i, [_vp] * 6 + [_kvp] + [_vp] * 7 + [_f, _sp, _vp, _sz, _vp, _vp, _vp]),
     "moska_profiler_create": (_i, [ctypes.POINTER(_vp), ctypes.c_int32]),
     "moska_profiler_destroy": (None, [_vp]),
     "moska_profiler_select": (_i, [_vp, ctypes.c_uint32]),
@@ -344,6 +362,60 @@ def bind_decode_step_fp8_host(q_host, q_dev, summaries, k8_shared, v8_shared, k_
             raise MoskaError(status, "moska_decode_step_fp8_host")
 
     return call
+
+
+def paged_kv(fmt, page_size, n_pages, max_pages, k_pages, v_pages, page_table, kv_len) -> MoskaPagedKv:
+    return MoskaPagedKv(fmt, page_size, n_pages, max_pages, _ptr(k_pages), _ptr(v_pages), _ptr(page_table),
+                        _ptr(kv_len))
+
+
+def paged_pool_bytes(fmt: int, n_pages: int, page_size: int, Hkv: int, D: int) -> int:
+    return _lib.moska_paged_pool_bytes(fmt, n_pages, page_size, Hkv, D)
+
+
+def default_unique_splits_fp4(B: int, Hkv: int, max_len: int) -> int:
+    return _lib.moska_default_unique_splits_fp4(B, Hkv, max_len)
+
+
+def kv_append_paged(q, q_stride, k, k_stride, v, v_stride, positions, cos_sin, n_positions, rot_dim, interleaved,
+                    row_start, n_requests, q_out, kv, s, stream=None) -> None:
+    """q, k and v are raw addresses (None for no q) with their row strides in elements: rows may be
+    columns of a wider tensor."""
+    _check(_lib.moska_kv_append_paged(q, q_stride, k, k_stride, v, v_stride, _ptr(positions), _ptr(cos_sin),
+                                      n_positions, rot_dim, interleaved, _ptr(row_start), n_requests,
+                                      _ptr(q_out), ctypes.byref(kv), ctypes.byref(s), _stream(stream)),
+           "moska_kv_append_paged")
+
+
+def kv_gather_paged(row_start, n_requests, k_out, v_out, kv, s, stream=None) -> None:
+    _check(_lib.moska_kv_gather_paged(_ptr(row_start), n_requests, _ptr(k_out), _ptr(v_out), ctypes.byref(kv),
+                                      ctypes.byref(s), _stream(stream)), "moska_kv_gather_paged")
+
+
+def unique_attn_paged(q, kv, o_part, lse_part, softmax_scale, s, stream=None) -> None:
+    _check(_lib.moska_unique_attn_paged(_ptr(q), ctypes.byref(kv), _ptr(o_part), _ptr(lse_part), softmax_scale,
+                                        ctypes.byref(s), _stream(stream)), "moska_unique_attn_paged")
+
+
+def paged_attn(q, kv, out, lse_out, softmax_scale, s, ws, stream=None) -> None:
+    ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(_lib.moska_paged_attn(_ptr(q), ctypes.byref(kv), _ptr(out), _ptr(lse_out), softmax_scale, ctypes.byref(s),
+                                 _ptr(ws), ws_bytes, _stream(stream)), "moska_paged_attn")
+
+
+def paged_attn_workspace_bytes(s: MoskaShape) -> int:
+    return _lib.moska_paged_attn_workspace_bytes(ctypes.byref(s))
+
+
+def decode_step_paged(q, summaries, k_shared, v_shared, k_scale_shared, v_scale_shared, kv, topk_idx, seg_offsets,
+                      seg_entries, o_part, lse_part, out, lse_out, softmax_scale, s, ws, stream=None,
+                      side_stream=None, prof=None) -> None:
+    ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(_lib.moska_decode_step_paged(
+        _ptr(q), _ptr(summaries), _ptr(k_shared), _ptr(v_shared), _ptr(k_scale_shared), _ptr(v_scale_shared),
+        ctypes.byref(kv), _ptr(topk_idx), _ptr(seg_offsets), _ptr(seg_entries), _ptr(o_part), _ptr(lse_part),
+        _ptr(out), _ptr(lse_out), softmax_scale, ctypes.byref(s), _ptr(ws), ws_bytes, _stream(stream),
+        None if side_stream is None else _stream(side_stream), prof), "moska_decode_step_paged")
 
 
 STAGES = ("route", "group", "shared", "unique", "merge")

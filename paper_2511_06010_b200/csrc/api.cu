@@ -5,7 +5,7 @@
 
 #include <nvtx3/nvToolsExt.h>
 
-#include "common.cuh"
+#include "paged.cuh"
 
 namespace moska {
 
@@ -503,12 +503,21 @@ struct UniqueKv {
     const float* k_scale = nullptr;
     const float* v_scale = nullptr;
     bool fp8 = false;
+    const moska_paged_kv* paged = nullptr;  // pages in either format; kv_start and kv_len are not used
+
+    double token_bytes(int D) const  // one KV head's bytes of a token
+    {
+        if (paged != nullptr && paged->format == MOSKA_KV_FP4) return fp4_block_bytes(D) / (double)kBlockTokens;
+        return fp8 ? 2.0 * D + 8.0 : 4.0 * D;
+    }
 };
 
 int unique_impl(const uint16_t* q, const UniqueKv& kv, const int64_t* kv_start, const int32_t* kv_len,
                 float* o_part, float* lse_part, float softmax_scale, const moska_shape* shape,
                 cudaStream_t st)
 {
+    if (kv.paged != nullptr)
+        return moska_unique_attn_paged(q, kv.paged, o_part, lse_part, softmax_scale, shape, st);
     if (kv.fp8)
         return moska_unique_attn_fp8(q, kv.k8, kv.v8, kv.k_scale, kv.v_scale, kv_start, kv_len, o_part,
                                      lse_part, softmax_scale, shape, st);
@@ -656,8 +665,8 @@ int decode_step_impl(const uint16_t* q, const float* summaries, const uint16_t* 
         // to start beside it (the routing chain in front of it takes a few hundred microseconds
         // under contention); for a short unique attention the tensor-core items run after it, on
         // all SMs.
-        const double unique_ms = (double)shape->unique_tokens * shape->Hkv *
-                                 (kv.fp8 ? 2.0 * shape->D + 8.0 : 4.0 * shape->D) / 7.0e9;
+        const double unique_ms =
+            (double)shape->unique_tokens * shape->Hkv * kv.token_bytes(shape->D) / 7.0e9;
         const bool beside = tc && (dense || unique_ms >= MOSKA_BESIDE_MS);
         if (tc && beside) MOSKA_TRY(shared_tc(dense, tc_sm_share(shape, dense, unique_ms), side));
         // the streaming tiles (every tile of a shape the tensor-core kernel does not serve, else the
@@ -915,6 +924,234 @@ int moska_decode_step_fp8_host(const uint16_t* q_host, uint16_t* q_dev, const fl
                                shape, ws, ws_bytes, stream, side_stream, prof, out_host, q_host));
     MOSKA_CUDA_TRY(cudaStreamSynchronize((cudaStream_t)stream));
     return MOSKA_OK;
+}
+
+namespace {
+// The shape fields that calls without a shared store rely on.
+int check_heads(const moska_shape* s)
+{
+    if (s == nullptr) return fail(MOSKA_ERR_INVALID_ARG, "shape is NULL");
+    if (s->B < 0 || s->Hq <= 0 || s->Hkv <= 0) return fail(MOSKA_ERR_INVALID_ARG, "B >= 0 and Hq, Hkv > 0 required");
+    if (s->Hq % s->Hkv != 0)
+        return fail(MOSKA_ERR_INVALID_ARG, "Hq = %d is not a multiple of Hkv = %d", s->Hq, s->Hkv);
+    if (s->Hq / s->Hkv > 8) return fail(MOSKA_ERR_UNSUPPORTED, "G = Hq / Hkv = %d > 8", s->Hq / s->Hkv);
+    if (s->D != 64 && s->D != 128) return fail(MOSKA_ERR_UNSUPPORTED, "D = %d, only 64 and 128 are built", s->D);
+    if (s->q_len < 0 || (s->q_len > 1 && s->B % s->q_len != 0))
+        return fail(MOSKA_ERR_INVALID_ARG, "q_len = %d must be >= 0 and divide B = %d", s->q_len, s->B);
+    return MOSKA_OK;
+}
+
+// Validates a paged store and turns it into what the kernels take.
+int paged_view(const moska_paged_kv* kv, PagedView* out)
+{
+    if (kv == nullptr) return fail(MOSKA_ERR_INVALID_ARG, "kv is NULL");
+    if (kv->format != MOSKA_KV_BF16 && kv->format != MOSKA_KV_FP4)
+        return fail(MOSKA_ERR_INVALID_ARG, "kv->format = %d", kv->format);
+    if (kv->page_size < kBlockTokens || kv->page_size > 32768 || (kv->page_size & (kv->page_size - 1)) != 0)
+        return fail(MOSKA_ERR_INVALID_ARG, "page_size = %d is not a power of two in 16..32768", kv->page_size);
+    if (kv->n_pages < 1 || kv->max_pages < 1)
+        return fail(MOSKA_ERR_INVALID_ARG, "n_pages and max_pages must be >= 1");
+    if ((long long)kv->max_pages * kv->page_size > (1LL << 30))
+        return fail(MOSKA_ERR_UNSUPPORTED, "a page-table row of more than 2^30 tokens");
+    REQUIRE_PTR(kv->k_pages, 16);
+    if (kv->format == MOSKA_KV_BF16) REQUIRE_PTR(kv->v_pages, 16);
+    REQUIRE_PTR(kv->page_table, 4);
+    REQUIRE_PTR(kv->kv_len, 4);
+    out->k = static_cast<uint8_t*>(kv->k_pages);
+    out->v = static_cast<uint8_t*>(kv->v_pages);
+    out->page_table = kv->page_table;
+    out->kv_len = kv->kv_len;
+    out->n_pages = kv->n_pages;
+    out->max_pages = kv->max_pages;
+    out->page_shift = 0;
+    while ((1 << out->page_shift) < kv->page_size) ++out->page_shift;
+    return MOSKA_OK;
+}
+
+// Which rows belong to which request (append and gather).
+int check_rows(const int32_t* row_start, int32_t n_requests, const moska_shape* s)
+{
+    if (n_requests < 1 && s->B > 0) return fail(MOSKA_ERR_INVALID_ARG, "n_requests = %d", n_requests);
+    if (row_start != nullptr) {
+        if (!aligned(row_start, 4)) return fail(MOSKA_ERR_INVALID_ARG, "row_start is not 4-byte aligned");
+        return MOSKA_OK;
+    }
+    const long long q_len = s->q_len > 1 ? s->q_len : 1;
+    if (s->B > 0 && n_requests * q_len != s->B)
+        return fail(MOSKA_ERR_INVALID_ARG, "without row_start, n_requests * q_len = %lld must be B = %d",
+                    n_requests * q_len, s->B);
+    return MOSKA_OK;
+}
+
+int check_paged_attn(const moska_paged_kv* kv, float softmax_scale, const moska_shape* s)
+{
+    const int G = s->Hq / s->Hkv;
+    if (s->q_len > 1 && (s->q_len * G > 16 || (kv->format == MOSKA_KV_BF16 && s->D != 128)))
+        return fail(MOSKA_ERR_UNSUPPORTED,
+                    "q_len = %d needs q_len * G <= 16, and D = 128 for bf16 pages; pass the tokens as batch rows "
+                    "with q_len = 1, a table row and a length of their own instead", s->q_len);
+    if (!(softmax_scale > 0.f) || !std::isfinite(softmax_scale))
+        return fail(MOSKA_ERR_INVALID_ARG, "softmax_scale must be finite and > 0");
+    if (s->n_unique_splits < 1) return fail(MOSKA_ERR_INVALID_ARG, "n_unique_splits must be >= 1");
+    return MOSKA_OK;
+}
+}  // namespace
+
+size_t moska_paged_pool_bytes(int32_t format, int32_t n_pages, int32_t page_size, int32_t Hkv, int32_t D)
+{
+    if (n_pages < 1 || Hkv < 1 || (D != 64 && D != 128) || page_size < kBlockTokens || page_size > 32768 ||
+        (page_size & (page_size - 1)) != 0)
+        return 0;
+    const size_t tokens = (size_t)n_pages * page_size;
+    if (format == MOSKA_KV_BF16) return tokens * Hkv * D * sizeof(uint16_t);
+    if (format == MOSKA_KV_FP4) return tokens / kBlockTokens * Hkv * fp4_block_bytes(D);
+    return 0;
+}
+
+int moska_default_unique_splits_fp4(int32_t B, int32_t Hkv, int32_t max_len)
+{
+    return moska_default_unique_splits_fp8(B, Hkv, max_len);
+}
+
+int moska_kv_append_paged(const uint16_t* q, int64_t q_stride, const uint16_t* k, int64_t k_stride,
+                          const uint16_t* v, int64_t v_stride, const int32_t* positions,
+                          const float* cos_sin, int32_t n_positions, int32_t rot_dim,
+                          int32_t interleaved, const int32_t* row_start, int32_t n_requests,
+                          uint16_t* q_out, const moska_paged_kv* kv, const moska_shape* shape,
+                          moska_stream stream)
+{
+    MOSKA_API_RANGE();
+    MOSKA_TRY(check_heads(shape));
+    PagedView view{};
+    MOSKA_TRY(paged_view(kv, &view));
+    MOSKA_TRY(check_rows(row_start, n_requests, shape));
+    if ((q == nullptr) != (q_out == nullptr))
+        return fail(MOSKA_ERR_INVALID_ARG, "q and q_out are given together or not at all");
+    if (q != nullptr) {
+        REQUIRE_PTR(q, 16);
+        REQUIRE_PTR(q_out, 16);
+        if (q_stride % 8 != 0 || q_stride < (int64_t)shape->Hq * shape->D)
+            return fail(MOSKA_ERR_INVALID_ARG, "q_stride = %lld must be a multiple of 8 and hold a row", (long long)q_stride);
+    }
+    REQUIRE_PTR(k, 16);
+    REQUIRE_PTR(v, 16);
+    const int64_t row = (int64_t)shape->Hkv * shape->D;
+    if (k_stride % 8 != 0 || k_stride < row || v_stride % 8 != 0 || v_stride < row)
+        return fail(MOSKA_ERR_INVALID_ARG, "k_stride = %lld, v_stride = %lld must be multiples of 8 and hold a row",
+                    (long long)k_stride, (long long)v_stride);
+    if (rot_dim < 0 || rot_dim > shape->D || rot_dim % 16 != 0)
+        return fail(MOSKA_ERR_INVALID_ARG, "rot_dim = %d is not a multiple of 16 in 0..D", rot_dim);
+    if (rot_dim > 0) {
+        REQUIRE_PTR(positions, 4);
+        REQUIRE_PTR(cos_sin, 16);
+        if (n_positions < 1) return fail(MOSKA_ERR_INVALID_ARG, "n_positions = %d", n_positions);
+    }
+    MOSKA_TRY(check_device());
+    MOSKA_TRY(status_word(&view.status));
+    return launch_append_paged(q, q_stride, k, k_stride, v, v_stride, positions, cos_sin, n_positions, rot_dim,
+                               interleaved, row_start, n_requests, q_out, view, kv->format == MOSKA_KV_FP4, shape,
+                               (cudaStream_t)stream);
+}
+
+int moska_kv_gather_paged(const int32_t* row_start, int32_t n_requests, uint16_t* k_out, uint16_t* v_out,
+                          const moska_paged_kv* kv, const moska_shape* shape, moska_stream stream)
+{
+    MOSKA_API_RANGE();
+    MOSKA_TRY(check_heads(shape));
+    PagedView view{};
+    MOSKA_TRY(paged_view(kv, &view));
+    MOSKA_TRY(check_rows(row_start, n_requests, shape));
+    REQUIRE_PTR(k_out, 16);
+    REQUIRE_PTR(v_out, 16);
+    MOSKA_TRY(check_device());
+    MOSKA_TRY(status_word(&view.status));
+    return launch_gather_paged(row_start, n_requests, k_out, v_out, view, kv->format == MOSKA_KV_FP4, shape,
+                               (cudaStream_t)stream);
+}
+
+int moska_unique_attn_paged(const uint16_t* q, const moska_paged_kv* kv, float* o_part, float* lse_part,
+                            float softmax_scale, const moska_shape* shape, moska_stream stream)
+{
+    MOSKA_API_RANGE();
+    MOSKA_TRY(check_shape(shape, false));
+    PagedView view{};
+    MOSKA_TRY(paged_view(kv, &view));
+    MOSKA_TRY(check_paged_attn(kv, softmax_scale, shape));
+    REQUIRE_PTR(q, 16);
+    REQUIRE_PTR(o_part, 16);
+    REQUIRE_PTR(lse_part, 4);
+    MOSKA_TRY(check_device());
+    MOSKA_TRY(status_word(&view.status));
+    const int n_slots = shape->shared_slots + shape->n_unique_splits;
+    return (kv->format == MOSKA_KV_FP4 ? launch_paged_fp4 : launch_paged_bf16)(
+        q, view, o_part, lse_part, shape->shared_slots, n_slots, nullptr, nullptr, softmax_scale, shape,
+        (cudaStream_t)stream);
+}
+
+size_t moska_paged_attn_workspace_bytes(const moska_shape* shape)
+{
+    if (check_heads(shape) != MOSKA_OK || shape->n_unique_splits < 2) return 0;
+    const size_t slots = (size_t)shape->B * shape->Hq * shape->n_unique_splits;
+    return round_up(slots * shape->D * sizeof(float), 256) + round_up(slots * sizeof(float), 256);
+}
+
+int moska_paged_attn(const uint16_t* q, const moska_paged_kv* kv, uint16_t* out, float* lse_out,
+                     float softmax_scale, const moska_shape* shape, void* ws, size_t ws_bytes,
+                     moska_stream stream)
+{
+    MOSKA_API_RANGE();
+    MOSKA_TRY(check_heads(shape));
+    PagedView view{};
+    MOSKA_TRY(paged_view(kv, &view));
+    MOSKA_TRY(check_paged_attn(kv, softmax_scale, shape));
+    REQUIRE_PTR(q, 16);
+    REQUIRE_PTR(out, 16);
+    if (lse_out != nullptr && !aligned(lse_out, 4)) return fail(MOSKA_ERR_INVALID_ARG, "lse_out is not 4-byte aligned");
+    const size_t need = moska_paged_attn_workspace_bytes(shape);
+    if (need > 0 && (ws == nullptr || !aligned(ws, 256) || ws_bytes < need))
+        return fail(MOSKA_ERR_WORKSPACE, "workspace missing, misaligned or smaller than %zu bytes", need);
+    MOSKA_TRY(check_device());
+    MOSKA_TRY(status_word(&view.status));
+    cudaStream_t st = (cudaStream_t)stream;
+    const auto attend = kv->format == MOSKA_KV_FP4 ? launch_paged_fp4 : launch_paged_bf16;
+    if (shape->n_unique_splits == 1)
+        return attend(q, view, nullptr, nullptr, 0, 1, out, lse_out, softmax_scale, shape, st);
+    float* o_part = static_cast<float*>(ws);
+    const size_t o_bytes = (size_t)shape->B * shape->Hq * shape->n_unique_splits * shape->D * sizeof(float);
+    float* lse_part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + round_up(o_bytes, 256));
+    MOSKA_TRY(attend(q, view, o_part, lse_part, 0, shape->n_unique_splits, nullptr, nullptr, softmax_scale, shape, st));
+    moska_shape slots = *shape;
+    slots.shared_slots = 0;
+    return launch_merge(o_part, lse_part, out, nullptr, lse_out, &slots, st);
+}
+
+int moska_decode_step_paged(const uint16_t* q, const float* summaries, const void* k_shared,
+                            const void* v_shared, const float* k_scale_shared, const float* v_scale_shared,
+                            const moska_paged_kv* kv, int32_t* topk_idx, int32_t* seg_offsets,
+                            int32_t* seg_entries, float* o_part, float* lse_part, uint16_t* out,
+                            float* lse_out, float softmax_scale, const moska_shape* shape, void* ws,
+                            size_t ws_bytes, moska_stream stream, moska_stream side_stream,
+                            moska_profiler* prof)
+{
+    MOSKA_API_RANGE();
+    MOSKA_TRY(check_shape(shape, summaries != nullptr));
+    PagedView view{};
+    MOSKA_TRY(paged_view(kv, &view));
+    MOSKA_TRY(check_paged_attn(kv, softmax_scale, shape));
+    if ((k_scale_shared == nullptr) != (v_scale_shared == nullptr))
+        return fail(MOSKA_ERR_INVALID_ARG, "k_scale_shared and v_scale_shared are given together or not at all");
+    UniqueKv unique;
+    unique.paged = kv;
+    SharedF8 f8;
+    f8.k8 = static_cast<const uint8_t*>(k_shared);
+    f8.v8 = static_cast<const uint8_t*>(v_shared);
+    f8.k_scale = k_scale_shared;
+    f8.v_scale = v_scale_shared;
+    const bool fp8 = k_scale_shared != nullptr;
+    return decode_step_impl(q, summaries, fp8 ? nullptr : static_cast<const uint16_t*>(k_shared),
+                            fp8 ? nullptr : static_cast<const uint16_t*>(v_shared), fp8 ? &f8 : nullptr, unique,
+                            nullptr, nullptr, topk_idx, seg_offsets, seg_entries, o_part, lse_part, out, lse_out,
+                            softmax_scale, shape, ws, ws_bytes, stream, side_stream, prof);
 }
 
 }  // extern "C"

@@ -154,4 +154,19 @@ int launch_merge_rows(const float* o_part, const float* lse_part, uint16_t* out,
                       float* lse_out, const moska_shape* s, long long row0, long long rows,
                       cudaStream_t st);
 
+// paged private store (paged.cuh)
+struct PagedView;
+int launch_append_paged(const uint16_t* q, int64_t q_stride, const uint16_t* k, int64_t k_stride, const uint16_t* v,
+                        int64_t v_stride, const int32_t* positions, const float* cos_sin, int n_positions,
+                        int rot_dim, int interleaved, const int32_t* row_start, int n_requests, uint16_t* q_out,
+                        const PagedView& kv, bool fp4, const moska_shape* s, cudaStream_t st);
+int launch_gather_paged(const int32_t* row_start, int n_requests, uint16_t* k_out, uint16_t* v_out,
+                        const PagedView& kv, bool fp4, const moska_shape* s, cudaStream_t st);
+// out == nullptr: partial slots slot0 .. slot0 + n_unique_splits of n_slots; else the final rows, which
+// needs n_unique_splits = 1
+int launch_paged_bf16(const uint16_t* q, const PagedView& kv, float* o_part, float* lse_part, int slot0, int n_slots,
+                      uint16_t* out, float* lse_out, float scale, const moska_shape* s, cudaStream_t st);
+int launch_paged_fp4(const uint16_t* q, const PagedView& kv, float* o_part, float* lse_part, int slot0, int n_slots,
+                     uint16_t* out, float* lse_out, float scale, const moska_shape* s, cudaStream_t st);
+
 }  // namespace moska

@@ -7,6 +7,14 @@
 namespace moska {
 namespace {
 
+// Larger of two, NaN if either is (a partial result over NaN scores makes its row NaN).
+__device__ __forceinline__ float max_or_nan(float a, float b)
+{
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+
 // One warp per query row.  Lane i owns elements [4i, 4i+4) of the head dimension.
 template <int D>
 __global__ void __launch_bounds__(256)
@@ -19,9 +27,9 @@ merge_kernel(const float* __restrict__ o_part, const float* __restrict__ lse_par
     if (r >= rows) return;
     const float* lse = lse_part + r * n_slots;
     float M = -INFINITY;
-    for (int i = lane; i < n_slots; i += 32) M = fmaxf(M, lse[i]);
+    for (int i = lane; i < n_slots; i += 32) M = max_or_nan(M, lse[i]);
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, off));
+    for (int off = 16; off > 0; off >>= 1) M = max_or_nan(M, __shfl_xor_sync(0xffffffffu, M, off));
 
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float W = 0.f;

@@ -1,0 +1,89 @@
+// The paged private store on the device: where a context token lives, and the byte layout of a
+// 16-token block of the 4-bit format (include/moska.h has the definition).
+#pragma once
+
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "common.cuh"
+
+namespace moska {
+
+constexpr int kBlockTokens = 16;        // tokens of a 4-bit block, and of a streaming tile
+constexpr float kFp4MaxScale = 10912.f; // largest f16 whose sixfold is finite in f16
+
+// moska_paged_kv as the kernels take it (page_size is a power of two: 1 << page_shift).
+struct PagedView {
+    uint8_t* k;
+    uint8_t* v;
+    const int32_t* page_table;
+    const int32_t* kv_len;
+    int32_t n_pages;
+    int32_t max_pages;
+    int32_t page_shift;
+    int* status;  // the device status word
+};
+
+__host__ __device__ constexpr int fp4_block_bytes(int D) { return 18 * D; }
+
+// Byte offsets inside a 4-bit block.
+template <int D>
+struct Fp4Block {
+    static_assert(D == 64 || D == 128, "head dimension");
+    static constexpr int kBytes = fp4_block_bytes(D);
+    static constexpr int kGroups = D / 32;  // scales of a token row
+    static constexpr int kV = 8 * D, kKScale = 16 * D, kVScale = 17 * D;
+    // position of value chunk x (D / 8 dimensions of both tokens of pair p) inside the pair's row
+    static __host__ __device__ constexpr int v_swap(int p) { return D == 128 ? 2 * (p & 3) : 4 * ((p >> 1) & 1); }
+    // first byte of dimensions d .. d + 7 (d a multiple of 8) of token t: four bytes
+    static __host__ __device__ constexpr int k_byte(int t, int d)
+    {
+        return t * (D / 2) + ((d & 31) >> 3) * (D / 8) + (d >> 5) * 4;
+    }
+    static __host__ __device__ constexpr int v_byte(int t, int d)
+    {
+        return kV + (t >> 1) * D + ((d / (D / 8)) ^ v_swap(t >> 1)) * (D / 8) + (t & 1) * (D / 16) + (d % (D / 8)) / 2;
+    }
+    static __host__ __device__ constexpr int k_scale(int t, int group) { return kKScale + 2 * (t * kGroups + group); }
+    static __host__ __device__ constexpr int v_scale(int t, int group) { return kVScale + 2 * (group * 16 + t); }
+};
+
+// Context length of request r, cut to what its page-table row can hold (reported where it was not
+// inside).
+__device__ __forceinline__ int paged_len(const PagedView& p, int r)
+{
+    const int len = __ldg(p.kv_len + r);
+    const long long most = (long long)p.max_pages << p.page_shift;
+    if (len < 0 || len > most) {
+        atomicMin(p.status, MOSKA_ERR_INVALID_ARG);
+        return len < 0 ? 0 : (int)most;
+    }
+    return len;
+}
+
+// Page `i` of a page-table row for a read: an index outside the pool is reported and becomes page 0.
+__device__ __forceinline__ int paged_page(const PagedView& p, const int32_t* row, int i)
+{
+    const int page = __ldg(row + i);
+    if (static_cast<unsigned>(page) < static_cast<unsigned>(p.n_pages)) return page;
+    atomicMin(p.status, MOSKA_ERR_INVALID_ARG);
+    return 0;
+}
+
+// Two E2M1 codes a byte -> two f16 values, exact; the four bytes of w give o[0..3].
+__device__ __forceinline__ void e2m1x8_to_f16x2(uint32_t w, uint32_t (&o)[4])
+{
+    asm("{\n"
+        ".reg .b8 b0, b1, b2, b3;\n"
+        "mov.b32 {b0, b1, b2, b3}, %4;\n"
+        "cvt.rn.f16x2.e2m1x2 %0, b0;\n"
+        "cvt.rn.f16x2.e2m1x2 %1, b1;\n"
+        "cvt.rn.f16x2.e2m1x2 %2, b2;\n"
+        "cvt.rn.f16x2.e2m1x2 %3, b3;\n"
+        "}\n"
+        : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3])
+        : "r"(w));
+}
+
+}  // namespace moska

@@ -89,16 +89,23 @@ struct CombineSmem {
 // (e < D/8): 16-byte pieces of 8 elements, piece j of a row at element 64*j + 8*g.
 __device__ __forceinline__ int v_dim_of(int g, int e) { return 64 * (e >> 3) + 8 * g + (e & 7); }
 
+// Where the tokens of a stream live: row (base(t0) + t) of the store for every token t of the 16-token
+// tile that holds token t0 (tiles start at multiples of 16 from t_begin).  Here: one contiguous range.
+struct ContiguousTokens {
+    static constexpr bool kPaged = false;
+    __device__ __forceinline__ int64_t base(int) const { return 0; }
+};
+
 // Attention of the NT*8 rows in `rows` (shared-memory resident descriptor, filled by the
 // caller, visible to all threads) over tokens [t_begin, t_end) of the stream
 // k_base/v_base + token * tok_stride (elements).  All threads of the CTA must call this.
 // Writes normalised o (fp32) and natural-log lse for every non-null row; a range without
 // tokens gives lse = -inf, o = 0.
-template <int D, int NT>
+template <int D, int NT, class Tokens = ContiguousTokens>
 __device__ __forceinline__ void attend_stream(const TileRows<NT>& rows, const uint16_t* k_base,
                                               const uint16_t* v_base, int64_t tok_stride,
                                               int t_begin, int t_end, float scale,
-                                              CombineSmem<D, NT>& sm)
+                                              CombineSmem<D, NT>& sm, const Tokens tokens = {})
 {
     static_assert(D == 64 || D == 128, "head dimension");
     constexpr int KU = D / 32;   // 16-byte K loads per token row and lane
@@ -137,35 +144,41 @@ __device__ __forceinline__ void attend_stream(const TileRows<NT>& rows, const ui
     uint4 kA[KU], kB[KU];      // K rows of tokens g and g+8 of the tile
     uint4 vr[4][VL];           // V rows of tokens 2c, 2c+1, 2c+8, 2c+9 of the tile
 
-    auto load_k = [&](int tile) {
+    auto load_k = [&](int tile, int64_t base) {
         const int t0 = t_begin + tile * kTileTokens;
         const int ta = min(t0 + g, last_tok), tb = min(t0 + 8 + g, last_tok);
-        const uint16_t* pa = k_base + (int64_t)ta * tok_stride + 8 * c;
-        const uint16_t* pb = k_base + (int64_t)tb * tok_stride + 8 * c;
+        const uint16_t* pa = k_base + (base + ta) * tok_stride + 8 * c;
+        const uint16_t* pb = k_base + (base + tb) * tok_stride + 8 * c;
 #pragma unroll
         for (int u = 0; u < KU; ++u) {
             kA[u] = ldg16(pa + 32 * u);
             kB[u] = ldg16(pb + 32 * u);
         }
     };
-    auto load_v = [&](int tile) {
+    auto load_v = [&](int tile, int64_t base) {
         const int t0 = t_begin + tile * kTileTokens;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int tt = min(t0 + 2 * c + (i & 1) + 8 * (i >> 1), last_tok);
-            const uint16_t* p = v_base + (int64_t)tt * tok_stride + 8 * g;
+            const uint16_t* p = v_base + (base + tt) * tok_stride + 8 * g;
 #pragma unroll
             for (int j = 0; j < VL; ++j) vr[i][j] = ldg16(p + 64 * j);
         }
     };
 
     int tile = warp;
+    // (bases are asked for one tile before the loads that need them)
+    auto base_of = [&](int i) { return i < n_tiles ? tokens.base(t_begin + i * kTileTokens) : (int64_t)0; };
+    int64_t base_next = base_of(tile + kWarps);
     if (tile < n_tiles) {
-        load_k(tile);
-        load_v(tile);
+        const int64_t base = base_of(tile);
+        load_k(tile, base);
+        load_v(tile, base);
     }
     for (; tile < n_tiles; tile += kWarps) {
         const int t0 = t_begin + tile * kTileTokens;
+        const int64_t base = base_next;  // of tile + kWarps
+        base_next = base_of(tile + 2 * kWarps);
         // ---- S^T = K Q^T
         float s[NT][4];
 #pragma unroll
@@ -179,7 +192,7 @@ __device__ __forceinline__ void attend_stream(const TileRows<NT>& rows, const ui
             }
         }
         const int next = tile + kWarps;
-        if (next < n_tiles) load_k(next);
+        if (next < n_tiles) load_k(next, base);
 
         // ---- online softmax over the 16 tokens (rows of S^T) for query columns 2c, 2c+1
         const bool va = (t0 + g) <= last_tok, vb = (t0 + 8 + g) <= last_tok;
@@ -243,7 +256,7 @@ __device__ __forceinline__ void attend_stream(const TileRows<NT>& rows, const ui
 #pragma unroll
             for (int n = 0; n < NT; ++n) mma_bf16_16816(oacc[n][mt], a0, a1, a2, a3, pb0[n], pb1[n]);
         }
-        if (next < n_tiles) load_v(next);
+        if (next < n_tiles) load_v(next, base);
     }
 
     // ---- combine the warps: per-lane sums of l over the 8 token lanes first
@@ -286,8 +299,15 @@ __device__ __forceinline__ void attend_stream(const TileRows<NT>& rows, const ui
                 den = fmaf(a, sm.l[w][r], den);
             }
         }
-        orow[d] = den > 0.f ? num / den : 0.f;
-        if (d == 0) rows.lse[r][0] = den > 0.f ? M * scale + logf(den) : -INFINITY;
+        if constexpr (Tokens::kPaged) {
+            if (M == -INFINITY)  // no token, or NaN scores alone: their sum is NaN
+                for (int w = 0; w < kWarps; ++w) den += sm.l[w][r];
+            tokens.store(orow, rows.lse[r], d, den == 0.f ? 0.f : num / den,
+                         den == 0.f ? -INFINITY : M * scale + logf(den));
+        } else {
+            orow[d] = den > 0.f ? num / den : 0.f;
+            if (d == 0) rows.lse[r][0] = den > 0.f ? M * scale + logf(den) : -INFINITY;
+        }
     }
 }
 
@@ -332,11 +352,12 @@ __device__ __forceinline__ uint4 lds16(uint32_t addr)
 // With kRowLast, row r only sees the tokens up to index row_last[r] of the stream (several query
 // tokens of one request, each one token further into the same context); `row_last` is an array of
 // NT * 8 ints visible to all threads.
-template <int NT, bool kRowLast = false>
+template <int NT, bool kRowLast = false, class Tokens = ContiguousTokens>
 __device__ __forceinline__ void attend_stream_staged(const TileRows<NT>& rows, const uint16_t* k_base,
                                                      const uint16_t* v_base, int64_t tok_stride,
                                                      int t_begin, int t_end, float scale,
-                                                     unsigned char* ring, const int* row_last = nullptr)
+                                                     unsigned char* ring, const int* row_last = nullptr,
+                                                     const Tokens tokens = {})
 {
     constexpr int D = 128, KU = 4, VL = 2, MT = 8;
     static_assert(sizeof(CombineSmem<D, NT>) <= kWarps * kStagedWarpBytes, "the combine step reuses the ring");
@@ -378,29 +399,44 @@ __device__ __forceinline__ void attend_stream_staged(const TileRows<NT>& rows, c
         }
         for (int r = 0; r < NT * 8; ++r) min_last = min(min_last, row_last[r]);
     }
+    int first_limit = 0x7fffffff, top_limit = -0x7fffffff;  // smallest and largest last token of the rows that exist
+    if constexpr (kRowLast && Tokens::kPaged) {
+        for (int r = 0; r < NT * 8; ++r) {
+            if (rows.o[r] == nullptr) continue;
+            first_limit = min(first_limit, row_last[r]);
+            top_limit = max(top_limit, row_last[r]);
+        }
+    }
     const uint32_t ring_base = static_cast<uint32_t>(__cvta_generic_to_shared(ring)) + warp * kStagedWarpBytes;
     // chunk `ch` of token row `t` (0..15) of the K (kv = 0) or V (kv = 1) tile in ring stage s
     auto slot = [&](int s, int kv, int t, int ch) {
         return ring_base + s * kStagedTileBytes + kv * (kTileTokens * 256) + t * 256 + ((ch ^ (t & 7)) << 4);
     };
     // cooperative copy of the i-th tile of this warp: 16 lanes per token row, two rows per instruction
-    auto issue = [&](int i) {
+    auto issue = [&](int i, int64_t base) {
         const int s = i % kStagedDepth;
         const int t0 = t_begin + (warp + i * kWarps) * kTileTokens;
         const int ch = lane & 15;
 #pragma unroll
         for (int it = 0; it < 8; ++it) {
             const int t = 2 * it + (lane >> 4);
-            const int64_t off = (int64_t)min(t0 + t, last_tok) * tok_stride + 8 * ch;
+            const int64_t off = (base + min(t0 + t, last_tok)) * tok_stride + 8 * ch;
             cp_async16(slot(s, 0, t, ch), k_base + off);
             cp_async16(slot(s, 1, t, ch), v_base + off);
         }
     };
+    auto base_of = [&](int i) {
+        return i < my_tiles ? tokens.base(t_begin + (warp + i * kWarps) * kTileTokens) : (int64_t)0;
+    };
+    int64_t base_first[kStagedDepth];
+#pragma unroll
+    for (int i = 0; i < kStagedDepth; ++i) base_first[i] = base_of(i);
 #pragma unroll
     for (int i = 0; i < kStagedDepth; ++i) {
-        if (i < my_tiles) issue(i);
+        if (i < my_tiles) issue(i, base_first[i]);
         cp_async_commit();  // one group per ring stage, empty ones included
     }
+    int64_t base_next = base_of(kStagedDepth);  // asked for one tile before the copies that need it
 
     for (int i = 0; i < my_tiles; ++i) {
         const int s = i % kStagedDepth;
@@ -476,32 +512,64 @@ __device__ __forceinline__ void attend_stream_staged(const TileRows<NT>& rows, c
                     oacc[n][mt][3] *= alpha[n][1];
                 }
         }
+        // the fragments of V^T, block by block, to add(n, mt, a0 .. a3)
+        auto add_pv = [&](const uint4 (&vr)[4][VL], auto&& add) {
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                const int e0 = mt, e1 = MT + mt;
+                const uint32_t sel0 = (e0 & 1) ? 0x7632u : 0x5410u;
+                const uint32_t sel1 = (e1 & 1) ? 0x7632u : 0x5410u;
+                auto word = [&](int r, int e) -> uint32_t {
+                    const uint4& x = vr[r][e >> 3];
+                    const int w = (e & 7) >> 1;
+                    return w == 0 ? x.x : (w == 1 ? x.y : (w == 2 ? x.z : x.w));
+                };
+                const uint32_t a0 = __byte_perm(word(0, e0), word(1, e0), sel0);
+                const uint32_t a1 = __byte_perm(word(0, e1), word(1, e1), sel1);
+                const uint32_t a2 = __byte_perm(word(2, e0), word(3, e0), sel0);
+                const uint32_t a3 = __byte_perm(word(2, e1), word(3, e1), sel1);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) add(n, mt, a0, a1, a2, a3);
+            }
+        };
         uint4 vr[4][VL];  // V rows of tokens 2c, 2c+1, 2c+8, 2c+9: chunk g of each half row
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int j = 0; j < VL; ++j)
                 vr[r][j] = lds16(slot(s, 1, 2 * c + (r & 1) + 8 * (r >> 1), g + 8 * j));
+        bool once = true;
+        if constexpr (kRowLast && Tokens::kPaged) {
+            // The tile holds tokens that not every row sees: one pass for each query token over the values
+            // that it sees, kept in its columns only (0 times a NaN behind a row's context is NaN).
+            once = t0 + kTileTokens - 1 <= min_last;
+            if (!once) {
+                for (int limit = first_limit; limit <= top_limit; ++limit) {
+                    uint4 seen[4][VL];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            const int e0 = mt, e1 = MT + mt;
-            const uint32_t sel0 = (e0 & 1) ? 0x7632u : 0x5410u;
-            const uint32_t sel1 = (e1 & 1) ? 0x7632u : 0x5410u;
-            auto word = [&](int r, int e) -> uint32_t {
-                const uint4& x = vr[r][e >> 3];
-                const int w = (e & 7) >> 1;
-                return w == 0 ? x.x : (w == 1 ? x.y : (w == 2 ? x.z : x.w));
-            };
-            const uint32_t a0 = __byte_perm(word(0, e0), word(1, e0), sel0);
-            const uint32_t a1 = __byte_perm(word(0, e1), word(1, e1), sel1);
-            const uint32_t a2 = __byte_perm(word(2, e0), word(3, e0), sel0);
-            const uint32_t a3 = __byte_perm(word(2, e1), word(3, e1), sel1);
+                    for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) mma_bf16_16816(oacc[n][mt], a0, a1, a2, a3, pb0[n], pb1[n]);
+                        for (int j = 0; j < VL; ++j)
+                            seen[r][j] = t0 + 2 * c + (r & 1) + 8 * (r >> 1) <= min(limit, last_tok)
+                                             ? vr[r][j] : make_uint4(0, 0, 0, 0);
+                    add_pv(seen, [&](int n, int mt, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+                        float x[4] = {oacc[n][mt][0], oacc[n][mt][1], oacc[n][mt][2], oacc[n][mt][3]};
+                        mma_bf16_16816(x, a0, a1, a2, a3, pb0[n], pb1[n]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (lim[n][e & 1] == limit) oacc[n][mt][e] = x[e];
+                    });
+                }
+            }
         }
+        if (once)
+            add_pv(vr, [&](int n, int mt, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3) {
+                mma_bf16_16816(oacc[n][mt], a0, a1, a2, a3, pb0[n], pb1[n]);
+            });
         __syncwarp();  // every lane has read the stage into registers: refill it
-        if (i + kStagedDepth < my_tiles) issue(i + kStagedDepth);
+        if (i + kStagedDepth < my_tiles) issue(i + kStagedDepth, base_next);
         cp_async_commit();
+        base_next = base_of(i + kStagedDepth + 1);
     }
     cp_async_wait<0>();
 
@@ -549,8 +617,15 @@ __device__ __forceinline__ void attend_stream_staged(const TileRows<NT>& rows, c
                 den = fmaf(a, sm.l[w][r], den);
             }
         }
-        orow[d] = den > 0.f ? num / den : 0.f;
-        if (d == 0) rows.lse[r][0] = den > 0.f ? M * scale + logf(den) : -INFINITY;
+        if constexpr (Tokens::kPaged) {
+            if (M == -INFINITY)  // no token, or NaN scores alone: their sum is NaN
+                for (int w = 0; w < kWarps; ++w) den += sm.l[w][r];
+            tokens.store(orow, rows.lse[r], d, den == 0.f ? 0.f : num / den,
+                         den == 0.f ? -INFINITY : M * scale + logf(den));
+        } else {
+            orow[d] = den > 0.f ? num / den : 0.f;
+            if (d == 0) rows.lse[r][0] = den > 0.f ? M * scale + logf(den) : -INFINITY;
+        }
     }
     __syncthreads();  // the ring may be refilled by a following call
 }

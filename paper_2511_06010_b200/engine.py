@@ -88,6 +88,11 @@ class MoskaLayer:
         M.unique_attn_fp8(q, f8.k8, f8.v8, f8.k_scale, f8.v_scale, kv_start, kv_len, self.o_part,
                           self.lse_part, self.scale, self.shape, stream)
 
+    def unique_paged(self, q, store, page_table, kv_len, stream=None):
+        """Unique KV Attention over a paged private store (`store`: a paged.PagedKvStore)."""
+        M.unique_attn_paged(q, store.kv(page_table, kv_len), self.o_part, self.lse_part, self.scale, self.shape,
+                            stream)
+
     def merge(self):
         M.merge(self.o_part, self.lse_part, self.out, self.out_f32, self.lse_out, self.shape)
 
@@ -143,6 +148,21 @@ class MoskaLayer:
                           f8.k_scale, f8.v_scale, kv_start, kv_len, self.topk_idx, self.seg_offsets,
                           self.seg_entries, self.o_part, self.lse_part, self.out, self.lse_out, self.scale,
                           self.shape, self.ws, None, self.side_stream if two_streams else None, prof)
+        return self.out
+
+    def step_paged(self, q, k_shared, v_shared, store, page_table, kv_len, two_streams=False, prof=None,
+                   unique_tokens=0, sf8=None):
+        """One decode step with a paged private store (`store`: a paged.PagedKvStore in either format).
+        The shared store is bf16, or FP8 when `sf8` is given (k_shared and v_shared are then not read)."""
+        self.shape.unique_tokens = int(unique_tokens)
+        two_streams = two_streams and self.overlap_routing
+        if two_streams and self.side_stream is None:
+            self.side_stream = torch.cuda.Stream(device=self.device, priority=-1)
+        shared = (k_shared, v_shared, None, None) if sf8 is None else (sf8.k8, sf8.v8, sf8.k_scale, sf8.v_scale)
+        M.decode_step_paged(q, None if self.dense else self.summaries, *shared, store.kv(page_table, kv_len),
+                            self.topk_idx, self.seg_offsets, self.seg_entries, self.o_part, self.lse_part, self.out,
+                            self.lse_out, self.scale, self.shape, self.ws, None,
+                            self.side_stream if two_streams else None, prof)
         return self.out
 
     def step_fp8_host(self, q_host, q_dev, out_host, sf8, f8, kv_start, kv_len, two_streams=False,

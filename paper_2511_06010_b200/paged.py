@@ -1,0 +1,226 @@
+"""A paged private KV store: pages in bf16 or in 4 bits, the calls that write and read them, and the
+host-side book of which pages a request holds.  No arithmetic: every step runs in the CUDA library;
+torch owns the memory and the streams.
+"""
+from __future__ import annotations
+
+import contextlib
+import math
+from typing import Optional
+
+import numpy as np
+import torch
+
+from . import binding as M
+
+FORMATS = {"bf16": M.KV_BF16, "fp4": M.KV_FP4}
+
+
+def _on(device):
+    """The library works on the current device: makes `device` current for a call."""
+    return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _expect(t, name, dtype, shape, device):
+    """Checks a dense tensor of a call (shape: None = any extent)."""
+    if t.dtype != dtype or t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)):
+        raise ValueError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the store on {device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t
+
+
+def _rows(t, name, n, heads, D, device):
+    """Address and row stride of [n][heads][D] rows whose heads are dense; rows may lie apart."""
+    if t.dtype != torch.bfloat16 or tuple(t.shape) != (n, heads, D):
+        raise ValueError(f"{name}: expected torch.bfloat16 {(n, heads, D)}, got {t.dtype} {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the store on {device}")
+    if t.numel() and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != D)):
+        raise ValueError(f"{name}: the heads of a row must be dense")
+    return t.data_ptr(), (t.stride(0) if n > 1 else heads * D)
+
+
+class PagedKvStore:
+    """Pools of pages holding the private keys and values of many requests.
+
+    bf16: `k_pages`, `v_pages` [n_pages][page_size][Hkv][D].  4-bit ("fp4": E2M1 codes, one f16 scale
+    per (token, KV head, 32 dimensions)): `pages4` uint8 [n_pages][Hkv][page_size / 16][18 D].
+    A store over existing pools: PagedKvStore(k_pages=.., v_pages=..) or PagedKvStore(pages4=..,
+    page_size=..); new ones: PagedKvStore.empty(...).  page_size is a power of two, 16..32768.
+    """
+
+    def __init__(self, k_pages=None, v_pages=None, pages4=None, page_size: Optional[int] = None):
+        if (pages4 is None) == (k_pages is None) or (k_pages is None) != (v_pages is None):
+            raise ValueError("give k_pages and v_pages, or pages4")
+        if pages4 is None:
+            self.fmt = "bf16"
+            self.n_pages, self.page_size, self.Hkv, self.D = k_pages.shape
+            if page_size not in (None, self.page_size):
+                raise ValueError(f"page_size = {page_size}, the pages hold {self.page_size}")
+            self.device = k_pages.device
+            for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+                _expect(t, name, torch.bfloat16, (self.n_pages, self.page_size, self.Hkv, self.D), self.device)
+            self.k_pages, self.v_pages, self.pages4 = k_pages, v_pages, None
+        else:
+            self.fmt = "fp4"
+            self.n_pages, self.Hkv, blocks, block_bytes = pages4.shape
+            self.page_size, self.D = 16 * blocks, block_bytes // 18
+            if page_size not in (None, self.page_size):
+                raise ValueError(f"page_size = {page_size}, the pages hold {self.page_size}")
+            self.device = pages4.device
+            _expect(pages4, "pages4", torch.uint8, (self.n_pages, self.Hkv, blocks, 18 * self.D), self.device)
+            self.k_pages, self.v_pages, self.pages4 = None, None, pages4
+        self._pool = self.k_pages if pages4 is None else pages4
+
+    @classmethod
+    def empty(cls, n_pages, page_size, Hkv, D, fmt="bf16", device="cuda"):
+        """A store of its own memory; the pages hold nothing yet."""
+        if page_size < 16 or page_size & (page_size - 1):
+            raise ValueError(f"page_size = {page_size} is not a power of two of at least 16")
+        if FORMATS[fmt] == M.KV_BF16:
+            k, v = (torch.empty(n_pages, page_size, Hkv, D, dtype=torch.bfloat16, device=device) for _ in range(2))
+            return cls(k_pages=k, v_pages=v)
+        return cls(pages4=torch.empty(n_pages, Hkv, page_size // 16, 18 * D, dtype=torch.uint8, device=device))
+
+    def kv(self, page_table, kv_len) -> M.MoskaPagedKv:
+        """The store seen through a page table int32 [R][max_pages] and context lengths int32 [R]."""
+        _expect(page_table, "page_table", torch.int32, (None, None), self.device)
+        _expect(kv_len, "kv_len", torch.int32, (page_table.shape[0],), self.device)
+        return M.paged_kv(FORMATS[self.fmt], self.page_size, self.n_pages, page_table.shape[1], self._pool,
+                          self.v_pages, page_table, kv_len)
+
+    def _row_args(self, page_table, n_rows, row_start, q_len):
+        n_requests = page_table.shape[0]
+        if row_start is not None:
+            _expect(row_start, "row_start", torch.int32, (n_requests + 1,), self.device)
+        elif n_rows != n_requests * q_len:
+            raise ValueError(f"{n_rows} rows for {n_requests} requests of {q_len} each: give row_start")
+        return n_requests
+
+    def append(self, q, k, v, page_table, kv_len, positions=None, cos_sin=None, row_start=None, interleaved=False,
+               q_out=None, q_len=1, stream=None):
+        """Writes the new rows k, v [N][Hkv][D] into the pages, keys rotated, and returns the rotated
+        queries (q [N][Hq][D], or None).  kv_len counts the tokens after the call.  Request r has rows
+        row_start[r] .. row_start[r+1] - 1, or q_len each without row_start.  cos_sin float
+        [positions][rot_dim] (cos, then sin; None: no rotation), positions int32 [N].  q, k and v may be
+        columns of one projection's output."""
+        n = k.shape[0]
+        n_requests = self._row_args(page_table, n, row_start, q_len)
+        kp, ks = _rows(k, "k", n, self.Hkv, self.D, self.device)
+        vp, vs = _rows(v, "v", n, self.Hkv, self.D, self.device)
+        Hq, qp, qs = self.Hkv, None, 0
+        if q is not None:
+            Hq = q.shape[1]
+            qp, qs = _rows(q, "q", n, Hq, self.D, self.device)
+            if q_out is None:
+                q_out = torch.empty(n, Hq, self.D, dtype=torch.bfloat16, device=self.device)
+            _expect(q_out, "q_out", torch.bfloat16, (n, Hq, self.D), self.device)
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        rot_dim = n_positions = 0
+        if cos_sin is not None:
+            _expect(cos_sin, "cos_sin", torch.float32, (None, None), self.device)
+            if positions is None:
+                raise ValueError("cos_sin without positions")
+            _expect(positions, "positions", torch.int32, (n,), self.device)
+            n_positions, rot_dim = cos_sin.shape
+        if n == 0:
+            return q_out
+        s = M.shape(n, Hq, self.Hkv, self.D, 1, 128, 1, q_len=q_len if row_start is None else 1)
+        with _on(self.device):
+            M.kv_append_paged(qp, qs, kp, ks, vp, vs, positions, cos_sin, n_positions, rot_dim, int(interleaved),
+                              row_start, n_requests, q_out, self.kv(page_table, kv_len), s, stream)
+        return q_out
+
+    def gather(self, page_table, kv_len, n_rows, row_start=None, q_len=1, k_out=None, v_out=None, stream=None):
+        """The last rows of the contexts as bf16 [n_rows][Hkv][D] keys and values; rows as in append.
+        Rows behind the last request keep what k_out and v_out hold."""
+        n_requests = self._row_args(page_table, n_rows, row_start, q_len)
+        if k_out is None:
+            k_out = torch.empty(n_rows, self.Hkv, self.D, dtype=torch.bfloat16, device=self.device)
+        if v_out is None:
+            v_out = torch.empty(n_rows, self.Hkv, self.D, dtype=torch.bfloat16, device=self.device)
+        for t, name in ((k_out, "k_out"), (v_out, "v_out")):
+            _expect(t, name, torch.bfloat16, (n_rows, self.Hkv, self.D), self.device)
+        if n_rows:
+            s = M.shape(n_rows, self.Hkv, self.Hkv, self.D, 1, 128, 1, q_len=q_len if row_start is None else 1)
+            with _on(self.device):
+                M.kv_gather_paged(row_start, n_requests, k_out, v_out, self.kv(page_table, kv_len), s, stream)
+        return k_out, v_out
+
+
+class PagedAttention:
+    """Attention of a batch over its paged private contexts alone (no shared store): owns the scratch
+    and the result buffers for one shape.  Calls share them: give every stream its own instance."""
+
+    def __init__(self, B, Hq, Hkv, D, max_len, fmt="bf16", q_len=1, n_unique_splits=None, device="cuda"):
+        """B counts batch rows: B / q_len requests of q_len query tokens; max_len: longest context."""
+        self.fmt = fmt
+        if n_unique_splits is None:
+            default = {"bf16": M.default_unique_splits, "fp4": M.default_unique_splits_fp4}[fmt]
+            n_unique_splits = default(B // max(1, q_len), Hkv, max(1, max_len))
+        self.shape = M.shape(B, Hq, Hkv, D, 1, 128, 1, n_unique_splits=n_unique_splits, q_len=q_len)
+        self.scale = 1.0 / math.sqrt(D)
+        self.out = torch.empty(B, Hq, D, dtype=torch.bfloat16, device=device)
+        self.lse = torch.empty(B, Hq, dtype=torch.float32, device=device)
+        self.device = self.out.device
+        self.ws = torch.empty(max(256, M.paged_attn_workspace_bytes(self.shape)), dtype=torch.uint8, device=device)
+
+    def __call__(self, q, store, page_table, kv_len, stream=None):
+        """q bf16 [B][Hq][D] -> (out bf16 [B][Hq][D], lse float [B][Hq]), this object's buffers."""
+        if store.fmt != self.fmt or (store.Hkv, store.D) != (self.shape.Hkv, self.shape.D):
+            raise ValueError("the store's format or heads are not this attention's")
+        _expect(q, "q", torch.bfloat16, self.out.shape, store.device)
+        if page_table.shape[0] * max(1, self.shape.q_len) != self.shape.B:
+            raise ValueError(f"{page_table.shape[0]} page-table rows for {self.shape.B} batch rows")
+        if self.device != store.device:
+            raise ValueError(f"the store is on {store.device}, the scratch on {self.device}")
+        with _on(self.device):
+            M.paged_attn(q, store.kv(page_table, kv_len), self.out, self.lse, self.scale, self.shape, self.ws, stream)
+        return self.out, self.lse
+
+
+class PageTable:
+    """Which pages every request slot holds: a free list on the host and the int32 table [slots][max_pages]
+    on the device.  Entries of pages that a slot does not hold are -1."""
+
+    def __init__(self, n_pages, page_size, slots, max_pages, device="cuda"):
+        self.page_size = page_size
+        self.host = np.full((slots, max_pages), -1, dtype=np.int32)
+        self.held = np.zeros(slots, dtype=np.int64)  # pages of each slot
+        self.free = list(range(n_pages - 1, -1, -1))
+        self.device_table = torch.full((slots, max_pages), -1, dtype=torch.int32, device=device)
+        self._changed = False
+
+    def reserve(self, slot: int, tokens: int) -> None:
+        """Gives the slot pages for a context of `tokens`; raises (and changes nothing) if there are too few."""
+        need = -(-int(tokens) // self.page_size)
+        more = need - int(self.held[slot])
+        if more <= 0:
+            return
+        if need > self.host.shape[1]:
+            raise ValueError(f"{tokens} tokens need {need} pages, a table row has {self.host.shape[1]}")
+        if more > len(self.free):
+            raise RuntimeError(f"{more} pages wanted, {len(self.free)} free")
+        for i in range(int(self.held[slot]), need):
+            self.host[slot, i] = self.free.pop()
+        self.held[slot] = need
+        self._changed = True
+
+    def release(self, slot: int) -> None:
+        """Takes the slot's pages back."""
+        n = int(self.held[slot])
+        self.free.extend(int(p) for p in self.host[slot, :n][::-1])
+        self.host[slot, :n] = -1
+        self.held[slot] = 0
+        self._changed = True
+
+    def table(self) -> torch.Tensor:
+        """The device table, brought up to date on the current stream."""
+        if self._changed:
+            self.device_table.copy_(torch.from_numpy(self.host))
+            self._changed = False
+        return self.device_table
