@@ -13,6 +13,8 @@
 // largest), P is rounded to f16 (half a step: 2^-11), row sums and statistics are fp32.
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "paged.cuh"
 #include "sm100.cuh"
 #include "stream_attn.cuh"
@@ -21,13 +23,21 @@ namespace moska {
 namespace {
 using namespace stream;
 
-constexpr int kSub = 2;    // blocks of a unit
-constexpr int kDepth = 4;  // units in flight per warp
+constexpr int kSub = 4;  // blocks of a unit
 
 template <int D>
 struct F4Ring {
+    static constexpr int kDepth = D == 128 ? 2 : 4;  // units in flight per warp
     static constexpr int kUnitBytes = kSub * Fp4Block<D>::kBytes;
     static constexpr int kBytes = kWarps * kDepth * kUnitBytes;
+};
+
+// Results of the warps before they are joined; rows padded by four floats (fewer bank conflicts).
+template <int D, int NT>
+struct F4Join {
+    float o[kWarps][NT * 8][D + 4];
+    float m[kWarps][NT * 8];  // log2 units
+    float l[kWarps][NT * 8];
 };
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
@@ -50,6 +60,14 @@ __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b)
 {
     const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
     return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// a where m has ones, b elsewhere
+__device__ __forceinline__ uint32_t select_bits(uint32_t m, uint32_t a, uint32_t b)
+{
+    uint32_t y;
+    asm("lop3.b32 %0, %1, %2, %3, 0xe4;" : "=r"(y) : "r"(a), "r"(b), "r"(m));
+    return y;
 }
 
 template <int N>  // N = 1, 2 or 4 words
@@ -89,10 +107,11 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
 {
     using B = Fp4Block<D>;
     constexpr int J = B::kGroups, MT = D / 16;
-    constexpr int kUnit = kSub * kBlockTokens, kRows = NT * 8;
+    constexpr int kUnit = kSub * kBlockTokens, kRows = NT * 8, kDepth = F4Ring<D>::kDepth;
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ uint64_t full[kWarps][kDepth];
     __shared__ int gave_up;
+    __shared__ int64_t row_of[kRows];  // result row of each query row, -1: none
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, c = lane & 3;
     const int G = a.Hq / a.Hkv;
@@ -102,6 +121,10 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
     const int q_len = a.q_len, n_rows = q_len * G;
 
     if (threadIdx.x == 0) gave_up = 0;
+    if (threadIdx.x < kRows) {
+        const int j = threadIdx.x;
+        row_of[j] = j < n_rows ? ((int64_t)r * q_len + j / G) * a.Hq + h * G + j % G : -1;
+    }
     if (lane == 0) {
 #pragma unroll
         for (int s = 0; s < kDepth; ++s) sm100::mbar_init(&full[warp][s], 1);
@@ -150,14 +173,15 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const int j = n * 8 + g;
-        const bool live = j < n_rows;
+        const int64_t row = row_of[j];
+        const bool live = row >= 0;
         float x[J][8];
         float top = 0.f;
 #pragma unroll
         for (int u = 0; u < J; ++u) {
             uint4 raw = make_uint4(0, 0, 0, 0);
             if (live)
-                raw = ldg16(a.q + (((int64_t)r * q_len + j / G) * a.Hq + h * G + j % G) * D + 32 * u + 8 * c);
+                raw = ldg16(a.q + row * D + 32 * u + 8 * c);
             const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -194,7 +218,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
         }
 
     float oacc[NT][MT][4];
-    float m_run[NT][2], l_run[NT][2];  // running maximum (in log2 units) and row sum of columns 2c, 2c + 1
+    float m_run[NT][2], l_run[NT][2];  // running maximum of the scores and row sum of columns 2c, 2c + 1
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         m_run[n][0] = m_run[n][1] = -INFINITY;
@@ -203,20 +227,21 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
         for (int mt = 0; mt < MT; ++mt) oacc[n][mt][0] = oacc[n][mt][1] = oacc[n][mt][2] = oacc[n][mt][3] = 0.f;
     }
 
-    int i = 0;
-    for (; i < mine; ++i) {
-        const int s = i % kDepth;
-        const int t0 = t_begin + (warp + i * kWarps) * kUnit;
-        const uint32_t at = ring_base + s * F4Ring<D>::kUnitBytes;
-        if (!__all_sync(0xffffffffu, sm100::mbar_wait(&full[warp][s], (i / kDepth) & 1, &gave_up))) {
-            if (lane == 0) atomicMin(a.kv.status, MOSKA_ERR_TIMEOUT);
-            break;
-        }
-        // ---- S^T of the unit's blocks, in log2 units
+    // One unit of the context, at `at` in the ring, from token t0.
+    auto unit_step = [&](auto is_tail, uint32_t at, int t0) {
+        constexpr bool tail = decltype(is_tail)::value;
+        // ---- S^T of the unit's blocks
         float sc[NT][kSub][4];
 #pragma unroll
         for (int b = 0; b < kSub; ++b) {
             const uint32_t blk = at + b * B::kBytes;
+            if constexpr (tail) {
+                if (t0 + b * kBlockTokens >= t_end) {  // not loaded
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) sc[n][b][0] = sc[n][b][1] = sc[n][b][2] = sc[n][b][3] = -INFINITY;
+                    continue;
+                }
+            }
             uint32_t ka[J], kb[J];
             lds_words<J>(blk + g * (D / 2) + c * (D / 8), ka);
             lds_words<J>(blk + (g + 8) * (D / 2) + c * (D / 8), kb);
@@ -245,8 +270,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
                 }
             }
         }
-        // ---- online softmax over the unit; only a unit that reaches past some row's last token is masked
-        const bool tail = t0 + kUnit > min(t_end, all_see);
+        // ---- online softmax over the unit
         bool grew = false;
         float alpha[NT][2];
 #pragma unroll
@@ -256,8 +280,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
             for (int b = 0; b < kSub; ++b) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    sc[n][b][e] *= unit[n][e & 1];
-                    if (tail && t0 + b * 16 + g + 8 * (e >> 1) >= min(t_end, seen[n][e & 1])) sc[n][b][e] = -INFINITY;
+                    if constexpr (tail)
+                        if (t0 + b * 16 + g + 8 * (e >> 1) >= min(t_end, seen[n][e & 1])) sc[n][b][e] = -INFINITY;
                 }
                 mx0 = fmaxf(mx0, fmaxf(sc[n][b][0], sc[n][b][2]));
                 mx1 = fmaxf(mx1, fmaxf(sc[n][b][1], sc[n][b][3]));
@@ -270,16 +294,18 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
             const float mn0 = fmaxf(m_run[n][0], mx0), mn1 = fmaxf(m_run[n][1], mx1);
             grew |= (mn0 > m_run[n][0]) | (mn1 > m_run[n][1]);
             // a row that has seen no token yet: keep its (empty) state free of inf - inf
-            const float ms0 = mn0 == -INFINITY ? 0.f : mn0, ms1 = mn1 == -INFINITY ? 0.f : mn1;
-            alpha[n][0] = fast_exp2(m_run[n][0] - ms0);
-            alpha[n][1] = fast_exp2(m_run[n][1] - ms1);
+            const float ms0 = tail && mn0 == -INFINITY ? 0.f : mn0 * unit[n][0];
+            const float ms1 = tail && mn1 == -INFINITY ? 0.f : mn1 * unit[n][1];
+            alpha[n][0] = fast_exp2(fmaf(m_run[n][0], unit[n][0], -ms0));
+            alpha[n][1] = fast_exp2(fmaf(m_run[n][1], unit[n][1], -ms1));
             m_run[n][0] = mn0;
             m_run[n][1] = mn1;
             float sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
             for (int b = 0; b < kSub; ++b) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sc[n][b][e] = fast_exp2(sc[n][b][e] - ((e & 1) ? ms1 : ms0));
+                for (int e = 0; e < 4; ++e)
+                    sc[n][b][e] = fast_exp2(fmaf(sc[n][b][e], unit[n][e & 1], (e & 1) ? -ms1 : -ms0));
                 sum0 += sc[n][b][0] + sc[n][b][2];
                 sum1 += sc[n][b][1] + sc[n][b][3];
             }
@@ -306,6 +332,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
 #pragma unroll
             for (int b = 0; b < kSub; ++b) {
                 const uint32_t blk = at + b * B::kBytes;
+                if constexpr (tail)
+                    if (t0 + b * kBlockTokens >= t_end) break;
                 uint32_t pb0[NT], pb1[NT];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
@@ -321,7 +349,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
                 constexpr int kLanesPerGroup = 8 / J;  // lane groups g that share a scale
                 lds_words<1>(blk + B::v_scale(2 * c, g / kLanesPerGroup), s0);
                 lds_words<1>(blk + B::v_scale(2 * c + 8, g / kLanesPerGroup), s1);
-                if (tail) {
+                if constexpr (tail) {
                     const int t = t0 + b * 16 + 2 * c, end = min(t_end, limit);
                     s0[0] &= (t < end ? 0xffffu : 0u) | (t + 1 < end ? 0xffff0000u : 0u);
                     s1[0] &= (t + 8 < end ? 0xffffu : 0u) | (t + 9 < end ? 0xffff0000u : 0u);
@@ -330,10 +358,10 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
                 for (int w = 0; w < W; ++w) {
                     // byte e: dimension 8 w + 2 e (even) or 8 w + 2 e + 1 (odd) of both tokens of a pair
                     const uint32_t m = 0x0f0f0f0fu;
-                    const uint32_t a_even = (va[w] & m) | ((va[W + w] << 4) & ~m);
-                    const uint32_t a_odd = ((va[w] >> 4) & m) | (va[W + w] & ~m);
-                    const uint32_t b_even = (vb[w] & m) | ((vb[W + w] << 4) & ~m);
-                    const uint32_t b_odd = ((vb[w] >> 4) & m) | (vb[W + w] & ~m);
+                    const uint32_t a_even = select_bits(m, va[w], va[W + w] << 4);
+                    const uint32_t a_odd = select_bits(m, va[w] >> 4, va[W + w]);
+                    const uint32_t b_even = select_bits(m, vb[w], vb[W + w] << 4);
+                    const uint32_t b_odd = select_bits(m, vb[w] >> 4, vb[W + w]);
                     uint32_t f0[4], f1[4], f2[4], f3[4];
                     e2m1x8_to_f16x2(a_even, f0);
                     e2m1x8_to_f16x2(a_odd, f1);
@@ -346,7 +374,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
                             float(&acc)[4] = oacc[n][4 * w + e];
-                            if (passes == 1) {
+                            if constexpr (!tail) {
                                 mma_f16(acc, a0, a1, a2, a3, pb0[n], pb1[n]);
                             } else {
                                 float x[4] = {acc[0], acc[1], acc[2], acc[3]};
@@ -360,6 +388,20 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
                 }
             }
         }
+    };
+
+    int i = 0;
+    for (; i < mine; ++i) {
+        const int s = i % kDepth;
+        const int t0 = t_begin + (warp + i * kWarps) * kUnit;
+        const uint32_t at = ring_base + s * F4Ring<D>::kUnitBytes;
+        if (!__all_sync(0xffffffffu, sm100::mbar_wait(&full[warp][s], (i / kDepth) & 1, &gave_up))) {
+            if (lane == 0) atomicMin(a.kv.status, MOSKA_ERR_TIMEOUT);
+            break;
+        }
+        // only a unit that reaches past some row's last token is masked
+        if (t0 + kUnit > min(t_end, all_see)) unit_step(std::true_type{}, at, t0);
+        else unit_step(std::false_type{}, at, t0);
         __syncwarp();  // every lane has read the stage into registers: refill it
         if (i + kDepth < mine) issue(i + kDepth, next_page);
         next_page = page_of(i + kDepth + 1);
@@ -372,54 +414,62 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
 
     // ---- combine the warps through the (now idle) ring
     __syncthreads();
-    CombineSmem<D, NT>& sm = *reinterpret_cast<CombineSmem<D, NT>*>(ring);
-    static_assert(sizeof(CombineSmem<D, NT>) <= F4Ring<D>::kBytes, "the combine step reuses the ring");
+    F4Join<D, NT>& sm = *reinterpret_cast<F4Join<D, NT>*>(ring);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int off = 4; off < 32; off <<= 1) {
             l_run[n][0] += __shfl_xor_sync(0xffffffffu, l_run[n][0], off);
             l_run[n][1] += __shfl_xor_sync(0xffffffffu, l_run[n][1], off);
         }
-        if (g == 0) {
-            sm.m[warp][n * 8 + 2 * c] = m_run[n][0];
-            sm.m[warp][n * 8 + 2 * c + 1] = m_run[n][1];
-            sm.l[warp][n * 8 + 2 * c] = l_run[n][0];
-            sm.l[warp][n * 8 + 2 * c + 1] = l_run[n][1];
-        }
+    static_assert(sizeof(F4Join<D, NT>) <= F4Ring<D>::kBytes, "the join reuses the ring");
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            const int d = g * (D / 8) + 2 * mt;  // rows g and g + 8 of block mt: dimensions d and d + 1
-            sm.o[warp][n * 8 + 2 * c][d] = oacc[n][mt][0];
-            sm.o[warp][n * 8 + 2 * c + 1][d] = oacc[n][mt][1];
-            sm.o[warp][n * 8 + 2 * c][d + 1] = oacc[n][mt][2];
-            sm.o[warp][n * 8 + 2 * c + 1][d + 1] = oacc[n][mt][3];
+    for (int n = 0; n < NT; ++n) {
+        if (n * 8 + 2 * c >= n_rows) continue;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int j = n * 8 + 2 * c + u;
+            if (g == 0) {
+                sm.m[warp][j] = m_run[n][u] * unit[n][u];
+                sm.l[warp][j] = l_run[n][u];
+            }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)  // rows g and g + 8 of block mt: dimensions d and d + 1
+                *reinterpret_cast<float2*>(&sm.o[warp][j][g * (D / 8) + 2 * mt]) = make_float2(oacc[n][mt][u], oacc[n][mt][2 + u]);
         }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < kRows * D; i += kThreads) {
-        const int j = i / D, d = i % D;
-        if (j >= n_rows) break;
-        const int64_t row = ((int64_t)r * q_len + j / G) * a.Hq + h * G + j % G;
+    // four dimensions a thread
+    for (int i = threadIdx.x; i < n_rows * (D / 4); i += kThreads) {
+        const int j = i / (D / 4), d = i % (D / 4) * 4;
+        const int64_t row = row_of[j];
         float M = sm.m[0][j];
 #pragma unroll
         for (int w = 1; w < kWarps; ++w) M = fmaxf(M, sm.m[w][j]);
-        float num = 0.f, den = 0.f;
+        float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+        float den = 0.f;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             // (all maxima -inf: no token, or NaN scores alone, whose sum is NaN)
             const float al = M != -INFINITY ? fast_exp2(sm.m[w][j] - M) : 1.f;
-            num = fmaf(al, sm.o[w][j][d], num);
+            const float4 o = *reinterpret_cast<const float4*>(&sm.o[w][j][d]);
+            num.x = fmaf(al, o.x, num.x);
+            num.y = fmaf(al, o.y, num.y);
+            num.z = fmaf(al, o.z, num.z);
+            num.w = fmaf(al, o.w, num.w);
             den = fmaf(al, sm.l[w][j], den);
         }
-        const float o = den == 0.f ? 0.f : num / den;
+        const float inv = den == 0.f ? 0.f : 1.f / den;
         const float lse = den == 0.f ? -INFINITY : M * kLn2 + logf(den);
+        num = make_float4(num.x * inv, num.y * inv, num.z * inv, num.w * inv);
         if (a.out != nullptr) {
-            a.out[row * D + d] = __bfloat16_as_ushort(__float2bfloat16_rn(o));
+            const __nv_bfloat162 lo = __floats2bfloat162_rn(num.x, num.y), hi = __floats2bfloat162_rn(num.z, num.w);
+            *reinterpret_cast<uint2*>(a.out + row * D + d) =
+                make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
             if (d == 0 && a.lse_out != nullptr) a.lse_out[row] = lse;
         } else {
             const int64_t slot = row * a.n_slots + a.slot0 + sp;
-            a.o_part[slot * D + d] = o;
+            *reinterpret_cast<float4*>(a.o_part + slot * D + d) = num;
             if (d == 0) a.lse_part[slot] = lse;
         }
     }
