@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
     }
     if (lane == 0) {
 #pragma unroll
-        for (int s = 0; s < kDepth; ++s) sm100::mbar_init(&full[warp][s], 1);
+        for (int s = 0; s < kDepth; ++s) sm100::mbar_init(&full[warp][s], kSub);
         sm100::fence_mbar_init();
         sm100::fence_proxy_async_smem();
     }
@@ -145,26 +145,44 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
     const uint32_t ring_base = sm100::smem_u32(ring) + warp * (kDepth * F4Ring<D>::kUnitBytes);
     const int32_t* pages = a.kv.page_table + (int64_t)r * a.kv.max_pages;
     const int shift = a.kv.page_shift;
-    // lane j < kSub: page of block j of this warp's i-th unit
-    auto page_of = [&](int i) {
-        const int tok = t_begin + (warp + i * kWarps) * kUnit + lane * kBlockTokens;
-        return lane < kSub && i < mine && tok < t_end ? paged_page(a.kv, pages, tok >> shift) : 0;
-    };
-    auto issue = [&](int i, int page) {
-        const int s = i % kDepth;
-        const int t0 = t_begin + (warp + i * kWarps) * kUnit;
-        const int blocks = min(kSub, (t_end - t0 + kBlockTokens - 1) / kBlockTokens);
-        if (lane == 0) sm100::mbar_arrive_expect_tx(&full[warp][s], blocks * B::kBytes);
-        __syncwarp();
-        if (lane < blocks) {
-            const int in_page = ((t0 & ((1 << shift) - 1)) >> 4) + lane;
-            const int block = in_page & ((1 << (shift - 4)) - 1);  // pages of fewer than kSub blocks wrap
-            const uint8_t* src = a.kv.k + ((((int64_t)page * a.Hkv + h) << (shift - 4)) + block) * B::kBytes;
-            bulk_load(ring_base + s * F4Ring<D>::kUnitBytes + lane * B::kBytes, src, B::kBytes, &full[warp][s]);
+    // Lane j < kSub loads block j of every unit: `ahead` is that block's token in the unit to ask for next.
+    // Pages are looked up one unit before the copy that needs them.
+    const bool loads = lane < kSub;
+    int ahead = t_begin + warp * kUnit + lane * kBlockTokens;
+    const uint32_t page_bytes = ((uint32_t)a.Hkv << (shift - 4)) * B::kBytes;
+    const uint8_t* pool = a.kv.k + ((uint64_t)h << (shift - 4)) * B::kBytes;
+    const uint32_t lane_slot = ring_base + lane * B::kBytes;
+    auto page_ahead = [&] { return loads && ahead < t_end ? paged_page(a.kv, pages, ahead >> shift) : 0; };
+    // starts the copy of the unit that `ahead` is in, into ring stage s; every loading lane arrives
+    auto issue = [&](int s, int page) {
+        if (loads) {
+            uint64_t* bar = &full[warp][s];
+            if (ahead < t_end) {
+                const uint32_t block = (uint32_t)(ahead >> 4) & ((1u << (shift - 4)) - 1);
+                sm100::mbar_arrive_expect_tx(bar, B::kBytes);
+                bulk_load(lane_slot + s * F4Ring<D>::kUnitBytes, pool + (uint64_t)(uint32_t)page * page_bytes + block * B::kBytes,
+                          B::kBytes, bar);
+            } else {
+                sm100::mbar_arrive(bar);
+            }
         }
+        ahead += kWarps * kUnit;
     };
-    for (int i = 0; i < kDepth && i < mine; ++i) issue(i, page_of(i));
-    int next_page = page_of(kDepth);
+    int next_page = page_ahead();
+    {
+        int first[kDepth];
+        first[0] = next_page;
+#pragma unroll
+        for (int s = 1; s < kDepth; ++s) {  // all lookups in flight before the first copy
+            ahead += kWarps * kUnit;
+            first[s] = page_ahead();
+        }
+        ahead -= (kDepth - 1) * kWarps * kUnit;
+#pragma unroll
+        for (int s = 0; s < kDepth; ++s)
+            if (s < mine) issue(s, first[s]);
+        next_page = page_ahead();
+    }
 
     // Q as the B operand: step 2 j + u covers dimensions 32 j + 8 c + 4 u .. + 3; the row is scaled by a
     // power of two so that its largest element lies in [1, 2)
@@ -208,7 +226,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
     }
     // tokens that columns 2c, 2c + 1 see: [0, seen)
     int seen[NT][2];
-    const int all_see = len - (q_len - 1);
+    const int all_see = len - (q_len - 1);  // tokens that every row sees
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -227,21 +245,15 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
         for (int mt = 0; mt < MT; ++mt) oacc[n][mt][0] = oacc[n][mt][1] = oacc[n][mt][2] = oacc[n][mt][3] = 0.f;
     }
 
-    // One unit of the context, at `at` in the ring, from token t0.
-    auto unit_step = [&](auto is_tail, uint32_t at, int t0) {
+    // SUB blocks at `at` in the ring, from token t0; `tail`: some row's context ends in them.
+    auto step = [&](auto subs, auto is_tail, uint32_t at, int t0) {
+        constexpr int SUB = decltype(subs)::value;
         constexpr bool tail = decltype(is_tail)::value;
         // ---- S^T of the unit's blocks
-        float sc[NT][kSub][4];
+        float sc[NT][SUB][4];
 #pragma unroll
-        for (int b = 0; b < kSub; ++b) {
+        for (int b = 0; b < SUB; ++b) {
             const uint32_t blk = at + b * B::kBytes;
-            if constexpr (tail) {
-                if (t0 + b * kBlockTokens >= t_end) {  // not loaded
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) sc[n][b][0] = sc[n][b][1] = sc[n][b][2] = sc[n][b][3] = -INFINITY;
-                    continue;
-                }
-            }
             uint32_t ka[J], kb[J];
             lds_words<J>(blk + g * (D / 2) + c * (D / 8), ka);
             lds_words<J>(blk + (g + 8) * (D / 2) + c * (D / 8), kb);
@@ -277,7 +289,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
         for (int n = 0; n < NT; ++n) {
             float mx0 = -INFINITY, mx1 = -INFINITY;
 #pragma unroll
-            for (int b = 0; b < kSub; ++b) {
+            for (int b = 0; b < SUB; ++b) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     if constexpr (tail)
@@ -302,7 +314,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
             m_run[n][1] = mn1;
             float sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
-            for (int b = 0; b < kSub; ++b) {
+            for (int b = 0; b < SUB; ++b) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     sc[n][b][e] = fast_exp2(fmaf(sc[n][b][e], unit[n][e & 1], (e & 1) ? -ms1 : -ms0));
@@ -330,10 +342,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
         for (int pass = 0; pass < passes; ++pass) {
             const int limit = len - (q_len - 1 - pass);  // tail: values of tokens from here on are hidden
 #pragma unroll
-            for (int b = 0; b < kSub; ++b) {
+            for (int b = 0; b < SUB; ++b) {
                 const uint32_t blk = at + b * B::kBytes;
-                if constexpr (tail)
-                    if (t0 + b * kBlockTokens >= t_end) break;
                 uint32_t pb0[NT], pb1[NT];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
@@ -390,21 +400,28 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
         }
     };
 
-    int i = 0;
-    for (; i < mine; ++i) {
-        const int s = i % kDepth;
-        const int t0 = t_begin + (warp + i * kWarps) * kUnit;
-        const uint32_t at = ring_base + s * F4Ring<D>::kUnitBytes;
-        if (!__all_sync(0xffffffffu, sm100::mbar_wait(&full[warp][s], (i / kDepth) & 1, &gave_up))) {
+    int i = 0, s = 0, t0 = t_begin + warp * kUnit;
+    uint32_t parity = 0;
+    const int masked = min(t_end, all_see);  // units that reach past this token go block by block, with masks
+    for (; i < mine; ++i, t0 += kWarps * kUnit) {
+        if (!__all_sync(0xffffffffu, sm100::mbar_wait(&full[warp][s], parity, &gave_up))) {
             if (lane == 0) atomicMin(a.kv.status, MOSKA_ERR_TIMEOUT);
             break;
         }
-        // only a unit that reaches past some row's last token is masked
-        if (t0 + kUnit > min(t_end, all_see)) unit_step(std::true_type{}, at, t0);
-        else unit_step(std::false_type{}, at, t0);
+        const uint32_t at = ring_base + s * F4Ring<D>::kUnitBytes;
+        if (t0 + kUnit <= masked) {
+            step(std::integral_constant<int, kSub>{}, std::false_type{}, at, t0);
+        } else {
+            for (int t = t0; t < min(t_end, t0 + kUnit); t += kBlockTokens)
+                step(std::integral_constant<int, 1>{}, std::true_type{}, at + ((t - t0) / kBlockTokens) * B::kBytes, t);
+        }
         __syncwarp();  // every lane has read the stage into registers: refill it
-        if (i + kDepth < mine) issue(i + kDepth, next_page);
-        next_page = page_of(i + kDepth + 1);
+        if (i + kDepth < mine) issue(s, next_page);
+        next_page = page_ahead();
+        if (++s == kDepth) {
+            s = 0;
+            parity ^= 1;
+        }
     }
     // gave up on unit i: the copies in flight end (each wait again has a limit) before the ring is reused
     for (int stop = min(mine, i + kDepth); i < stop; ++i) {
