@@ -42,6 +42,16 @@ int check_shape(const moska_shape* s, bool needs_k);
 // MOSKA_OK if the current device is compute capability 10.x.
 int check_device();
 
+#ifdef __CUDACC__
+// Larger of two, NaN if either is.
+__device__ __forceinline__ float max_or_nan(float a, float b)
+{
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+#endif
+
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 

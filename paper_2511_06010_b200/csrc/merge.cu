@@ -7,14 +7,6 @@
 namespace moska {
 namespace {
 
-// Larger of two, NaN if either is (a partial result over NaN scores makes its row NaN).
-__device__ __forceinline__ float max_or_nan(float a, float b)
-{
-    float y;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-    return y;
-}
-
 // One warp per query row.  Lane i owns elements [4i, 4i+4) of the head dimension.
 template <int D>
 __global__ void __launch_bounds__(256)

@@ -104,122 +104,229 @@ __device__ __forceinline__ uint32_t e2m1_code(float x, float s)
     return c | ((__float_as_uint(x) >> 28) & 8u);
 }
 
-template <int D, bool kFp4>
-__global__ void __launch_bounds__(kAppendThreads)
-append_kernel(const uint16_t* __restrict__ q, int64_t q_stride, const uint16_t* __restrict__ k, int64_t k_stride,
-              const uint16_t* __restrict__ v, int64_t v_stride, const int32_t* __restrict__ positions,
-              const float* __restrict__ cos_sin, int n_positions, int rot_dim, int interleaved,
-              const int32_t* __restrict__ row_start, int n_requests, uint16_t* __restrict__ q_out, PagedView kv,
-              int Hq, int Hkv, int q_len)
+// The E2M1 codes of y[0..7] for scale s, y[0] in the lowest four bits.  Products with 1 / s a little
+// too small and a little too large (2^-20; their own error is below 3 2^-24) enclose the quotient: where
+// the conversion gives both the same code that is the quotient's, elsewhere (near a tie, a few in a
+// million) the codes are compared out.
+__device__ __forceinline__ uint32_t e2m1x8(const float (&y)[8], float s)
 {
-    constexpr int T = D / 8;                    // threads of one head: eight dimensions each
-    constexpr int kHeads = kAppendThreads / T;  // heads in flight
-    const int row = blockIdx.x;
-    const int t = threadIdx.x % T, d0 = 8 * t;
-    const RowPlace at = place_row(kv, row, q_len, row_start, n_requests);
-    if (at.token < 0) return;  // padding
+    const float inv = s > 0.f ? __fdiv_rn(1.f, s) : 0.f;
+    uint32_t w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float m = i == 0 ? inv * (1.f - 0x1p-20f) : inv * (1.f + 0x1p-20f);
+        asm("{\n"
+            ".reg .b8 b0, b1, b2, b3;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n"
+            "mov.b32 %0, {b0, b1, b2, b3};\n"
+            "}\n"
+            : "=r"(w[i])
+            : "f"(y[0] * m), "f"(y[1] * m), "f"(y[2] * m), "f"(y[3] * m), "f"(y[4] * m), "f"(y[5] * m),
+              "f"(y[6] * m), "f"(y[7] * m));
+    }
+    if (w[0] != w[1]) {
+        w[0] = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[0] |= e2m1_code(y[e], s) << (4 * e);
+    }
+    return w[0];
+}
 
-    // this thread's part of the rotation: y = x c + sign (partner s)
-    const bool rotated = d0 < rot_dim;
-    float c[8], s[8];
+struct AppendArgs {
+    const uint16_t *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;
+    const int32_t* positions;
+    const float* cos_sin;
+    int n_positions, rot_dim;
+    const int32_t* row_start;
+    int n_requests;
+    uint16_t* q_out;
+    PagedView kv;
+    int rows, Hq, Hkv, q_len;
+    int warps_per_row;
+};
+
+// (a, b) -> (a c - b s, b c + a s) on two 8-element pieces.
+template <bool kInterleaved>
+__device__ __forceinline__ void rotate_pair(const uint4& lo, const uint4& hi, const float (&c)[8], const float (&s)[8],
+                                            float (&y)[8], float (&z)[8])
+{
+    float a[8], b[8];
+    unpack8(lo, a);
+    unpack8(hi, b);
+    if constexpr (kInterleaved) {  // pairs of neighbours: angles 0..3 are the first piece's, 4..7 the second's
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { c[i] = 1.f; s[i] = 0.f; }
-    const int half = rot_dim / 2;
-    if (rot_dim > 0) {
-        const int pos = __ldg(positions + row);
-        if (static_cast<unsigned>(pos) >= static_cast<unsigned>(n_positions)) {
-            if (threadIdx.x == 0) atomicMin(kv.status, MOSKA_ERR_INVALID_ARG);
-            return;
+        for (int i = 0; i < 4; ++i) {
+            y[2 * i] = __fsub_rn(__fmul_rn(a[2 * i], c[i]), __fmul_rn(a[2 * i + 1], s[i]));
+            y[2 * i + 1] = __fadd_rn(__fmul_rn(a[2 * i + 1], c[i]), __fmul_rn(a[2 * i], s[i]));
+            z[2 * i] = __fsub_rn(__fmul_rn(b[2 * i], c[4 + i]), __fmul_rn(b[2 * i + 1], s[4 + i]));
+            z[2 * i + 1] = __fadd_rn(__fmul_rn(b[2 * i + 1], c[4 + i]), __fmul_rn(b[2 * i], s[4 + i]));
         }
-        if (rotated) {
-            const float* cs = cos_sin + (int64_t)pos * rot_dim;
-            if (interleaved) {
-                const float4 a = __ldg(reinterpret_cast<const float4*>(cs + d0 / 2));
-                const float4 b = __ldg(reinterpret_cast<const float4*>(cs + half + d0 / 2));
-                c[0] = c[1] = a.x; c[2] = c[3] = a.y; c[4] = c[5] = a.z; c[6] = c[7] = a.w;
-                s[0] = s[1] = b.x; s[2] = s[3] = b.y; s[4] = s[5] = b.z; s[6] = s[7] = b.w;
-            } else {
-                const float* p = cs + (d0 < half ? d0 : d0 - half);
+    } else {  // the second piece is the first one's partner
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const float4 a = __ldg(reinterpret_cast<const float4*>(p + 4 * i));
-                    const float4 b = __ldg(reinterpret_cast<const float4*>(p + half + 4 * i));
-                    c[4 * i] = a.x; c[4 * i + 1] = a.y; c[4 * i + 2] = a.z; c[4 * i + 3] = a.w;
-                    s[4 * i] = b.x; s[4 * i + 1] = b.y; s[4 * i + 2] = b.z; s[4 * i + 3] = b.w;
-                }
-            }
+        for (int i = 0; i < 8; ++i) {
+            y[i] = __fsub_rn(__fmul_rn(a[i], c[i]), __fmul_rn(b[i], s[i]));
+            z[i] = __fadd_rn(__fmul_rn(b[i], c[i]), __fmul_rn(a[i], s[i]));
         }
     }
-    const bool first = d0 < half;
-    // eight rotated elements from `src` (this head's row)
-    auto load_rotated = [&](const uint16_t* src, float (&y)[8]) {
-        float x[8];
-        unpack8(__ldg(reinterpret_cast<const uint4*>(src + d0)), x);
-        if (!rotated) {
+}
+
+__device__ __forceinline__ void load4(const float* p, float* x)
+{
+    const float4 v = __ldg(reinterpret_cast<const float4*>(p));
+    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+}
+
+// A warp (or several, for few rows) per row.  Rotated or copied bf16 heads: D / 16 lanes a head, each with
+// two 8-element pieces that are each other's partners where the head is rotated, so an element is read
+// and widened once.  4-bit heads: D / 8 lanes a head with neighbouring pieces, because a scale covers 32
+// neighbouring dimensions; their partners come from the same lines again.
+// The first loads are on their way before it is known where the row goes.
+template <int D, bool kFp4, bool kInterleaved>
+__global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs a)
+{
+    const int lane = threadIdx.x & 31;
+    const int warp = blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5);
+    const int row = warp / a.warps_per_row, part = warp - row * a.warps_per_row;
+    if (row >= a.rows) return;
+    const int n_q = a.q != nullptr ? a.Hq : 0;
+    const int rot = a.rot_dim, half = rot / 2;
+    const uint16_t* q_row = a.q + row * a.q_stride;
+    const uint16_t* k_row = a.k + row * a.k_stride;
+    const uint16_t* v_row = a.v + row * a.v_stride;
+
+    constexpr int T = D / 16, kHeads = 32 / T;  // lanes of a head, heads of a pass
+    constexpr int kAhead = 4;                   // passes whose loads are in flight
+    const int n_k = n_q + (kFp4 ? 0 : a.Hkv), n_copy = n_k + (kFp4 ? 0 : a.Hkv);  // heads: queries, keys, values
+    const int passes = (n_copy + kHeads - 1) / kHeads;
+    const int t = lane % T;
+    const bool rotated = t < rot / 16;
+    // this lane's pieces
+    const int da = rotated ? 8 * t : rot + 16 * (t - rot / 16), db = rotated && !kInterleaved ? da + half : rotated ? half + 8 * t : da + 8;
+    uint4 lo[kAhead], hi[kAhead];
+    auto load = [&](int pass0) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = x[i];
-        } else if (interleaved) {
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                y[i] = __fsub_rn(__fmul_rn(x[i], c[i]), __fmul_rn(x[i + 1], s[i]));
-                y[i + 1] = __fadd_rn(__fmul_rn(x[i + 1], c[i]), __fmul_rn(x[i], s[i]));
-            }
-        } else {
-            float z[8];  // the partner half's eight elements
-            unpack8(__ldg(reinterpret_cast<const uint4*>(src + (first ? d0 + half : d0 - half))), z);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float a = __fmul_rn(x[i], c[i]), b = __fmul_rn(z[i], s[i]);
-                y[i] = first ? __fsub_rn(a, b) : __fadd_rn(a, b);
-            }
+        for (int u = 0; u < kAhead; ++u) {
+            const int i = (pass0 + u * a.warps_per_row) * kHeads + lane / T;
+            if (i >= n_copy) break;
+            const uint16_t* src = i < n_q ? q_row + i * D : i < n_k ? k_row + (i - n_q) * D : v_row + (i - n_k) * D;
+            lo[u] = __ldg(reinterpret_cast<const uint4*>(src + da));
+            hi[u] = __ldg(reinterpret_cast<const uint4*>(src + db));
         }
     };
+    load(part);
+    const int pos = rot > 0 ? __ldg(a.positions + row) : 0;
+    const bool known = rot == 0 || static_cast<unsigned>(pos) < static_cast<unsigned>(a.n_positions);
+    const float* table = a.cos_sin + (int64_t)(known ? pos : 0) * rot;
+    float c[8], s[8];
+    if (rotated) {
+        // angle of dimension d: d mod half, or d / 2 interleaved
+        const int fa = kInterleaved ? da / 2 : da, fb = kInterleaved ? db / 2 : da + 4;
+        load4(table + fa, c);
+        load4(table + fb, c + 4);
+        load4(table + half + fa, s);
+        load4(table + half + fb, s + 4);
+    }
+    const RowPlace at = place_row(a.kv, row, a.q_len, a.row_start, a.n_requests);
+    if (at.token < 0) return;  // padding
+    if (!known) {
+        if (lane == 0) atomicMin(a.kv.status, MOSKA_ERR_INVALID_ARG);
+        return;
+    }
+    const int slot = at.token & ((1 << a.kv.page_shift) - 1);  // row inside the page
+    const int64_t page_row = (((int64_t)at.page << a.kv.page_shift) + slot) * a.Hkv * D;  // bf16
 
-    const int slot = at.token & ((1 << kv.page_shift) - 1);  // row inside the page
-    const int n_q = q != nullptr ? Hq : 0, n_all = n_q + 2 * Hkv;
-    for (int i = blockIdx.y * kHeads + threadIdx.x / T; i < n_all; i += gridDim.y * kHeads) {
-        if (i < n_q) {
-            float y[8];
-            load_rotated(q + row * q_stride + (int64_t)i * D, y);
-            *reinterpret_cast<uint4*>(q_out + ((int64_t)row * Hq + i) * D + d0) = pack8(y);
-            continue;
+    for (int pass0 = part; pass0 < passes; pass0 += kAhead * a.warps_per_row) {
+        if (pass0 != part) load(pass0);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int i = (pass0 + u * a.warps_per_row) * kHeads + lane / T;
+            if (i >= n_copy) break;
+            if (rotated && i < n_k) {
+                float y[8], z[8];
+                rotate_pair<kInterleaved>(lo[u], hi[u], c, s, y, z);
+                lo[u] = pack8(y);
+                hi[u] = pack8(z);
+            }
+            uint16_t* to;
+            if (i < n_q) to = a.q_out + ((int64_t)row * a.Hq + i) * D;
+            else if (at.page < 0) break;
+            else if (i < n_k) to = reinterpret_cast<uint16_t*>(a.kv.k) + page_row + (i - n_q) * D;
+            else to = reinterpret_cast<uint16_t*>(a.kv.v) + page_row + (i - n_k) * D;
+            *reinterpret_cast<uint4*>(to + da) = lo[u];
+            *reinterpret_cast<uint4*>(to + db) = hi[u];
         }
-        const bool is_v = i >= n_q + Hkv;
-        const int h = i - n_q - (is_v ? Hkv : 0);
-        float y[8];
-        if (is_v) unpack8(__ldg(reinterpret_cast<const uint4*>(v + row * v_stride + (int64_t)h * D + d0)), y);
-        else load_rotated(k + row * k_stride + (int64_t)h * D, y);
-        if constexpr (!kFp4) {
-            if (at.page < 0) continue;
-            const int64_t to = ((((int64_t)at.page << kv.page_shift) + slot) * Hkv + h) * D + d0;
-            *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(is_v ? kv.v : kv.k) + to) = pack8(y);
-        } else {
-            using B = Fp4Block<D>;
-            // largest magnitude of the 32 dimensions (four neighbouring threads); a NaN or an infinity
-            // anywhere in them makes the sum of x - x NaN
-            float top = 0.f, odd = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                top = fmaxf(top, fabsf(y[e]));
-                odd += y[e] - y[e];
+    }
+    if constexpr (kFp4) {
+        if (at.page < 0) return;
+        using B = Fp4Block<D>;
+        constexpr int T4 = D / 8, kHeads4 = 32 / T4;
+        const int n_kv = 2 * a.Hkv, passes4 = (n_kv + kHeads4 - 1) / kHeads4;
+        const int t4 = lane % T4, d = 8 * t4;
+        const bool turned = d < rot, first = d < half;
+        const int d_other = kInterleaved ? d : first ? d + half : d - half;
+        float c4[8], s4[8];  // interleaved: four angles
+        if (turned) {
+            const int f = kInterleaved ? d / 2 : first ? d : d - half;
+            load4(table + f, c4);
+            load4(table + half + f, s4);
+            if constexpr (!kInterleaved) {
+                load4(table + f + 4, c4 + 4);
+                load4(table + half + f + 4, s4 + 4);
             }
-            const unsigned group = 0xfu << (threadIdx.x & 28);
+        }
+        const int tok = slot & (kBlockTokens - 1);
+        uint8_t* blocks = a.kv.k + ((((int64_t)at.page * a.Hkv) << (a.kv.page_shift - 4)) + (slot >> 4)) * B::kBytes;
+        const int64_t head_bytes = (int64_t)B::kBytes << (a.kv.page_shift - 4);
+        // the parts that have no bf16 pass left over begin
+        for (int pass = (part + a.warps_per_row - passes % a.warps_per_row) % a.warps_per_row; pass < passes4;
+             pass += a.warps_per_row) {
+            const int i = pass * kHeads4 + lane / T4;
+            const bool live = i < n_kv, is_v = i >= a.Hkv;
+            const int h = is_v ? i - a.Hkv : i;
+            float y[8];
 #pragma unroll
-            for (int off = 1; off < 4; off <<= 1) {
-                top = fmaxf(top, __shfl_xor_sync(group, top, off));
-                odd += __shfl_xor_sync(group, odd, off);
+            for (int e = 0; e < 8; ++e) y[e] = 0.f;
+            if (live) {
+                const uint16_t* src = (is_v ? v_row : k_row) + h * D;
+                unpack8(__ldg(reinterpret_cast<const uint4*>(src + d)), y);
+                if (turned && !is_v) {
+                    float x[8], z[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = y[e];
+                    if constexpr (kInterleaved) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            y[2 * e] = __fsub_rn(__fmul_rn(x[2 * e], c4[e]), __fmul_rn(x[2 * e + 1], s4[e]));
+                            y[2 * e + 1] = __fadd_rn(__fmul_rn(x[2 * e + 1], c4[e]), __fmul_rn(x[2 * e], s4[e]));
+                        }
+                    } else {
+                        unpack8(__ldg(reinterpret_cast<const uint4*>(src + d_other)), z);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float p = __fmul_rn(x[e], c4[e]), o = __fmul_rn(z[e], s4[e]);
+                            y[e] = first ? __fsub_rn(p, o) : __fadd_rn(p, o);
+                        }
+                    }
+                }
             }
-            const __half sh = __float2half_rn(fminf(__fdiv_rn(top, 6.f), kFp4MaxScale) + odd);
-            const float sf = __half2float(sh);
-            uint32_t w = 0;
+            // largest magnitude of the 32 dimensions (four neighbouring lanes), NaN if one is
+            float top = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w |= e2m1_code(y[e], sf) << (4 * e);
-            if (at.page < 0) continue;
-            const int tok = slot & (kBlockTokens - 1);
-            uint8_t* blk = kv.k + ((((int64_t)at.page * Hkv + h) << (kv.page_shift - 4)) + (slot >> 4)) * B::kBytes;
-            *reinterpret_cast<uint32_t*>(blk + (is_v ? B::v_byte(tok, d0) : B::k_byte(tok, d0))) = w;
-            if ((t & 3) == 0)
-                *reinterpret_cast<__half*>(blk + (is_v ? B::v_scale(tok, t >> 2) : B::k_scale(tok, t >> 2))) = sh;
+            for (int e = 0; e < 8; ++e) top = max_or_nan(top, fabsf(y[e]));
+            top = max_or_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max_or_nan(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const float scale = top < INFINITY ? fminf(__fdiv_rn(top, 6.f), kFp4MaxScale) : NAN;
+            const __half sh = __float2half_rn(scale);
+            const uint32_t w = e2m1x8(y, __half2float(sh));
+            if (!live) continue;
+            uint8_t* blk = blocks + h * head_bytes;
+            *reinterpret_cast<uint32_t*>(blk + (is_v ? B::v_byte(tok, d) : B::k_byte(tok, d))) = w;
+            if ((t4 & 3) == 0)
+                *reinterpret_cast<__half*>(blk + (is_v ? B::v_scale(tok, t4 >> 2) : B::k_scale(tok, t4 >> 2))) = sh;
         }
     }
 }
@@ -284,15 +391,25 @@ int launch_append_paged(const uint16_t* q, int64_t q_stride, const uint16_t* k, 
                         const PagedView& kv, bool fp4, const moska_shape* s, cudaStream_t st)
 {
     if (s->B == 0) return MOSKA_OK;
-    const int q_len = s->q_len > 1 ? s->q_len : 1;
-    const dim3 grid = row_grid(s->B, (q != nullptr ? s->Hq : 0) + 2 * s->Hkv, kAppendThreads / (s->D / 8));
-    auto go = [&](auto kernel) {
-        kernel<<<grid, kAppendThreads, 0, st>>>(q, q_stride, k, k_stride, v, v_stride, positions, cos_sin, n_positions,
-                                                rot_dim, interleaved, row_start, n_requests, q_out, kv, s->Hq, s->Hkv,
-                                                q_len);
-    };
-    if (s->D == 128) fp4 ? go(append_kernel<128, true>) : go(append_kernel<128, false>);
-    else fp4 ? go(append_kernel<64, true>) : go(append_kernel<64, false>);
+    // one warp a row; few rows: several, until every SM has a CTA of work or a warp has one pass of heads
+    const int heads = (q != nullptr ? s->Hq : 0) + 2 * s->Hkv;
+    const int passes = (heads * (s->D / 16) + 31) / 32;
+    long long per_row = (148LL * 16 + s->B - 1) / s->B;
+    if (per_row > passes) per_row = passes;
+    const AppendArgs args{q, k, v, q_stride, k_stride, v_stride, positions, cos_sin, n_positions, rot_dim, row_start,
+                          n_requests, q_out, kv, s->B, s->Hq, s->Hkv, s->q_len > 1 ? s->q_len : 1, (int)per_row};
+    constexpr int kWarpsPerCta = kAppendThreads / 32;
+    const long long warps = s->B * per_row;
+    const unsigned grid = (unsigned)((warps + kWarpsPerCta - 1) / kWarpsPerCta);
+    if (warps > 0x7fffffffLL) return fail(MOSKA_ERR_UNSUPPORTED, "too many rows");
+    auto go = [&](auto kernel) { kernel<<<grid, kAppendThreads, 0, st>>>(args); };
+    if (s->D == 128) {
+        if (interleaved) fp4 ? go(append_kernel<128, true, true>) : go(append_kernel<128, false, true>);
+        else fp4 ? go(append_kernel<128, true, false>) : go(append_kernel<128, false, false>);
+    } else {
+        if (interleaved) fp4 ? go(append_kernel<64, true, true>) : go(append_kernel<64, false, true>);
+        else fp4 ? go(append_kernel<64, true, false>) : go(append_kernel<64, false, false>);
+    }
     MOSKA_LAUNCH_CHECK("append_kernel");
     return MOSKA_OK;
 }
