@@ -281,38 +281,43 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs
         const int tok = slot & (kBlockTokens - 1);
         uint8_t* blocks = a.kv.k + ((((int64_t)at.page * a.Hkv) << (a.kv.page_shift - 4)) + (slot >> 4)) * B::kBytes;
         const int64_t head_bytes = (int64_t)B::kBytes << (a.kv.page_shift - 4);
-        // the parts that have no bf16 pass left over begin
-        for (int pass = (part + a.warps_per_row - passes % a.warps_per_row) % a.warps_per_row; pass < passes4;
-             pass += a.warps_per_row) {
+        // the parts that have no bf16 pass left over begin; a pass's loads are one pass ahead
+        int pass = (part + a.warps_per_row - passes % a.warps_per_row) % a.warps_per_row;
+        uint4 own = make_uint4(0, 0, 0, 0), other = own;
+        auto load_kv = [&](int p) {
+            const int i = p * kHeads4 + lane / T4;
+            if (i >= n_kv) return;
+            const uint16_t* src = i >= a.Hkv ? v_row + (i - a.Hkv) * D : k_row + i * D;
+            own = __ldg(reinterpret_cast<const uint4*>(src + d));
+            if (!kInterleaved && turned && i < a.Hkv) other = __ldg(reinterpret_cast<const uint4*>(src + d_other));
+        };
+        load_kv(pass);
+        for (; pass < passes4; pass += a.warps_per_row) {
             const int i = pass * kHeads4 + lane / T4;
             const bool live = i < n_kv, is_v = i >= a.Hkv;
             const int h = is_v ? i - a.Hkv : i;
-            float y[8];
+            float x[8], y[8];
+            unpack8(own, x);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = 0.f;
-            if (live) {
-                const uint16_t* src = (is_v ? v_row : k_row) + h * D;
-                unpack8(__ldg(reinterpret_cast<const uint4*>(src + d)), y);
-                if (turned && !is_v) {
-                    float x[8], z[8];
+            for (int e = 0; e < 8; ++e) y[e] = x[e];
+            if (turned && !is_v) {
+                if constexpr (kInterleaved) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = y[e];
-                    if constexpr (kInterleaved) {
+                    for (int e = 0; e < 4; ++e) {
+                        y[2 * e] = __fsub_rn(__fmul_rn(x[2 * e], c4[e]), __fmul_rn(x[2 * e + 1], s4[e]));
+                        y[2 * e + 1] = __fadd_rn(__fmul_rn(x[2 * e + 1], c4[e]), __fmul_rn(x[2 * e], s4[e]));
+                    }
+                } else {
+                    float z[8];
+                    unpack8(other, z);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            y[2 * e] = __fsub_rn(__fmul_rn(x[2 * e], c4[e]), __fmul_rn(x[2 * e + 1], s4[e]));
-                            y[2 * e + 1] = __fadd_rn(__fmul_rn(x[2 * e + 1], c4[e]), __fmul_rn(x[2 * e], s4[e]));
-                        }
-                    } else {
-                        unpack8(__ldg(reinterpret_cast<const uint4*>(src + d_other)), z);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float p = __fmul_rn(x[e], c4[e]), o = __fmul_rn(z[e], s4[e]);
-                            y[e] = first ? __fsub_rn(p, o) : __fadd_rn(p, o);
-                        }
+                    for (int e = 0; e < 8; ++e) {
+                        const float p = __fmul_rn(x[e], c4[e]), o = __fmul_rn(z[e], s4[e]);
+                        y[e] = first ? __fsub_rn(p, o) : __fadd_rn(p, o);
                     }
                 }
             }
+            load_kv(pass + a.warps_per_row);
             // largest magnitude of the 32 dimensions (four neighbouring lanes), NaN if one is
             float top = 0.f;
 #pragma unroll
@@ -331,56 +336,77 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs
     }
 }
 
+// Warps of a row of append or gather: one for many rows; for few rows several, until every SM has sixteen
+// warps or a warp has one pass of heads left.
+int warps_per_row(int rows, int passes)
+{
+    const long long n = (148LL * 16 + rows - 1) / rows;
+    return (int)(n < passes ? n : passes);
+}
+
+// Reading rows back: a warp (or several) per row, D / 8 lanes a head, eight elements a lane.
 template <int D, bool kFp4>
 __global__ void __launch_bounds__(kAppendThreads)
 gather_kernel(const int32_t* __restrict__ row_start, int n_requests, uint16_t* __restrict__ k_out,
-              uint16_t* __restrict__ v_out, PagedView kv, int Hkv, int q_len)
+              uint16_t* __restrict__ v_out, PagedView kv, int rows, int Hkv, int q_len, int per_row)
 {
-    constexpr int T = D / 8, kHeads = kAppendThreads / T;
-    const int row = blockIdx.x;
-    const int t = threadIdx.x % T, d0 = 8 * t;
+    constexpr int T = D / 8, kHeads = 32 / T, kAhead = 4;
+    const int lane = threadIdx.x & 31;
+    const int warp = blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5);
+    const int row = warp / per_row, part = warp - row * per_row;
+    if (row >= rows) return;
+    const int t = lane % T, d = 8 * t;
     const RowPlace at = place_row(kv, row, q_len, row_start, n_requests);
-    if (at.token < 0) return;
-    if (at.page < 0) return;  // an index outside the pool has been reported
-    const int page = at.page;
+    if (at.token < 0 || at.page < 0) return;  // padding; an index outside the pool has been reported
     const int slot = at.token & ((1 << kv.page_shift) - 1);
-    for (int i = blockIdx.y * kHeads + threadIdx.x / T; i < 2 * Hkv; i += gridDim.y * kHeads) {
-        const bool is_v = i >= Hkv;
-        const int h = is_v ? i - Hkv : i;
-        uint4 y;
-        if constexpr (!kFp4) {
-            const int64_t from = ((((int64_t)page << kv.page_shift) + slot) * Hkv + h) * D + d0;
-            y = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(is_v ? kv.v : kv.k) + from));
-        } else {
-            using B = Fp4Block<D>;
-            const int tok = slot & (kBlockTokens - 1);
-            const uint8_t* blk = kv.k + ((((int64_t)page * Hkv + h) << (kv.page_shift - 4)) + (slot >> 4)) * B::kBytes;
-            const uint32_t w =
-                __ldg(reinterpret_cast<const uint32_t*>(blk + (is_v ? B::v_byte(tok, d0) : B::k_byte(tok, d0))));
-            const float s =
-                __half2float(*reinterpret_cast<const __half*>(blk + (is_v ? B::v_scale(tok, t >> 2) : B::k_scale(tok, t >> 2))));
-            uint32_t f[4];
-            e2m1x8_to_f16x2(w, f);
-            float x[8];
+    const int passes = (2 * Hkv + kHeads - 1) / kHeads;
+    using B = Fp4Block<D>;
+    const int tok = slot & (kBlockTokens - 1);
+    const uint8_t* blocks = kv.k + ((((int64_t)at.page * Hkv) << (kv.page_shift - 4)) + (slot >> 4)) * B::kBytes;
+    const int64_t head_bytes = (int64_t)B::kBytes << (kv.page_shift - 4);
+    const int64_t page_row = (((int64_t)at.page << kv.page_shift) + slot) * Hkv * D;  // bf16
+    const int k_at = B::k_byte(tok, d), v_at = B::v_byte(tok, d), ks_at = B::k_scale(tok, t >> 2), vs_at = B::v_scale(tok, t >> 2);
+    for (int pass0 = part; pass0 < passes; pass0 += kAhead * per_row) {
+        uint4 raw[kAhead];
+        uint32_t code[kAhead];
+        __half scale[kAhead];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&f[e]));
-                x[2 * e] = p.x * s;
-                x[2 * e + 1] = p.y * s;
+        for (int u = 0; u < kAhead; ++u) {
+            const int i = (pass0 + u * per_row) * kHeads + lane / T;
+            if (i >= 2 * Hkv) break;
+            const bool is_v = i >= Hkv;
+            const int h = is_v ? i - Hkv : i;
+            if constexpr (kFp4) {
+                const uint8_t* blk = blocks + h * head_bytes;
+                code[u] = __ldg(reinterpret_cast<const uint32_t*>(blk + (is_v ? v_at : k_at)));
+                scale[u] = __ldg(reinterpret_cast<const __half*>(blk + (is_v ? vs_at : ks_at)));
+            } else {
+                raw[u] = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(is_v ? kv.v : kv.k) +
+                                                              page_row + h * D + d));
             }
-            y = pack8(x);
         }
-        *reinterpret_cast<uint4*>((is_v ? v_out : k_out) + ((int64_t)row * Hkv + h) * D + d0) = y;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int i = (pass0 + u * per_row) * kHeads + lane / T;
+            if (i >= 2 * Hkv) break;
+            const bool is_v = i >= Hkv;
+            const int h = is_v ? i - Hkv : i;
+            if constexpr (kFp4) {
+                const float s = __half2float(scale[u]);
+                uint32_t f[4];
+                e2m1x8_to_f16x2(code[u], f);
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&f[e]));
+                    x[2 * e] = p.x * s;
+                    x[2 * e + 1] = p.y * s;
+                }
+                raw[u] = pack8(x);
+            }
+            *reinterpret_cast<uint4*>((is_v ? v_out : k_out) + ((int64_t)row * Hkv + h) * D + d) = raw[u];
+        }
     }
-}
-
-// One CTA a row as long as there are rows for every SM; few rows: their heads over several CTAs.
-dim3 row_grid(int rows, int heads, int heads_per_pass)
-{
-    const int passes = (heads + heads_per_pass - 1) / heads_per_pass;
-    int y = (148 * 4 + rows - 1) / rows;
-    if (y > passes) y = passes;
-    return dim3((unsigned)rows, (unsigned)(y < 1 ? 1 : y));
 }
 
 }  // namespace
@@ -391,15 +417,12 @@ int launch_append_paged(const uint16_t* q, int64_t q_stride, const uint16_t* k, 
                         const PagedView& kv, bool fp4, const moska_shape* s, cudaStream_t st)
 {
     if (s->B == 0) return MOSKA_OK;
-    // one warp a row; few rows: several, until every SM has a CTA of work or a warp has one pass of heads
     const int heads = (q != nullptr ? s->Hq : 0) + 2 * s->Hkv;
-    const int passes = (heads * (s->D / 16) + 31) / 32;
-    long long per_row = (148LL * 16 + s->B - 1) / s->B;
-    if (per_row > passes) per_row = passes;
+    const int per_row = warps_per_row(s->B, (heads * (s->D / 16) + 31) / 32);
     const AppendArgs args{q, k, v, q_stride, k_stride, v_stride, positions, cos_sin, n_positions, rot_dim, row_start,
-                          n_requests, q_out, kv, s->B, s->Hq, s->Hkv, s->q_len > 1 ? s->q_len : 1, (int)per_row};
+                          n_requests, q_out, kv, s->B, s->Hq, s->Hkv, s->q_len > 1 ? s->q_len : 1, per_row};
     constexpr int kWarpsPerCta = kAppendThreads / 32;
-    const long long warps = s->B * per_row;
+    const long long warps = (long long)s->B * per_row;
     const unsigned grid = (unsigned)((warps + kWarpsPerCta - 1) / kWarpsPerCta);
     if (warps > 0x7fffffffLL) return fail(MOSKA_ERR_UNSUPPORTED, "too many rows");
     auto go = [&](auto kernel) { kernel<<<grid, kAppendThreads, 0, st>>>(args); };
@@ -419,9 +442,13 @@ int launch_gather_paged(const int32_t* row_start, int n_requests, uint16_t* k_ou
 {
     if (s->B == 0) return MOSKA_OK;
     const int q_len = s->q_len > 1 ? s->q_len : 1;
-    const dim3 grid = row_grid(s->B, 2 * s->Hkv, kAppendThreads / (s->D / 8));
+    const int per_row = warps_per_row(s->B, (2 * s->Hkv * (s->D / 8) + 31) / 32);
+    constexpr int kWarpsPerCta = kAppendThreads / 32;
+    const long long warps = (long long)s->B * per_row;
+    if (warps > 0x7fffffffLL) return fail(MOSKA_ERR_UNSUPPORTED, "too many rows");
+    const unsigned grid = (unsigned)((warps + kWarpsPerCta - 1) / kWarpsPerCta);
     auto go = [&](auto kernel) {
-        kernel<<<grid, kAppendThreads, 0, st>>>(row_start, n_requests, k_out, v_out, kv, s->Hkv, q_len);
+        kernel<<<grid, kAppendThreads, 0, st>>>(row_start, n_requests, k_out, v_out, kv, s->B, s->Hkv, q_len, per_row);
     };
     if (s->D == 128) fp4 ? go(gather_kernel<128, true>) : go(gather_kernel<128, false>);
     else fp4 ? go(gather_kernel<64, true>) : go(gather_kernel<64, false>);
