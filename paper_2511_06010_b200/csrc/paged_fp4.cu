@@ -335,12 +335,23 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
                     oacc[n][mt][3] *= alpha[n][1];
                 }
         }
-        // ---- O^T += V^T P.  A unit whose tokens not every row sees is passed once for each query token over
-        // the values that it sees, kept in its columns only: 0 times a NaN behind a row's context is NaN.
+        // ---- O^T += V^T P.  Where a token that not every row sees holds NaN, the block is passed once for each
+        // query token over the values that it sees, kept in its columns only: 0 times NaN is NaN.
         // (Rows behind the whole context hold anything; codes are finite, so zero scales make them 0.)
-        const int passes = tail ? q_len : 1;
+        int passes = 1;
+        if constexpr (tail) {
+            // (SUB is 1 here) a scale above the largest that append writes, infinities and NaN included
+            uint32_t s0[1], s1[1];
+            lds_words<1>(at + B::v_scale(2 * c, g * J / 8), s0);
+            lds_words<1>(at + B::v_scale(2 * c + 8, g * J / 8), s1);
+            const int t = t0 + 2 * c;
+            auto odd = [&](uint32_t bits, int tok) { return (bits & 0x7fffu) > 0x7154u && tok >= all_see && tok < t_end; };
+            const bool bad = odd(s0[0], t) || odd(s0[0] >> 16, t + 1) || odd(s1[0], t + 8) || odd(s1[0] >> 16, t + 9);
+            if (__any_sync(0xffffffffu, bad)) passes = q_len;
+        }
         for (int pass = 0; pass < passes; ++pass) {
-            const int limit = len - (q_len - 1 - pass);  // tail: values of tokens from here on are hidden
+            // tail: values of tokens from here on are hidden
+            const int limit = passes == 1 ? len : len - (q_len - 1 - pass);
 #pragma unroll
             for (int b = 0; b < SUB; ++b) {
                 const uint32_t blk = at + b * B::kBytes;
@@ -384,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
                             float(&acc)[4] = oacc[n][4 * w + e];
-                            if constexpr (!tail) {
+                            if (!tail || passes == 1) {
                                 mma_f16(acc, a0, a1, a2, a3, pb0[n], pb1[n]);
                             } else {
                                 float x[4] = {acc[0], acc[1], acc[2], acc[3]};
