@@ -494,8 +494,9 @@ typedef struct moska_paged_kv {
  * field is out of range.  Host only, pure. */
 size_t moska_paged_pool_bytes(int32_t format, int32_t n_pages, int32_t page_size, int32_t Hkv, int32_t D);
 
-/* A reasonable n_unique_splits for the 4-bit store (for bf16 pages: moska_default_unique_splits). */
-int moska_default_unique_splits_fp4(int32_t B, int32_t Hkv, int32_t max_len);
+/* A reasonable n_unique_splits for a paged store whose longest context has `max_len` tokens.  Host
+ * only, pure. */
+int moska_default_paged_splits(int32_t format, int32_t n_requests, int32_t Hkv, int32_t D, int32_t max_len);
 
 /*
  * Appends new tokens to a paged store, with the position rotation applied on the way.  For every new

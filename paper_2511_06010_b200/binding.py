@@ -78,7 +78,7 @@ EXPORTS = {
     "moska_decode_step_host": (_i, [_vp] * 16 + [_f, _sp, _vp, _sz, _vp, _vp, _vp]),
     "moska_decode_step_fp8_host": (_i, [_vp] * 20 + [_f, _sp, _vp, _sz, _vp, _vp, _vp]),
     "moska_paged_pool_bytes": (_sz, [ctypes.c_int32] * 5),
-    "moska_default_unique_splits_fp4": (_i, [ctypes.c_int32] * 3),
+    "moska_default_paged_splits": (_i, [ctypes.c_int32] * 5),
     "moska_kv_append_paged": (_i, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp] + [ctypes.c_int32] * 3 +
                               [_vp, ctypes.c_int32, _vp, _kvp, _sp, _vp]),
     "moska_kv_gather_paged": (_i, [_vp, ctypes.c_int32, _vp, _vp, _kvp, _sp, _vp]),
@@ -373,8 +373,8 @@ def paged_pool_bytes(fmt: int, n_pages: int, page_size: int, Hkv: int, D: int) -
     return _lib.moska_paged_pool_bytes(fmt, n_pages, page_size, Hkv, D)
 
 
-def default_unique_splits_fp4(B: int, Hkv: int, max_len: int) -> int:
-    return _lib.moska_default_unique_splits_fp4(B, Hkv, max_len)
+def default_paged_splits(fmt: int, n_requests: int, Hkv: int, D: int, max_len: int) -> int:
+    return _lib.moska_default_paged_splits(fmt, n_requests, Hkv, D, max_len)
 
 
 def kv_append_paged(q, q_stride, k, k_stride, v, v_stride, positions, cos_sin, n_positions, rot_dim, interleaved,

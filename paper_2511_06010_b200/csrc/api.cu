@@ -1008,9 +1008,22 @@ size_t moska_paged_pool_bytes(int32_t format, int32_t n_pages, int32_t page_size
     return 0;
 }
 
-int moska_default_unique_splits_fp4(int32_t B, int32_t Hkv, int32_t max_len)
+int moska_default_paged_splits(int32_t format, int32_t n_requests, int32_t Hkv, int32_t D, int32_t max_len)
 {
-    return moska_default_unique_splits_fp8(B, Hkv, max_len);
+    // A CTA has fixed costs (its length, its first page and its first copies one after another, the join of
+    // its warps), so that splits cost about as much as they balance: the smallest sum, as for the FP8
+    // store, at s = sqrt(a len slots / (n ov)) with a = 0.7 and fixed costs of ov tokens that fit the
+    // sweeps (bf16: 1 at 64 contexts of 4096 tokens and 8 heads, 154 against 167 us at 2 and 170 at 4; 4-6 at
+    // 64 of 1K to 32K.  4 bits: 1-2, 6, and 12-16 at one context of 8191), and 512 tokens at least.
+    if (n_requests <= 0 || Hkv <= 0 || max_len <= 0) return 1;
+    const bool fp4 = format == MOSKA_KV_FP4;
+    const double len = max_len * (D == 64 ? 0.5 : 1.0), slots = 148.0 * (fp4 ? 3.0 : 2.0);
+    long long s = llround(sqrt(0.7 * len * slots / ((double)n_requests * Hkv * (fp4 ? 620.0 : 780.0))));
+    const long long cap = ((long long)max_len + 511) / 512;
+    if (s > cap) s = cap;
+    if (s < 1) s = 1;
+    if (s > 64) s = 64;
+    return (int)s;
 }
 
 int moska_kv_append_paged(const uint16_t* q, int64_t q_stride, const uint16_t* k, int64_t k_stride,
@@ -1120,9 +1133,7 @@ int moska_paged_attn(const uint16_t* q, const moska_paged_kv* kv, uint16_t* out,
     const size_t o_bytes = (size_t)shape->B * shape->Hq * shape->n_unique_splits * shape->D * sizeof(float);
     float* lse_part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + round_up(o_bytes, 256));
     MOSKA_TRY(attend(q, view, o_part, lse_part, 0, shape->n_unique_splits, nullptr, nullptr, softmax_scale, shape, st));
-    moska_shape slots = *shape;
-    slots.shared_slots = 0;
-    return launch_merge(o_part, lse_part, out, nullptr, lse_out, &slots, st);
+    return launch_paged_merge(o_part, lse_part, out, lse_out, shape, st);
 }
 
 int moska_decode_step_paged(const uint16_t* q, const float* summaries, const void* k_shared,

@@ -176,6 +176,9 @@ int launch_gather_paged(const int32_t* row_start, int n_requests, uint16_t* k_ou
 // needs n_unique_splits = 1
 int launch_paged_bf16(const uint16_t* q, const PagedView& kv, float* o_part, float* lse_part, int slot0, int n_slots,
                       uint16_t* out, float* lse_out, float scale, const moska_shape* s, cudaStream_t st);
+// the final rows from n_unique_splits partial ones, launched early behind one of the two kernels above
+int launch_paged_merge(const float* o_part, const float* lse_part, uint16_t* out, float* lse_out, const moska_shape* s,
+                       cudaStream_t st);
 int launch_paged_fp4(const uint16_t* q, const PagedView& kv, float* o_part, float* lse_part, int slot0, int n_slots,
                      uint16_t* out, float* lse_out, float scale, const moska_shape* s, cudaStream_t st);
 

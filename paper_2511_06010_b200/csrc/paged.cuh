@@ -71,6 +71,11 @@ __device__ __forceinline__ int paged_page(const PagedView& p, const int32_t* row
     return 0;
 }
 
+// The merge behind an attention kernel is launched while that one runs (programmatic dependent launch):
+// its own launch is hidden, and it waits for the results itself.
+__device__ __forceinline__ void dependents_may_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_results() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // Two E2M1 codes a byte -> two f16 values, exact; the four bytes of w give o[0..3].
 __device__ __forceinline__ void e2m1x8_to_f16x2(uint32_t w, uint32_t (&o)[4])
 {

@@ -51,6 +51,7 @@ __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 3) paged_bf16_kernel(
     const int h = blockIdx.x % a.Hkv;
     const int sp = (blockIdx.x / a.Hkv) % a.n_splits;
     const int r = blockIdx.x / (a.Hkv * a.n_splits);
+    dependents_may_launch();
     const int len = paged_len(a.kv, r);
     if (threadIdx.x < NT * 8) {
         const int j = threadIdx.x;
@@ -79,7 +80,67 @@ __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 3) paged_bf16_kernel(
         attend_stream<D, NT>(rows, kb, vb, stride, t0, t1, a.scale, *reinterpret_cast<CombineSmem<D, NT>*>(ring), tokens);
 }
 
+// Final rows from the partial rows of n splits (up to 64): a warp per row, D / 32 dimensions a lane; lane
+// i holds the weight of splits i and i + 32.
+template <int D>
+__global__ void __launch_bounds__(128)
+paged_merge_kernel(const float* __restrict__ o_part, const float* __restrict__ lse_part, uint16_t* __restrict__ out,
+                   float* __restrict__ lse_out, int rows, int n)
+{
+    constexpr int W = D / 32;
+    const int lane = threadIdx.x & 31;
+    const int row = blockIdx.x * 4 + (threadIdx.x >> 5);
+    wait_for_results();
+    if (row >= rows) return;
+    const float* lse = lse_part + (int64_t)row * n;
+    const float* o = o_part + (int64_t)row * n * D + W * lane;
+    float l[2] = {lane < n ? lse[lane] : -INFINITY, lane + 32 < n ? lse[lane + 32] : -INFINITY};
+    float M = max_or_nan(l[0], l[1]);
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) M = max_or_nan(M, __shfl_xor_sync(0xffffffffu, M, off));
+    float acc[W], total = 0.f;
+#pragma unroll
+    for (int e = 0; e < W; ++e) acc[e] = 0.f;
+    if (M != -INFINITY) {
+        const float w[2] = {__expf(l[0] - M), __expf(l[1] - M)};
+#pragma unroll 8
+        for (int i = 0; i < n; ++i) {
+            const float wi = __shfl_sync(0xffffffffu, i < 32 ? w[0] : w[1], i & 31);
+            total += wi;
+#pragma unroll
+            for (int e = 0; e < W; ++e) acc[e] = fmaf(wi, o[(int64_t)i * D + e], acc[e]);
+        }
+        const float inv = 1.f / total;
+#pragma unroll
+        for (int e = 0; e < W; ++e) acc[e] *= inv;
+    }
+#pragma unroll
+    for (int e = 0; e < W; e += 2)
+        *reinterpret_cast<__nv_bfloat162*>(out + (int64_t)row * D + W * lane + e) = __floats2bfloat162_rn(acc[e], acc[e + 1]);
+    if (lane == 0 && lse_out != nullptr) lse_out[row] = M == -INFINITY ? -INFINITY : M + logf(total);
+}
+
 }  // namespace
+
+int launch_paged_merge(const float* o_part, const float* lse_part, uint16_t* out, float* lse_out, const moska_shape* s,
+                       cudaStream_t st)
+{
+    const long long rows = (long long)s->B * s->Hq;
+    if (rows == 0) return MOSKA_OK;
+    if (rows > 0x7fffffffLL) return fail(MOSKA_ERR_UNSUPPORTED, "too many rows");
+    cudaLaunchConfig_t config{};
+    config.gridDim = dim3((unsigned)((rows + 3) / 4));
+    config.blockDim = dim3(128);
+    config.stream = st;
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    config.attrs = &early;
+    config.numAttrs = 1;
+    MOSKA_CUDA_TRY(cudaLaunchKernelEx(&config, s->D == 128 ? paged_merge_kernel<128> : paged_merge_kernel<64>, o_part,
+                                      lse_part, out, lse_out, (int)rows, (int)s->n_unique_splits));
+    return MOSKA_OK;
+}
 
 // `out` == nullptr: partial slots slot0 .. of n_slots; else the final rows (one split).
 int launch_paged_bf16(const uint16_t* q, const PagedView& kv, float* o_part, float* lse_part, int slot0, int n_slots,

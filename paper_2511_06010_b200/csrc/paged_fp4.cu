@@ -27,7 +27,7 @@ constexpr int kSub = 4;  // blocks of a unit
 
 template <int D>
 struct F4Ring {
-    static constexpr int kDepth = D == 128 ? 2 : 4;  // units in flight per warp
+    static constexpr int kDepth = 2;  // units in flight per warp
     static constexpr int kUnitBytes = kSub * Fp4Block<D>::kBytes;
     static constexpr int kBytes = kWarps * kDepth * kUnitBytes;
 };
@@ -102,8 +102,13 @@ struct AttnArgs {
     int Hq, Hkv, n_splits, slot0, n_slots, q_len;
 };
 
+// CTAs per SM.  D = 128: 154 registers (a fourth CTA would need 128: spills, slower).  D = 64: 113; four
+// take 24 us over 128 contexts of 2000 tokens where three take 33.  Two column blocks: 200-255 registers.
 template <int D, int NT>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(const AttnArgs a)
+constexpr int kCtasPerSm = NT == 2 ? 2 : D == 128 ? 3 : 4;
+
+template <int D, int NT>
+__global__ void __launch_bounds__(kThreads, kCtasPerSm<D, NT>) paged_fp4_kernel(const AttnArgs a)
 {
     using B = Fp4Block<D>;
     constexpr int J = B::kGroups, MT = D / 16;
@@ -120,6 +125,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2) paged_fp4_kernel(co
     const int r = blockIdx.x / (a.Hkv * a.n_splits);
     const int q_len = a.q_len, n_rows = q_len * G;
 
+    dependents_may_launch();
     if (threadIdx.x == 0) gave_up = 0;
     if (threadIdx.x < kRows) {
         const int j = threadIdx.x;

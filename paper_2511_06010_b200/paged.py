@@ -196,8 +196,7 @@ class PagedAttention:
         """B counts batch rows: B / q_len requests of q_len query tokens; max_len: longest context."""
         self.fmt = fmt
         if n_unique_splits is None:
-            default = {"bf16": M.default_unique_splits, "fp4": M.default_unique_splits_fp4}[fmt]
-            n_unique_splits = default(B // max(1, q_len), Hkv, max(1, max_len))
+            n_unique_splits = M.default_paged_splits(FORMATS[fmt], B // max(1, q_len), Hkv, D, max(1, max_len))
         self.shape = _shape(B, Hq, Hkv, D, n_unique_splits, q_len)
         self.scale = 1.0 / math.sqrt(D)
         self.out = torch.empty(B, Hq, D, dtype=torch.bfloat16, device=device)
@@ -216,6 +215,8 @@ class PagedAttention:
         if store._index != index:
             raise ValueError(f"the store is on {store.device}, the results on {self.out.device}")
         kv = store.kv(page_table, kv_len)
+        if not self._requests:
+            return self.out, self.lse
         if page_table.shape[0] != self._requests:
             raise ValueError(f"{page_table.shape[0]} page-table rows for {self._requests} requests")
         _call(_attend, "moska_paged_attn", index, _dense(q, "q", torch.bfloat16, self.out.shape, index),

@@ -108,8 +108,10 @@ def test_pool_sizes_and_splits(M):
     assert M.paged_pool_bytes(M.KV_FP4, 100000, 1024, 8, 128) == 100000 * 64 * 8 * 18 * 128  # beyond 32 bits
     for bad in ((2, 3, 32, 8, 128), (0, 0, 32, 8, 128), (0, 3, 24, 8, 128), (0, 3, 32, 0, 128), (0, 3, 32, 8, 96)):
         assert M.paged_pool_bytes(*bad) == 0
-    assert M.default_unique_splits_fp4(0, 8, 100) == 1
-    assert 1 <= M.default_unique_splits_fp4(1, 8, 1 << 20) <= 64
+    for fmt in (M.KV_BF16, M.KV_FP4):
+        assert M.default_paged_splits(fmt, 0, 8, 128, 100) == 1 and M.default_paged_splits(fmt, 4, 8, 128, 0) == 1
+        assert M.default_paged_splits(fmt, 1000, 8, 128, 500) == 1 and M.default_paged_splits(fmt, 1, 8, 64, 512) == 1
+        assert 1 < M.default_paged_splits(fmt, 1, 8, 128, 8191) <= 16 and M.default_paged_splits(fmt, 1, 1, 128, 1 << 30) == 64
     assert ctypes.sizeof(M.MoskaPagedKv) == 4 * 4 + 4 * 8
 
 
