@@ -23,10 +23,12 @@ namespace moska {
 namespace {
 using namespace stream;
 
-constexpr int kSub = 4;  // blocks of a unit
+template <int NT>
+constexpr int kSubOf = 4;  // blocks of a unit
 
-template <int D>
+template <int D, int NT>
 struct F4Ring {
+    static constexpr int kSub = kSubOf<NT>;
     static constexpr int kDepth = 2;  // units in flight per warp
     static constexpr int kUnitBytes = kSub * Fp4Block<D>::kBytes;
     static constexpr int kBytes = kWarps * kDepth * kUnitBytes;
@@ -111,8 +113,8 @@ template <int D, int NT>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm<D, NT>) paged_fp4_kernel(const AttnArgs a)
 {
     using B = Fp4Block<D>;
-    constexpr int J = B::kGroups, MT = D / 16;
-    constexpr int kUnit = kSub * kBlockTokens, kRows = NT * 8, kDepth = F4Ring<D>::kDepth;
+    constexpr int J = B::kGroups, MT = D / 16, kSub = kSubOf<NT>;
+    constexpr int kUnit = kSub * kBlockTokens, kRows = NT * 8, kDepth = F4Ring<D, NT>::kDepth;
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ uint64_t full[kWarps][kDepth];
     __shared__ int gave_up;
@@ -148,7 +150,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<D, NT>) paged_fp4_kernel(
     const int n_units = (t_end - t_begin + kUnit - 1) / kUnit;
     const int mine = n_units > warp ? (n_units - warp + kWarps - 1) / kWarps : 0;
 
-    const uint32_t ring_base = sm100::smem_u32(ring) + warp * (kDepth * F4Ring<D>::kUnitBytes);
+    const uint32_t ring_base = sm100::smem_u32(ring) + warp * (kDepth * F4Ring<D, NT>::kUnitBytes);
     const int32_t* pages = a.kv.page_table + (int64_t)r * a.kv.max_pages;
     const int shift = a.kv.page_shift;
     // Lane j < kSub loads block j of every unit: `ahead` is that block's token in the unit to ask for next.
@@ -166,7 +168,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<D, NT>) paged_fp4_kernel(
             if (ahead < t_end) {
                 const uint32_t block = (uint32_t)(ahead >> 4) & ((1u << (shift - 4)) - 1);
                 sm100::mbar_arrive_expect_tx(bar, B::kBytes);
-                bulk_load(lane_slot + s * F4Ring<D>::kUnitBytes, pool + (uint64_t)(uint32_t)page * page_bytes + block * B::kBytes,
+                bulk_load(lane_slot + s * F4Ring<D, NT>::kUnitBytes, pool + (uint64_t)(uint32_t)page * page_bytes + block * B::kBytes,
                           B::kBytes, bar);
             } else {
                 sm100::mbar_arrive(bar);
@@ -288,58 +290,65 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<D, NT>) paged_fp4_kernel(
                 }
             }
         }
-        // ---- online softmax over the unit
+        // ---- online softmax over the unit.  The maximum that P is relative to only moves when a score passes
+        // it by more than 2^8 (in P; f16 holds 2^16): rescaling the accumulators is rare that way.
+        float mx[NT][2];
         bool grew = false;
-        float alpha[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float mx0 = -INFINITY, mx1 = -INFINITY;
+            mx[n][0] = mx[n][1] = -INFINITY;
 #pragma unroll
             for (int b = 0; b < SUB; ++b) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     if constexpr (tail)
                         if (t0 + b * 16 + g + 8 * (e >> 1) >= min(t_end, seen[n][e & 1])) sc[n][b][e] = -INFINITY;
+                    mx[n][e & 1] = fmaxf(mx[n][e & 1], sc[n][b][e]);
                 }
-                mx0 = fmaxf(mx0, fmaxf(sc[n][b][0], sc[n][b][2]));
-                mx1 = fmaxf(mx1, fmaxf(sc[n][b][1], sc[n][b][3]));
             }
 #pragma unroll
             for (int off = 4; off < 32; off <<= 1) {
-                mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, off));
-                mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, off));
+                mx[n][0] = fmaxf(mx[n][0], __shfl_xor_sync(0xffffffffu, mx[n][0], off));
+                mx[n][1] = fmaxf(mx[n][1], __shfl_xor_sync(0xffffffffu, mx[n][1], off));
             }
-            const float mn0 = fmaxf(m_run[n][0], mx0), mn1 = fmaxf(m_run[n][1], mx1);
-            grew |= (mn0 > m_run[n][0]) | (mn1 > m_run[n][1]);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) grew |= fmaf(mx[n][e], unit[n][e], -m_run[n][e]) > 8.f;
+        }
+        if (__any_sync(0xffffffffu, grew)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float alpha[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float top = mx[n][e] * unit[n][e];
+                    // (m_run = -inf: no token seen yet, nothing to rescale; top = -inf: none in this unit either)
+                    const bool moves = top > m_run[n][e];
+                    alpha[e] = moves ? fast_exp2(m_run[n][e] - top) : 1.f;
+                    if (moves) m_run[n][e] = top;
+                    l_run[n][e] *= alpha[e];
+                }
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                    oacc[n][mt][0] *= alpha[0];
+                    oacc[n][mt][1] *= alpha[1];
+                    oacc[n][mt][2] *= alpha[0];
+                    oacc[n][mt][3] *= alpha[1];
+                }
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
             // a row that has seen no token yet: keep its (empty) state free of inf - inf
-            const float ms0 = tail && mn0 == -INFINITY ? 0.f : mn0 * unit[n][0];
-            const float ms1 = tail && mn1 == -INFINITY ? 0.f : mn1 * unit[n][1];
-            alpha[n][0] = fast_exp2(fmaf(m_run[n][0], unit[n][0], -ms0));
-            alpha[n][1] = fast_exp2(fmaf(m_run[n][1], unit[n][1], -ms1));
-            m_run[n][0] = mn0;
-            m_run[n][1] = mn1;
-            float sum0 = 0.f, sum1 = 0.f;
+            const float ms0 = tail && m_run[n][0] == -INFINITY ? 0.f : m_run[n][0];
+            const float ms1 = tail && m_run[n][1] == -INFINITY ? 0.f : m_run[n][1];
 #pragma unroll
             for (int b = 0; b < SUB; ++b) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     sc[n][b][e] = fast_exp2(fmaf(sc[n][b][e], unit[n][e & 1], (e & 1) ? -ms1 : -ms0));
-                sum0 += sc[n][b][0] + sc[n][b][2];
-                sum1 += sc[n][b][1] + sc[n][b][3];
+                l_run[n][0] += sc[n][b][0] + sc[n][b][2];
+                l_run[n][1] += sc[n][b][1] + sc[n][b][3];
             }
-            l_run[n][0] = fmaf(l_run[n][0], alpha[n][0], sum0);
-            l_run[n][1] = fmaf(l_run[n][1], alpha[n][1], sum1);
-        }
-        if (__any_sync(0xffffffffu, grew)) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                    oacc[n][mt][0] *= alpha[n][0];
-                    oacc[n][mt][1] *= alpha[n][1];
-                    oacc[n][mt][2] *= alpha[n][0];
-                    oacc[n][mt][3] *= alpha[n][1];
-                }
         }
         // ---- O^T += V^T P.  Where a token that not every row sees holds NaN, the block is passed once for each
         // query token over the values that it sees, kept in its columns only: 0 times NaN is NaN.
@@ -425,7 +434,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<D, NT>) paged_fp4_kernel(
             if (lane == 0) atomicMin(a.kv.status, MOSKA_ERR_TIMEOUT);
             break;
         }
-        const uint32_t at = ring_base + s * F4Ring<D>::kUnitBytes;
+        const uint32_t at = ring_base + s * F4Ring<D, NT>::kUnitBytes;
         if (t0 + kUnit <= masked) {
             step(std::integral_constant<int, kSub>{}, std::false_type{}, at, t0);
         } else {
@@ -456,7 +465,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<D, NT>) paged_fp4_kernel(
             l_run[n][0] += __shfl_xor_sync(0xffffffffu, l_run[n][0], off);
             l_run[n][1] += __shfl_xor_sync(0xffffffffu, l_run[n][1], off);
         }
-    static_assert(sizeof(F4Join<D, NT>) <= F4Ring<D>::kBytes, "the join reuses the ring");
+    static_assert(sizeof(F4Join<D, NT>) <= F4Ring<D, NT>::kBytes, "the join reuses the ring");
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         if (n * 8 + 2 * c >= n_rows) continue;
@@ -464,7 +473,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<D, NT>) paged_fp4_kernel(
         for (int u = 0; u < 2; ++u) {
             const int j = n * 8 + 2 * c + u;
             if (g == 0) {
-                sm.m[warp][j] = m_run[n][u] * unit[n][u];
+                sm.m[warp][j] = m_run[n][u];
                 sm.l[warp][j] = l_run[n][u];
             }
 #pragma unroll
@@ -528,8 +537,8 @@ int launch_paged_fp4(const uint16_t* q, const PagedView& kv, float* o_part, floa
     };
     const bool two = q_len * (s->Hq / s->Hkv) > 8;
     if (s->D == 128)
-        return two ? go(paged_fp4_kernel<128, 2>, F4Ring<128>::kBytes) : go(paged_fp4_kernel<128, 1>, F4Ring<128>::kBytes);
-    return two ? go(paged_fp4_kernel<64, 2>, F4Ring<64>::kBytes) : go(paged_fp4_kernel<64, 1>, F4Ring<64>::kBytes);
+        return two ? go(paged_fp4_kernel<128, 2>, F4Ring<128, 2>::kBytes) : go(paged_fp4_kernel<128, 1>, F4Ring<128, 1>::kBytes);
+    return two ? go(paged_fp4_kernel<64, 2>, F4Ring<64, 2>::kBytes) : go(paged_fp4_kernel<64, 1>, F4Ring<64, 1>::kBytes);
 }
 
 }  // namespace moska
