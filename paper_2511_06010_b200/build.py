@@ -1,4 +1,5 @@
-"""Builds csrc/libmoska.so for sm_100a with nvcc (cross-compiles without a GPU).
+"""Builds csrc/libmoska.so for sm_100a with nvcc (cross-compiles without a GPU), and _paged_call.so, the
+paged store's argument marshalling as a CPython module, with the host compiler.
 
 Every .cu file is compiled to an object of its own (in parallel, only when it or a header is
 newer than the object) under csrc/_build/, then linked.  Run as
@@ -12,6 +13,7 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -20,6 +22,8 @@ OBJ_DIR = os.path.join(CSRC, "_build")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(CSRC, "libmoska.so")
 LIB_DEBUG = os.path.join(CSRC, "libmoska_debug.so")
+CALL_SOURCE = os.path.join(CSRC, "paged_call.cpp")
+CALL = os.path.join(HERE, "_paged_call.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",
@@ -47,8 +51,29 @@ def _stale(lib: str = LIB) -> bool:
     return _newer(sources() + _headers(), lib)
 
 
+def build_call(force: bool = False) -> str:
+    """Compiles the marshalling module against torch's headers."""
+    if not force and not _newer([CALL_SOURCE, os.path.join(INCLUDE, "moska.h")], CALL):
+        return CALL
+    import torch
+
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    include = [INCLUDE, os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+               sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
+    part = f"{CALL}.{os.getpid()}"
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-w",
+                           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+                           *(x for d in include for x in ("-I", d)), CALL_SOURCE, "-o", part,
+                           "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
+    os.replace(part, CALL)
+    return CALL
+
+
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
     lib = LIB_DEBUG if debug else LIB
+    if not debug:
+        build_call(force)
     if not force and not _stale(lib):
         return lib
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")

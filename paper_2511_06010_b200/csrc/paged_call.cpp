@@ -1,0 +1,346 @@
+// Argument marshalling of the paged store's calls as a CPython module: checks the tensors, fills the C
+// structs and calls the entry points of libmoska (their addresses are given by bind()).  The same in
+// Python costs 10 us a call, more than the kernels of a decode step over few requests take (2.6 us for
+// 64 new tokens); here it is one.
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <ATen/ATen.h>
+#include <c10/cuda/CUDAGuard.h>
+#include <c10/cuda/CUDAStream.h>
+
+#include "moska.h"
+
+namespace {
+
+using Append = int (*)(const uint16_t*, int64_t, const uint16_t*, int64_t, const uint16_t*, int64_t, const int32_t*,
+                       const float*, int32_t, int32_t, int32_t, const int32_t*, int32_t, uint16_t*, const moska_paged_kv*,
+                       const moska_shape*, moska_stream);
+using Gather = int (*)(const int32_t*, int32_t, uint16_t*, uint16_t*, const moska_paged_kv*, const moska_shape*, moska_stream);
+using Attend = int (*)(const uint16_t*, const moska_paged_kv*, uint16_t*, float*, float, const moska_shape*, void*, size_t,
+                       moska_stream);
+Append g_append = nullptr;
+Gather g_gather = nullptr;
+Attend g_attend = nullptr;
+PyObject* g_error = nullptr;  // MoskaError(status, where)
+
+struct Failed {};  // a Python exception is set
+
+[[noreturn]] void refuse(const std::string& text)
+{
+    PyErr_SetString(PyExc_ValueError, text.c_str());
+    throw Failed{};
+}
+
+std::string describe(const at::Tensor& t)
+{
+    std::ostringstream s;
+    s << "got " << t.dtype() << " " << t.sizes() << " on " << t.device();
+    return s.str();
+}
+
+const at::Tensor& tensor(PyObject* o, const char* name)
+{
+    if (!THPVariable_Check(o)) refuse(std::string(name) + ": expected a tensor");
+    return THPVariable_Unpack(o);
+}
+
+void* dense(const at::Tensor& t, const char* name, at::ScalarType type, at::IntArrayRef shape, c10::Device device)
+{
+    if (t.scalar_type() != type || t.sizes() != shape || t.device() != device || !t.is_contiguous()) {
+        std::ostringstream s;
+        s << name << ": expected a contiguous " << type << " " << shape << " on " << device << ", " << describe(t)
+          << (t.is_contiguous() ? "" : ", not contiguous");
+        refuse(s.str());
+    }
+    return t.data_ptr();
+}
+
+// [n][heads][D] rows whose heads are dense; rows may lie apart
+uint16_t* rows(const at::Tensor& t, const char* name, at::IntArrayRef shape, c10::Device device, int64_t* stride)
+{
+    if (t.scalar_type() != at::kBFloat16 || t.sizes() != shape || t.device() != device) {
+        std::ostringstream s;
+        s << name << ": expected bfloat16 " << shape << " on " << device << ", " << describe(t);
+        refuse(s.str());
+    }
+    if (shape[0] > 0 && (t.stride(2) != 1 || (shape[1] > 1 && t.stride(1) != shape[2])))
+        refuse(std::string(name) + ": the heads of a row must be dense");
+    *stride = shape[0] > 1 ? t.stride(0) : shape[1] * shape[2];
+    return static_cast<uint16_t*>(t.data_ptr());
+}
+
+long whole(PyObject* o)
+{
+    const long v = PyLong_AsLong(o);
+    if (v == -1 && PyErr_Occurred()) throw Failed{};
+    return v;
+}
+
+// What a PagedKvStore keeps of its pools.
+struct Store {
+    moska_paged_kv kv;  // format, page_size, n_pages and the pools
+    int32_t Hkv, D;
+    c10::Device device;
+};
+
+Store* store_of(PyObject* o)
+{
+    auto* s = static_cast<Store*>(PyCapsule_GetPointer(o, "moska.store"));
+    if (s == nullptr) throw Failed{};
+    return s;
+}
+
+moska_paged_kv seen_through(const Store& s, PyObject* table_o, PyObject* len_o)
+{
+    const at::Tensor& table = tensor(table_o, "page_table");
+    if (table.dim() != 2) refuse("page_table: expected [requests][pages], " + describe(table));
+    moska_paged_kv kv = s.kv;
+    kv.page_table = static_cast<const int32_t*>(dense(table, "page_table", at::kInt, table.sizes(), s.device));
+    kv.kv_len = static_cast<const int32_t*>(dense(tensor(len_o, "kv_len"), "kv_len", at::kInt, {table.size(0)}, s.device));
+    if (table.size(0) > INT32_MAX || table.size(1) > INT32_MAX) refuse("page_table: too large");
+    kv.max_pages = static_cast<int32_t>(table.size(1));
+    return kv;
+}
+
+moska_shape shape_of(int64_t B, int64_t Hq, int64_t Hkv, int64_t D, long q_len)
+{
+    if (B > INT32_MAX || Hq > INT32_MAX) refuse("too many rows or heads");
+    return moska_shape{(int32_t)B, (int32_t)Hq, (int32_t)Hkv, (int32_t)D, 1, 128, 1, 1, 1, 0, (int32_t)q_len};
+}
+
+const int32_t* first_rows(PyObject* o, int64_t n_requests, int64_t n_rows, long q_len, c10::Device device)
+{
+    if (o != Py_None)
+        return static_cast<const int32_t*>(dense(tensor(o, "row_start"), "row_start", at::kInt, {n_requests + 1}, device));
+    if (n_rows != n_requests * q_len) {
+        std::ostringstream s;
+        s << n_rows << " rows for " << n_requests << " requests of " << q_len << " each: give row_start";
+        refuse(s.str());
+    }
+    return nullptr;
+}
+
+// A Python stream address, or the device's current stream; the device is current while this lives.
+struct OnDevice {
+    c10::cuda::OptionalCUDAGuard guard;
+    moska_stream stream = nullptr;
+    OnDevice(c10::Device device, PyObject* stream_o)
+    {
+        if (device.is_cuda()) guard.set_device(device);
+        if (stream_o != Py_None) {
+            stream = PyLong_AsVoidPtr(stream_o);
+            if (stream == nullptr && PyErr_Occurred()) throw Failed{};
+        } else if (device.is_cuda()) {
+            stream = c10::cuda::getCurrentCUDAStream(device.index()).stream();
+        }
+    }
+};
+
+void check(int status, const char* where)
+{
+    if (status == MOSKA_OK) return;
+    PyObject* e = PyObject_CallFunction(g_error, "is", status, where);
+    if (e != nullptr) {
+        PyErr_SetObject(g_error, e);
+        Py_DECREF(e);
+    }
+    throw Failed{};
+}
+
+// Runs `body`; C++ exceptions become Python's.
+template <class Body>
+PyObject* guarded(Py_ssize_t given, Py_ssize_t wanted, Body body)
+{
+    try {
+        if (given != wanted) refuse("wrong number of arguments");
+        return body();
+    } catch (const Failed&) {
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+    }
+    return nullptr;
+}
+
+PyObject* none()
+{
+    Py_INCREF(Py_None);
+    return Py_None;
+}
+
+// bind(append, gather, paged_attn, MoskaError): addresses of the entry points
+PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded(n, 4, [&] {
+        g_append = reinterpret_cast<Append>(PyLong_AsVoidPtr(a[0]));
+        g_gather = reinterpret_cast<Gather>(PyLong_AsVoidPtr(a[1]));
+        g_attend = reinterpret_cast<Attend>(PyLong_AsVoidPtr(a[2]));
+        if (PyErr_Occurred()) throw Failed{};
+        Py_INCREF(a[3]);
+        Py_XDECREF(g_error);
+        g_error = a[3];
+        return none();
+    });
+}
+
+// store(format, page_size, n_pages, Hkv, D, k_pages, v_pages or None): a handle; the pools are checked here
+PyObject* py_store(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded(n, 7, [&] {
+        const long format = whole(a[0]), page_size = whole(a[1]), n_pages = whole(a[2]), Hkv = whole(a[3]), D = whole(a[4]);
+        if (n_pages > INT32_MAX || Hkv > INT32_MAX) refuse("too many pages or heads");
+        const at::Tensor& k = tensor(a[5], "k_pages");
+        auto s = std::make_unique<Store>(Store{{}, (int32_t)Hkv, (int32_t)D, k.device()});
+        s->kv.format = (int32_t)format;
+        s->kv.page_size = (int32_t)page_size;
+        s->kv.n_pages = (int32_t)n_pages;
+        if (format == MOSKA_KV_FP4) {
+            s->kv.k_pages = dense(k, "pages4", at::kByte, {n_pages, Hkv, page_size / 16, 18 * D}, s->device);
+        } else {
+            s->kv.k_pages = dense(k, "k_pages", at::kBFloat16, {n_pages, page_size, Hkv, D}, s->device);
+            s->kv.v_pages = dense(tensor(a[6], "v_pages"), "v_pages", at::kBFloat16, {n_pages, page_size, Hkv, D}, s->device);
+        }
+        PyObject* o = PyCapsule_New(s.get(), "moska.store", [](PyObject* c) {
+            delete static_cast<Store*>(PyCapsule_GetPointer(c, "moska.store"));
+        });
+        if (o == nullptr) throw Failed{};
+        s.release();
+        return o;
+    });
+}
+
+// view(store, page_table, kv_len) -> the eight fields of moska_paged_kv
+PyObject* py_view(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded(n, 3, [&] {
+        const moska_paged_kv kv = seen_through(*store_of(a[0]), a[1], a[2]);
+        PyObject* o = Py_BuildValue("(iiiiKKKK)", kv.format, kv.page_size, kv.n_pages, kv.max_pages,
+                                    (unsigned long long)(uintptr_t)kv.k_pages, (unsigned long long)(uintptr_t)kv.v_pages,
+                                    (unsigned long long)(uintptr_t)kv.page_table, (unsigned long long)(uintptr_t)kv.kv_len);
+        if (o == nullptr) throw Failed{};
+        return o;
+    });
+}
+
+// append(store, q, k, v, page_table, kv_len, positions, cos_sin, row_start, interleaved, q_out, q_len, stream)
+PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    return guarded(n_args, 13, [&] {
+        const Store& s = *store_of(a[0]);
+        const moska_paged_kv kv = seen_through(s, a[4], a[5]);
+        const at::Tensor &k = tensor(a[2], "k"), &v = tensor(a[3], "v");
+        if (k.dim() != 3) refuse("k: expected [rows][heads][D], " + describe(k));
+        const int64_t n = k.size(0), n_requests = tensor(a[4], "page_table").size(0);
+        long q_len = whole(a[11]);
+        const int32_t* first = first_rows(a[8], n_requests, n, q_len, s.device);
+        if (first != nullptr) q_len = 1;
+        int64_t qs = 0, ks = 0, vs = 0, Hq = s.Hkv;
+        uint16_t* kp = rows(k, "k", {n, s.Hkv, s.D}, s.device, &ks);
+        uint16_t* vp = rows(v, "v", {n, s.Hkv, s.D}, s.device, &vs);
+        uint16_t *qp = nullptr, *to = nullptr;
+        at::Tensor q_out;
+        if (a[1] != Py_None) {
+            const at::Tensor& q = tensor(a[1], "q");
+            if (q.dim() != 3) refuse("q: expected [rows][heads][D], " + describe(q));
+            Hq = q.size(1);
+            const int64_t shape[3] = {n, Hq, s.D};
+            qp = rows(q, "q", shape, s.device, &qs);
+            q_out = a[10] == Py_None ? at::empty(shape, q.options()) : tensor(a[10], "q_out");
+            to = static_cast<uint16_t*>(dense(q_out, "q_out", at::kBFloat16, shape, s.device));
+        } else if (a[10] != Py_None) {
+            refuse("q_out without q");
+        }
+        int64_t n_positions = 0, rot_dim = 0;
+        const int32_t* at_position = nullptr;
+        const float* table = nullptr;
+        if (a[7] != Py_None) {
+            const at::Tensor& cs = tensor(a[7], "cos_sin");
+            if (a[6] == Py_None || cs.dim() != 2) refuse("cos_sin is [positions][rot_dim] and comes with positions");
+            n_positions = cs.size(0);
+            rot_dim = cs.size(1);
+            if (n_positions > INT32_MAX || rot_dim > INT32_MAX) refuse("cos_sin: too large");
+            table = static_cast<const float*>(dense(cs, "cos_sin", at::kFloat, cs.sizes(), s.device));
+            at_position = static_cast<const int32_t*>(dense(tensor(a[6], "positions"), "positions", at::kInt, {n}, s.device));
+        }
+        const int turned = PyObject_IsTrue(a[9]);
+        if (turned < 0) throw Failed{};
+        if (n > 0) {
+            const moska_shape shape = shape_of(n, Hq, s.Hkv, s.D, q_len);
+            const OnDevice on(s.device, a[12]);
+            check(g_append(qp, qs, kp, ks, vp, vs, at_position, table, (int32_t)n_positions, (int32_t)rot_dim, turned, first,
+                           (int32_t)n_requests, to, &kv, &shape, on.stream),
+                  "moska_kv_append_paged");
+        }
+        return q_out.defined() ? THPVariable_Wrap(q_out) : none();
+    });
+}
+
+// gather(store, page_table, kv_len, n_rows, row_start, q_len, k_out, v_out, stream)
+PyObject* py_gather(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    return guarded(n_args, 9, [&] {
+        const Store& s = *store_of(a[0]);
+        const moska_paged_kv kv = seen_through(s, a[1], a[2]);
+        const int64_t n = whole(a[3]), n_requests = tensor(a[1], "page_table").size(0);
+        long q_len = whole(a[5]);
+        if (n < 0) refuse("n_rows is negative");
+        const int32_t* first = first_rows(a[4], n_requests, n, q_len, s.device);
+        if (first != nullptr) q_len = 1;
+        const int64_t shape[3] = {n, s.Hkv, s.D};
+        const auto options = at::TensorOptions().dtype(at::kBFloat16).device(s.device);
+        const at::Tensor k = a[6] == Py_None ? at::empty(shape, options) : tensor(a[6], "k_out");
+        const at::Tensor v = a[7] == Py_None ? at::empty(shape, options) : tensor(a[7], "v_out");
+        auto* kp = static_cast<uint16_t*>(dense(k, "k_out", at::kBFloat16, shape, s.device));
+        auto* vp = static_cast<uint16_t*>(dense(v, "v_out", at::kBFloat16, shape, s.device));
+        if (n > 0) {
+            const moska_shape c_shape = shape_of(n, s.Hkv, s.Hkv, s.D, q_len);
+            const OnDevice on(s.device, a[8]);
+            check(g_gather(first, (int32_t)n_requests, kp, vp, &kv, &c_shape, on.stream), "moska_kv_gather_paged");
+        }
+        PyObject* pair = PyTuple_New(2);
+        if (pair == nullptr) throw Failed{};
+        PyTuple_SET_ITEM(pair, 0, THPVariable_Wrap(k));
+        PyTuple_SET_ITEM(pair, 1, THPVariable_Wrap(v));
+        return pair;
+    });
+}
+
+// attend(store, q, page_table, kv_len, out, lse, scale, q_len, n_unique_splits, ws, stream)
+PyObject* py_attend(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    return guarded(n_args, 11, [&] {
+        const Store& s = *store_of(a[0]);
+        const moska_paged_kv kv = seen_through(s, a[2], a[3]);
+        const at::Tensor &q = tensor(a[1], "q"), &out = tensor(a[4], "out"), &lse = tensor(a[5], "lse"), &ws = tensor(a[9], "ws");
+        if (out.dim() != 3 || out.size(2) != s.D) refuse("out: expected [rows][heads][D], " + describe(out));
+        const int64_t B = out.size(0), Hq = out.size(1), n_requests = tensor(a[2], "page_table").size(0);
+        const long q_len = whole(a[7]);
+        auto* qp = static_cast<uint16_t*>(dense(q, "q", at::kBFloat16, out.sizes(), s.device));
+        auto* op = static_cast<uint16_t*>(dense(out, "out", at::kBFloat16, out.sizes(), s.device));
+        auto* lp = static_cast<float*>(dense(lse, "lse", at::kFloat, {B, Hq}, s.device));
+        void* wp = dense(ws, "ws", at::kByte, ws.sizes(), s.device);
+        if (n_requests * (q_len > 1 ? q_len : 1) != B) {
+            std::ostringstream e;
+            e << n_requests << " page-table rows for " << B << " batch rows of " << q_len << " each request";
+            refuse(e.str());
+        }
+        if (B > 0) {
+            moska_shape shape = shape_of(B, Hq, s.Hkv, s.D, q_len);
+            shape.n_unique_splits = (int32_t)whole(a[8]);
+            const double scale = PyFloat_AsDouble(a[6]);
+            if (PyErr_Occurred()) throw Failed{};
+            const OnDevice on(s.device, a[10]);
+            check(g_attend(qp, &kv, op, lp, (float)scale, &shape, wp, (size_t)ws.numel(), on.stream), "moska_paged_attn");
+        }
+        return none();
+    });
+}
+
+#define METHOD(name, fn) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fn)), METH_FASTCALL, nullptr}
+PyMethodDef methods[] = {METHOD("bind", py_bind),     METHOD("store", py_store),   METHOD("view", py_view),
+                         METHOD("append", py_append), METHOD("gather", py_gather), METHOD("attend", py_attend),
+                         {nullptr, nullptr, 0, nullptr}};
+PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_paged_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__paged_call() { return PyModule_Create(&module_def); }
