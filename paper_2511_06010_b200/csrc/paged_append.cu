@@ -104,13 +104,25 @@ __device__ __forceinline__ uint32_t e2m1_code(float x, float s)
     return c | ((__float_as_uint(x) >> 28) & 8u);
 }
 
+// x / 6, correctly rounded for every x whose quotient is normal: a quotient from the rounded reciprocal and
+// one correction with its exact remainder (Markstein, "Computation of elementary functions on the IBM
+// RISC System/6000 processor", 1990).  Smaller quotients are below what an f16 scale can tell from 0.
+__device__ __forceinline__ float sixth(float x)
+{
+    const float y = 1.f / 6.f;  // folded at compile time
+    const float q = __fmul_rn(x, y);
+    return fmaf(fmaf(-6.f, q, x), y, q);
+}
+
 // The E2M1 codes of y[0..7] for scale s, y[0] in the lowest four bits.  Products with 1 / s a little
-// too small and a little too large (2^-20; their own error is below 3 2^-24) enclose the quotient: where
+// too small and a little too large (2^-20; their own error is below 2^-22) enclose the quotient: where
 // the conversion gives both the same code that is the quotient's, elsewhere (near a tie, a few in a
 // million) the codes are compared out.
 __device__ __forceinline__ uint32_t e2m1x8(const float (&y)[8], float s)
 {
-    const float inv = s > 0.f ? __fdiv_rn(1.f, s) : 0.f;
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));  // within 2^-23; s is 0, NaN or at least 2^-24
+    inv = s > 0.f ? inv : 0.f;
     uint32_t w[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -186,7 +198,7 @@ __device__ __forceinline__ void load4(const float* p, float* x)
 // neighbouring dimensions; their partners come from the same lines again.
 // The first loads are on their way before it is known where the row goes.
 template <int D, bool kFp4, bool kInterleaved>
-__global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs a)
+__global__ void __launch_bounds__(kAppendThreads, 3) append_kernel(const AppendArgs a)
 {
     const int lane = threadIdx.x & 31;
     const int warp = blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5);
@@ -263,75 +275,89 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendArgs
     if constexpr (kFp4) {
         if (at.page < 0) return;
         using B = Fp4Block<D>;
-        constexpr int T4 = D / 8, kHeads4 = 32 / T4;
+        constexpr int T4 = D / 16, kHeads4 = 32 / T4;  // sixteen neighbouring dimensions a lane: two pieces
         const int n_kv = 2 * a.Hkv, passes4 = (n_kv + kHeads4 - 1) / kHeads4;
-        const int t4 = lane % T4, d = 8 * t4;
-        const bool turned = d < rot, first = d < half;
-        const int d_other = kInterleaved ? d : first ? d + half : d - half;
-        float c4[8], s4[8];  // interleaved: four angles
-        if (turned) {
-            const int f = kInterleaved ? d / 2 : first ? d : d - half;
-            load4(table + f, c4);
-            load4(table + half + f, s4);
+        const int t4 = lane % T4, d = 16 * t4;
+        float c4[2][8], s4[2][8];  // interleaved: four angles a piece; sine negative in the first half
+        int d_other[2];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const int dp = d + 8 * p;
+            const bool first = dp < half;
+            d_other[p] = first ? dp + half : dp - half;
+            if (dp >= rot) continue;
+            const int f = kInterleaved ? dp / 2 : first ? dp : d_other[p];
+            load4(table + f, c4[p]);
+            load4(table + half + f, s4[p]);
             if constexpr (!kInterleaved) {
-                load4(table + f + 4, c4 + 4);
-                load4(table + half + f + 4, s4 + 4);
+                load4(table + f + 4, c4[p] + 4);
+                load4(table + half + f + 4, s4[p] + 4);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s4[p][e] = first ? -s4[p][e] : s4[p][e];
             }
         }
         const int tok = slot & (kBlockTokens - 1);
         uint8_t* blocks = a.kv.k + ((((int64_t)at.page * a.Hkv) << (a.kv.page_shift - 4)) + (slot >> 4)) * B::kBytes;
-        const int64_t head_bytes = (int64_t)B::kBytes << (a.kv.page_shift - 4);
+        const int head_bytes = B::kBytes << (a.kv.page_shift - 4);
         // the parts that have no bf16 pass left over begin; a pass's loads are one pass ahead
         int pass = (part + a.warps_per_row - passes % a.warps_per_row) % a.warps_per_row;
-        uint4 own = make_uint4(0, 0, 0, 0), other = own;
-        auto load_kv = [&](int p) {
-            const int i = p * kHeads4 + lane / T4;
+        uint4 own[2] = {}, other[2] = {};
+        auto load_kv = [&](int next) {
+            const int i = next * kHeads4 + lane / T4;
             if (i >= n_kv) return;
             const uint16_t* src = i >= a.Hkv ? v_row + (i - a.Hkv) * D : k_row + i * D;
-            own = __ldg(reinterpret_cast<const uint4*>(src + d));
-            if (!kInterleaved && turned && i < a.Hkv) other = __ldg(reinterpret_cast<const uint4*>(src + d_other));
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                own[p] = __ldg(reinterpret_cast<const uint4*>(src + d + 8 * p));
+                if (!kInterleaved && d + 8 * p < rot && i < a.Hkv)
+                    other[p] = __ldg(reinterpret_cast<const uint4*>(src + d_other[p]));
+            }
         };
         load_kv(pass);
         for (; pass < passes4; pass += a.warps_per_row) {
             const int i = pass * kHeads4 + lane / T4;
             const bool live = i < n_kv, is_v = i >= a.Hkv;
             const int h = is_v ? i - a.Hkv : i;
-            float x[8], y[8];
-            unpack8(own, x);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = x[e];
-            if (turned && !is_v) {
-                if constexpr (kInterleaved) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        y[2 * e] = __fsub_rn(__fmul_rn(x[2 * e], c4[e]), __fmul_rn(x[2 * e + 1], s4[e]));
-                        y[2 * e + 1] = __fadd_rn(__fmul_rn(x[2 * e + 1], c4[e]), __fmul_rn(x[2 * e], s4[e]));
-                    }
-                } else {
-                    float z[8];
-                    unpack8(other, z);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float p = __fmul_rn(x[e], c4[e]), o = __fmul_rn(z[e], s4[e]);
-                        y[e] = first ? __fsub_rn(p, o) : __fadd_rn(p, o);
-                    }
-                }
-            }
-            load_kv(pass + a.warps_per_row);
-            // largest magnitude of the 32 dimensions (four neighbouring lanes), NaN if one is
+            float y[2][8];
             float top = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = max_or_nan(top, fabsf(y[e]));
+            for (int p = 0; p < 2; ++p) {
+                unpack8(own[p], y[p]);
+                if (d + 8 * p < rot && !is_v) {
+                    if constexpr (kInterleaved) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float x0 = y[p][2 * e], x1 = y[p][2 * e + 1];
+                            y[p][2 * e] = __fsub_rn(__fmul_rn(x0, c4[p][e]), __fmul_rn(x1, s4[p][e]));
+                            y[p][2 * e + 1] = __fadd_rn(__fmul_rn(x1, c4[p][e]), __fmul_rn(x0, s4[p][e]));
+                        }
+                    } else {
+                        float z[8];
+                        unpack8(other[p], z);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) y[p][e] = __fadd_rn(__fmul_rn(y[p][e], c4[p][e]), __fmul_rn(z[e], s4[p][e]));
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = max_or_nan(top, fabsf(y[p][e]));
+            }
+            load_kv(pass + a.warps_per_row);
+            // largest magnitude of the 32 dimensions (two lanes), NaN if one is
             top = max_or_nan(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = max_or_nan(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const float scale = top < INFINITY ? fminf(__fdiv_rn(top, 6.f), kFp4MaxScale) : NAN;
-            const __half sh = __float2half_rn(scale);
-            const uint32_t w = e2m1x8(y, __half2float(sh));
+            const __half sh = __float2half_rn(top < INFINITY ? fminf(sixth(top), kFp4MaxScale) : NAN);
+            const float sf = __half2float(sh);
+            const uint32_t w0 = e2m1x8(y[0], sf), w1 = e2m1x8(y[1], sf);
             if (!live) continue;
-            uint8_t* blk = blocks + h * head_bytes;
-            *reinterpret_cast<uint32_t*>(blk + (is_v ? B::v_byte(tok, d) : B::k_byte(tok, d))) = w;
-            if ((t4 & 3) == 0)
-                *reinterpret_cast<__half*>(blk + (is_v ? B::v_scale(tok, t4 >> 2) : B::k_scale(tok, t4 >> 2))) = sh;
+            uint8_t* blk = blocks + (int64_t)h * head_bytes;
+            if (is_v) {  // sixteen dimensions are one piece (D = 128) or two (D = 64) of the pair's row
+                *reinterpret_cast<uint32_t*>(blk + B::v_byte(tok, d)) = w0;
+                *reinterpret_cast<uint32_t*>(blk + B::v_byte(tok, d + 8)) = w1;
+                if ((t4 & 1) == 0) *reinterpret_cast<__half*>(blk + B::v_scale(tok, t4 >> 1)) = sh;
+            } else {
+                *reinterpret_cast<uint32_t*>(blk + B::k_byte(tok, d)) = w0;
+                *reinterpret_cast<uint32_t*>(blk + B::k_byte(tok, d + 8)) = w1;
+                if ((t4 & 1) == 0) *reinterpret_cast<__half*>(blk + B::k_scale(tok, t4 >> 1)) = sh;
+            }
         }
     }
 }
