@@ -480,7 +480,7 @@ enum { MOSKA_KV_BF16 = 0, MOSKA_KV_FP4 = 1 };
 
 typedef struct moska_paged_kv {
     int32_t format;            /* MOSKA_KV_BF16 or MOSKA_KV_FP4                                    */
-    int32_t page_size;         /* tokens per page: a power of two, 16..32768                       */
+    int32_t page_size;         /* tokens per page: a power of two, 16..32768, at most 2^30 elements */
     int32_t n_pages;           /* pages in the pool, >= 1                                          */
     int32_t max_pages;         /* entries in a row of the page table, >= 1                         */
     void* k_pages;             /* keys, or the 4-bit pool (keys and values)                        */

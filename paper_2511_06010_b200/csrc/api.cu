@@ -942,7 +942,7 @@ int check_heads(const moska_shape* s)
 }
 
 // Validates a paged store and turns it into what the kernels take.
-int paged_view(const moska_paged_kv* kv, PagedView* out)
+int paged_view(const moska_paged_kv* kv, const moska_shape* s, PagedView* out)
 {
     if (kv == nullptr) return fail(MOSKA_ERR_INVALID_ARG, "kv is NULL");
     if (kv->format != MOSKA_KV_BF16 && kv->format != MOSKA_KV_FP4)
@@ -953,6 +953,8 @@ int paged_view(const moska_paged_kv* kv, PagedView* out)
         return fail(MOSKA_ERR_INVALID_ARG, "n_pages and max_pages must be >= 1");
     if ((long long)kv->max_pages * kv->page_size > (1LL << 30))
         return fail(MOSKA_ERR_UNSUPPORTED, "a page-table row of more than 2^30 tokens");
+    if ((long long)kv->page_size * s->Hkv * s->D > (1LL << 30))
+        return fail(MOSKA_ERR_UNSUPPORTED, "a page of more than 2^30 elements");
     REQUIRE_PTR(kv->k_pages, 16);
     if (kv->format == MOSKA_KV_BF16) REQUIRE_PTR(kv->v_pages, 16);
     REQUIRE_PTR(kv->page_table, 4);
@@ -1014,12 +1016,16 @@ int moska_default_paged_splits(int32_t format, int32_t n_requests, int32_t Hkv, 
     // its warps), so that splits cost about as much as they balance: the smallest sum, as for the FP8
     // store, at s = sqrt(a len slots / (n ov)) with a = 0.7 and fixed costs of ov tokens that fit the
     // sweeps (bf16: 1 at 64 contexts of 4096 tokens and 8 heads, 154 against 167 us at 2 and 170 at 4; 4-6 at
-    // 64 of 1K to 32K.  4 bits: 1-2, 6, and 12-16 at one context of 8191), and 512 tokens at least.
+    // 64 of 1K to 32K; 4 bits: 1-2 and 4-6), and 256 tokens at least.
     if (n_requests <= 0 || Hkv <= 0 || max_len <= 0) return 1;
     const bool fp4 = format == MOSKA_KV_FP4;
     const double len = max_len * (D == 64 ? 0.5 : 1.0), slots = 148.0 * (fp4 ? 3.0 : 2.0);
     long long s = llround(sqrt(0.7 * len * slots / ((double)n_requests * Hkv * (fp4 ? 620.0 : 780.0))));
-    const long long cap = ((long long)max_len + 511) / 512;
+    // few contexts: as many splits as there are places for CTAs (one context of 8191 tokens and 8 heads in 4
+    // bits: 9.1 us at 32 splits, 10.0 at 16, 11.9 at 8)
+    const long long places = (long long)slots / ((long long)n_requests * Hkv);
+    if (s < places) s = places;
+    const long long cap = ((long long)max_len + 255) / 256;
     if (s > cap) s = cap;
     if (s < 1) s = 1;
     if (s > 64) s = 64;
@@ -1036,7 +1042,7 @@ int moska_kv_append_paged(const uint16_t* q, int64_t q_stride, const uint16_t* k
     MOSKA_API_RANGE();
     MOSKA_TRY(check_heads(shape));
     PagedView view{};
-    MOSKA_TRY(paged_view(kv, &view));
+    MOSKA_TRY(paged_view(kv, shape, &view));
     MOSKA_TRY(check_rows(row_start, n_requests, shape));
     if ((q == nullptr) != (q_out == nullptr))
         return fail(MOSKA_ERR_INVALID_ARG, "q and q_out are given together or not at all");
@@ -1072,7 +1078,7 @@ int moska_kv_gather_paged(const int32_t* row_start, int32_t n_requests, uint16_t
     MOSKA_API_RANGE();
     MOSKA_TRY(check_heads(shape));
     PagedView view{};
-    MOSKA_TRY(paged_view(kv, &view));
+    MOSKA_TRY(paged_view(kv, shape, &view));
     MOSKA_TRY(check_rows(row_start, n_requests, shape));
     REQUIRE_PTR(k_out, 16);
     REQUIRE_PTR(v_out, 16);
@@ -1088,7 +1094,7 @@ int moska_unique_attn_paged(const uint16_t* q, const moska_paged_kv* kv, float* 
     MOSKA_API_RANGE();
     MOSKA_TRY(check_shape(shape, false));
     PagedView view{};
-    MOSKA_TRY(paged_view(kv, &view));
+    MOSKA_TRY(paged_view(kv, shape, &view));
     MOSKA_TRY(check_paged_attn(kv, softmax_scale, shape));
     REQUIRE_PTR(q, 16);
     REQUIRE_PTR(o_part, 16);
@@ -1115,7 +1121,7 @@ int moska_paged_attn(const uint16_t* q, const moska_paged_kv* kv, uint16_t* out,
     MOSKA_API_RANGE();
     MOSKA_TRY(check_heads(shape));
     PagedView view{};
-    MOSKA_TRY(paged_view(kv, &view));
+    MOSKA_TRY(paged_view(kv, shape, &view));
     MOSKA_TRY(check_paged_attn(kv, softmax_scale, shape));
     REQUIRE_PTR(q, 16);
     REQUIRE_PTR(out, 16);
@@ -1147,7 +1153,7 @@ int moska_decode_step_paged(const uint16_t* q, const float* summaries, const voi
     MOSKA_API_RANGE();
     MOSKA_TRY(check_shape(shape, summaries != nullptr));
     PagedView view{};
-    MOSKA_TRY(paged_view(kv, &view));
+    MOSKA_TRY(paged_view(kv, shape, &view));
     MOSKA_TRY(check_paged_attn(kv, softmax_scale, shape));
     if ((k_scale_shared == nullptr) != (v_scale_shared == nullptr))
         return fail(MOSKA_ERR_INVALID_ARG, "k_scale_shared and v_scale_shared are given together or not at all");

@@ -126,11 +126,12 @@ struct OnDevice {
     moska_stream stream = nullptr;
     OnDevice(c10::Device device, PyObject* stream_o)
     {
-        if (device.is_cuda()) guard.set_device(device);
+        if (!device.is_cuda()) refuse("the store is not on a GPU");
+        guard.set_device(device);
         if (stream_o != Py_None) {
             stream = PyLong_AsVoidPtr(stream_o);
             if (stream == nullptr && PyErr_Occurred()) throw Failed{};
-        } else if (device.is_cuda()) {
+        } else {
             stream = c10::cuda::getCurrentCUDAStream(device.index()).stream();
         }
     }

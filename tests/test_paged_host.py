@@ -54,6 +54,23 @@ def test_bad_stores_are_refused_by_every_call(M, over, status, text):
     refused(M, status, lambda: M.decode_step_paged(A, A, A, A, None, None, bad, A, A, A, A, A, A, A, 1.0, s, None, stream=0), text)
 
 
+def test_pages_beyond_32_bit_arithmetic_are_refused(M):
+    wide = M.shape(4, 512, 512, 128, 4, 128, 2)
+    refused(M, M.ERR_UNSUPPORTED, lambda: M.paged_attn(A, kv(M, page_size=32768, max_pages=1), A, A, 1.0, wide, None, stream=0), "2^30")
+
+
+def test_calls_on_the_cpu_are_refused():
+    from paper_2511_06010_b200.paged import PagedAttention, PagedKvStore
+
+    st = PagedKvStore.empty(2, 16, 1, 64, device="cpu")
+    table, length = torch.zeros(1, 1, dtype=torch.int32), torch.ones(1, dtype=torch.int32)
+    k = torch.zeros(1, 1, 64, dtype=torch.bfloat16)
+    for call in (lambda: st.append(None, k, k, table, length), lambda: st.gather(table, length, 1),
+                 lambda: PagedAttention(1, 1, 1, 64, 1, device="cpu")(k, st, table, length)):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+
+
 def test_bad_append_arguments_are_refused(M):
     good = dict(q=A, qs=1024, k=A, ks=256, v=A, vs=256, pos=A, cs=A, n=10, rot=128, il=0, rows=None, req=4, out=A)
 
@@ -111,7 +128,7 @@ def test_pool_sizes_and_splits(M):
     for fmt in (M.KV_BF16, M.KV_FP4):
         assert M.default_paged_splits(fmt, 0, 8, 128, 100) == 1 and M.default_paged_splits(fmt, 4, 8, 128, 0) == 1
         assert M.default_paged_splits(fmt, 1000, 8, 128, 500) == 1 and M.default_paged_splits(fmt, 1, 8, 64, 512) == 1
-        assert 1 < M.default_paged_splits(fmt, 1, 8, 128, 8191) <= 16 and M.default_paged_splits(fmt, 1, 1, 128, 1 << 30) == 64
+        assert 16 <= M.default_paged_splits(fmt, 1, 8, 128, 8191) <= 32 and M.default_paged_splits(fmt, 1, 1, 128, 1 << 30) == 64
     assert ctypes.sizeof(M.MoskaPagedKv) == 4 * 4 + 4 * 8
 
 
