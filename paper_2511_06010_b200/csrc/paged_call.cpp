@@ -8,6 +8,9 @@
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
+#include <memory>
+#include <string>
+
 #include "moska.h"
 
 namespace {
@@ -31,11 +34,17 @@ struct Failed {};  // a Python exception is set
     throw Failed{};
 }
 
+std::string text(at::IntArrayRef shape)
+{
+    std::string s = "(";
+    for (size_t i = 0; i < shape.size(); ++i) s += (i > 0 ? ", " : "") + std::to_string(shape[i]);
+    return s + ")";
+}
+
 std::string describe(const at::Tensor& t)
 {
-    std::ostringstream s;
-    s << "got " << t.dtype() << " " << t.sizes() << " on " << t.device();
-    return s.str();
+    return std::string("got ") + c10::toString(t.scalar_type()) + " " + text(t.sizes()) + " on " + t.device().str() +
+           (t.is_contiguous() ? "" : ", not contiguous");
 }
 
 const at::Tensor& tensor(PyObject* o, const char* name)
@@ -46,23 +55,17 @@ const at::Tensor& tensor(PyObject* o, const char* name)
 
 void* dense(const at::Tensor& t, const char* name, at::ScalarType type, at::IntArrayRef shape, c10::Device device)
 {
-    if (t.scalar_type() != type || t.sizes() != shape || t.device() != device || !t.is_contiguous()) {
-        std::ostringstream s;
-        s << name << ": expected a contiguous " << type << " " << shape << " on " << device << ", " << describe(t)
-          << (t.is_contiguous() ? "" : ", not contiguous");
-        refuse(s.str());
-    }
+    if (t.scalar_type() != type || t.sizes() != shape || t.device() != device || !t.is_contiguous())
+        refuse(std::string(name) + ": expected a contiguous " + c10::toString(type) + " " + text(shape) + " on " + device.str() +
+               ", " + describe(t));
     return t.data_ptr();
 }
 
 // [n][heads][D] rows whose heads are dense; rows may lie apart
 uint16_t* rows(const at::Tensor& t, const char* name, at::IntArrayRef shape, c10::Device device, int64_t* stride)
 {
-    if (t.scalar_type() != at::kBFloat16 || t.sizes() != shape || t.device() != device) {
-        std::ostringstream s;
-        s << name << ": expected bfloat16 " << shape << " on " << device << ", " << describe(t);
-        refuse(s.str());
-    }
+    if (t.scalar_type() != at::kBFloat16 || t.sizes() != shape || t.device() != device)
+        refuse(std::string(name) + ": expected BFloat16 " + text(shape) + " on " + device.str() + ", " + describe(t));
     if (shape[0] > 0 && (t.stride(2) != 1 || (shape[1] > 1 && t.stride(1) != shape[2])))
         refuse(std::string(name) + ": the heads of a row must be dense");
     *stride = shape[0] > 1 ? t.stride(0) : shape[1] * shape[2];
@@ -112,11 +115,9 @@ const int32_t* first_rows(PyObject* o, int64_t n_requests, int64_t n_rows, long 
 {
     if (o != Py_None)
         return static_cast<const int32_t*>(dense(tensor(o, "row_start"), "row_start", at::kInt, {n_requests + 1}, device));
-    if (n_rows != n_requests * q_len) {
-        std::ostringstream s;
-        s << n_rows << " rows for " << n_requests << " requests of " << q_len << " each: give row_start";
-        refuse(s.str());
-    }
+    if (n_rows != n_requests * q_len)
+        refuse(std::to_string(n_rows) + " rows for " + std::to_string(n_requests) + " requests of " + std::to_string(q_len) +
+               " each: give row_start");
     return nullptr;
 }
 
@@ -319,11 +320,9 @@ PyObject* py_attend(PyObject*, PyObject* const* a, Py_ssize_t n_args)
         auto* op = static_cast<uint16_t*>(dense(out, "out", at::kBFloat16, out.sizes(), s.device));
         auto* lp = static_cast<float*>(dense(lse, "lse", at::kFloat, {B, Hq}, s.device));
         void* wp = dense(ws, "ws", at::kByte, ws.sizes(), s.device);
-        if (n_requests * (q_len > 1 ? q_len : 1) != B) {
-            std::ostringstream e;
-            e << n_requests << " page-table rows for " << B << " batch rows of " << q_len << " each request";
-            refuse(e.str());
-        }
+        if (n_requests * (q_len > 1 ? q_len : 1) != B)
+            refuse(std::to_string(n_requests) + " page-table rows for " + std::to_string(B) + " batch rows, " +
+                   std::to_string(q_len) + " a request");
         if (B > 0) {
             moska_shape shape = shape_of(B, Hq, s.Hkv, s.D, q_len);
             shape.n_unique_splits = (int32_t)whole(a[8]);

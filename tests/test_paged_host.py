@@ -127,7 +127,7 @@ def test_pool_sizes_and_splits(M):
         assert M.paged_pool_bytes(*bad) == 0
     for fmt in (M.KV_BF16, M.KV_FP4):
         assert M.default_paged_splits(fmt, 0, 8, 128, 100) == 1 and M.default_paged_splits(fmt, 4, 8, 128, 0) == 1
-        assert M.default_paged_splits(fmt, 1000, 8, 128, 500) == 1 and M.default_paged_splits(fmt, 1, 8, 64, 512) == 1
+        assert M.default_paged_splits(fmt, 1000, 8, 128, 500) == 1 and M.default_paged_splits(fmt, 1, 8, 64, 256) == 1
         assert 16 <= M.default_paged_splits(fmt, 1, 8, 128, 8191) <= 32 and M.default_paged_splits(fmt, 1, 1, 128, 1 << 30) == 64
     assert ctypes.sizeof(M.MoskaPagedKv) == 4 * 4 + 4 * 8
 
