@@ -14,10 +14,14 @@ class MoskaLayer:
     """Owns the scratch of a decode step for a fixed shape and calls the C ABI in path order."""
 
     def __init__(self, B, Hq, Hkv, D, C, L, k, max_unique_len, dense=False, dense_slots=None,
-                 n_unique_splits=None, device="cuda", fp8_unique=False, q_len=1):
-        """B counts batch rows; with q_len > 1 they are B / q_len requests of q_len query tokens."""
+                 n_unique_splits=None, device="cuda", fp8_unique=False, q_len=1, paged_fmt=None):
+        """B counts batch rows; with q_len > 1 they are B / q_len requests of q_len query tokens.
+        fp8_unique, paged_fmt ("bf16" or "fp4"): the private store that the default splits are for."""
         self.device = torch.device(device)
         self.dense = dense
+        if n_unique_splits is None and paged_fmt is not None:
+            n_unique_splits = M.default_paged_splits({"bf16": M.KV_BF16, "fp4": M.KV_FP4}[paged_fmt],
+                                                     B // max(1, q_len), Hkv, D, max(1, max_unique_len))
         if n_unique_splits is None:
             default = M.default_unique_splits_fp8 if fp8_unique else M.default_unique_splits
             n_unique_splits = default(B // max(1, q_len), Hkv, max(1, max_unique_len))
@@ -88,9 +92,16 @@ class MoskaLayer:
         M.unique_attn_fp8(q, f8.k8, f8.v8, f8.k_scale, f8.v_scale, kv_start, kv_len, self.o_part,
                           self.lse_part, self.scale, self.shape, stream)
 
+    def _paged_kv(self, store, page_table, kv_len):
+        requests = self.shape.B // max(1, self.shape.q_len)
+        if page_table.shape[0] != requests or (store.Hkv, store.D) != (self.shape.Hkv, self.shape.D):
+            raise ValueError(f"the layer has {requests} requests, {self.shape.Hkv} KV heads of {self.shape.D}; the page table "
+                             f"{page_table.shape[0]} rows, the store {store.Hkv} heads of {store.D}")
+        return store.kv(page_table, kv_len)
+
     def unique_paged(self, q, store, page_table, kv_len, stream=None):
         """Unique KV Attention over a paged private store (`store`: a paged.PagedKvStore)."""
-        M.unique_attn_paged(q, store.kv(page_table, kv_len), self.o_part, self.lse_part, self.scale, self.shape,
+        M.unique_attn_paged(q, self._paged_kv(store, page_table, kv_len), self.o_part, self.lse_part, self.scale, self.shape,
                             stream)
 
     def merge(self):
@@ -159,7 +170,7 @@ class MoskaLayer:
         if two_streams and self.side_stream is None:
             self.side_stream = torch.cuda.Stream(device=self.device, priority=-1)
         shared = (k_shared, v_shared, None, None) if sf8 is None else (sf8.k8, sf8.v8, sf8.k_scale, sf8.v_scale)
-        M.decode_step_paged(q, None if self.dense else self.summaries, *shared, store.kv(page_table, kv_len),
+        M.decode_step_paged(q, None if self.dense else self.summaries, *shared, self._paged_kv(store, page_table, kv_len),
                             self.topk_idx, self.seg_offsets, self.seg_entries, self.o_part, self.lse_part, self.out,
                             self.lse_out, self.scale, self.shape, self.ws, None,
                             self.side_stream if two_streams else None, prof)

@@ -331,6 +331,51 @@ def test_pages_beyond_32_bit_offsets(fmt):
         assert (np.abs(lse[r].double().cpu().numpy() - l) <= l_tol).all()
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "fp4"])
+@pytest.mark.parametrize("splits", [5, 6, 33, 64])
+def test_many_splits_of_few_and_of_many_rows(fmt, splits):
+    """The merge's two forms (a warp or four a row), splits without tokens among them."""
+    from paper_2511_06010_b200.paged import PagedAttention
+
+    for R_, Hkv, lens in ((1, 2, [3000]), (3, 1, [70, 0, 2111]), (300, 2, [1 + 3 * i for i in range(300)])):
+        Hq = 8 * Hkv
+        st, table, length, q = _attention_case(fmt, 128, Hq, Hkv, 64, 1, splits, lens, seed=splits)
+        attention = PagedAttention(R_, Hq, Hkv, 128, max(lens), fmt=fmt, n_unique_splits=splits)
+        attention.out.fill_(float("nan"))
+        out, lse = attention(q.cuda(), st, table.cuda(), length)
+        keep = range(0, R_, max(1, R_ // 7))  # the reference of a few requests
+        sub = torch.tensor(list(keep))
+        _check(out[sub], lse[sub], st, table[sub], [lens[i] for i in keep], q[sub], 1, attention.scale)
+        assert torch.isfinite(out.float()).all()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp4"])
+def test_two_streams_at_once(fmt):
+    """Two attentions with scratch of their own on two streams, and appends to other requests of the same
+    pool beside them: equal to one after the other."""
+    from paper_2511_06010_b200.paged import PagedAttention
+
+    lens = [900, 33, 1500, 64]
+    st, table, length, q = _attention_case(fmt, 128, 16, 2, 32, 1, 3, [n + 40 for n in lens], seed=21)
+    table, q = table.cuda(), q.cuda()
+    short = torch.tensor(lens, dtype=torch.int32).cuda()  # tokens behind it are written while it is read
+    pair = [PagedAttention(4, 16, 2, 128, 1600, fmt=fmt, n_unique_splits=3) for _ in range(2)]
+    want = [t.clone() for t in pair[0](q, st, table, short)]
+    rows = R.make_bf16((160, 2, 128), torch.Generator().manual_seed(22)).cuda()
+    grown = short + 40
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for stream, attention in zip(streams, pair):
+            with torch.cuda.stream(stream):
+                attention.out.fill_(0)
+                attention(q, st, table, short)
+        st.append(None, rows, rows, table, grown, q_len=40, stream=streams[2])
+        torch.cuda.synchronize()
+        for attention in pair:
+            assert torch.equal(attention.out, want[0]) and torch.equal(attention.lse, want[1])
+
+
 # ---- a run of the operators together ---------------------------------------------------------------
 @pytest.mark.parametrize("fmt", ["bf16", "fp4"])
 def test_prompts_then_decode_steps(fmt):
@@ -451,8 +496,11 @@ def test_decode_step_with_a_paged_store(fmt, shared, mode):
     sh = W.make_shared_store(w, "cuda")
     sf8 = W.quantize_shared_store_fp8(sh) if shared == "fp8" else None
     q = W.make_queries(w, sh, 0, "cuda")
-    layer = MoskaLayer(w.B, w.Hq, w.Hkv, w.D, w.C, w.L, w.k, 1000, dense=dense, dense_slots=w.C if dense else None)
+    layer = MoskaLayer(w.B, w.Hq, w.Hkv, w.D, w.C, w.L, w.k, 1000, dense=dense, dense_slots=w.C if dense else None,
+                       paged_fmt=fmt)
     layer.build_summaries(sh.k_shared)
+    with pytest.raises(ValueError):
+        layer.step_paged(q, sh.k_shared, sh.v_shared, st, table[:-1].cuda(), length[:-1])
     out = layer.step_paged(q, sh.k_shared, sh.v_shared, st, table.cuda(), length, two_streams=mode.startswith("two"),
                            unique_tokens=1 << 26 if "long" in mode else 0, sf8=sf8)
     torch.cuda.synchronize()
