@@ -1051,6 +1051,9 @@ int moska_kv_append_paged(const uint16_t* q, int64_t q_stride, const uint16_t* k
         REQUIRE_PTR(q_out, 16);
         if (q_stride % 8 != 0 || q_stride < (int64_t)shape->Hq * shape->D)
             return fail(MOSKA_ERR_INVALID_ARG, "q_stride = %lld must be a multiple of 8 and hold a row", (long long)q_stride);
+        const int64_t row = (int64_t)shape->Hq * shape->D;
+        if (shape->B > 0 && q < q_out + shape->B * row && q_out < q + (shape->B - 1) * q_stride + row)
+            return fail(MOSKA_ERR_INVALID_ARG, "q_out overlaps q");
     }
     REQUIRE_PTR(k, 16);
     REQUIRE_PTR(v, 16);

@@ -2,6 +2,7 @@
 // structs and calls the entry points of libmoska (their addresses are given by bind()).  The same in
 // Python costs 10 us a call, more than the kernels of a decode step over few requests take (2.6 us for
 // 64 new tokens); here it is one.
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
@@ -157,8 +158,8 @@ PyObject* guarded(Py_ssize_t given, Py_ssize_t wanted, Body body)
         if (given != wanted) refuse("wrong number of arguments");
         return body();
     } catch (const Failed&) {
-    } catch (const std::exception& e) {
-        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {  // torch's own, out of memory among them
+        torch::translate_exception_to_python(std::current_exception());
     }
     return nullptr;
 }

@@ -53,11 +53,14 @@ class PagedKvStore:
         if page_size not in (None, self.page_size):
             raise ValueError(f"page_size = {page_size}, the pages hold {self.page_size}")
         self.device, self.k_pages, self.v_pages, self.pages4 = pool.device, k_pages, v_pages, pages4
+        self._pools = (pool, v_pages)  # what the handle points into
         self._handle = _call.store(FORMATS[self.fmt], self.page_size, self.n_pages, self.Hkv, self.D, pool, v_pages)
 
     @classmethod
     def empty(cls, n_pages, page_size, Hkv, D, fmt="bf16", device="cuda"):
         """A store of its own memory; the pages hold nothing yet."""
+        if fmt not in FORMATS:
+            raise ValueError(f"fmt = {fmt!r} is not one of {sorted(FORMATS)}")
         if page_size < 16 or page_size & (page_size - 1):
             raise ValueError(f"page_size = {page_size} is not a power of two of at least 16")
         if FORMATS[fmt] == M.KV_BF16:

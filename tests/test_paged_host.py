@@ -72,7 +72,7 @@ def test_calls_on_the_cpu_are_refused():
 
 
 def test_bad_append_arguments_are_refused(M):
-    good = dict(q=A, qs=1024, k=A, ks=256, v=A, vs=256, pos=A, cs=A, n=10, rot=128, il=0, rows=None, req=4, out=A)
+    good = dict(q=A, qs=1024, k=A, ks=256, v=A, vs=256, pos=A, cs=A, n=10, rot=128, il=0, rows=None, req=4, out=2 * A)
 
     def call(D=128, shape=None, **over):
         a = dict(good, **over)
@@ -84,6 +84,8 @@ def test_bad_append_arguments_are_refused(M):
                  dict(vs=255), dict(k=None), dict(v=A + 4), dict(rot=8), dict(rot=144), dict(rot=-16), dict(pos=None),
                  dict(cs=A + 8), dict(n=0), dict(req=3), dict(req=0), dict(rows=A + 2)):
         refused(M, M.ERR_INVALID_ARG, call(**over))
+    for out in (A + 0x1000, A - 0x1000, A):  # four rows of 2 KB each
+        refused(M, M.ERR_INVALID_ARG, call(out=out), "overlaps")
     refused(M, M.ERR_UNSUPPORTED, call(shape=dict(D=96)))
     refused(M, M.ERR_UNSUPPORTED, call(shape=dict(Hq=64)))
     refused(M, M.ERR_INVALID_ARG, call(shape=dict(Hq=9)))
@@ -152,6 +154,8 @@ def test_store_checks_its_tensors():
             st.append(a.pop("q"), a.pop("k"), a.pop("v"), table, length, **a)
     with pytest.raises(ValueError):
         PagedKvStore.empty(4, 24, 2, 64, device="cpu")
+    with pytest.raises(ValueError):
+        PagedKvStore.empty(4, 32, 2, 64, "fp8", device="cpu")
     with pytest.raises(ValueError):
         PagedKvStore(k_pages=st.k_pages)
 
