@@ -107,10 +107,11 @@ const char* moska_last_error(void);
 /* Waits for the current device to finish, stores the sticky device-side status word in
  * *status_host (host pointer) and clears it.  0 means no kernel of the library raised anything.
  * MOSKA_ERR_TIMEOUT: a CTA of the tensor-core Shared KV Attention kernel, or a warp of the 4-bit
- * paged attention, gave up on one of its bounded waits (TMA, MMA or bulk-copy completion).  MOSKA_ERR_INVALID_ARG: a grouping call (either entry
- * point) met a chunk index outside [0, C) or a (request, KV head) list that is not strictly
- * ascending, shared attention met an entry of seg_entries outside [0, B*Hkv*k), or a call on a
- * paged store met a page index, a length or a position that is out of range.  In every
+ * paged attention, gave up on one of its bounded waits (TMA, MMA or bulk-copy completion).
+ * MOSKA_ERR_INVALID_ARG: a grouping call (either entry point) met a chunk index outside [0, C) or
+ * a (request, KV head) list that is not strictly ascending, shared attention met an entry of
+ * seg_entries outside [0, B*Hkv*k), or a call on a paged store met a page index, a length or a
+ * position that is out of range.  In every
  * case the outputs of the steps since the last read are not valid.  MOSKA_ERR_CORRUPT (debug
  * build only): guard words of the workspace were overwritten or a work list would have overflowed.
  * The most negative code raised since the last read is the one reported. */

@@ -1014,13 +1014,15 @@ int moska_default_paged_splits(int32_t format, int32_t n_requests, int32_t Hkv, 
 {
     // A CTA has fixed costs (its length, its first page and its first copies one after another, the join of
     // its warps), so that splits cost about as much as they balance: the smallest sum, as for the FP8
-    // store, at s = sqrt(a len slots / (n ov)) with a = 0.7 and fixed costs of ov tokens that fit the
-    // sweeps (bf16: 1 at 64 contexts of 4096 tokens and 8 heads, 154 against 167 us at 2 and 170 at 4; 4-6 at
-    // 64 of 1K to 32K; 4 bits: 1-2 and 4-6), and 256 tokens at least.
+    // store, at s = sqrt(a len slots / (n ov)) with fixed costs of ov tokens.  a fits sweeps of 16 to 256
+    // requests of 2K to 32K tokens and 8 heads: 0.7 in order (4 bits, 200 of 1K to 8K: 200 us at 2 splits, 207
+    // at 1), 0.2 where the longest come first, which balances most of it (64 of 1K to 32K: 202 us at 2 or
+    // 3, 220 at 6; 64 of 1K to 4K: 51 at 1, 58 at 2; but 64 x 4096: 64.9 at 1, 63.2 at 2).  256 tokens at least.
     if (n_requests <= 0 || Hkv <= 0 || max_len <= 0) return 1;
     const bool fp4 = format == MOSKA_KV_FP4;
     const double len = max_len * (D == 64 ? 0.5 : 1.0), slots = 148.0 * (fp4 ? 3.0 : 2.0);
-    long long s = llround(sqrt(0.7 * len * slots / ((double)n_requests * Hkv * (fp4 ? 620.0 : 780.0))));
+    const double a = n_requests <= kMaxOrdered ? 0.2 : 0.7;
+    long long s = llround(sqrt(a * len * slots / ((double)n_requests * Hkv * 620.0)));
     // few contexts: as many splits as there are places for CTAs (one context of 8191 tokens and 8 heads in 4
     // bits: 9.1 us at 32 splits, 10.0 at 16, 11.9 at 8)
     const long long places = (long long)slots / ((long long)n_requests * Hkv);

@@ -12,6 +12,7 @@
 namespace moska {
 namespace {
 using namespace stream;
+static_assert(kThreads == kMaxOrdered, "a request a thread");
 
 struct PagedTokens {
     static constexpr bool kPaged = true;
@@ -40,6 +41,7 @@ struct PagedArgs {
     float* lse_out;
     float scale;
     int Hq, Hkv, n_splits, slot0, n_slots, q_len;
+    int ordered;  // requests that are taken longest context first (0: in order)
 };
 
 // One CTA per (request, KV head, split).  kMulti: several query tokens per request.
@@ -49,12 +51,15 @@ __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 3) paged_bf16_kernel(
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ TileRows<NT> rows;
     __shared__ int row_last[NT * 8];
+    __shared__ OrderSmem order;
     const int G = a.Hq / a.Hkv;
     const int h = blockIdx.x % a.Hkv;
     const int sp = (blockIdx.x / a.Hkv) % a.n_splits;
-    const int r = blockIdx.x / (a.Hkv * a.n_splits);
+    int r = blockIdx.x / (a.Hkv * a.n_splits);
     dependents_may_launch();
-    const int len = paged_len(a.kv, r);
+    int len;
+    if (a.ordered > 0) r = request_at(a.kv, a.ordered, r, order, len);
+    else len = paged_len(a.kv, r);
     if (threadIdx.x < NT * 8) {
         const int j = threadIdx.x;
         const bool live = j < a.q_len * G;
@@ -187,7 +192,8 @@ int launch_paged_bf16(const uint16_t* q, const PagedView& kv, float* o_part, flo
     const long long grid = (long long)(s->B / q_len) * s->Hkv * s->n_unique_splits;
     if (grid == 0) return MOSKA_OK;
     if (grid > 0x7fffffffLL) return fail(MOSKA_ERR_UNSUPPORTED, "paged attention grid too large");
-    const PagedArgs a{q, kv, o_part, lse_part, out, lse_out, scale, s->Hq, s->Hkv, s->n_unique_splits, slot0, n_slots, q_len};
+    const PagedArgs a{q, kv, o_part, lse_part, out, lse_out, scale, s->Hq, s->Hkv, s->n_unique_splits, slot0, n_slots, q_len,
+                      longest_first(s->B / q_len, grid) ? s->B / q_len : 0};
     auto go = [&](auto kernel, int smem) {
         MOSKA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
         kernel<<<(unsigned)grid, kThreads, smem, st>>>(a);

@@ -22,6 +22,7 @@
 namespace moska {
 namespace {
 using namespace stream;
+static_assert(kThreads == kMaxOrdered, "a request a thread");
 
 template <int NT>
 constexpr int kSubOf = 4;  // blocks of a unit
@@ -102,6 +103,7 @@ struct AttnArgs {
     float* lse_out;
     float scale;
     int Hq, Hkv, n_splits, slot0, n_slots, q_len;
+    int ordered;  // requests that are taken longest context first (0: in order)
 };
 
 // CTAs per SM.  D = 128: 154 registers (a fourth CTA would need 128: spills, slower).  D = 64: 113; four
@@ -118,16 +120,20 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<D, NT>) paged_fp4_kernel(
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ uint64_t full[kWarps][kDepth];
     __shared__ int gave_up;
+    __shared__ OrderSmem order;
     __shared__ int64_t row_of[kRows];  // result row of each query row, -1: none
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, c = lane & 3;
     const int G = a.Hq / a.Hkv;
     const int h = blockIdx.x % a.Hkv;
     const int sp = (blockIdx.x / a.Hkv) % a.n_splits;
-    const int r = blockIdx.x / (a.Hkv * a.n_splits);
+    int r = blockIdx.x / (a.Hkv * a.n_splits);
     const int q_len = a.q_len, n_rows = q_len * G;
 
     dependents_may_launch();
+    int len;
+    if (a.ordered > 0) r = request_at(a.kv, a.ordered, r, order, len);
+    else len = paged_len(a.kv, r);
     if (threadIdx.x == 0) gave_up = 0;
     if (threadIdx.x < kRows) {
         const int j = threadIdx.x;
@@ -142,7 +148,6 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<D, NT>) paged_fp4_kernel(
     __syncthreads();
 
     // this split's tokens: equal parts rounded up to a pass of the CTA's warps
-    const int len = paged_len(a.kv, r);
     constexpr int kPass = kWarps * kUnit;
     int per = (len + a.n_splits - 1) / a.n_splits;
     per = (per + kPass - 1) / kPass * kPass;
@@ -528,7 +533,8 @@ int launch_paged_fp4(const uint16_t* q, const PagedView& kv, float* o_part, floa
     const long long grid = (long long)(s->B / q_len) * s->Hkv * s->n_unique_splits;
     if (grid == 0) return MOSKA_OK;
     if (grid > 0x7fffffffLL) return fail(MOSKA_ERR_UNSUPPORTED, "paged attention grid too large");
-    const AttnArgs a{q, kv, o_part, lse_part, out, lse_out, scale, s->Hq, s->Hkv, s->n_unique_splits, slot0, n_slots, q_len};
+    const AttnArgs a{q, kv, o_part, lse_part, out, lse_out, scale, s->Hq, s->Hkv, s->n_unique_splits, slot0, n_slots, q_len,
+                     longest_first(s->B / q_len, grid) ? s->B / q_len : 0};
     auto go = [&](auto kernel, int ring) {
         MOSKA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ring));
         kernel<<<(unsigned)grid, kThreads, ring, st>>>(a);

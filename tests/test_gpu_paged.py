@@ -350,6 +350,46 @@ def test_many_splits_of_few_and_of_many_rows(fmt, splits):
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "fp4"])
+@pytest.mark.parametrize("requests", [2, 7, 8, 9, 127, 128, 129])
+@pytest.mark.parametrize("kind", ["equal", "ties", "ragged", "one longer"])
+def test_order_of_the_requests(fmt, requests, kind):
+    """More CTAs than SMs: requests are taken longest first, up to 128 of them; every one exactly once."""
+    from paper_2511_06010_b200.paged import PagedAttention
+
+    rng = np.random.default_rng(requests)
+    lens = {"equal": [35] * requests, "ties": list(16 * rng.integers(0, 5, requests)), "ragged": list(rng.integers(0, 300, requests)),
+            "one longer": [20] * (requests - 1) + [21]}[kind]
+    lens = [int(n) for n in lens]
+    Hq = Hkv = 4
+    splits = 160 // (requests * Hkv) + 1  # more than 148 CTAs
+    st, table, length, q = _attention_case(fmt, 128, Hq, Hkv, 16, 1, splits, lens, seed=requests)
+    attention = PagedAttention(requests, Hq, Hkv, 128, max(lens), fmt=fmt, n_unique_splits=splits)
+    attention.out.fill_(float("nan"))
+    attention.lse.fill_(float("nan"))
+    out, lse = attention(q.cuda(), st, table.cuda(), length)
+    _check(out, lse, st, table, lens, q, 1, attention.scale)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp4"])
+def test_bad_lengths_leave_the_order_whole(fmt):
+    """A length out of range is reported; every other request still has its own result."""
+    from paper_2511_06010_b200 import binding as M
+    from paper_2511_06010_b200.paged import PagedAttention
+
+    lens = [50 + 3 * (i % 11) for i in range(40)]
+    bad = {3: 2**31 - 1, 4: -1, 17: -2**31, 18: 2**31 - 1, 39: 1000}
+    st, table, length, q = _attention_case(fmt, 128, 4, 4, 16, 1, 1, lens, poison=False)
+    for r, n in bad.items():
+        length[r] = n
+    attention = PagedAttention(40, 4, 4, 128, 100, fmt=fmt, n_unique_splits=1)
+    attention.out.fill_(float("nan"))
+    out, lse = attention(q.cuda(), st, table.cuda(), length)
+    assert M.device_status() == M.ERR_INVALID_ARG
+    good = [r for r in range(40) if r not in bad]
+    _check(out[good], lse[good], st, table[good], [lens[r] for r in good], q[good], 1, attention.scale)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp4"])
 def test_two_streams_at_once(fmt):
     """Two attentions with scratch of their own on two streams, and appends to other requests of the same
     pool beside them: equal to one after the other."""
