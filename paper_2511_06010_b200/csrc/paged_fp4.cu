@@ -24,8 +24,10 @@ namespace {
 using namespace stream;
 static_assert(kThreads == kMaxOrdered, "a request a thread");
 
+// Blocks of a unit; of two column blocks four spill at 255 registers (48 x 4 query tokens: 62 us, 64 at four,
+// 76 at two).
 template <int NT>
-constexpr int kSubOf = 4;  // blocks of a unit
+constexpr int kSubOf = NT == 2 ? 3 : 4;
 
 template <int D, int NT>
 struct F4Ring {
@@ -106,8 +108,9 @@ struct AttnArgs {
     int ordered;  // requests that are taken longest context first (0: in order)
 };
 
-// CTAs per SM.  D = 128: 154 registers (a fourth CTA would need 128: spills, slower).  D = 64: 113; four
-// take 24 us over 128 contexts of 2000 tokens where three take 33.  Two column blocks: 200-255 registers.
+// CTAs per SM.  D = 128: 164 registers (a fourth CTA would need 128: spills, slower).  D = 64: 123; four
+// take 24 us over 128 contexts of 2000 tokens where three take 33.  Two column blocks: 252 registers
+// (three CTAs of 168 spill: 69 us over 48 x 4 query tokens where two take 62).
 template <int D, int NT>
 constexpr int kCtasPerSm = NT == 2 ? 2 : D == 128 ? 3 : 4;
 
