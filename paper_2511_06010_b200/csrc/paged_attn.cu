@@ -88,12 +88,12 @@ __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 3) paged_bf16_kernel(
 }
 
 // Final rows from the partial rows of n splits: R warps a row, each with every R-th split and eight of its
-// loads in flight (the rows come from L2: latency counts), joined through shared memory.
+// loads in flight (the rows come from L2: latency counts), joined through shared memory.  The partial rows
+// are written while this kernel may already run: no __restrict__, which would let their loads pass the wait.
 constexpr int kMergeWarps = 4;
 template <int D, int R>
 __global__ void __launch_bounds__(kMergeWarps * 32)
-paged_merge_kernel(const float* __restrict__ o_part, const float* __restrict__ lse_part, uint16_t* __restrict__ out,
-                   float* __restrict__ lse_out, long long rows, int n)
+paged_merge_kernel(const float* o_part, const float* lse_part, uint16_t* out, float* lse_out, long long rows, int n)
 {
     constexpr int W = D / 32;  // dimensions a lane
     using Vec = typename std::conditional<W == 4, float4, float2>::type;
