@@ -41,24 +41,25 @@ struct PagedArgs {
     float* lse_out;
     float scale;
     int Hq, Hkv, n_splits, slot0, n_slots, q_len;
-    int ordered;  // requests that are taken longest context first (0: in order)
+    int n_requests;
 };
 
 // One CTA per (request, KV head, split).  kMulti: several query tokens per request.
-template <int D, int NT, bool kMulti>
+// kOrdered: requests longest context first.
+template <int D, int NT, bool kMulti, bool kOrdered>
 __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 3) paged_bf16_kernel(const PagedArgs a)
 {
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ TileRows<NT> rows;
     __shared__ int row_last[NT * 8];
-    __shared__ OrderSmem order;
+    __shared__ typename std::conditional<kOrdered, OrderSmem, int>::type order;
     const int G = a.Hq / a.Hkv;
     const int h = blockIdx.x % a.Hkv;
     const int sp = (blockIdx.x / a.Hkv) % a.n_splits;
     int r = blockIdx.x / (a.Hkv * a.n_splits);
     dependents_may_launch();
     int len;
-    if (a.ordered > 0) r = request_at(a.kv, a.ordered, r, order, len);
+    if constexpr (kOrdered) r = request_at(a.kv, a.n_requests, r, order, len);
     else len = paged_len(a.kv, r);
     if (threadIdx.x < NT * 8) {
         const int j = threadIdx.x;
@@ -193,7 +194,7 @@ int launch_paged_bf16(const uint16_t* q, const PagedView& kv, float* o_part, flo
     if (grid == 0) return MOSKA_OK;
     if (grid > 0x7fffffffLL) return fail(MOSKA_ERR_UNSUPPORTED, "paged attention grid too large");
     const PagedArgs a{q, kv, o_part, lse_part, out, lse_out, scale, s->Hq, s->Hkv, s->n_unique_splits, slot0, n_slots, q_len,
-                      longest_first(s->B / q_len, grid) ? s->B / q_len : 0};
+                      s->B / q_len};
     auto go = [&](auto kernel, int smem) {
         MOSKA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
         kernel<<<(unsigned)grid, kThreads, smem, st>>>(a);
@@ -201,10 +202,14 @@ int launch_paged_bf16(const uint16_t* q, const PagedView& kv, float* o_part, flo
         return (int)MOSKA_OK;
     };
     constexpr int kRing = kWarps * kStagedWarpBytes;
-    if (s->D == 64) return go(paged_bf16_kernel<64, 1, false>, (int)sizeof(CombineSmem<64, 1>));
-    if (q_len == 1) return go(paged_bf16_kernel<128, 1, false>, kRing);
-    if (q_len * (s->Hq / s->Hkv) <= 8) return go(paged_bf16_kernel<128, 1, true>, kRing);
-    return go(paged_bf16_kernel<128, 2, true>, kRing);
+    auto form = [&](auto ordered) {
+        constexpr bool O = decltype(ordered)::value;
+        if (s->D == 64) return go(paged_bf16_kernel<64, 1, false, O>, (int)sizeof(CombineSmem<64, 1>));
+        if (q_len == 1) return go(paged_bf16_kernel<128, 1, false, O>, kRing);
+        if (q_len * (s->Hq / s->Hkv) <= 8) return go(paged_bf16_kernel<128, 1, true, O>, kRing);
+        return go(paged_bf16_kernel<128, 2, true, O>, kRing);
+    };
+    return longest_first(a.n_requests, grid) ? form(std::true_type{}) : form(std::false_type{});
 }
 
 }  // namespace moska

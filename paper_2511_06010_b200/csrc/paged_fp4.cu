@@ -105,7 +105,7 @@ struct AttnArgs {
     float* lse_out;
     float scale;
     int Hq, Hkv, n_splits, slot0, n_slots, q_len;
-    int ordered;  // requests that are taken longest context first (0: in order)
+    int n_requests;
 };
 
 // CTAs per SM.  D = 128: 164 registers (a fourth CTA would need 128: spills, slower).  D = 64: 123; four
@@ -114,7 +114,8 @@ struct AttnArgs {
 template <int D, int NT>
 constexpr int kCtasPerSm = NT == 2 ? 2 : D == 128 ? 3 : 4;
 
-template <int D, int NT>
+// kOrdered: requests longest context first.
+template <int D, int NT, bool kOrdered>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm<D, NT>) paged_fp4_kernel(const AttnArgs a)
 {
     using B = Fp4Block<D>;
@@ -123,7 +124,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<D, NT>) paged_fp4_kernel(
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ uint64_t full[kWarps][kDepth];
     __shared__ int gave_up;
-    __shared__ OrderSmem order;
+    __shared__ typename std::conditional<kOrdered, OrderSmem, int>::type order;
     __shared__ int64_t row_of[kRows];  // result row of each query row, -1: none
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, c = lane & 3;
@@ -135,8 +136,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<D, NT>) paged_fp4_kernel(
 
     dependents_may_launch();
     int len;
-    if (a.ordered > 0) r = request_at(a.kv, a.ordered, r, order, len);
-    else len = paged_len(a.kv, r);
+    if constexpr (kOrdered) r = request_at(a.kv, a.n_requests, r, order, len);
     if (threadIdx.x == 0) gave_up = 0;
     if (threadIdx.x < kRows) {
         const int j = threadIdx.x;
@@ -150,6 +150,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<D, NT>) paged_fp4_kernel(
     }
     __syncthreads();
 
+    if constexpr (!kOrdered) len = paged_len(a.kv, r);
     // this split's tokens: equal parts rounded up to a pass of the CTA's warps
     constexpr int kPass = kWarps * kUnit;
     int per = (len + a.n_splits - 1) / a.n_splits;
@@ -537,7 +538,7 @@ int launch_paged_fp4(const uint16_t* q, const PagedView& kv, float* o_part, floa
     if (grid == 0) return MOSKA_OK;
     if (grid > 0x7fffffffLL) return fail(MOSKA_ERR_UNSUPPORTED, "paged attention grid too large");
     const AttnArgs a{q, kv, o_part, lse_part, out, lse_out, scale, s->Hq, s->Hkv, s->n_unique_splits, slot0, n_slots, q_len,
-                     longest_first(s->B / q_len, grid) ? s->B / q_len : 0};
+                     s->B / q_len};
     auto go = [&](auto kernel, int ring) {
         MOSKA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ring));
         kernel<<<(unsigned)grid, kThreads, ring, st>>>(a);
@@ -545,9 +546,13 @@ int launch_paged_fp4(const uint16_t* q, const PagedView& kv, float* o_part, floa
         return (int)MOSKA_OK;
     };
     const bool two = q_len * (s->Hq / s->Hkv) > 8;
-    if (s->D == 128)
-        return two ? go(paged_fp4_kernel<128, 2>, F4Ring<128, 2>::kBytes) : go(paged_fp4_kernel<128, 1>, F4Ring<128, 1>::kBytes);
-    return two ? go(paged_fp4_kernel<64, 2>, F4Ring<64, 2>::kBytes) : go(paged_fp4_kernel<64, 1>, F4Ring<64, 1>::kBytes);
+    auto form = [&](auto ordered) {
+        constexpr bool O = decltype(ordered)::value;
+        if (s->D == 128)
+            return two ? go(paged_fp4_kernel<128, 2, O>, F4Ring<128, 2>::kBytes) : go(paged_fp4_kernel<128, 1, O>, F4Ring<128, 1>::kBytes);
+        return two ? go(paged_fp4_kernel<64, 2, O>, F4Ring<64, 2>::kBytes) : go(paged_fp4_kernel<64, 1, O>, F4Ring<64, 1>::kBytes);
+    };
+    return longest_first(a.n_requests, grid) ? form(std::true_type{}) : form(std::false_type{});
 }
 
 }  // namespace moska
