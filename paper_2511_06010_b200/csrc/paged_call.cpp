@@ -6,6 +6,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
@@ -85,6 +86,7 @@ struct Store {
     moska_paged_kv kv;  // format, page_size, n_pages and the pools
     int32_t Hkv, D;
     c10::Device device;
+    at::Tensor k, v;    // the pools (4 bits: no v)
 };
 
 Store* store_of(PyObject* o)
@@ -122,20 +124,44 @@ const int32_t* first_rows(PyObject* o, int64_t n_requests, int64_t n_rows, long 
     return nullptr;
 }
 
-// A Python stream address, or the device's current stream; the device is current while this lives.
+// A Python stream address, or the device's current stream; the device and the stream are current while this
+// lives.  What a call allocates then comes from the memory of the stream that writes it: a block of another
+// stream's may still be in use there.  On a stream other than the one that the caller is on, the allocator
+// is told who uses what: reads() for what the kernels touch, returns() for results, which the caller's
+// stream goes on with.  Without that a tensor dropped early would be handed out again too soon.
 struct OnDevice {
     c10::cuda::OptionalCUDAGuard guard;
+    c10::cuda::OptionalCUDAStreamGuard stream_guard;
     moska_stream stream = nullptr;
+    c10::optional<c10::cuda::CUDAStream> here, callers;  // set if they differ
     OnDevice(c10::Device device, PyObject* stream_o)
     {
         if (!device.is_cuda()) refuse("the store is not on a GPU");
         guard.set_device(device);
-        if (stream_o != Py_None) {
-            stream = PyLong_AsVoidPtr(stream_o);
-            if (stream == nullptr && PyErr_Occurred()) throw Failed{};
-        } else {
-            stream = c10::cuda::getCurrentCUDAStream(device.index()).stream();
-        }
+        const c10::cuda::CUDAStream current = c10::cuda::getCurrentCUDAStream(device.index());
+        stream = current.stream();
+        if (stream_o == Py_None) return;
+        stream = PyLong_AsVoidPtr(stream_o);
+        if (stream == nullptr && PyErr_Occurred()) throw Failed{};
+        // (torch knows the legacy default stream as 0 alone)
+        const auto known = stream == cudaStreamLegacy ? nullptr : static_cast<cudaStream_t>(stream);
+        if (known == current.stream()) return;
+        here = c10::cuda::getStreamFromExternal(known, device.index());
+        callers = current;
+        stream_guard.reset_stream(*here);
+    }
+    void reads(const at::Tensor& t) const
+    {
+        if (here && t.defined()) c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), *here);
+    }
+    void reads(PyObject* o) const
+    {
+        if (here && THPVariable_Check(o)) reads(THPVariable_Unpack(o));
+    }
+    void returns(const at::Tensor& t) const
+    {
+        reads(t);
+        if (here && t.defined()) c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), *callers);
     }
 };
 
@@ -192,7 +218,7 @@ PyObject* py_store(PyObject*, PyObject* const* a, Py_ssize_t n)
         const long format = whole(a[0]), page_size = whole(a[1]), n_pages = whole(a[2]), Hkv = whole(a[3]), D = whole(a[4]);
         if (n_pages > INT32_MAX || Hkv > INT32_MAX) refuse("too many pages or heads");
         const at::Tensor& k = tensor(a[5], "k_pages");
-        auto s = std::make_unique<Store>(Store{{}, (int32_t)Hkv, (int32_t)D, k.device()});
+        auto s = std::make_unique<Store>(Store{{}, (int32_t)Hkv, (int32_t)D, k.device(), k, {}});
         s->kv.format = (int32_t)format;
         s->kv.page_size = (int32_t)page_size;
         s->kv.n_pages = (int32_t)n_pages;
@@ -200,7 +226,8 @@ PyObject* py_store(PyObject*, PyObject* const* a, Py_ssize_t n)
             s->kv.k_pages = dense(k, "pages4", at::kByte, {n_pages, Hkv, page_size / 16, 18 * D}, s->device);
         } else {
             s->kv.k_pages = dense(k, "k_pages", at::kBFloat16, {n_pages, page_size, Hkv, D}, s->device);
-            s->kv.v_pages = dense(tensor(a[6], "v_pages"), "v_pages", at::kBFloat16, {n_pages, page_size, Hkv, D}, s->device);
+            s->v = tensor(a[6], "v_pages");
+            s->kv.v_pages = dense(s->v, "v_pages", at::kBFloat16, {n_pages, page_size, Hkv, D}, s->device);
         }
         PyObject* o = PyCapsule_New(s.get(), "moska.store", [](PyObject* c) {
             delete static_cast<Store*>(PyCapsule_GetPointer(c, "moska.store"));
@@ -247,8 +274,10 @@ PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n_args)
             Hq = q.size(1);
             const int64_t shape[3] = {n, Hq, s.D};
             qp = rows(q, "q", shape, s.device, &qs);
-            q_out = a[10] == Py_None ? at::empty(shape, q.options()) : tensor(a[10], "q_out");
-            to = static_cast<uint16_t*>(dense(q_out, "q_out", at::kBFloat16, shape, s.device));
+            if (a[10] != Py_None) {
+                q_out = tensor(a[10], "q_out");
+                to = static_cast<uint16_t*>(dense(q_out, "q_out", at::kBFloat16, shape, s.device));
+            }
         } else if (a[10] != Py_None) {
             refuse("q_out without q");
         }
@@ -266,12 +295,23 @@ PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n_args)
         }
         const int turned = PyObject_IsTrue(a[9]);
         if (turned < 0) throw Failed{};
+        const auto result = [&] { return at::empty({n, Hq, s.D}, at::TensorOptions().dtype(at::kBFloat16).device(s.device)); };
         if (n > 0) {
             const moska_shape shape = shape_of(n, Hq, s.Hkv, s.D, q_len);
             const OnDevice on(s.device, a[12]);
+            if (qp != nullptr && !q_out.defined()) {
+                q_out = result();
+                to = static_cast<uint16_t*>(q_out.data_ptr());
+            }
             check(g_append(qp, qs, kp, ks, vp, vs, at_position, table, (int32_t)n_positions, (int32_t)rot_dim, turned, first,
                            (int32_t)n_requests, to, &kv, &shape, on.stream),
                   "moska_kv_append_paged");
+            for (int i = 1; i < 9; ++i) on.reads(a[i]);
+            on.reads(s.k);
+            on.reads(s.v);
+            on.returns(q_out);
+        } else if (a[1] != Py_None && !q_out.defined()) {
+            q_out = result();
         }
         return q_out.defined() ? THPVariable_Wrap(q_out) : none();
     });
@@ -290,19 +330,37 @@ PyObject* py_gather(PyObject*, PyObject* const* a, Py_ssize_t n_args)
         if (first != nullptr) q_len = 1;
         const int64_t shape[3] = {n, s.Hkv, s.D};
         const auto options = at::TensorOptions().dtype(at::kBFloat16).device(s.device);
-        const at::Tensor k = a[6] == Py_None ? at::empty(shape, options) : tensor(a[6], "k_out");
-        const at::Tensor v = a[7] == Py_None ? at::empty(shape, options) : tensor(a[7], "v_out");
-        auto* kp = static_cast<uint16_t*>(dense(k, "k_out", at::kBFloat16, shape, s.device));
-        auto* vp = static_cast<uint16_t*>(dense(v, "v_out", at::kBFloat16, shape, s.device));
+        at::Tensor out[2];
+        uint16_t* to[2] = {nullptr, nullptr};
+        constexpr const char* names[2] = {"k_out", "v_out"};
+        for (int i = 0; i < 2; ++i) {
+            if (a[6 + i] == Py_None) continue;
+            out[i] = tensor(a[6 + i], names[i]);
+            to[i] = static_cast<uint16_t*>(dense(out[i], names[i], at::kBFloat16, shape, s.device));
+        }
+        const auto allocate = [&] {
+            for (int i = 0; i < 2; ++i) {
+                if (out[i].defined()) continue;
+                out[i] = at::empty(shape, options);
+                to[i] = static_cast<uint16_t*>(out[i].data_ptr());
+            }
+        };
         if (n > 0) {
             const moska_shape c_shape = shape_of(n, s.Hkv, s.Hkv, s.D, q_len);
             const OnDevice on(s.device, a[8]);
-            check(g_gather(first, (int32_t)n_requests, kp, vp, &kv, &c_shape, on.stream), "moska_kv_gather_paged");
+            allocate();
+            check(g_gather(first, (int32_t)n_requests, to[0], to[1], &kv, &c_shape, on.stream), "moska_kv_gather_paged");
+            for (int i : {1, 2, 4}) on.reads(a[i]);
+            on.reads(s.k);
+            on.reads(s.v);
+            for (const at::Tensor& t : out) on.returns(t);
+        } else {
+            allocate();
         }
         PyObject* pair = PyTuple_New(2);
         if (pair == nullptr) throw Failed{};
-        PyTuple_SET_ITEM(pair, 0, THPVariable_Wrap(k));
-        PyTuple_SET_ITEM(pair, 1, THPVariable_Wrap(v));
+        PyTuple_SET_ITEM(pair, 0, THPVariable_Wrap(out[0]));
+        PyTuple_SET_ITEM(pair, 1, THPVariable_Wrap(out[1]));
         return pair;
     });
 }
@@ -331,6 +389,11 @@ PyObject* py_attend(PyObject*, PyObject* const* a, Py_ssize_t n_args)
             if (PyErr_Occurred()) throw Failed{};
             const OnDevice on(s.device, a[10]);
             check(g_attend(qp, &kv, op, lp, (float)scale, &shape, wp, (size_t)ws.numel(), on.stream), "moska_paged_attn");
+            for (int i : {1, 2, 3, 9}) on.reads(a[i]);
+            on.reads(s.k);
+            on.reads(s.v);
+            on.returns(out);
+            on.returns(lse);
         }
         return none();
     });

@@ -23,6 +23,13 @@ _call.bind(*(ctypes.cast(getattr(M._lib, "moska_" + n), ctypes.c_void_p).value
              for n in ("kv_append_paged", "kv_gather_paged", "paged_attn")), M.MoskaError)
 
 
+def _settled(device) -> None:
+    """Waits until the device's current stream is done: fresh memory of the allocator may be what that stream was
+    still using, and the calls may run on another one."""
+    if device.type == "cuda" and not torch.cuda.is_current_stream_capturing():
+        torch.cuda.current_stream(device).synchronize()
+
+
 def _address(stream):
     """None (the current stream of the store's device), a stream object or a raw address -> what the calls take."""
     return stream if stream is None or isinstance(stream, int) else stream.cuda_stream
@@ -35,6 +42,9 @@ class PagedKvStore:
     per (token, KV head, 32 dimensions)): `pages4` uint8 [n_pages][Hkv][page_size / 16][18 D].
     A store over existing pools: PagedKvStore(k_pages=.., v_pages=..) or PagedKvStore(pages4=..,
     page_size=..); new ones: PagedKvStore.empty(...).  page_size is a power of two, 16..32768.
+
+    Calls run on the current stream, or on `stream`: their inputs have to be ready there, and their results are.
+    Results that a call makes, its inputs and the pools may be dropped at any time, on either stream.
     """
 
     def __init__(self, k_pages=None, v_pages=None, pages4=None, page_size: Optional[int] = None):
@@ -65,8 +75,11 @@ class PagedKvStore:
             raise ValueError(f"page_size = {page_size} is not a power of two of at least 16")
         if FORMATS[fmt] == M.KV_BF16:
             k, v = (torch.empty(n_pages, page_size, Hkv, D, dtype=torch.bfloat16, device=device) for _ in range(2))
-            return cls(k_pages=k, v_pages=v)
-        return cls(pages4=torch.empty(n_pages, Hkv, page_size // 16, 18 * D, dtype=torch.uint8, device=device))
+            st = cls(k_pages=k, v_pages=v)
+        else:
+            st = cls(pages4=torch.empty(n_pages, Hkv, page_size // 16, 18 * D, dtype=torch.uint8, device=device))
+        _settled(st.device)
+        return st
 
     def kv(self, page_table, kv_len) -> M.MoskaPagedKv:
         """The store seen through a page table int32 [R][max_pages] and context lengths int32 [R]."""
@@ -102,6 +115,7 @@ class PagedAttention:
         self.out = torch.empty(B, Hq, D, dtype=torch.bfloat16, device=device)
         self.lse = torch.empty(B, Hq, dtype=torch.float32, device=device)
         self.ws = torch.empty(M.paged_attn_workspace_bytes(self.shape), dtype=torch.uint8, device=device)
+        _settled(self.out.device)
 
     def __call__(self, q, store, page_table, kv_len, stream=None):
         """q bf16 [B][Hq][D] -> (out bf16 [B][Hq][D], lse float [B][Hq]), this object's buffers."""
