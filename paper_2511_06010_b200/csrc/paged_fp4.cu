@@ -13,6 +13,7 @@
 // largest), P is rounded to f16 (half a step: 2^-11), row sums and statistics are fp32.
 #include <cuda_bf16.h>
 
+#include <cfloat>
 #include <type_traits>
 
 #include "paged.cuh"
@@ -237,7 +238,8 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<D, NT>) paged_fp4_kernel(
             qf[n][2 * u + 1][0] = f16x2(x[u][4] * down, x[u][5] * down);
             qf[n][2 * u + 1][1] = f16x2(x[u][6] * down, x[u][7] * down);
         }
-        const float mul = a.scale * kLog2e * up;
+        // (neither 0 nor infinite: the -inf of a hidden token, or a score of 0, times that would be NaN)
+        const float mul = fminf(fmaxf(a.scale * up * kLog2e, FLT_MIN), FLT_MAX);
         unit[n][0] = __shfl_sync(0xffffffffu, mul, (2 * c) * 4);
         unit[n][1] = __shfl_sync(0xffffffffu, mul, (2 * c + 1) * 4);
     }
