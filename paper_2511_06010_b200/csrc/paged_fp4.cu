@@ -25,6 +25,8 @@ namespace {
 using namespace stream;
 static_assert(kThreads == kMaxOrdered, "a request a thread");
 
+constexpr float kBelow = 7.f, kMost = 15.f;  // log2 of P: of the largest when the reference is taken, at most
+
 // Blocks of a unit; of two column blocks four spill at 255 registers (48 x 4 query tokens: 62 us, 64 at four,
 // 76 at two).
 template <int NT>
@@ -255,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<D, NT>) paged_fp4_kernel(
         }
 
     float oacc[NT][MT][4];
-    float m_run[NT][2], l_run[NT][2];  // running maximum of the scores and row sum of columns 2c, 2c + 1
+    float m_run[NT][2], l_run[NT][2];  // reference of the scores (log2 units) and row sum of columns 2c, 2c + 1
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         m_run[n][0] = m_run[n][1] = -INFINITY;
@@ -301,8 +303,10 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<D, NT>) paged_fp4_kernel(
                 }
             }
         }
-        // ---- online softmax over the unit.  The maximum that P is relative to only moves when a score passes
-        // it by more than 2^8 (in P; f16 holds 2^16): rescaling the accumulators is rare that way.
+        // ---- online softmax over the unit.  P is relative to a reference (m_run) taken so that the largest P so
+        // far is 2^kBelow; it moves again when one would pass 2^kMost.  Rescaling the accumulators is rare that
+        // way, and f16 (steps of 2^-24 at its lower end) holds probabilities down to 2^-31 of the row's
+        // largest: what rounds to 0 adds up to less than 2^-12 in a million tokens.
         float mx[NT][2];
         bool grew = false;
 #pragma unroll
@@ -323,7 +327,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<D, NT>) paged_fp4_kernel(
                 mx[n][1] = fmaxf(mx[n][1], __shfl_xor_sync(0xffffffffu, mx[n][1], off));
             }
 #pragma unroll
-            for (int e = 0; e < 2; ++e) grew |= fmaf(mx[n][e], unit[n][e], -m_run[n][e]) > 8.f;
+            for (int e = 0; e < 2; ++e) grew |= fmaf(mx[n][e], unit[n][e], -m_run[n][e]) > kMost;
         }
         if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
@@ -331,7 +335,7 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm<D, NT>) paged_fp4_kernel(
                 float alpha[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float top = mx[n][e] * unit[n][e];
+                    const float top = mx[n][e] * unit[n][e] - kBelow;
                     // (m_run = -inf: no token seen yet, nothing to rescale; top = -inf: none in this unit either)
                     const bool moves = top > m_run[n][e];
                     alpha[e] = moves ? fast_exp2(m_run[n][e] - top) : 1.f;
