@@ -517,7 +517,10 @@ int moska_default_paged_splits(int32_t format, int32_t n_requests, int32_t Hkv, 
  *   row_start   NULL: shape->B rows, shape->q_len (0 or 1 = one) for each of n_requests = B / q_len
  *               requests, in order.  Else int32 [n_requests + 1], ascending: request r has rows
  *               row_start[r] .. row_start[r+1] - 1; rows from row_start[n_requests] to B are padding.
- *   q_out       bf16 [B][Hq][D] (16-byte aligned), not overlapping q
+ *   q_out       bf16 [B][Hq][D] (16-byte aligned)
+ * Rows are read and written at once, in no order: q_out, the pools and the range from the first to the last
+ * row of q, of k and of v may not overlap, but for q, k and v with one another.  A call where they do, or
+ * whose k_pages and v_pages do, is refused.
  * With n_r rows, row i of request r becomes context token kv_len[r] - n_r + i: kv_len counts the
  * tokens after the call.  Where that is negative the row is padding.  For padding rows nothing is
  * written, q_out included.  The rotation is (a, b) -> (a cos - b sin, b cos + a sin) in fp32, each
@@ -539,7 +542,7 @@ int moska_kv_append_paged(const uint16_t* q, int64_t q_stride, const uint16_t* k
  * Rows and requests as in moska_kv_append_paged: row i of request r is context token kv_len[r] - n_r
  * + i (kv->kv_len may be another array than the store's own lengths, to read an earlier range).
  * Padding rows are left as they were.
- *   k_out, v_out  bf16 [B][Hkv][D]   (16-byte aligned)
+ *   k_out, v_out  bf16 [B][Hkv][D]   (16-byte aligned), overlapping neither one another nor the pools
  */
 int moska_kv_gather_paged(const int32_t* row_start, int32_t n_requests, uint16_t* k_out, uint16_t* v_out,
                           const moska_paged_kv* kv, const moska_shape* shape, moska_stream stream);

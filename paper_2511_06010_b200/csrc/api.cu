@@ -985,6 +985,35 @@ int check_rows(const int32_t* row_start, int32_t n_requests, const moska_shape* 
     return MOSKA_OK;
 }
 
+// A buffer of a call, for the check that what it writes is apart from what it reads and writes elsewhere.
+struct Extent {
+    const char* name;
+    uintptr_t begin;
+    size_t bytes;
+};
+
+int check_apart(const Extent& a, const Extent& b)
+{
+    if (a.begin < b.begin + b.bytes && b.begin < a.begin + a.bytes && a.bytes > 0 && b.bytes > 0)
+        return fail(MOSKA_ERR_INVALID_ARG, "%s overlaps %s", a.name, b.name);
+    return MOSKA_OK;
+}
+
+// The rows of a strided argument, first to last.
+Extent extent_of(const char* name, const void* p, int64_t stride, int64_t row, int32_t rows)
+{
+    return {name, reinterpret_cast<uintptr_t>(p),
+            p == nullptr || rows == 0 ? 0 : ((size_t)(rows - 1) * stride + row) * sizeof(uint16_t)};
+}
+
+// The pools of a store: keys and values, or the one of the 4-bit format and nothing.
+void pool_extents(const moska_paged_kv* kv, const moska_shape* s, Extent (&pool)[2])
+{
+    const size_t bytes = moska_paged_pool_bytes(kv->format, kv->n_pages, kv->page_size, s->Hkv, s->D);
+    pool[0] = {"k_pages", reinterpret_cast<uintptr_t>(kv->k_pages), bytes};
+    pool[1] = {"v_pages", reinterpret_cast<uintptr_t>(kv->v_pages), kv->format == MOSKA_KV_BF16 ? bytes : 0};
+}
+
 int check_paged_attn(const moska_paged_kv* kv, float softmax_scale, const moska_shape* s)
 {
     const int G = s->Hq / s->Hkv;
@@ -1053,13 +1082,10 @@ int moska_kv_append_paged(const uint16_t* q, int64_t q_stride, const uint16_t* k
         REQUIRE_PTR(q_out, 16);
         if (q_stride % 8 != 0 || q_stride < (int64_t)shape->Hq * shape->D)
             return fail(MOSKA_ERR_INVALID_ARG, "q_stride = %lld must be a multiple of 8 and hold a row", (long long)q_stride);
-        const int64_t row = (int64_t)shape->Hq * shape->D;
-        if (shape->B > 0 && q < q_out + shape->B * row && q_out < q + (shape->B - 1) * q_stride + row)
-            return fail(MOSKA_ERR_INVALID_ARG, "q_out overlaps q");
     }
     REQUIRE_PTR(k, 16);
     REQUIRE_PTR(v, 16);
-    const int64_t row = (int64_t)shape->Hkv * shape->D;
+    const int64_t row = (int64_t)shape->Hkv * shape->D, q_row = (int64_t)shape->Hq * shape->D;
     if (k_stride % 8 != 0 || k_stride < row || v_stride % 8 != 0 || v_stride < row)
         return fail(MOSKA_ERR_INVALID_ARG, "k_stride = %lld, v_stride = %lld must be multiples of 8 and hold a row",
                     (long long)k_stride, (long long)v_stride);
@@ -1070,6 +1096,17 @@ int moska_kv_append_paged(const uint16_t* q, int64_t q_stride, const uint16_t* k
         REQUIRE_PTR(cos_sin, 16);
         if (n_positions < 1) return fail(MOSKA_ERR_INVALID_ARG, "n_positions = %d", n_positions);
     }
+    // rows are read and written at once, in no order
+    Extent pool[2];
+    pool_extents(kv, shape, pool);
+    const Extent to = extent_of("q_out", q_out, q_row, q_row, shape->B);
+    for (const Extent& from : {extent_of("q", q, q_stride, q_row, shape->B), extent_of("k", k, k_stride, row, shape->B),
+                               extent_of("v", v, v_stride, row, shape->B)}) {
+        MOSKA_TRY(check_apart(to, from));
+        for (const Extent& p : pool) MOSKA_TRY(check_apart(from, p));
+    }
+    for (const Extent& p : pool) MOSKA_TRY(check_apart(to, p));
+    MOSKA_TRY(check_apart(pool[0], pool[1]));
     MOSKA_TRY(check_device());
     MOSKA_TRY(status_word(&view.status));
     return launch_append_paged(q, q_stride, k, k_stride, v, v_stride, positions, cos_sin, n_positions, rot_dim,
@@ -1087,6 +1124,15 @@ int moska_kv_gather_paged(const int32_t* row_start, int32_t n_requests, uint16_t
     MOSKA_TRY(check_rows(row_start, n_requests, shape));
     REQUIRE_PTR(k_out, 16);
     REQUIRE_PTR(v_out, 16);
+    Extent pool[2];
+    pool_extents(kv, shape, pool);
+    const int64_t row = (int64_t)shape->Hkv * shape->D;
+    const Extent k_to = extent_of("k_out", k_out, row, row, shape->B), v_to = extent_of("v_out", v_out, row, row, shape->B);
+    MOSKA_TRY(check_apart(k_to, v_to));
+    for (const Extent& p : pool) {
+        MOSKA_TRY(check_apart(k_to, p));
+        MOSKA_TRY(check_apart(v_to, p));
+    }
     MOSKA_TRY(check_device());
     MOSKA_TRY(status_word(&view.status));
     return launch_gather_paged(row_start, n_requests, k_out, v_out, view, kv->format == MOSKA_KV_FP4, shape,
