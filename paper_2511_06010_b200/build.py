@@ -1,5 +1,6 @@
-"""Builds csrc/libmoska.so for sm_100a with nvcc (cross-compiles without a GPU), and _paged_call.so, the
-paged store's argument marshalling as a CPython module, with the host compiler.
+"""Builds csrc/libmoska.so for sm_100a with nvcc (cross-compiles without a GPU), and then, where torch is
+installed, _paged_call.so, the paged store's argument marshalling as a CPython module, with the host compiler.
+The library needs nvcc alone: a C program links it without Python.
 
 Every .cu file is compiled to an object of its own (in parallel, only when it or a header is
 newer than the object) under csrc/_build/, then linked.  Run as
@@ -15,6 +16,7 @@ import subprocess
 import sys
 import sysconfig
 from concurrent.futures import ThreadPoolExecutor
+from typing import Optional
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -51,29 +53,39 @@ def _stale(lib: str = LIB) -> bool:
     return _newer(sources() + _headers(), lib)
 
 
-def build_call(force: bool = False) -> str:
-    """Compiles the marshalling module against torch's headers."""
+def build_call(force: bool = False) -> Optional[str]:
+    """Compiles the marshalling module against torch's headers; None where there is no torch for CUDA."""
     if not force and not _newer([CALL_SOURCE, os.path.join(INCLUDE, "moska.h")], CALL):
         return CALL
-    import torch
-
+    try:
+        import torch
+    except ImportError:
+        return None
+    if torch.version.cuda is None:
+        return None
     root = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
-    include = [INCLUDE, os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
-               sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
+    system = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+              sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
     part = f"{CALL}.{os.getpid()}"
-    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-w",
+    subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wextra",
                            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
-                           *(x for d in include for x in ("-I", d)), CALL_SOURCE, "-o", part,
+                           "-I", INCLUDE, *(x for d in system for x in ("-isystem", d)), CALL_SOURCE, "-o", part,
                            "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
     os.replace(part, CALL)
     return CALL
 
 
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
-    lib = LIB_DEBUG if debug else LIB
+    lib = build_library(force, verbose, debug)
     if not debug:
         build_call(force)
+    return lib
+
+
+def build_library(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
+    """The CUDA library alone, or its debug form."""
+    lib = LIB_DEBUG if debug else LIB
     if not force and not _stale(lib):
         return lib
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
