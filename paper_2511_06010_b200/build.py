@@ -53,16 +53,23 @@ def _stale(lib: str = LIB) -> bool:
     return _newer(sources() + _headers(), lib)
 
 
+def _built_for(torch_version: str) -> bool:
+    """Whether the module that is there says that it was compiled against this torch (paged_call.cpp, BUILT_FOR)."""
+    with open(CALL, "rb") as f:
+        return f"torch {torch_version};".encode() in f.read()
+
+
 def build_call(force: bool = False) -> Optional[str]:
-    """Compiles the marshalling module against torch's headers; None where there is no torch for CUDA."""
-    if not force and not _newer([CALL_SOURCE, os.path.join(INCLUDE, "moska.h")], CALL):
-        return CALL
+    """Compiles the marshalling module against torch's headers (whose layout of tensors is that torch's alone); None
+    where there is no torch for CUDA."""
     try:
         import torch
     except ImportError:
         return None
     if torch.version.cuda is None:
         return None
+    if not force and not _newer([CALL_SOURCE, os.path.join(INCLUDE, "moska.h")], CALL) and _built_for(str(torch.__version__)):
+        return CALL
     root = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
     system = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
@@ -70,6 +77,7 @@ def build_call(force: bool = False) -> Optional[str]:
     part = f"{CALL}.{os.getpid()}"
     subprocess.check_call([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wextra",
                            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+                           f'-DBUILT_FOR="torch {torch.__version__};"',
                            "-I", INCLUDE, *(x for d in system for x in ("-isystem", d)), CALL_SOURCE, "-o", part,
                            "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
     os.replace(part, CALL)

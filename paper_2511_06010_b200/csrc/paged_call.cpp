@@ -407,4 +407,9 @@ PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_paged_call", nullptr, -1, met
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__paged_call() { return PyModule_Create(&module_def); }
+PyMODINIT_FUNC PyInit__paged_call()
+{
+    PyObject* m = PyModule_Create(&module_def);
+    if (m != nullptr && PyModule_AddStringConstant(m, "built_for", BUILT_FOR) < 0) Py_CLEAR(m);
+    return m;
+}

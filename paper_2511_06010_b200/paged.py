@@ -18,6 +18,10 @@ if not os.path.exists(os.path.join(os.path.dirname(os.path.abspath(__file__)), "
     raise ImportError("_paged_call.so is missing: build it with `python -m paper_2511_06010_b200.build`")
 from . import _paged_call as _call  # noqa: E402
 
+if _call.built_for != f"torch {torch.__version__};":  # it reads torch's tensors by that torch's layout
+    raise ImportError(f"_paged_call.so was built for {_call.built_for} this is {torch.__version__}: build it again with "
+                      "`python -m paper_2511_06010_b200.build`")
+
 FORMATS = {"bf16": M.KV_BF16, "fp4": M.KV_FP4}
 _call.bind(*(ctypes.cast(getattr(M._lib, "moska_" + n), ctypes.c_void_p).value
              for n in ("kv_append_paged", "kv_gather_paged", "paged_attn")), M.MoskaError)

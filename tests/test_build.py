@@ -19,3 +19,25 @@ def test_the_library_is_built_without_torch(tmp_path):
     r = subprocess.run([sys.executable, "-c", program], cwd=ROOT, capture_output=True, text=True, timeout=900)
     assert r.returncode == 0, r.stderr
     assert r.stdout.strip() == str(tmp_path / "libmoska.so") and os.listdir(tmp_path) == ["libmoska.so"]
+
+
+def test_a_module_built_for_another_torch_is_refused_and_built_again():
+    from paper_2511_06010_b200 import build
+
+    build.build()
+    program = ("import torch\n"
+               "torch.__version__ = '0.0'\n"
+               "from paper_2511_06010_b200 import build as b\n"
+               "b.os.replace = lambda *a: b.os.remove(a[0])\n"   # what it would build is thrown away
+               "made = []\n"
+               "b.subprocess.check_call = lambda c, **k: (made.append(c), open(c[c.index('-o') + 1], 'w').close())\n"
+               "b.build_call()\n"
+               "assert len(made) == 1, 'not built again'\n"
+               "try:\n"
+               "    import paper_2511_06010_b200.paged\n"
+               "except ImportError as e:\n"
+               "    assert 'build it again' in str(e), e\n"
+               "else:\n"
+               "    raise SystemExit('imported')\n")
+    r = subprocess.run([sys.executable, "-c", program], cwd=ROOT, capture_output=True, text=True, timeout=900)
+    assert r.returncode == 0, r.stderr + r.stdout
