@@ -4,6 +4,7 @@ torch owns the memory and the streams.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -132,7 +133,11 @@ class PagedAttention:
 
 class PageTable:
     """Which pages every request slot holds: a free list on the host and the int32 table [slots][max_pages]
-    on the device.  Entries of pages that a slot does not hold are -1."""
+    on the device.  Entries of pages that a slot does not hold are -1.
+
+    There is one device table, at one address (a captured graph finds the pages of each replay in it).  It is
+    rewritten by table(), so that calls reading it and table() have to follow one another on a stream: pass
+    table() the stream that the calls run on."""
 
     def __init__(self, n_pages, page_size, slots, max_pages, device="cuda"):
         self.page_size = page_size
@@ -140,6 +145,7 @@ class PageTable:
         self.held = np.zeros(slots, dtype=np.int64)  # pages of each slot
         self.free = list(range(n_pages - 1, -1, -1))
         self.device_table = torch.full((slots, max_pages), -1, dtype=torch.int32, device=device)
+        _settled(self.device_table.device)
         self._changed = False
 
     def reserve(self, slot: int, tokens: int) -> None:
@@ -165,9 +171,18 @@ class PageTable:
         self.held[slot] = 0
         self._changed = True
 
-    def table(self) -> torch.Tensor:
-        """The device table, brought up to date on the current stream."""
+    def table(self, stream=None) -> torch.Tensor:
+        """The device table, brought up to date on `stream` (the current one of its device without): after the calls
+        queued there, before those to come.  Returns when the copy is done."""
         if self._changed:
-            self.device_table.copy_(torch.from_numpy(self.host))
+            with self._on(stream):
+                self.device_table.copy_(torch.from_numpy(self.host))
             self._changed = False
         return self.device_table
+
+    def _on(self, stream):
+        if stream is None or self.device_table.device.type != "cuda":
+            return contextlib.nullcontext()
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=self.device_table.device)
+        return torch.cuda.stream(stream)

@@ -131,10 +131,10 @@ def test_an_attention_dropped_while_it_runs_on_another_stream(fmt):
 
 def test_buffers_of_new_objects_are_not_in_use_any_more():
     """A store or an attention is ready for every stream: nothing queued before may still write to its memory."""
-    from paper_2511_06010_b200.paged import PagedAttention, PagedKvStore
+    from paper_2511_06010_b200.paged import PagedAttention, PagedKvStore, PageTable
 
     for make in (lambda: PagedAttention(3, 16, 2, 128, 64, n_unique_splits=2), lambda: PagedKvStore.empty(4, 16, 2, 128),
-                 lambda: PagedKvStore.empty(4, 16, 2, 128, "fp4")):
+                 lambda: PagedKvStore.empty(4, 16, 2, 128, "fp4"), lambda: PageTable(4, 16, 2, 2)):
         torch.cuda._sleep(BUSY)
         assert not torch.cuda.current_stream().query()
         make()
@@ -161,3 +161,50 @@ def test_capture_with_a_stream_of_its_own():
     assert torch.equal(twice, q + q)
     ko, _ = st.gather(table, length, k.shape[0], q_len=64)
     assert torch.equal(ko, k2)
+
+
+@pytest.mark.parametrize("raw", [False, True])
+@pytest.mark.parametrize("fmt", ["bf16", "fp4"])
+def test_a_page_table_changes_behind_the_calls_that_read_it(fmt, raw):
+    """Calls queued on a stream still find the pages of their time when the book is changed and brought up to date
+    there, and calls that follow find the new ones."""
+    from paper_2511_06010_b200.paged import PagedAttention, PagedKvStore, PageTable
+
+    gen = torch.Generator().manual_seed(42)
+    Hq, Hkv, D, page, T = 16, 2, 128, 16, 64
+    st = PagedKvStore.empty(12, page, Hkv, D, fmt)
+    book = PageTable(12, page, 2, 4)
+    assert (book.table(0) == -1).all()
+    book.reserve(0, 1)
+    assert (book.table(0).cpu().numpy() == book.host).all()  # 0: the default stream's address
+    side = torch.cuda.Stream()
+    stream = side.cuda_stream if raw else side
+    length = torch.tensor([T, T], dtype=torch.int32).cuda()
+    k, v, k2, v2 = (R.make_bf16((2 * T, Hkv, D), gen).cuda() for _ in range(4))
+    q = R.make_bf16((2, Hq, D), gen).cuda()
+    one, two = (PagedAttention(2, Hq, Hkv, D, T, fmt=fmt, n_unique_splits=2) for _ in range(2))
+    for slot in (0, 1):
+        book.reserve(slot, T)
+    st.append(None, k, v, book.table(), length, q_len=T)
+    first = [t.clone() for t in one(q, st, book.table(), length)]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(BUSY)
+    out = one(q, st, book.table(), length, stream=stream)
+    old = book.host.copy()
+    book.release(0)                        # ... while that waits: other pages, or none
+    book.release(1)
+    book.reserve(0, T)
+    assert book.table(stream) is book.device_table
+    assert torch.equal(out[0], first[0]) and torch.equal(out[1], first[1])
+    book.reserve(1, T)
+    new = book.table(stream)
+    st.append(None, k2, v2, new, length, q_len=T, stream=stream)
+    out2 = two(q, st, book.table(stream), length, stream=stream)
+    torch.cuda.synchronize()
+    assert (book.device_table.cpu().numpy() == book.host).all() and (old != book.host).any()
+    fresh = PagedKvStore.empty(12, page, Hkv, D, fmt)
+    straight = torch.arange(8, dtype=torch.int32).reshape(2, 4).cuda()
+    fresh.append(None, k2, v2, straight, length, q_len=T)
+    want = one(q, fresh, straight, length)
+    assert torch.equal(out2[0], want[0]) and torch.equal(out2[1], want[1])
