@@ -306,7 +306,11 @@ PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n_args)
             check(g_append(qp, qs, kp, ks, vp, vs, at_position, table, (int32_t)n_positions, (int32_t)rot_dim, turned, first,
                            (int32_t)n_requests, to, &kv, &shape, on.stream),
                   "moska_kv_append_paged");
-            for (int i = 1; i < 9; ++i) on.reads(a[i]);
+            for (int i : {1, 2, 3, 4, 5, 8}) on.reads(a[i]);
+            if (table != nullptr) {
+                on.reads(a[6]);
+                on.reads(a[7]);
+            }
             on.reads(s.k);
             on.reads(s.v);
             on.returns(q_out);
