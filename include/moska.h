@@ -523,7 +523,7 @@ int moska_default_paged_splits(int32_t format, int32_t n_requests, int32_t Hkv, 
  * whose k_pages and v_pages do, is refused.
  * With n_r rows, row i of request r becomes context token kv_len[r] - n_r + i: kv_len counts the
  * tokens after the call.  Where that is negative the row is padding.  For padding rows nothing is
- * written, q_out included.  The rotation is (a, b) -> (a cos - b sin, b cos + a sin) in fp32, each
+ * written, q_out included (they keep what the buffer held).  The rotation is (a, b) -> (a cos - b sin, b cos + a sin) in fp32, each
  * product and sum rounded, the result rounded once to bf16, or to 4 bits: scale = f16(max|x| / 6) (at
  * most 10912), code = the E2M1 value nearest to x / scale, ties to the even code.  A NaN or an
  * infinity makes its 32 dimensions NaN.  Rows of one call must be different tokens; nothing outside
@@ -549,9 +549,14 @@ int moska_kv_gather_paged(const int32_t* row_start, int32_t n_requests, uint16_t
 
 /*
  * Unique KV Attention over a paged private store: the same partial results and slots as
- * moska_unique_attn.  4-bit format: Q (scaled by a power of two per row) and the codes multiply
- * exactly in f16 with fp32 accumulation, scales and softmax are fp32, values are widened to f16
- * (code * scale) and P is rounded to f16.  With q_len > 1: q_len * G <= 16, and D = 128 for bf16.
+ * moska_unique_attn.  With q_len > 1: q_len * G <= 16, and D = 128 for bf16.  Scores are summed in fp32,
+ * softmax and row sums are fp32.  Held in 16 bits:
+ *   bf16 format   P in bf16 (half a step: 2^-8)
+ *   4-bit format  queries in f16, scaled by a power of two per row: exact down to 2^-17 of the row's largest
+ *                 element, below that within 2^-25 of it; codes (exact); values as code * scale in f16 (2^-11,
+ *                 or 2^-25 absolute below 2^-14; value scales above 10912, which append does not write, overflow);
+ *                 P in f16 (2^-11; below 2^-21 of the row's largest within 2^-32 of that, so what is smaller
+ *                 counts in the row sum alone)
  *   softmax_scale  finite, > 0
  */
 int moska_unique_attn_paged(const uint16_t* q, const moska_paged_kv* kv, float* o_part, float* lse_part,

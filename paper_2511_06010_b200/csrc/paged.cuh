@@ -63,8 +63,8 @@ __device__ __forceinline__ int checked_len(const PagedView& p, int len)
 __device__ __forceinline__ int paged_len(const PagedView& p, int r) { return checked_len(p, __ldg(p.kv_len + r)); }
 
 // Attention takes the requests longest context first, so that no CTA of a long one starts when the others
-// are done.  4 bits, 64 requests of 1K to 32K: 248 -> 200 us at 2 splits, 48 x 4 query tokens 82 -> 64 us
-// at 1; bf16 676 -> 620 us at 2.  More requests than threads are many CTAs to a place and stay in order.
+// are done (default splits: 4 bits, 64 requests of 1K to 32K 260 -> 242 us, 48 x 4 query tokens 82 -> 64 us; bf16, 64
+// requests of 1K to 32K 703 -> 640 us).  More requests than threads are many CTAs to a place and stay in order.
 constexpr int kMaxOrdered = 128;
 struct OrderSmem {
     uint4 key[kMaxOrdered / 8];

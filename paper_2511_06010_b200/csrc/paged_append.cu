@@ -194,8 +194,8 @@ __device__ __forceinline__ void load4(const float* p, float* x)
 
 // A warp (or several, for few rows) per row.  Rotated or copied bf16 heads: D / 16 lanes a head, each with
 // two 8-element pieces that are each other's partners where the head is rotated, so an element is read
-// and widened once.  4-bit heads: D / 8 lanes a head with neighbouring pieces, because a scale covers 32
-// neighbouring dimensions; their partners come from the same lines again.
+// and widened once.  4-bit heads: D / 16 lanes a head too, each with sixteen neighbouring dimensions (a scale
+// covers 32 of them: two lanes); their partners come from the same lines again.
 // The first loads are on their way before it is known where the row goes.
 template <int D, bool kFp4, bool kInterleaved>
 __global__ void __launch_bounds__(kAppendThreads, 3) append_kernel(const AppendArgs a)

@@ -9,8 +9,9 @@
 // f16 in registers (cvt.rn.f16x2.e2m1x2, exact) for m16n8k16 MMAs with fp32 accumulation:
 //   S^T  = sum_j kscale[token][j] (K4_j Q_j^T)     one accumulator per 32 dimensions, scaled after it
 //   O^T += (V4 vscale[token][j])^T P               values scaled in f16, two tokens to a register
-// Q is scaled per row by a power of two into f16's range (exact but for elements 2^24 below the row's
-// largest), P is rounded to f16 (half a step: 2^-11), row sums and statistics are fp32.
+// Q is scaled per row by a power of two into f16's range: a bf16 element has eight bits and f16's steps end at
+// 2^-24, so it is exact down to 2^-17 of the row's largest, and within 2^-25 of that below.  P is rounded to f16
+// (half a step: 2^-11; 2^-32 of the row's largest at the lower end), row sums and statistics are fp32.
 #include <cuda_bf16.h>
 
 #include <cfloat>

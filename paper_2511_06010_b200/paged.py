@@ -96,13 +96,14 @@ class PagedKvStore:
         queries (q [N][Hq][D], or None).  kv_len counts the tokens after the call.  Request r has rows
         row_start[r] .. row_start[r+1] - 1, or q_len each without row_start.  cos_sin float
         [positions][rot_dim] (cos, then sin; None: no rotation), positions int32 [N].  q, k and v may be
-        columns of one projection's output."""
+        columns of one projection's output.  Padding rows (behind the last request, or of no token of a context)
+        are not written: they keep what q_out held, and in a result made here they hold anything."""
         return _call.append(self._handle, q, k, v, page_table, kv_len, positions, cos_sin, row_start, interleaved, q_out,
                             q_len, _address(stream))
 
     def gather(self, page_table, kv_len, n_rows, row_start=None, q_len=1, k_out=None, v_out=None, stream=None):
         """The last rows of the contexts as bf16 [n_rows][Hkv][D] keys and values; rows as in append.
-        Rows behind the last request keep what k_out and v_out hold."""
+        Padding rows keep what k_out and v_out held, as in append."""
         return _call.gather(self._handle, page_table, kv_len, n_rows, row_start, q_len, k_out, v_out, _address(stream))
 
 
