@@ -364,7 +364,7 @@ def _verify_plain(s):
         px = p[each, x]
         row = at[each, cur]
         qx = s["draft_probs"][row, x].double() if c["drafts"] else torch.ones_like(px)
-        taken = tried & (u[:, j] * qx * z < px)
+        taken = tried & (px > 0) & (u[:, j] * qx * z < px)
         failed = tried & ~taken
         if c["drafts"]:
             left = (p / z.unsqueeze(1) - s["draft_probs"][row].double()).clamp_(min=0.0)
@@ -543,7 +543,7 @@ def _exact_verify(s):
             if parents[a + j] != cur or not 0 <= x < V:
                 continue
             q = row(s["draft_probs"], a + cur) if c["drafts"] else None
-            if u[a + j] * (q[x] if c["drafts"] else 1.0) * z < p[x]:
+            if p[x] > 0 and u[a + j] * (q[x] if c["drafts"] else 1.0) * z < p[x]:
                 path.append(j)
                 cur, p, z = j, row(s["target_probs"], a + j), 1.0
             elif c["drafts"]:
