@@ -590,6 +590,104 @@ int moska_decode_step_paged(const uint16_t* q, const float* summaries, const voi
                             size_t ws_bytes, moska_stream stream, moska_stream side_stream,
                             moska_profiler* prof);
 
+/* ---- speculative decoding over a paged private store -----------------------------------------------
+ * A request's drafted tokens are a TREE.  Its nodes are consecutive batch rows, a parent before its
+ * children; parents[row] is the index, within the request, of the parent of that row's node, -1 for
+ * none.  Node 0 is the token that the last step sampled, the others are drafts.  The nodes' keys and values are
+ * appended like any rows (moska_kv_append_paged, a node's position being its depth behind the committed
+ * tokens), so that with T nodes they are context tokens kv_len[r] - T .. kv_len[r] - 1.  Then follow
+ * attention (each node sees the committed tokens, its ancestors and itself), verification, and the
+ * commit that keeps the accepted path's rows.
+ *   row_start   NULL: shape->q_len nodes for each of n_requests = B / q_len requests.  Else int32
+ *               [n_requests + 1], ascending: request r has rows row_start[r] .. row_start[r+1] - 1, at most
+ *               shape->q_len (more raise MOSKA_ERR_INVALID_ARG in the device status word, and the first
+ *               q_len count); rows from row_start[n_requests] to B are padding and left as they were.
+ *   parents     int32 [B].  A value that is not in -1 .. i - 1 for node i raises MOSKA_ERR_INVALID_ARG in the
+ *               device status word and counts as -1.  NULL (attention): a chain, node i under node i - 1.
+ * q_len is 1 .. MOSKA_TREE_MAX_NODES in these calls (0 = 1).  A request whose kv_len is smaller than its
+ * number of nodes is (partly) padding: nodes whose token index is negative hold nothing and see nothing.
+ */
+#define MOSKA_TREE_MAX_NODES 64
+
+/*
+ * Attention of the trees' nodes over the paged contexts that they end: final rows, both storage formats,
+ * D = 64 and 128.
+ *   q        bf16  [B][Hq][D]   (16-byte aligned)
+ *   out      bf16  [B][Hq][D]   (16-byte aligned); a row that sees nothing is 0
+ *   lse_out  float [B][Hq]      may be NULL; -inf for such a row
+ *   ws       moska_tree_attn_workspace_bytes(shape) bytes, 256-byte aligned; calls that share it must
+ *            not overlap.  Not read or written (may be NULL) with n_unique_splits = 1.
+ * shape: B, Hq, Hkv, D, q_len and n_unique_splits are read.  What a node does not see has no influence on it,
+ * infinities and NaN included.  Scores, softmax and row sums are fp32.
+ */
+int moska_tree_attn(const uint16_t* q, const moska_paged_kv* kv, const int32_t* parents, const int32_t* row_start,
+                    int32_t n_requests, uint16_t* out, float* lse_out, float softmax_scale, const moska_shape* shape,
+                    void* ws, size_t ws_bytes, moska_stream stream);
+size_t moska_tree_attn_workspace_bytes(const moska_shape* shape);
+
+/* A reasonable n_unique_splits for trees of up to `nodes` nodes that end contexts of up to `max_len`
+ * tokens.  Host only, pure. */
+int moska_default_tree_splits(int32_t format, int32_t n_requests, int32_t nodes, int32_t Hq, int32_t Hkv, int32_t D,
+                              int32_t max_len);
+
+/* Unique KV Attention of trees of shape->q_len nodes each: the partial results and slots of
+ * moska_unique_attn_paged, for a step that also attends to a shared store. */
+int moska_unique_attn_tree(const uint16_t* q, const moska_paged_kv* kv, const int32_t* parents, float* o_part,
+                           float* lse_part, float softmax_scale, const moska_shape* shape, moska_stream stream);
+
+/* moska_decode_step_paged for trees of shape->q_len nodes each: the shared store is attended to by every
+ * node as by a request of its own, the private context as in moska_tree_attn. */
+int moska_decode_step_tree(const uint16_t* q, const float* summaries, const void* k_shared,
+                           const void* v_shared, const float* k_scale_shared, const float* v_scale_shared,
+                           const moska_paged_kv* kv, const int32_t* parents, int32_t* topk_idx, int32_t* seg_offsets,
+                           int32_t* seg_entries, float* o_part, float* lse_part, uint16_t* out,
+                           float* lse_out, float softmax_scale, const moska_shape* shape, void* ws,
+                           size_t ws_bytes, moska_stream stream, moska_stream side_stream,
+                           moska_profiler* prof);
+
+/*
+ * Verification of drafted tokens against the target's probabilities, from given random numbers: the walk
+ * down each tree that keeps the target's distribution.  With cur = 0, P = row cur of target_probs and Z = 1,
+ * for the nodes j = 1, 2, .. whose parent is cur, in order, with x = tokens[j]:
+ *   accepted if P(x) > 0 and u_accept[j] q Z < P(x), q = draft_probs[cur][x] (1 without draft_probs): cur = j,
+ *   P = row j of target_probs, Z = 1; children of the new cur follow.  Else, with Q = row cur of draft_probs,
+ *   P becomes max(P / Z - Q, 0) and Z its sum (both stay where that sum is 0); without draft_probs (a draft that
+ *   was picked, not drawn) Z loses P(x) and P(x) becomes 0.
+ * At the end next_token is the first v with P(0) + .. + P(v) > u_next[r] sum(P) and P(v) > 0 (the last v with
+ * P(v) > 0 if there is none, -1 if P is 0 everywhere).  P, Z and the sums are held in 64 bits.
+ *   target_probs  [B][V] of prob_type, row i (elements i target_stride ..) behind node i; entries that are
+ *                 not > 0 (NaN included) count as 0
+ *   draft_probs   the same, with draft_stride; row i is what the children of node i were drawn from.
+ *                 May be NULL
+ *   tokens        int32 [B]; a node whose token is not in [0, V) is not tried
+ *   u_accept      float [B], u_next float [n_requests]: in [0, 1)
+ *   path          int32 [n_requests][max_nodes]: the accepted nodes, 0 first, then -1
+ *   n_path        int32 [n_requests]: how many (0 for a request without nodes, whose next_token is -1)
+ *   next_token    int32 [n_requests]
+ * B, row_start and max_nodes as B, row_start and q_len above.  The results may not overlap one another or the inputs.
+ */
+enum { MOSKA_PROB_F32 = 0, MOSKA_PROB_BF16 = 1 };
+int moska_verify_tree(const void* target_probs, int64_t target_stride, const void* draft_probs, int64_t draft_stride,
+                      int32_t prob_type, int32_t V, const int32_t* tokens, const int32_t* parents,
+                      const float* u_accept, const float* u_next, const int32_t* row_start, int32_t n_requests,
+                      int32_t max_nodes, int32_t B, int32_t* path, int32_t* n_path, int32_t* next_token,
+                      moska_stream stream);
+
+/*
+ * Keeps the rows of accepted paths: with T nodes and c = kv_len[r] - T committed tokens, context token
+ * c + path[r][j] is moved to c + j for every j < n_path[r], keys and values, as the bytes that they are, and
+ * kv_len_out[r] = c + n_path[r] (what is behind it stays in the pages and counts no more).
+ *   path        int32 [n_requests][path_stride], strictly ascending within n_path[r], each in [0, T)
+ *   n_path      int32 [n_requests], 0 .. min(T, path_stride)
+ *   kv_len_out  int32 [n_requests], apart from kv->kv_len
+ * A path that is not so raises MOSKA_ERR_INVALID_ARG in the device status word; its request is left as it
+ * was, kv_len_out[r] = kv_len[r].  The same, without an error, for a request with kv_len[r] < T (padding).
+ * Nodes' pages belong to one request alone.  shape: B, Hkv, D and q_len are read.
+ */
+int moska_kv_commit_paged(const int32_t* path, int32_t path_stride, const int32_t* n_path, const int32_t* row_start,
+                          int32_t n_requests, int32_t* kv_len_out, const moska_paged_kv* kv, const moska_shape* shape,
+                          moska_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -36,6 +36,8 @@ class MoskaPagedKv(ctypes.Structure):
 
 
 KV_BF16, KV_FP4 = 0, 1
+PROB_F32, PROB_BF16 = 0, 1
+TREE_MAX_NODES = 64
 
 
 class MoskaError(RuntimeError):
@@ -86,6 +88,13 @@ EXPORTS = {
     "moska_paged_attn": (_i, [_vp, _kvp, _vp, _vp, _f, _sp, _vp, _sz, _vp]),
     "moska_paged_attn_workspace_bytes": (_sz, [_sp]),
     "moska_decode_step_paged": (_i, [_vp] * 6 + [_kvp] + [_vp] * 7 + [_f, _sp, _vp, _sz, _vp, _vp, _vp]),
+    "moska_default_tree_splits": (_i, [ctypes.c_int32] * 7),
+    "moska_tree_attn_workspace_bytes": (_sz, [_sp]),
+    "moska_tree_attn": (_i, [_vp, _kvp, _vp, _vp, ctypes.c_int32, _vp, _vp, _f, _sp, _vp, _sz, _vp]),
+    "moska_unique_attn_tree": (_i, [_vp, _kvp, _vp, _vp, _vp, _f, _sp, _vp]),
+    "moska_decode_step_tree": (_i, [_vp] * 6 + [_kvp] + [_vp] * 8 + [_f, _sp, _vp, _sz, _vp, _vp, _vp]),
+    "moska_verify_tree": (_i, [_vp, _i64, _vp, _i64] + [ctypes.c_int32] * 2 + [_vp] * 5 + [ctypes.c_int32] * 3 + [_vp] * 4),
+    "moska_kv_commit_paged": (_i, [_vp, ctypes.c_int32, _vp, _vp, ctypes.c_int32, _vp, _kvp, _sp, _vp]),
     "moska_profiler_create": (_i, [ctypes.POINTER(_vp), ctypes.c_int32]),
     "moska_profiler_destroy": (None, [_vp]),
     "moska_profiler_select": (_i, [_vp, ctypes.c_uint32]),
@@ -416,6 +425,49 @@ def decode_step_paged(q, summaries, k_shared, v_shared, k_scale_shared, v_scale_
         ctypes.byref(kv), _ptr(topk_idx), _ptr(seg_offsets), _ptr(seg_entries), _ptr(o_part), _ptr(lse_part),
         _ptr(out), _ptr(lse_out), softmax_scale, ctypes.byref(s), _ptr(ws), ws_bytes, _stream(stream),
         None if side_stream is None else _stream(side_stream), prof), "moska_decode_step_paged")
+
+
+def default_tree_splits(fmt: int, n_requests: int, nodes: int, Hq: int, Hkv: int, D: int, max_len: int) -> int:
+    return _lib.moska_default_tree_splits(fmt, n_requests, nodes, Hq, Hkv, D, max_len)
+
+
+def tree_attn(q, kv, parents, row_start, n_requests, out, lse_out, softmax_scale, s, ws, stream=None) -> None:
+    ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(_lib.moska_tree_attn(_ptr(q), ctypes.byref(kv), _ptr(parents), _ptr(row_start), n_requests, _ptr(out), _ptr(lse_out),
+                                softmax_scale, ctypes.byref(s), _ptr(ws), ws_bytes, _stream(stream)), "moska_tree_attn")
+
+
+def tree_attn_workspace_bytes(s: MoskaShape) -> int:
+    return _lib.moska_tree_attn_workspace_bytes(ctypes.byref(s))
+
+
+def unique_attn_tree(q, kv, parents, o_part, lse_part, softmax_scale, s, stream=None) -> None:
+    _check(_lib.moska_unique_attn_tree(_ptr(q), ctypes.byref(kv), _ptr(parents), _ptr(o_part), _ptr(lse_part), softmax_scale,
+                                       ctypes.byref(s), _stream(stream)), "moska_unique_attn_tree")
+
+
+def decode_step_tree(q, summaries, k_shared, v_shared, k_scale_shared, v_scale_shared, kv, parents, topk_idx, seg_offsets,
+                     seg_entries, o_part, lse_part, out, lse_out, softmax_scale, s, ws, stream=None,
+                     side_stream=None, prof=None) -> None:
+    ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(_lib.moska_decode_step_tree(
+        _ptr(q), _ptr(summaries), _ptr(k_shared), _ptr(v_shared), _ptr(k_scale_shared), _ptr(v_scale_shared),
+        ctypes.byref(kv), _ptr(parents), _ptr(topk_idx), _ptr(seg_offsets), _ptr(seg_entries), _ptr(o_part), _ptr(lse_part),
+        _ptr(out), _ptr(lse_out), softmax_scale, ctypes.byref(s), _ptr(ws), ws_bytes, _stream(stream),
+        None if side_stream is None else _stream(side_stream), prof), "moska_decode_step_tree")
+
+
+def verify_tree(target_probs, target_stride, draft_probs, draft_stride, prob_type, V, tokens, parents, u_accept, u_next,
+                row_start, n_requests, max_nodes, B, path, n_path, next_token, stream=None) -> None:
+    """target_probs and draft_probs as addresses: their rows may lie apart."""
+    _check(_lib.moska_verify_tree(target_probs, target_stride, draft_probs, draft_stride, prob_type, V, _ptr(tokens),
+                                  _ptr(parents), _ptr(u_accept), _ptr(u_next), _ptr(row_start), n_requests, max_nodes, B,
+                                  _ptr(path), _ptr(n_path), _ptr(next_token), _stream(stream)), "moska_verify_tree")
+
+
+def kv_commit_paged(path, path_stride, n_path, row_start, n_requests, kv_len_out, kv, s, stream=None) -> None:
+    _check(_lib.moska_kv_commit_paged(_ptr(path), path_stride, _ptr(n_path), _ptr(row_start), n_requests, _ptr(kv_len_out),
+                                      ctypes.byref(kv), ctypes.byref(s), _stream(stream)), "moska_kv_commit_paged")
 
 
 STAGES = ("route", "group", "shared", "unique", "merge")

@@ -504,6 +504,8 @@ struct UniqueKv {
     const float* v_scale = nullptr;
     bool fp8 = false;
     const moska_paged_kv* paged = nullptr;  // pages in either format; kv_start and kv_len are not used
+    const int32_t* parents = nullptr;       // pages: the batch rows are nodes of drafted trees (`tree`) with these parents
+    bool tree = false;
 
     double token_bytes(int D) const  // one KV head's bytes of a token
     {
@@ -516,6 +518,7 @@ int unique_impl(const uint16_t* q, const UniqueKv& kv, const int64_t* kv_start, 
                 float* o_part, float* lse_part, float softmax_scale, const moska_shape* shape,
                 cudaStream_t st)
 {
+    if (kv.tree) return moska_unique_attn_tree(q, kv.paged, kv.parents, o_part, lse_part, softmax_scale, shape, st);
     if (kv.paged != nullptr)
         return moska_unique_attn_paged(q, kv.paged, o_part, lse_part, softmax_scale, shape, st);
     if (kv.fp8)
@@ -1026,6 +1029,24 @@ int check_paged_attn(const moska_paged_kv* kv, float softmax_scale, const moska_
     if (s->n_unique_splits < 1) return fail(MOSKA_ERR_INVALID_ARG, "n_unique_splits must be >= 1");
     return MOSKA_OK;
 }
+// A step over pages: the shared store is bf16, or FP8 where it has scales.
+int step_with_shared(const uint16_t* q, const float* summaries, const void* k_shared, const void* v_shared,
+                     const float* k_scale_shared, const float* v_scale_shared, const UniqueKv& unique, int32_t* topk_idx,
+                     int32_t* seg_offsets, int32_t* seg_entries, float* o_part, float* lse_part, uint16_t* out, float* lse_out,
+                     float softmax_scale, const moska_shape* shape, void* ws, size_t ws_bytes, moska_stream stream,
+                     moska_stream side_stream, moska_profiler* prof)
+{
+    SharedF8 f8;
+    f8.k8 = static_cast<const uint8_t*>(k_shared);
+    f8.v8 = static_cast<const uint8_t*>(v_shared);
+    f8.k_scale = k_scale_shared;
+    f8.v_scale = v_scale_shared;
+    const bool fp8 = k_scale_shared != nullptr;
+    return decode_step_impl(q, summaries, fp8 ? nullptr : static_cast<const uint16_t*>(k_shared),
+                            fp8 ? nullptr : static_cast<const uint16_t*>(v_shared), fp8 ? &f8 : nullptr, unique,
+                            nullptr, nullptr, topk_idx, seg_offsets, seg_entries, o_part, lse_part, out, lse_out,
+                            softmax_scale, shape, ws, ws_bytes, stream, side_stream, prof);
+}
 }  // namespace
 
 size_t moska_paged_pool_bytes(int32_t format, int32_t n_pages, int32_t page_size, int32_t Hkv, int32_t D)
@@ -1210,16 +1231,227 @@ int moska_decode_step_paged(const uint16_t* q, const float* summaries, const voi
         return fail(MOSKA_ERR_INVALID_ARG, "k_scale_shared and v_scale_shared are given together or not at all");
     UniqueKv unique;
     unique.paged = kv;
-    SharedF8 f8;
-    f8.k8 = static_cast<const uint8_t*>(k_shared);
-    f8.v8 = static_cast<const uint8_t*>(v_shared);
-    f8.k_scale = k_scale_shared;
-    f8.v_scale = v_scale_shared;
-    const bool fp8 = k_scale_shared != nullptr;
-    return decode_step_impl(q, summaries, fp8 ? nullptr : static_cast<const uint16_t*>(k_shared),
-                            fp8 ? nullptr : static_cast<const uint16_t*>(v_shared), fp8 ? &f8 : nullptr, unique,
-                            nullptr, nullptr, topk_idx, seg_offsets, seg_entries, o_part, lse_part, out, lse_out,
-                            softmax_scale, shape, ws, ws_bytes, stream, side_stream, prof);
+    return step_with_shared(q, summaries, k_shared, v_shared, k_scale_shared, v_scale_shared, unique, topk_idx, seg_offsets,
+                            seg_entries, o_part, lse_part, out, lse_out, softmax_scale, shape, ws, ws_bytes, stream,
+                            side_stream, prof);
+}
+
+namespace {
+// The rows of trees: shape->q_len nodes at most, in order or by row_start.
+int check_tree(const int32_t* parents, const int32_t* row_start, int32_t n_requests, int32_t max_nodes, int32_t B, TreeRows* out)
+{
+    const int32_t nodes = max_nodes > 1 ? max_nodes : 1;
+    if (max_nodes < 0 || nodes > MOSKA_TREE_MAX_NODES)
+        return fail(MOSKA_ERR_INVALID_ARG, "%d nodes a tree, 1..%d are possible", max_nodes, MOSKA_TREE_MAX_NODES);
+    if (n_requests < 0 || (n_requests == 0 && B > 0) || B < 0)
+        return fail(MOSKA_ERR_INVALID_ARG, "n_requests = %d for B = %d rows", n_requests, B);
+    if (row_start == nullptr && (long long)n_requests * nodes != B)
+        return fail(MOSKA_ERR_INVALID_ARG, "without row_start, n_requests * nodes = %lld must be B = %d",
+                    (long long)n_requests * nodes, B);
+    if (!aligned(row_start, 4)) return fail(MOSKA_ERR_INVALID_ARG, "row_start is not 4-byte aligned");
+    if (!aligned(parents, 4)) return fail(MOSKA_ERR_INVALID_ARG, "parents is not 4-byte aligned");
+    *out = TreeRows{parents, row_start, n_requests, nodes, B};
+    return MOSKA_OK;
+}
+
+// shape without the condition that q_len divides B: with row_start it is the largest tree
+int check_tree_heads(const moska_shape* s)
+{
+    if (s == nullptr) return fail(MOSKA_ERR_INVALID_ARG, "shape is NULL");
+    moska_shape one = *s;
+    one.q_len = 0;
+    return check_heads(&one);
+}
+
+int check_tree_attn(float softmax_scale, const moska_shape* s)
+{
+    if (!(softmax_scale > 0.f) || !std::isfinite(softmax_scale))
+        return fail(MOSKA_ERR_INVALID_ARG, "softmax_scale must be finite and > 0");
+    if (s->n_unique_splits < 1) return fail(MOSKA_ERR_INVALID_ARG, "n_unique_splits must be >= 1");
+    return MOSKA_OK;
+}
+}  // namespace
+
+int moska_default_tree_splits(int32_t format, int32_t n_requests, int32_t nodes, int32_t Hq, int32_t Hkv, int32_t D,
+                              int32_t max_len)
+{
+    if (n_requests <= 0 || nodes <= 0 || Hkv <= 0 || Hq < Hkv || max_len <= 0) return 1;
+    return default_tree_splits(format == MOSKA_KV_FP4, n_requests, nodes, Hq / Hkv, Hkv, D, max_len);
+}
+
+size_t moska_tree_attn_workspace_bytes(const moska_shape* shape)
+{
+    if (check_tree_heads(shape) != MOSKA_OK || shape->n_unique_splits < 2) return 0;
+    const size_t slots = (size_t)shape->B * shape->Hq * shape->n_unique_splits;
+    return round_up(slots * shape->D * sizeof(float), 256) + round_up(slots * sizeof(float), 256);
+}
+
+int moska_tree_attn(const uint16_t* q, const moska_paged_kv* kv, const int32_t* parents, const int32_t* row_start,
+                    int32_t n_requests, uint16_t* out, float* lse_out, float softmax_scale, const moska_shape* shape,
+                    void* ws, size_t ws_bytes, moska_stream stream)
+{
+    MOSKA_API_RANGE();
+    MOSKA_TRY(check_tree_heads(shape));
+    PagedView view{};
+    MOSKA_TRY(paged_view(kv, shape, &view));
+    TreeRows tree{};
+    MOSKA_TRY(check_tree(parents, row_start, n_requests, shape->q_len, shape->B, &tree));
+    MOSKA_TRY(check_tree_attn(softmax_scale, shape));
+    REQUIRE_PTR(q, 16);
+    REQUIRE_PTR(out, 16);
+    if (lse_out != nullptr && !aligned(lse_out, 4)) return fail(MOSKA_ERR_INVALID_ARG, "lse_out is not 4-byte aligned");
+    const size_t need = moska_tree_attn_workspace_bytes(shape);
+    if (need > 0 && (ws == nullptr || !aligned(ws, 256) || ws_bytes < need))
+        return fail(MOSKA_ERR_WORKSPACE, "workspace missing, misaligned or smaller than %zu bytes", need);
+    MOSKA_TRY(check_device());
+    MOSKA_TRY(status_word(&view.status));
+    const bool fp4 = kv->format == MOSKA_KV_FP4;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (shape->n_unique_splits == 1)
+        return launch_tree_attn(q, view, fp4, tree, nullptr, nullptr, 0, 1, out, lse_out, softmax_scale, shape, st);
+    float* o_part = static_cast<float*>(ws);
+    const size_t o_bytes = (size_t)shape->B * shape->Hq * shape->n_unique_splits * shape->D * sizeof(float);
+    float* lse_part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + round_up(o_bytes, 256));
+    MOSKA_TRY(launch_tree_attn(q, view, fp4, tree, o_part, lse_part, 0, shape->n_unique_splits, nullptr, nullptr,
+                               softmax_scale, shape, st));
+    return launch_paged_merge(o_part, lse_part, out, lse_out, shape, st, row_start == nullptr ? nullptr : row_start + n_requests);
+}
+
+int moska_unique_attn_tree(const uint16_t* q, const moska_paged_kv* kv, const int32_t* parents, float* o_part,
+                           float* lse_part, float softmax_scale, const moska_shape* shape, moska_stream stream)
+{
+    MOSKA_API_RANGE();
+    MOSKA_TRY(check_shape(shape, false));
+    PagedView view{};
+    MOSKA_TRY(paged_view(kv, shape, &view));
+    TreeRows tree{};
+    MOSKA_TRY(check_tree(parents, nullptr, shape->B / (shape->q_len > 1 ? shape->q_len : 1), shape->q_len, shape->B, &tree));
+    MOSKA_TRY(check_tree_attn(softmax_scale, shape));
+    REQUIRE_PTR(q, 16);
+    REQUIRE_PTR(o_part, 16);
+    REQUIRE_PTR(lse_part, 4);
+    MOSKA_TRY(check_device());
+    MOSKA_TRY(status_word(&view.status));
+    return launch_tree_attn(q, view, kv->format == MOSKA_KV_FP4, tree, o_part, lse_part, shape->shared_slots,
+                            shape->shared_slots + shape->n_unique_splits, nullptr, nullptr, softmax_scale, shape,
+                            (cudaStream_t)stream);
+}
+
+int moska_decode_step_tree(const uint16_t* q, const float* summaries, const void* k_shared,
+                           const void* v_shared, const float* k_scale_shared, const float* v_scale_shared,
+                           const moska_paged_kv* kv, const int32_t* parents, int32_t* topk_idx, int32_t* seg_offsets,
+                           int32_t* seg_entries, float* o_part, float* lse_part, uint16_t* out,
+                           float* lse_out, float softmax_scale, const moska_shape* shape, void* ws,
+                           size_t ws_bytes, moska_stream stream, moska_stream side_stream,
+                           moska_profiler* prof)
+{
+    MOSKA_API_RANGE();
+    MOSKA_TRY(check_shape(shape, summaries != nullptr));
+    PagedView view{};
+    MOSKA_TRY(paged_view(kv, shape, &view));
+    TreeRows tree{};
+    MOSKA_TRY(check_tree(parents, nullptr, shape->B / (shape->q_len > 1 ? shape->q_len : 1), shape->q_len, shape->B, &tree));
+    MOSKA_TRY(check_tree_attn(softmax_scale, shape));
+    if ((k_scale_shared == nullptr) != (v_scale_shared == nullptr))
+        return fail(MOSKA_ERR_INVALID_ARG, "k_scale_shared and v_scale_shared are given together or not at all");
+    UniqueKv unique;
+    unique.paged = kv;
+    unique.parents = parents;
+    unique.tree = true;
+    return step_with_shared(q, summaries, k_shared, v_shared, k_scale_shared, v_scale_shared, unique, topk_idx, seg_offsets,
+                            seg_entries, o_part, lse_part, out, lse_out, softmax_scale, shape, ws, ws_bytes, stream,
+                            side_stream, prof);
+}
+
+int moska_verify_tree(const void* target_probs, int64_t target_stride, const void* draft_probs, int64_t draft_stride,
+                      int32_t prob_type, int32_t V, const int32_t* tokens, const int32_t* parents,
+                      const float* u_accept, const float* u_next, const int32_t* row_start, int32_t n_requests,
+                      int32_t max_nodes, int32_t B, int32_t* path, int32_t* n_path, int32_t* next_token,
+                      moska_stream stream)
+{
+    MOSKA_API_RANGE();
+    if (prob_type != MOSKA_PROB_F32 && prob_type != MOSKA_PROB_BF16)
+        return fail(MOSKA_ERR_INVALID_ARG, "prob_type = %d", prob_type);
+    if (V < 1 || V > (1 << 30)) return fail(MOSKA_ERR_INVALID_ARG, "V = %d is not in 1..2^30", V);
+    TreeRows tree{};
+    MOSKA_TRY(check_tree(parents, row_start, n_requests, max_nodes, B, &tree));
+    const size_t size = prob_type == MOSKA_PROB_F32 ? sizeof(float) : sizeof(uint16_t);
+    if (B > 0) {
+        REQUIRE_PTR(target_probs, size);
+        REQUIRE_PTR(tokens, 4);
+        REQUIRE_PTR(parents, 4);
+        REQUIRE_PTR(u_accept, 4);
+    }
+    if (!aligned(draft_probs, size)) return fail(MOSKA_ERR_INVALID_ARG, "draft_probs is not %zu-byte aligned", size);
+    if (target_stride < V || (draft_probs != nullptr && draft_stride < V))
+        return fail(MOSKA_ERR_INVALID_ARG, "target_stride = %lld, draft_stride = %lld must hold a row of %d",
+                    (long long)target_stride, (long long)draft_stride, V);
+    if (n_requests > 0) {
+        REQUIRE_PTR(u_next, 4);
+        REQUIRE_PTR(path, 4);
+        REQUIRE_PTR(n_path, 4);
+        REQUIRE_PTR(next_token, 4);
+    }
+    auto extent = [](const char* name, const void* p, size_t bytes) {
+        return Extent{name, reinterpret_cast<uintptr_t>(p), p == nullptr ? 0 : bytes};
+    };
+    auto span = [&](int64_t stride) { return B == 0 ? 0 : ((size_t)(B - 1) * stride + V) * size; };
+    const size_t rows = (size_t)B * 4, requests = (size_t)n_requests * 4;
+    const Extent to[3] = {extent("path", path, requests * tree.max_nodes), extent("n_path", n_path, requests),
+                          extent("next_token", next_token, requests)};
+    const Extent from[7] = {extent("target_probs", target_probs, span(target_stride)),
+                            extent("draft_probs", draft_probs, span(draft_stride)), extent("tokens", tokens, rows),
+                            extent("parents", parents, rows), extent("u_accept", u_accept, rows),
+                            extent("u_next", u_next, requests), extent("row_start", row_start, requests + 4)};
+    for (int i = 0; i < 3; ++i) {
+        for (int j = 0; j < i; ++j) MOSKA_TRY(check_apart(to[j], to[i]));
+        for (const Extent& f : from) MOSKA_TRY(check_apart(to[i], f));
+    }
+    MOSKA_TRY(check_device());
+    int* status = nullptr;
+    MOSKA_TRY(status_word(&status));
+    return launch_verify(target_probs, target_stride, draft_probs, draft_stride, prob_type == MOSKA_PROB_BF16, V, tokens,
+                         u_accept, u_next, tree, path, n_path, next_token, status, (cudaStream_t)stream);
+}
+
+int moska_kv_commit_paged(const int32_t* path, int32_t path_stride, const int32_t* n_path, const int32_t* row_start,
+                          int32_t n_requests, int32_t* kv_len_out, const moska_paged_kv* kv, const moska_shape* shape,
+                          moska_stream stream)
+{
+    MOSKA_API_RANGE();
+    if (shape == nullptr) return fail(MOSKA_ERR_INVALID_ARG, "shape is NULL");
+    moska_shape heads = *shape;  // (no queries here)
+    heads.Hq = heads.Hkv;
+    heads.q_len = 0;
+    MOSKA_TRY(check_heads(&heads));
+    PagedView view{};
+    MOSKA_TRY(paged_view(kv, &heads, &view));
+    TreeRows tree{};
+    MOSKA_TRY(check_tree(nullptr, row_start, n_requests, shape->q_len, shape->B, &tree));
+    if (path_stride < 1) return fail(MOSKA_ERR_INVALID_ARG, "path_stride = %d", path_stride);
+    REQUIRE_PTR(path, 4);
+    REQUIRE_PTR(n_path, 4);
+    REQUIRE_PTR(kv_len_out, 4);
+    const size_t requests = (size_t)n_requests * 4;
+    auto extent = [](const char* name, const void* p, size_t bytes) {
+        return Extent{name, reinterpret_cast<uintptr_t>(p), p == nullptr ? 0 : bytes};
+    };
+    Extent pool[2];
+    pool_extents(kv, &heads, pool);
+    const Extent to = extent("kv_len_out", kv_len_out, requests);
+    const Extent from[5] = {extent("kv_len", kv->kv_len, requests), extent("path", path, requests * path_stride),
+                            extent("n_path", n_path, requests), extent("row_start", row_start, requests + 4),
+                            extent("page_table", kv->page_table, requests * kv->max_pages)};
+    for (const Extent& f : from) {
+        MOSKA_TRY(check_apart(to, f));
+        for (const Extent& p : pool) MOSKA_TRY(check_apart(f, p));
+    }
+    for (const Extent& p : pool) MOSKA_TRY(check_apart(to, p));
+    MOSKA_TRY(check_apart(pool[0], pool[1]));
+    MOSKA_TRY(check_device());
+    MOSKA_TRY(status_word(&view.status));
+    return launch_commit_paged(path, path_stride, n_path, tree, kv_len_out, view, kv->format == MOSKA_KV_FP4, shape,
+                               (cudaStream_t)stream);
 }
 
 }  // extern "C"

@@ -23,9 +23,19 @@ using Append = int (*)(const uint16_t*, int64_t, const uint16_t*, int64_t, const
 using Gather = int (*)(const int32_t*, int32_t, uint16_t*, uint16_t*, const moska_paged_kv*, const moska_shape*, moska_stream);
 using Attend = int (*)(const uint16_t*, const moska_paged_kv*, uint16_t*, float*, float, const moska_shape*, void*, size_t,
                        moska_stream);
+using Commit = int (*)(const int32_t*, int32_t, const int32_t*, const int32_t*, int32_t, int32_t*, const moska_paged_kv*,
+                       const moska_shape*, moska_stream);
+using TreeAttend = int (*)(const uint16_t*, const moska_paged_kv*, const int32_t*, const int32_t*, int32_t, uint16_t*, float*,
+                           float, const moska_shape*, void*, size_t, moska_stream);
+using Verify = int (*)(const void*, int64_t, const void*, int64_t, int32_t, int32_t, const int32_t*, const int32_t*,
+                       const float*, const float*, const int32_t*, int32_t, int32_t, int32_t, int32_t*, int32_t*, int32_t*,
+                       moska_stream);
 Append g_append = nullptr;
 Gather g_gather = nullptr;
 Attend g_attend = nullptr;
+Commit g_commit = nullptr;
+TreeAttend g_tree_attend = nullptr;
+Verify g_verify = nullptr;
 PyObject* g_error = nullptr;  // MoskaError(status, where)
 
 struct Failed {};  // a Python exception is set
@@ -136,7 +146,7 @@ struct OnDevice {
     c10::optional<c10::cuda::CUDAStream> here, callers;  // set if they differ
     OnDevice(c10::Device device, PyObject* stream_o)
     {
-        if (!device.is_cuda()) refuse("the store is not on a GPU");
+        if (!device.is_cuda()) refuse("the tensors are not on a GPU");
         guard.set_device(device);
         const c10::cuda::CUDAStream current = c10::cuda::getCurrentCUDAStream(device.index());
         stream = current.stream();
@@ -196,17 +206,20 @@ PyObject* none()
     return Py_None;
 }
 
-// bind(append, gather, paged_attn, MoskaError): addresses of the entry points
+// bind(append, gather, paged_attn, commit, tree_attn, verify, MoskaError): addresses of the entry points
 PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
-    return guarded(n, 4, [&] {
+    return guarded(n, 7, [&] {
         g_append = reinterpret_cast<Append>(PyLong_AsVoidPtr(a[0]));
         g_gather = reinterpret_cast<Gather>(PyLong_AsVoidPtr(a[1]));
         g_attend = reinterpret_cast<Attend>(PyLong_AsVoidPtr(a[2]));
+        g_commit = reinterpret_cast<Commit>(PyLong_AsVoidPtr(a[3]));
+        g_tree_attend = reinterpret_cast<TreeAttend>(PyLong_AsVoidPtr(a[4]));
+        g_verify = reinterpret_cast<Verify>(PyLong_AsVoidPtr(a[5]));
         if (PyErr_Occurred()) throw Failed{};
-        Py_INCREF(a[3]);
+        Py_INCREF(a[6]);
         Py_XDECREF(g_error);
-        g_error = a[3];
+        g_error = a[6];
         return none();
     });
 }
@@ -403,9 +416,168 @@ PyObject* py_attend(PyObject*, PyObject* const* a, Py_ssize_t n_args)
     });
 }
 
+// int32 [n], or nothing
+const int32_t* whole_numbers(PyObject* o, const char* name, int64_t n, c10::Device device)
+{
+    return o == Py_None ? nullptr : static_cast<const int32_t*>(dense(tensor(o, name), name, at::kInt, {n}, device));
+}
+
+// the largest tree of a call whose requests have it (without row_start) or at most it
+long most_nodes(PyObject* o)
+{
+    const long n = whole(o);
+    if (n < 1 || n > MOSKA_TREE_MAX_NODES)
+        refuse("max_nodes = " + std::to_string(n) + ", 1.." + std::to_string(MOSKA_TREE_MAX_NODES) + " are possible");
+    return n;
+}
+
+// tree_attend(store, q, page_table, kv_len, parents, row_start, out, lse, scale, max_nodes, n_unique_splits, ws, stream)
+PyObject* py_tree_attend(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    return guarded(n_args, 13, [&] {
+        const Store& s = *store_of(a[0]);
+        const moska_paged_kv kv = seen_through(s, a[2], a[3]);
+        const at::Tensor &q = tensor(a[1], "q"), &out = tensor(a[6], "out"), &lse = tensor(a[7], "lse"), &ws = tensor(a[11], "ws");
+        if (out.dim() != 3 || out.size(2) != s.D) refuse("out: expected [rows][heads][D], " + describe(out));
+        const int64_t B = out.size(0), Hq = out.size(1), n_requests = tensor(a[2], "page_table").size(0);
+        const long nodes = most_nodes(a[9]);
+        auto* qp = static_cast<uint16_t*>(dense(q, "q", at::kBFloat16, out.sizes(), s.device));
+        auto* op = static_cast<uint16_t*>(dense(out, "out", at::kBFloat16, out.sizes(), s.device));
+        auto* lp = static_cast<float*>(dense(lse, "lse", at::kFloat, {B, Hq}, s.device));
+        void* wp = dense(ws, "ws", at::kByte, ws.sizes(), s.device);
+        const int32_t* parents = whole_numbers(a[4], "parents", B, s.device);
+        const int32_t* first = first_rows(a[5], n_requests, B, nodes, s.device);
+        if (B > 0) {
+            moska_shape shape = shape_of(B, Hq, s.Hkv, s.D, nodes);
+            shape.n_unique_splits = (int32_t)whole(a[10]);
+            const double scale = PyFloat_AsDouble(a[8]);
+            if (PyErr_Occurred()) throw Failed{};
+            const OnDevice on(s.device, a[12]);
+            check(g_tree_attend(qp, &kv, parents, first, (int32_t)n_requests, op, lp, (float)scale, &shape, wp,
+                                (size_t)ws.numel(), on.stream),
+                  "moska_tree_attn");
+            for (int i : {1, 2, 3, 4, 5, 11}) on.reads(a[i]);
+            on.reads(s.k);
+            on.reads(s.v);
+            on.returns(out);
+            on.returns(lse);
+        }
+        return none();
+    });
+}
+
+// commit(store, page_table, kv_len, path, n_path, row_start, max_nodes, kv_len_out, stream) -> kv_len_out
+PyObject* py_commit(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    return guarded(n_args, 9, [&] {
+        const Store& s = *store_of(a[0]);
+        const moska_paged_kv kv = seen_through(s, a[1], a[2]);
+        const int64_t n = tensor(a[1], "page_table").size(0);
+        const long nodes = most_nodes(a[6]);
+        const at::Tensor& path = tensor(a[3], "path");
+        if (path.dim() != 2 || path.size(1) < 1 || path.size(1) > INT32_MAX) refuse("path: expected [requests][nodes], " + describe(path));
+        auto* pp = static_cast<const int32_t*>(dense(path, "path", at::kInt, {n, path.size(1)}, s.device));
+        auto* np = static_cast<const int32_t*>(dense(tensor(a[4], "n_path"), "n_path", at::kInt, {n}, s.device));
+        const int32_t* first = whole_numbers(a[5], "row_start", n + 1, s.device);
+        at::Tensor to;
+        int32_t* tp = nullptr;
+        if (a[7] != Py_None) {
+            to = tensor(a[7], "kv_len_out");
+            tp = static_cast<int32_t*>(dense(to, "kv_len_out", at::kInt, {n}, s.device));
+        }
+        if (n * nodes > INT32_MAX) refuse("too many nodes");
+        const auto result = [&] { return at::empty({n}, at::TensorOptions().dtype(at::kInt).device(s.device)); };
+        if (n > 0) {
+            const moska_shape shape = shape_of(n * nodes, s.Hkv, s.Hkv, s.D, nodes);
+            const OnDevice on(s.device, a[8]);
+            if (tp == nullptr) {
+                to = result();
+                tp = static_cast<int32_t*>(to.data_ptr());
+            }
+            check(g_commit(pp, (int32_t)path.size(1), np, first, (int32_t)n, tp, &kv, &shape, on.stream), "moska_kv_commit_paged");
+            for (int i : {1, 2, 3, 4, 5}) on.reads(a[i]);
+            on.reads(s.k);
+            on.reads(s.v);
+            on.returns(to);
+        } else if (tp == nullptr) {
+            to = result();
+        }
+        return THPVariable_Wrap(to);
+    });
+}
+
+// [rows][V] probabilities whose rows may lie apart
+const void* probabilities(const at::Tensor& t, const char* name, at::ScalarType type, int64_t B, int64_t V, c10::Device device,
+                          int64_t* stride)
+{
+    if (t.dim() != 2 || t.scalar_type() != type || t.size(0) != B || t.size(1) != V || t.device() != device)
+        refuse(std::string(name) + ": expected " + c10::toString(type) + " (" + std::to_string(B) + ", " + std::to_string(V) + ") on " +
+               device.str() + ", " + describe(t));
+    if (V > 1 && t.stride(1) != 1) refuse(std::string(name) + ": the entries of a row must be neighbours");
+    if (B > 1 && t.stride(0) < V) refuse(std::string(name) + ": rows must not overlap");
+    *stride = B > 1 ? t.stride(0) : V;
+    return t.data_ptr();
+}
+
+// verify(target_probs, draft_probs, tokens, parents, u_accept, u_next, row_start, max_nodes, path, n_path, next_token, stream)
+// -> (path, n_path, next_token)
+PyObject* py_verify(PyObject*, PyObject* const* a, Py_ssize_t n_args)
+{
+    return guarded(n_args, 12, [&] {
+        const at::Tensor &target = tensor(a[0], "target_probs"), &u_next = tensor(a[5], "u_next");
+        const c10::Device device = target.device();
+        const at::ScalarType type = target.scalar_type();
+        if (target.dim() != 2 || target.size(1) < 1 || (type != at::kFloat && type != at::kBFloat16))
+            refuse("target_probs: expected Float or BFloat16 [rows][vocabulary], " + describe(target));
+        if (u_next.dim() != 1) refuse("u_next: expected [requests], " + describe(u_next));
+        const int64_t B = target.size(0), V = target.size(1), n = u_next.size(0);
+        if (B > INT32_MAX || V > INT32_MAX || n > INT32_MAX) refuse("too many rows or requests, or too large a vocabulary");
+        const long nodes = most_nodes(a[7]);
+        int64_t t_stride = V, d_stride = V;
+        const void* tp = probabilities(target, "target_probs", type, B, V, device, &t_stride);
+        const void* dp = a[1] == Py_None ? nullptr
+                                         : probabilities(tensor(a[1], "draft_probs"), "draft_probs", type, B, V, device, &d_stride);
+        auto* tokens = static_cast<const int32_t*>(dense(tensor(a[2], "tokens"), "tokens", at::kInt, {B}, device));
+        auto* parents = static_cast<const int32_t*>(dense(tensor(a[3], "parents"), "parents", at::kInt, {B}, device));
+        auto* u = static_cast<const float*>(dense(tensor(a[4], "u_accept"), "u_accept", at::kFloat, {B}, device));
+        auto* un = static_cast<const float*>(dense(u_next, "u_next", at::kFloat, {n}, device));
+        const int32_t* first = first_rows(a[6], n, B, nodes, device);
+        at::Tensor out[3];
+        constexpr const char* names[3] = {"path", "n_path", "next_token"};
+        const int64_t path_shape[2] = {n, nodes};
+        const auto shape = [&](int i) { return i == 0 ? at::IntArrayRef(path_shape, 2) : at::IntArrayRef(path_shape, 1); };
+        for (int i = 0; i < 3; ++i) {
+            if (a[8 + i] == Py_None) continue;
+            out[i] = tensor(a[8 + i], names[i]);
+            dense(out[i], names[i], at::kInt, shape(i), device);
+        }
+        const auto allocate = [&] {
+            for (int i = 0; i < 3; ++i)
+                if (!out[i].defined()) out[i] = at::empty(shape(i), at::TensorOptions().dtype(at::kInt).device(device));
+        };
+        if (n > 0) {
+            const OnDevice on(device, a[11]);
+            allocate();
+            check(g_verify(tp, t_stride, dp, d_stride, type == at::kFloat ? MOSKA_PROB_F32 : MOSKA_PROB_BF16, (int32_t)V, tokens,
+                           parents, u, un, first, (int32_t)n, (int32_t)nodes, (int32_t)B, static_cast<int32_t*>(out[0].data_ptr()),
+                           static_cast<int32_t*>(out[1].data_ptr()), static_cast<int32_t*>(out[2].data_ptr()), on.stream),
+                  "moska_verify_tree");
+            for (int i = 0; i < 7; ++i) on.reads(a[i]);
+            for (const at::Tensor& t : out) on.returns(t);
+        } else {
+            allocate();
+        }
+        PyObject* three = PyTuple_New(3);
+        if (three == nullptr) throw Failed{};
+        for (int i = 0; i < 3; ++i) PyTuple_SET_ITEM(three, i, THPVariable_Wrap(out[i]));
+        return three;
+    });
+}
+
 #define METHOD(name, fn) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fn)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD("bind", py_bind),     METHOD("store", py_store),   METHOD("view", py_view),
                          METHOD("append", py_append), METHOD("gather", py_gather), METHOD("attend", py_attend),
+                         METHOD("commit", py_commit), METHOD("tree_attend", py_tree_attend), METHOD("verify", py_verify),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_paged_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -19,7 +19,10 @@ class MoskaLayer:
         fp8_unique, paged_fmt ("bf16" or "fp4"): the private store that the default splits are for."""
         self.device = torch.device(device)
         self.dense = dense
-        if n_unique_splits is None and paged_fmt is not None:
+        if n_unique_splits is None and paged_fmt is not None and q_len * (Hq // Hkv) > 16:  # trees alone
+            n_unique_splits = M.default_tree_splits({"bf16": M.KV_BF16, "fp4": M.KV_FP4}[paged_fmt], B // q_len, q_len, Hq, Hkv,
+                                                    D, max(1, max_unique_len))
+        elif n_unique_splits is None and paged_fmt is not None:
             n_unique_splits = M.default_paged_splits({"bf16": M.KV_BF16, "fp4": M.KV_FP4}[paged_fmt],
                                                      B // max(1, q_len), Hkv, D, max(1, max_unique_len))
         if n_unique_splits is None:
@@ -99,8 +102,19 @@ class MoskaLayer:
                              f"{page_table.shape[0]} rows, the store {store.Hkv} heads of {store.D}")
         return store.kv(page_table, kv_len)
 
-    def unique_paged(self, q, store, page_table, kv_len, stream=None):
-        """Unique KV Attention over a paged private store (`store`: a paged.PagedKvStore)."""
+    def _parents(self, parents):
+        if parents.dtype != torch.int32 or parents.shape != (self.shape.B,) or parents.device != self.out.device:
+            raise ValueError(f"parents: expected int32 ({self.shape.B},) on {self.out.device}, got {parents.dtype} "
+                             f"{tuple(parents.shape)} on {parents.device}")
+        return parents
+
+    def unique_paged(self, q, store, page_table, kv_len, stream=None, parents=None):
+        """Unique KV Attention over a paged private store (`store`: a paged.PagedKvStore).  With `parents` the q_len rows
+        of a request are the nodes of a drafted tree."""
+        if parents is not None:
+            M.unique_attn_tree(q, self._paged_kv(store, page_table, kv_len), self._parents(parents), self.o_part, self.lse_part,
+                               self.scale, self.shape, stream)
+            return
         M.unique_attn_paged(q, self._paged_kv(store, page_table, kv_len), self.o_part, self.lse_part, self.scale, self.shape,
                             stream)
 
@@ -162,18 +176,22 @@ class MoskaLayer:
         return self.out
 
     def step_paged(self, q, k_shared, v_shared, store, page_table, kv_len, two_streams=False, prof=None,
-                   unique_tokens=0, sf8=None):
+                   unique_tokens=0, sf8=None, parents=None):
         """One decode step with a paged private store (`store`: a paged.PagedKvStore in either format).
-        The shared store is bf16, or FP8 when `sf8` is given (k_shared and v_shared are then not read)."""
+        The shared store is bf16, or FP8 when `sf8` is given (k_shared and v_shared are then not read).
+        `parents` int32 [B]: the q_len rows of a request are the nodes of a drafted tree (up to 64)."""
         self.shape.unique_tokens = int(unique_tokens)
         two_streams = two_streams and self.overlap_routing
         if two_streams and self.side_stream is None:
             self.side_stream = torch.cuda.Stream(device=self.device, priority=-1)
         shared = (k_shared, v_shared, None, None) if sf8 is None else (sf8.k8, sf8.v8, sf8.k_scale, sf8.v_scale)
-        M.decode_step_paged(q, None if self.dense else self.summaries, *shared, self._paged_kv(store, page_table, kv_len),
-                            self.topk_idx, self.seg_offsets, self.seg_entries, self.o_part, self.lse_part, self.out,
-                            self.lse_out, self.scale, self.shape, self.ws, None,
-                            self.side_stream if two_streams else None, prof)
+        rest = (self.topk_idx, self.seg_offsets, self.seg_entries, self.o_part, self.lse_part, self.out, self.lse_out,
+                self.scale, self.shape, self.ws, None, self.side_stream if two_streams else None, prof)
+        kv = self._paged_kv(store, page_table, kv_len)
+        if parents is None:
+            M.decode_step_paged(q, None if self.dense else self.summaries, *shared, kv, *rest)
+        else:
+            M.decode_step_tree(q, None if self.dense else self.summaries, *shared, kv, self._parents(parents), *rest)
         return self.out
 
     def step_fp8_host(self, q_host, q_dev, out_host, sf8, f8, kv_start, kv_len, two_streams=False,

@@ -25,7 +25,8 @@ if _call.built_for != f"torch {torch.__version__};":  # it reads torch's tensors
 
 FORMATS = {"bf16": M.KV_BF16, "fp4": M.KV_FP4}
 _call.bind(*(ctypes.cast(getattr(M._lib, "moska_" + n), ctypes.c_void_p).value
-             for n in ("kv_append_paged", "kv_gather_paged", "paged_attn")), M.MoskaError)
+             for n in ("kv_append_paged", "kv_gather_paged", "paged_attn", "kv_commit_paged", "tree_attn", "verify_tree")),
+           M.MoskaError)
 
 
 def _settled(device) -> None:
@@ -105,6 +106,13 @@ class PagedKvStore:
         """The last rows of the contexts as bf16 [n_rows][Hkv][D] keys and values; rows as in append.
         Padding rows keep what k_out and v_out held, as in append."""
         return _call.gather(self._handle, page_table, kv_len, n_rows, row_start, q_len, k_out, v_out, _address(stream))
+
+    def commit(self, page_table, kv_len, path, n_path, max_nodes, row_start=None, kv_len_out=None, stream=None):
+        """Keeps the rows of the accepted paths of drafted trees (speculative.verify gives path int32 [R][nodes] and
+        n_path int32 [R]): the rows of request r's nodes path[r][:n_path[r]] become the first ones behind its committed
+        context.  Its tree is the last max_nodes tokens of its context, or with row_start row_start[r+1] - row_start[r]
+        (at most max_nodes).  Returns the context lengths after it (kv_len_out, apart from kv_len)."""
+        return _call.commit(self._handle, page_table, kv_len, path, n_path, row_start, max_nodes, kv_len_out, _address(stream))
 
 
 class PagedAttention:
