@@ -615,9 +615,10 @@ int moska_decode_step_paged(const uint16_t* q, const float* summaries, const voi
  *   q        bf16  [B][Hq][D]   (16-byte aligned)
  *   out      bf16  [B][Hq][D]   (16-byte aligned); a row that sees nothing is 0
  *   lse_out  float [B][Hq]      may be NULL; -inf for such a row
- *   ws       moska_tree_attn_workspace_bytes(shape) bytes, 256-byte aligned; calls that share it must
- *            not overlap.  Not read or written (may be NULL) with n_unique_splits = 1.
- * shape: B, Hq, Hkv, D, q_len and n_unique_splits are read.  What a node does not see has no influence on it,
+ *   ws       moska_tree_attn_workspace_bytes(shape) bytes (20 MB for D = 128), 256-byte aligned; calls that
+ *            share it must not overlap.  Not read or written (may be NULL) with n_unique_splits = 1.
+ * shape: B, Hq, Hkv, D, q_len and n_unique_splits are read: a context is cut into at most that many parts, as the
+ * work of all contexts is shared among the SMs; 64 lets any batch be shared evenly, and costs no more than 2.  What a node does not see has no influence on it,
  * infinities and NaN included.  Scores, softmax and row sums are fp32.
  */
 int moska_tree_attn(const uint16_t* q, const moska_paged_kv* kv, const int32_t* parents, const int32_t* row_start,
@@ -625,10 +626,9 @@ int moska_tree_attn(const uint16_t* q, const moska_paged_kv* kv, const int32_t* 
                     void* ws, size_t ws_bytes, moska_stream stream);
 size_t moska_tree_attn_workspace_bytes(const moska_shape* shape);
 
-/* A reasonable n_unique_splits for trees of up to `nodes` nodes that end contexts of up to `max_len`
- * tokens.  Host only, pure. */
-int moska_default_tree_splits(int32_t format, int32_t n_requests, int32_t nodes, int32_t Hq, int32_t Hkv, int32_t D,
-                              int32_t max_len);
+/* A reasonable n_unique_splits of moska_unique_attn_tree and the step below, for trees of up to `nodes` nodes
+ * that end contexts of up to `max_len` tokens.  Host only, pure. */
+int moska_default_tree_splits(int32_t n_requests, int32_t nodes, int32_t Hq, int32_t Hkv, int32_t max_len);
 
 /* Unique KV Attention of trees of shape->q_len nodes each: the partial results and slots of
  * moska_unique_attn_paged, for a step that also attends to a shared store. */

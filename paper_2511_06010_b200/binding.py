@@ -88,7 +88,7 @@ EXPORTS = {
     "moska_paged_attn": (_i, [_vp, _kvp, _vp, _vp, _f, _sp, _vp, _sz, _vp]),
     "moska_paged_attn_workspace_bytes": (_sz, [_sp]),
     "moska_decode_step_paged": (_i, [_vp] * 6 + [_kvp] + [_vp] * 7 + [_f, _sp, _vp, _sz, _vp, _vp, _vp]),
-    "moska_default_tree_splits": (_i, [ctypes.c_int32] * 7),
+    "moska_default_tree_splits": (_i, [ctypes.c_int32] * 5),
     "moska_tree_attn_workspace_bytes": (_sz, [_sp]),
     "moska_tree_attn": (_i, [_vp, _kvp, _vp, _vp, ctypes.c_int32, _vp, _vp, _f, _sp, _vp, _sz, _vp]),
     "moska_unique_attn_tree": (_i, [_vp, _kvp, _vp, _vp, _vp, _f, _sp, _vp]),
@@ -427,8 +427,8 @@ def decode_step_paged(q, summaries, k_shared, v_shared, k_scale_shared, v_scale_
         None if side_stream is None else _stream(side_stream), prof), "moska_decode_step_paged")
 
 
-def default_tree_splits(fmt: int, n_requests: int, nodes: int, Hq: int, Hkv: int, D: int, max_len: int) -> int:
-    return _lib.moska_default_tree_splits(fmt, n_requests, nodes, Hq, Hkv, D, max_len)
+def default_tree_splits(n_requests: int, nodes: int, Hq: int, Hkv: int, max_len: int) -> int:
+    return _lib.moska_default_tree_splits(n_requests, nodes, Hq, Hkv, max_len)
 
 
 def tree_attn(q, kv, parents, row_start, n_requests, out, lse_out, softmax_scale, s, ws, stream=None) -> None:

@@ -1272,18 +1272,16 @@ int check_tree_attn(float softmax_scale, const moska_shape* s)
 }
 }  // namespace
 
-int moska_default_tree_splits(int32_t format, int32_t n_requests, int32_t nodes, int32_t Hq, int32_t Hkv, int32_t D,
-                              int32_t max_len)
+int moska_default_tree_splits(int32_t n_requests, int32_t nodes, int32_t Hq, int32_t Hkv, int32_t max_len)
 {
-    if (n_requests <= 0 || nodes <= 0 || Hkv <= 0 || Hq < Hkv || max_len <= 0) return 1;
-    return default_tree_splits(format == MOSKA_KV_FP4, n_requests, nodes, Hq / Hkv, Hkv, D, max_len);
+    if (n_requests <= 0 || nodes <= 0 || Hkv <= 0 || Hq < Hkv || Hq / Hkv > 8 || max_len <= 0) return 1;
+    return default_tree_splits(n_requests, nodes, Hq / Hkv, Hkv, max_len);
 }
 
 size_t moska_tree_attn_workspace_bytes(const moska_shape* shape)
 {
     if (check_tree_heads(shape) != MOSKA_OK || shape->n_unique_splits < 2) return 0;
-    const size_t slots = (size_t)shape->B * shape->Hq * shape->n_unique_splits;
-    return round_up(slots * shape->D * sizeof(float), 256) + round_up(slots * sizeof(float), 256);
+    return tree_cut_bytes(shape->D);
 }
 
 int moska_tree_attn(const uint16_t* q, const moska_paged_kv* kv, const int32_t* parents, const int32_t* row_start,
@@ -1306,15 +1304,8 @@ int moska_tree_attn(const uint16_t* q, const moska_paged_kv* kv, const int32_t* 
     MOSKA_TRY(check_device());
     MOSKA_TRY(status_word(&view.status));
     const bool fp4 = kv->format == MOSKA_KV_FP4;
-    cudaStream_t st = (cudaStream_t)stream;
-    if (shape->n_unique_splits == 1)
-        return launch_tree_attn(q, view, fp4, tree, nullptr, nullptr, 0, 1, out, lse_out, softmax_scale, shape, st);
-    float* o_part = static_cast<float*>(ws);
-    const size_t o_bytes = (size_t)shape->B * shape->Hq * shape->n_unique_splits * shape->D * sizeof(float);
-    float* lse_part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + round_up(o_bytes, 256));
-    MOSKA_TRY(launch_tree_attn(q, view, fp4, tree, o_part, lse_part, 0, shape->n_unique_splits, nullptr, nullptr,
-                               softmax_scale, shape, st));
-    return launch_paged_merge(o_part, lse_part, out, lse_out, shape, st, row_start == nullptr ? nullptr : row_start + n_requests);
+    return launch_tree_attn(q, view, fp4, tree, nullptr, nullptr, 0, 1, out, lse_out, need > 0 ? ws : nullptr, softmax_scale, shape,
+                            (cudaStream_t)stream);
 }
 
 int moska_unique_attn_tree(const uint16_t* q, const moska_paged_kv* kv, const int32_t* parents, float* o_part,
@@ -1333,7 +1324,7 @@ int moska_unique_attn_tree(const uint16_t* q, const moska_paged_kv* kv, const in
     MOSKA_TRY(check_device());
     MOSKA_TRY(status_word(&view.status));
     return launch_tree_attn(q, view, kv->format == MOSKA_KV_FP4, tree, o_part, lse_part, shape->shared_slots,
-                            shape->shared_slots + shape->n_unique_splits, nullptr, nullptr, softmax_scale, shape,
+                            shape->shared_slots + shape->n_unique_splits, nullptr, nullptr, nullptr, softmax_scale, shape,
                             (cudaStream_t)stream);
 }
 

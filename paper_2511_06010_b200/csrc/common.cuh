@@ -177,9 +177,8 @@ int launch_gather_paged(const int32_t* row_start, int n_requests, uint16_t* k_ou
 int launch_paged_bf16(const uint16_t* q, const PagedView& kv, float* o_part, float* lse_part, int slot0, int n_slots,
                       uint16_t* out, float* lse_out, float scale, const moska_shape* s, cudaStream_t st);
 // the final rows from n_unique_splits partial ones, launched early behind one of the two kernels above
-// (n_rows: device address of how many of the B rows there are, nullptr: all)
 int launch_paged_merge(const float* o_part, const float* lse_part, uint16_t* out, float* lse_out, const moska_shape* s,
-                       cudaStream_t st, const int32_t* n_rows = nullptr);
+                       cudaStream_t st);
 int launch_paged_fp4(const uint16_t* q, const PagedView& kv, float* o_part, float* lse_part, int slot0, int n_slots,
                      uint16_t* out, float* lse_out, float scale, const moska_shape* s, cudaStream_t st);
 
@@ -189,11 +188,13 @@ struct TreeRows {
     const int32_t* row_start;  // nullptr: max_nodes rows a request
     int32_t n_requests, max_nodes, n_rows;
 };
-// out == nullptr: partial slots, as above
+// out == nullptr: partial slots, as above; else the final rows, with n_unique_splits > 1 by way of ws
+// (tree_cut_bytes)
 int launch_tree_attn(const uint16_t* q, const PagedView& kv, bool fp4, const TreeRows& tree, float* o_part, float* lse_part,
-                     int slot0, int n_slots, uint16_t* out, float* lse_out, float scale, const moska_shape* s,
+                     int slot0, int n_slots, uint16_t* out, float* lse_out, void* ws, float scale, const moska_shape* s,
                      cudaStream_t st);
-int default_tree_splits(bool fp4, int n_requests, int nodes, int G, int Hkv, int D, int max_len);
+int default_tree_splits(int n_requests, int nodes, int G, int Hkv, int max_len);
+size_t tree_cut_bytes(int D);
 int launch_commit_paged(const int32_t* path, int path_stride, const int32_t* n_path, const TreeRows& tree, int32_t* kv_len_out,
                         const PagedView& kv, bool fp4, const moska_shape* s, cudaStream_t st);
 int launch_verify(const void* target, int64_t target_stride, const void* draft, int64_t draft_stride, bool bf16, int V,

@@ -94,8 +94,7 @@ __global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 3) paged_bf16_kernel(
 constexpr int kMergeWarps = 4;
 template <int D, int R>
 __global__ void __launch_bounds__(kMergeWarps * 32)
-paged_merge_kernel(const float* o_part, const float* lse_part, uint16_t* out, float* lse_out, long long rows, int n,
-                   const int32_t* n_rows, int Hq)
+paged_merge_kernel(const float* o_part, const float* lse_part, uint16_t* out, float* lse_out, long long rows, int n)
 {
     constexpr int W = D / 32;  // dimensions a lane
     using Vec = typename std::conditional<W == 4, float4, float2>::type;
@@ -104,7 +103,6 @@ paged_merge_kernel(const float* o_part, const float* lse_part, uint16_t* out, fl
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t row = (int64_t)blockIdx.x * (kMergeWarps / R) + warp / R;
     wait_for_results();
-    if (n_rows != nullptr) rows = min(rows, (long long)__ldg(n_rows) * Hq);
     if (row >= rows) return;  // (R = 1: no barrier follows)
     const float* lse = lse_part + row * n;
     const float* o = o_part + row * n * D + W * lane;
@@ -163,7 +161,7 @@ paged_merge_kernel(const float* o_part, const float* lse_part, uint16_t* out, fl
 }  // namespace
 
 int launch_paged_merge(const float* o_part, const float* lse_part, uint16_t* out, float* lse_out, const moska_shape* s,
-                       cudaStream_t st, const int32_t* n_rows)
+                       cudaStream_t st)
 {
     const long long rows = (long long)s->B * s->Hq;
     if (rows == 0) return MOSKA_OK;
@@ -183,7 +181,7 @@ int launch_paged_merge(const float* o_part, const float* lse_part, uint16_t* out
     config.numAttrs = 1;
     const auto kernel = s->D == 128 ? (wide ? paged_merge_kernel<128, kMergeWarps> : paged_merge_kernel<128, 1>)
                                     : (wide ? paged_merge_kernel<64, kMergeWarps> : paged_merge_kernel<64, 1>);
-    MOSKA_CUDA_TRY(cudaLaunchKernelEx(&config, kernel, o_part, lse_part, out, lse_out, rows, n, n_rows, s->Hq));
+    MOSKA_CUDA_TRY(cudaLaunchKernelEx(&config, kernel, o_part, lse_part, out, lse_out, rows, n));
     return MOSKA_OK;
 }
 

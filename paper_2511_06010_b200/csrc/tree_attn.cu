@@ -1,19 +1,24 @@
 // Attention of the nodes of drafted trees over the paged contexts that they end, on the 5th-generation tensor cores.
 //
-// The T G query rows of a request's KV head (T nodes, G heads each) share one context.  A CTA takes up to 128 of them
-// (whole nodes) and a split of the context, in tiles of 128 tokens:
-//   S = Q K^T          tcgen05.mma, both operands in shared memory, 128 x 128 scores in tensor memory
-//   P = exp2(S - m)    a thread per row: TMEM -> registers -> 16 bits, back over the columns of S
-//   O += P V           tcgen05.mma, P from TMEM, V from shared memory, a 64-dimension half at a time
-// Two CTAs share an SM (half of its shared and of its tensor memory each): while one is in its softmax the other
-// has the tensor cores, and one's prologue and epilogue run under the other's tiles.  The CTAs of a KV head's row tiles
-// are neighbours in the grid, so that the second and later read the context from L2.
+// The T G query rows of a request's KV head (T nodes, G heads each) share one context.  Work comes in units: up to 128 of
+// these rows (whole nodes) and the context in tiles of 128 tokens:
+//   S = Q K^T          tcgen05.mma, Q in tensor memory, K in shared memory: 128 x 128 scores in tensor memory
+//   P = exp2(S - m)    two threads per row: TMEM -> registers -> 16 bits, back over the columns of S
+//   O += P V           tcgen05.mma, P from TMEM, V from shared memory
+// Scores have two buffers, so that the next tile's product runs under this tile's softmax; Q has two, so that the next
+// unit's first product runs under this unit's end.  TMEM: O, S, S, Q, Q = 512 columns.
 //
-// Warps 0-3: softmax (thread i: row i = TMEM lane i).  Warp 4: copies.  Warp 5: MMAs.  4-bit pages: warps 6-9 widen.
-// Operands lie in a ring of 16 KB slots (128 tokens x 64 dimensions, rows of 128 bytes with the 128-byte swizzle).
+// One CTA per SM.  All tiles of all units, row tiles slowest, then requests, then heads, form one line that is cut into equal
+// parts, one per CTA, whatever the lengths: a CTA walks the units in its part.  A unit that a cut divides leaves partial
+// rows, which a second kernel joins.  (Row tiles slowest: with trees of one size the CTAs of the row tiles walk the same
+// contexts at the same time, and all but the first find them in L2.)
+//
+// Warps 0-7: softmax (thread i and i + 128: row i % 128 = TMEM lane, columns 0-63 and 64-127).  Warp 8: copies.  Warp 9: MMAs.
+// 4-bit pages: warps 10-13 widen.  Operands lie in a ring of slots, a K or a V tile each, as halves of 64 dimensions in rows of
+// 128 bytes with the 128-byte swizzle.
 //   bf16: one TMA box of min(page_size, 128) tokens a page and half.
-//   4 bits: bulk copies of the key part or the value part (codes, then scales) of four 16-token blocks into a ring of their
-//   own; a warp per block widens them to f16 operands, code times scale (half a step: 2^-11).  Queries are f16 too,
+//   4 bits: bulk copies of the key parts or the value parts (codes, then scales) of the tile's 16-token blocks into a ring of
+//   their own; a warp widens every fourth to f16 operands, code times scale (half a step: 2^-11).  Queries are f16 too,
 //   scaled by a power of two per row.
 //
 // What a node sees: committed tokens, and of the last T tokens those whose bit is set in its 64-bit word of ancestors.
@@ -33,53 +38,69 @@ namespace moska {
 namespace {
 using namespace sm100;
 
-constexpr int kTile = 128;                 // tokens of a tile
-constexpr int kSlotBytes = kTile * 64 * 2;  // 64 dimensions of a tile
-constexpr int kTileRows = 128;             // query rows of a CTA
-constexpr int kLoadWarp = 4, kMmaWarp = 5, kWidenWarp0 = 6;
+constexpr int kTile = 128;      // tokens of a tile
+constexpr int kTileRows = 128;  // query rows of a unit
+constexpr int kHalfBytes = kTile * 64 * 2;
+constexpr int kSoftmaxThreads = 256;
+constexpr int kLoadWarp = 8, kMmaWarp = 9, kWidenWarp0 = 10, kWidenWarps = 4;
+constexpr int kMaxRowTiles = 4;  // 64 nodes of up to 8 heads
+constexpr int kMaxCtas = 148;    // parts of the line of tiles
+constexpr uint32_t kColO = 0, kColS = 128, kColQ = 384;  // tensor-memory columns
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kRescaleAt = 8.f;  // log2 units that a row's maximum may grow before its sums are rescaled
 
 template <int D, bool F4>
 struct Cfg {
     static constexpr int kHalves = D / 64;
-    static constexpr int kThreads = F4 ? 320 : 192;
-    static constexpr int kSlots = F4 ? (D == 128 ? 4 : 5) : (D == 128 ? 5 : 6);
-    static constexpr int kUnitBlocks = 4;              // 16-token blocks of a unit of codes
-    static constexpr int kPartBytes = 9 * D;           // codes and scales of a block's keys, or of its values
-    static constexpr int kUnitBytes = kUnitBlocks * kPartBytes;
-    static constexpr int kUnits = F4 ? (D == 128 ? 3 : 6) : 0;
+    static constexpr int kThreads = F4 ? 448 : 320;
+    static constexpr int kSlotBytes = kHalves * kHalfBytes;
+    static constexpr int kSlots = F4 ? (D == 128 ? 4 : 8) : (D == 128 ? 6 : 12);
+    static constexpr int kBlocks = kTile / kBlockTokens;  // 16-token blocks of a unit of codes
+    static constexpr int kPartBytes = 9 * D;              // codes and scales of a block's keys, or of its values
+    static constexpr int kUnitBytes = kBlocks * kPartBytes;
+    static constexpr int kUnits = F4 ? (D == 128 ? 8 : 16) : 1;
 };
 
-// One CTA's shared memory: half of an SM's.
+// A CTA's part of the line of tiles.
+struct Part {
+    long long p0, p1, per;  // tiles p0 .. p1 - 1; `per` in a full part
+    long long start;        // first tile of the unit that p0 is in: (row tile, request, head)
+    int rt, r, h;
+    int longest[kSoftmaxThreads / 32];
+    long long tiles[kMaxRowTiles][kSoftmaxThreads / 32];  // of each warp's requests
+};
+
 template <int D, bool F4>
 struct Smem {
     using C = Cfg<D, F4>;
-    uint8_t q[C::kHalves][kSlotBytes];
-    uint8_t slot[C::kSlots][kSlotBytes];
+    uint8_t slot[C::kSlots][C::kSlotBytes];
     uint8_t unit[F4 ? C::kUnits * C::kUnitBytes : 16];
-    float row_unit[F4 ? kTileRows : 4];  // log2 units of one score of a row
+    float top[2][2][kTileRows];  // row maxima of the two column halves; alternate tiles
+    float sum[2][kTileRows];     // row sums of the halves at a unit's end; 4 bits: largest query elements at its start
+    TreeSmem tree;
     uint64_t full[C::kSlots], empty[C::kSlots];
-    uint64_t unit_full[F4 ? C::kUnits : 1], unit_empty[F4 ? C::kUnits : 1];
-    uint64_t q_full, s_full, p_full, o_full;
-    unsigned long long bad;  // tree tokens with values that are not finite
+    uint64_t unit_full[C::kUnits], unit_empty[C::kUnits];
+    uint64_t q_full[2], s_full[2], p_full[2], pv_done;
+    unsigned long long bad[8];  // tree tokens with values that are not finite; units take turns
+    Part part;
     uint32_t tmem_base;
     int gave_up;
 };
-constexpr int kMostSmem = 115712;  // 2 x (that + 1 KB that the system takes) = 228 KB
+constexpr int kMostSmem = 232448;
 static_assert(sizeof(Smem<128, false>) <= kMostSmem && sizeof(Smem<128, true>) <= kMostSmem &&
                   sizeof(Smem<64, false>) <= kMostSmem && sizeof(Smem<64, true>) <= kMostSmem,
-              "two CTAs share an SM");
-static_assert(sizeof(TreeSmem) <= kSlotBytes, "the ancestors' scratch lies where the queries come");
+              "an SM's shared memory");
 
 struct TreeArgs {
     const uint16_t* q;
     PagedView kv;
     TreeRows tree;
-    float* o_part;  // partial slots (nullptr: `out` gets the final rows)
+    float* o_part;  // partial slots of the rows (nullptr: `out` gets the final rows)
     float* lse_part;
     uint16_t* out;
     float* lse_out;
+    float* o_cut;   // partial rows of units that a cut divides [CTA][2][128][D] (final rows only)
+    float* lse_cut;
     float scale;
     int Hq, Hkv, n_splits, slot0, n_slots;
     int row_tiles;       // of the largest tree
@@ -97,6 +118,38 @@ __device__ __forceinline__ float fmax3(float a, float b, float c)
 {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
+// two fp32 at once
+__device__ __forceinline__ float2 ffma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("{\n"
+        ".reg .b64 ra, rb, rc, rd;\n"
+        "mov.b64 ra, {%2, %3};\n"
+        "mov.b64 rb, {%4, %5};\n"
+        "mov.b64 rc, {%6, %7};\n"
+        "fma.rn.f32x2 rd, ra, rb, rc;\n"
+        "mov.b64 {%0, %1}, rd;\n"
+        "}\n"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+
+__device__ __forceinline__ float2 fadd2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n"
+        ".reg .b64 ra, rb, rd;\n"
+        "mov.b64 ra, {%2, %3};\n"
+        "mov.b64 rb, {%4, %5};\n"
+        "add.rn.f32x2 rd, ra, rb;\n"
+        "mov.b64 {%0, %1}, rd;\n"
+        "}\n"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
 }
 
@@ -140,73 +193,164 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int* g
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, gave_up));
 }
 
-// What all roles of a CTA know.
-struct Work {
-    int first, nodes;   // the request's rows
-    int len, committed;
-    int h, r, split;
-    int node0, rows;    // first node of the row tile, its rows
-    int tile0, tiles;   // tiles of the split
+__device__ __forceinline__ void softmax_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+// True in one lane of the calling warp (converged).  With it, and loops that the whole warp runs, descriptors stay in
+// uniform registers: under `lane == 0` an MMA took about 90 cycles to issue.
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t yes;
+    asm volatile(
+        "{\n"
+        ".reg .pred p;\n"
+        "elect.sync _|p, 0xffffffff;\n"
+        "selp.u32 %0, 1, 0, p;\n"
+        "}\n"
+        : "=r"(yes));
+    return yes != 0;
+}
+
+// ---- the line of tiles ------------------------------------------------------------------------------
+// Tiles of request r's context (an empty one counts as one, so that its rows are written) and its row tiles.
+struct Request {
+    int first, nodes, len, tiles, row_tiles;
 };
 
-__device__ __forceinline__ Work work_of(const TreeArgs& a)
+__device__ __forceinline__ Request request_of(const TreeArgs& a, int r)
 {
-    Work w;
-    int x = blockIdx.x;
-    const int rt = x % a.row_tiles;
-    x /= a.row_tiles;
-    w.h = x % a.Hkv;
-    x /= a.Hkv;
-    w.split = x % a.n_splits;
-    w.r = x / a.n_splits;
-    const int2 rows = tree_rows(a.tree, w.r, a.kv.status);
-    w.first = rows.x;
-    w.nodes = rows.y;
-    w.len = paged_len(a.kv, w.r);
-    w.committed = w.len - w.nodes;
-    w.node0 = rt * a.nodes_per_tile;
-    w.rows = min(a.nodes_per_tile, max(0, w.nodes - w.node0)) * (a.Hq / a.Hkv);
-    const int all = (w.len + kTile - 1) / kTile, per = (all + a.n_splits - 1) / a.n_splits;
-    w.tile0 = min(all, w.split * per);
-    w.tiles = min(all, w.tile0 + per) - w.tile0;
-    return w;
+    Request q;
+    const int2 rows = tree_rows(a.tree, r, a.kv.status);
+    q.first = rows.x;
+    q.nodes = rows.y;
+    q.len = paged_len(a.kv, r);
+    q.tiles = max(1, (q.len + kTile - 1) / kTile);
+    q.row_tiles = (q.nodes + a.nodes_per_tile - 1) / a.nodes_per_tile;
+    return q;
 }
 
-// Rows of a query tile: bf16 as they are, or f16 times a power of two that brings the row's largest element into
-// [1, 2) (exact down to 2^-17 of it, within 2^-25 of it below); 128-byte swizzled operand rows, 0 where there is no row.
-template <int D, bool F4>
-__device__ __forceinline__ void stage_queries(Smem<D, F4>& sm, const TreeArgs& a, const Work& w, int warp, int lane)
+// Finds part `cta` of `ctas`: for kSoftmaxThreads threads, in shared memory that all of the CTA may read after its next
+// barrier (p0 >= p1: nothing).  Each thread counts a stretch of requests; the tiles before a warp, a lane and a request are
+// then added up.
+__device__ __forceinline__ void find_part(const TreeArgs& a, int cta, int ctas, Part& part)
 {
-    constexpr int kLanes = D / 8, kRows = 32 / kLanes;  // lanes of a row, rows at once
-    const int G = a.Hq / a.Hkv, ch = lane % kLanes;
-#pragma unroll 4
-    for (int i0 = 0; i0 < 32; i0 += kRows) {
-        const int i = warp * 32 + i0 + lane / kLanes;
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (i < w.rows)
-            x = __ldg(reinterpret_cast<const uint4*>(
-                a.q + ((int64_t)(w.first + w.node0 + i / G) * a.Hq + w.h * G + i % G) * D + 8 * ch));
-        if constexpr (F4) {
-            const uint32_t word[4] = {x.x, x.y, x.z, x.w};
-            float f[8], top = 0.f;
+    constexpr int kWarps = kSoftmaxThreads / 32;
+    const int i = threadIdx.x, warp = i >> 5, lane = i & 31, R = a.tree.n_requests;
+    const int stretch = (R + kSoftmaxThreads - 1) / kSoftmaxThreads;
+    const int r0 = min((long long)R, (long long)i * stretch), r1 = min(R, r0 + stretch);
+    long long mine[kMaxRowTiles] = {}, upto[kMaxRowTiles] = {};
+    int longest = 0;
+    for (int r = r0; r < r1; ++r) {
+        const Request q = request_of(a, r);
+        if (q.row_tiles > 0) longest = max(longest, q.tiles);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                f[2 * e] = __uint_as_float(word[e] << 16);
-                f[2 * e + 1] = __uint_as_float(word[e] & 0xffff0000u);
-                top = fmaxf(top, fmaxf(fabsf(f[2 * e]), fabsf(f[2 * e + 1])));
-            }
+        for (int k = 0; k < kMaxRowTiles; ++k)
+            if (k < q.row_tiles) mine[k] += q.tiles;
+    }
 #pragma unroll
-            for (int off = 1; off < kLanes; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-            const int e = min(max((int)(__float_as_uint(top) >> 23), 2), 252) - 127;
-            const float down = __uint_as_float((uint32_t)(127 - e) << 23), up = __uint_as_float((uint32_t)(127 + e) << 23);
-            // (neither 0 nor infinite: the -inf of a hidden token, or a score of 0, times that would be NaN)
-            if (ch == 0) sm.row_unit[i] = fminf(fmaxf(a.scale * up * kLog2e, FLT_MIN), FLT_MAX);
-            x = make_uint4(f16x2(f[0] * down, f[1] * down), f16x2(f[2] * down, f[3] * down), f16x2(f[4] * down, f[5] * down),
-                           f16x2(f[6] * down, f[7] * down));
+    for (int k = 0; k < kMaxRowTiles; ++k) {
+        if (k >= a.row_tiles) continue;
+        upto[k] = mine[k];
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, upto[k], off);
+            if (lane >= off) upto[k] += y;
         }
-        *reinterpret_cast<uint4*>(&sm.q[ch >> 3][i * 128 + (((ch & 7) ^ (i & 7)) << 4)]) = x;
+        if (lane == 31) part.tiles[k][warp] = upto[k];
+    }
+    longest = __reduce_max_sync(0xffffffffu, longest);
+    if (lane == 0) part.longest[warp] = longest;
+    softmax_barrier();
+    long long total = 0;
+    for (int k = 0; k < a.row_tiles; ++k)
+        for (int x = 0; x < kWarps; ++x) total += part.tiles[k][x];
+    for (int x = 0; x < kWarps; ++x) longest = max(longest, part.longest[x]);
+    total *= a.Hkv;
+    // equal parts; no unit in more of them than there may be
+    long long per = (total + ctas - 1) / ctas;
+    if (a.n_splits > 1) per = max(per, (long long)(longest + a.n_splits - 2) / (a.n_splits - 1));
+    per = max(1ll, per);
+    const long long p0 = cta * per, p1 = min(total, p0 + per);
+    if (i == 0) {
+        part.p0 = p0;
+        part.p1 = p1;
+        part.per = per;
+    }
+    long long before = 0;  // tiles of the row tiles before k
+#pragma unroll
+    for (int k = 0; k < kMaxRowTiles; ++k) {
+        if (k >= a.row_tiles) continue;
+        long long ahead = 0;
+        for (int x = 0; x < warp; ++x) ahead += part.tiles[k][x];
+        long long at = before + (ahead + upto[k] - mine[k]) * a.Hkv;
+        if (p0 < p1 && p0 >= at && p0 < at + mine[k] * a.Hkv) {  // one thread: the part begins in its stretch
+            for (int r = r0; r < r1; ++r) {
+                const Request q = request_of(a, r);
+                if (q.row_tiles <= k) continue;
+                if (p0 < at + (long long)q.tiles * a.Hkv) {
+                    part.rt = k;
+                    part.r = r;
+                    part.h = (int)((p0 - at) / q.tiles);
+                    part.start = at + (long long)part.h * q.tiles;
+                    break;
+                }
+                at += (long long)q.tiles * a.Hkv;
+            }
+        }
+        for (int x = 0; x < kWarps; ++x) before += part.tiles[k][x] * a.Hkv;
     }
 }
+
+// The units of a part, one after another.
+struct Walk {
+    int rt, r, h;
+    Request q;
+    long long start;   // of the unit, on the line
+    int tile0, tiles;  // of its tiles, those in this part
+
+    __device__ __forceinline__ int committed() const { return q.len - q.nodes; }
+    __device__ __forceinline__ int node0(const TreeArgs& a) const { return rt * a.nodes_per_tile; }
+    __device__ __forceinline__ int rows(const TreeArgs& a) const
+    {
+        return min(a.nodes_per_tile, q.nodes - node0(a)) * (a.Hq / a.Hkv);
+    }
+    __device__ __forceinline__ void cut(const TreeArgs& a, const Part& p)
+    {
+        tile0 = 0;
+        tiles = q.tiles;
+        if (a.n_splits == 1) return;  // units are not divided: the part in which one begins takes it
+        tile0 = (int)(max(p.p0, start) - start);
+        tiles = (int)(min(p.p1, start + q.tiles) - start) - tile0;
+    }
+    __device__ __forceinline__ bool next(const TreeArgs& a, const Part& p)
+    {
+        start += q.tiles;
+        if (start >= p.p1) return false;
+        if (++h == a.Hkv) {
+            h = 0;
+            do {
+                if (++r == a.tree.n_requests) {
+                    r = 0;
+                    if (++rt == a.row_tiles) return false;
+                }
+                q = request_of(a, r);
+            } while (q.row_tiles <= rt);
+        }
+        cut(a, p);
+        return true;
+    }
+    // the first one; false if there is none
+    __device__ __forceinline__ bool begin(const TreeArgs& a, const Part& p)
+    {
+        if (p.p0 >= p.p1) return false;
+        rt = p.rt;
+        r = p.r;
+        h = p.h;
+        start = p.start;
+        q = request_of(a, r);
+        cut(a, p);
+        return a.n_splits > 1 || start >= p.p0 || next(a, p);
+    }
+};
 
 // Columns 32 c .. 32 c + 31 of a tile that begins at token t0: those that a row sees.
 __device__ __forceinline__ uint32_t seen_columns(int t, int committed, int len, unsigned long long sees)
@@ -222,375 +366,466 @@ __device__ __forceinline__ uint32_t seen_columns(int t, int committed, int len, 
     return t + 32 <= len ? bits : len > t ? bits & ((1u << (len - t)) - 1u) : 0u;
 }
 
+// ---- softmax ----------------------------------------------------------------------------------------
 template <int D, bool F4>
-__device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, const TreeArgs& a, const Work& w, uint32_t tmem, int warp, int lane)
-{
+struct Softmax {
     using C = Cfg<D, F4>;
-    const int i = threadIdx.x, G = a.Hq / a.Hkv;
-    int* gave_up = &sm.gave_up;
+    Smem<D, F4>& sm;
+    const TreeArgs& a;
+    const uint32_t tmem;  // with this warp's lanes
+    const int warp, half, i;
 
-    // ---- what this row sees: the ancestors' words, in memory that the queries take next
-    TreeSmem& ts = *reinterpret_cast<TreeSmem*>(sm.q[0]);
-    if (i < MOSKA_TREE_MAX_NODES)
-        tree_ancestors(ts, i, i < w.nodes ? tree_parent(a.tree, w.first, i, a.kv.status) : -1,
-                       [] { asm volatile("bar.sync 2, 64;" ::: "memory"); });
-    asm volatile("bar.sync 1, 128;" ::: "memory");
-    const bool live = i < w.rows;
-    const int node = w.node0 + i / G;
-    unsigned long long sees = 0;
-    if (live && w.committed + node >= 0) sees = ts.bits[node];
-    if (w.committed < 0) sees &= ~0ull << min(63, -w.committed);  // nodes without a token
-    asm volatile("bar.sync 1, 128;" ::: "memory");
-    stage_queries<D, F4>(sm, a, w, warp, lane);
-    fence_proxy_async_smem();
-    mbar_arrive(&sm.q_full);
+    // the two threads of the rows of a warp
+    __device__ __forceinline__ void row_barrier() const { asm volatile("bar.sync %0, 64;" ::"r"(2 + (warp & 3)) : "memory"); }
 
-    const int64_t row = (int64_t)(w.first + node) * a.Hq + w.h * G + i % G;
-    const int64_t slot = row * a.n_slots + a.slot0 + w.split;
-    const uint32_t t_s = tmem + (static_cast<uint32_t>(warp * 32) << 16), t_o = t_s + kTile;
-    const bool warp_live = warp * 32 < w.rows;
-    if constexpr (F4) asm volatile("bar.sync 1, 128;" ::: "memory");  // row_unit
-    const float unit = F4 ? sm.row_unit[F4 ? i : 0] : a.scale * kLog2e;
-    float m_ref = -INFINITY, l_sum = 0.f;
-    bool alive = true;
-    for (int j = 0; j < w.tiles; ++j) {
-        const int t0 = (w.tile0 + j) * kTile;
-        const bool ends = t0 + kTile > w.committed;  // some row does not see all of the tile
-        if constexpr (!F4) {
-            if (ends) {
-                // Values behind the context, and those of drafted tokens that are not finite, become 0: token row i here
-                const int t = t0 + i;
-                const int seq = j * 2 * C::kHalves + C::kHalves;
+    // The row of the next unit: what it sees, and its query into tensor memory.  In 4-bit pages queries are f16 times a
+    // power of two that brings the row's largest element into [1, 2) (exact down to 2^-17 of it, within 2^-25 of it below);
+    // `unit`: log2 units of one score.
+    __device__ __forceinline__ void prepare(const Walk& w, bool new_request, uint32_t n_unit, unsigned long long& sees, float& unit)
+    {
+        softmax_barrier();  // all have left the unit before the last: its `bad`, and the ancestors, may go
+        if (threadIdx.x == 0) sm.bad[(n_unit - 2) & 7] = 0;
+        if (new_request) {
+            if (threadIdx.x < MOSKA_TREE_MAX_NODES) {
+                const int x = threadIdx.x;
+                tree_ancestors(sm.tree, x, x < w.q.nodes ? tree_parent(a.tree, w.q.first, x, a.kv.status) : -1,
+                               [] { asm volatile("bar.sync 7, 64;" ::: "memory"); });
+            }
+            softmax_barrier();
+        }
+        const int G = a.Hq / a.Hkv, node = w.node0(a) + i / G, committed = w.committed();
+        const bool live = i < w.rows(a);
+        sees = live && committed + node >= 0 ? sm.tree.bits[node] : 0;
+        if (committed < 0) sees &= ~0ull << min(63, -committed);  // nodes without a token
+        constexpr int kWords = D / 4;  // of half a row
+        uint32_t x[kWords];
+        const uint4* from = reinterpret_cast<const uint4*>(a.q + ((int64_t)(w.q.first + node) * a.Hq + w.h * G + i % G) * D) +
+                            half * (kWords / 4);
 #pragma unroll
-                for (int hv = 0; hv < C::kHalves; ++hv)
-                    alive = alive && warp_wait(&sm.full[(seq + hv) % C::kSlots], ((seq + hv) / C::kSlots) & 1, gave_up);
-                if (!alive) break;
-                if (t >= w.committed) {
+        for (int e = 0; e < kWords / 4; ++e) {
+            const uint4 v = live ? __ldg(from + e) : make_uint4(0, 0, 0, 0);
+            x[4 * e] = v.x;
+            x[4 * e + 1] = v.y;
+            x[4 * e + 2] = v.z;
+            x[4 * e + 3] = v.w;
+        }
+        if constexpr (F4) {
+            float top = 0.f;
 #pragma unroll
-                    for (int hv = 0; hv < C::kHalves; ++hv) {
-                        uint8_t* at = &sm.slot[(seq + hv) % C::kSlots][i * 128];
+            for (int e = 0; e < kWords; ++e)
+                top = fmax3(top, fabsf(__uint_as_float(x[e] << 16)), fabsf(__uint_as_float(x[e] & 0xffff0000u)));
+            sm.top[0][half][i] = top;  // (free: between two units)
+            row_barrier();
+            top = fmaxf(top, sm.top[0][half ^ 1][i]);
+            row_barrier();
+            const int e2 = min(max((int)(__float_as_uint(top) >> 23), 2), 252) - 127;
+            const float down = __uint_as_float((uint32_t)(127 - e2) << 23), up = __uint_as_float((uint32_t)(127 + e2) << 23);
+            // (neither 0 nor infinite: the -inf of a hidden token, or a score of 0, times that would be NaN)
+            unit = fminf(fmaxf(a.scale * up * kLog2e, FLT_MIN), FLT_MAX);
+#pragma unroll
+            for (int e = 0; e < kWords; ++e)
+                x[e] = f16x2(__uint_as_float(x[e] << 16) * down, __uint_as_float(x[e] & 0xffff0000u) * down);
+        } else {
+            unit = a.scale * kLog2e;
+        }
+        const uint32_t to = tmem + kColQ + (n_unit & 1) * 64 + half * kWords;
+        if constexpr (kWords == 32) tmem_st32(to, x);
+        else tmem_st16(to, x);
+        tmem_st_wait();
+        tc_fence_before_sync();
+        mbar_arrive(&sm.q_full[n_unit & 1]);
+    }
+
+    // Values of tile g behind the context, and those of drafted tokens that are not finite, become 0 (bf16): token row i, this
+    // thread's half of it.
+    __device__ __forceinline__ bool clean_values(const Walk& w, int t0, uint32_t g, uint32_t n_unit)
+    {
+        const uint32_t seq = 2 * g + 1;
+        if (!warp_wait(&sm.full[seq % C::kSlots], (seq / C::kSlots) & 1, &sm.gave_up)) return false;
+        const int t = t0 + i, behind = t - w.committed();
+        if (behind >= 0) {
+            constexpr int kPieces = C::kHalves * 4;  // 16-byte pieces of half a row
+            uint8_t* at = sm.slot[seq % C::kSlots] + (C::kHalves == 2 ? half * kHalfBytes : 0) + i * 128;
+            const int first = C::kHalves == 2 ? 0 : 4 * half;
 #pragma unroll 1
-                        for (int x = 0; x < 8; ++x) {
-                            uint4* p = reinterpret_cast<uint4*>(at + (((x + i) & 7) << 4));
-                            const uint4 v = t < w.len ? *p : make_uint4(0, 0, 0, 0);
-                            uint32_t word[4] = {v.x, v.y, v.z, v.w};
-                            bool odd = false;
+            for (int x = 0; x < kPieces; ++x) {
+                uint4* p = reinterpret_cast<uint4*>(at + (((first + x + i) & 7) << 4));
+                const uint4 v = t < w.q.len ? *p : make_uint4(0, 0, 0, 0);
+                uint32_t word[4] = {v.x, v.y, v.z, v.w};
+                bool odd = false;
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                if ((word[e] & 0x7f80u) == 0x7f80u) { word[e] &= 0xffff0000u; odd = true; }
-                                if ((word[e] & 0x7f800000u) == 0x7f800000u) { word[e] &= 0xffffu; odd = true; }
-                            }
-                            if (odd) atomicOr(&sm.bad, 1ull << (t - w.committed));
-                            if (odd || t >= w.len) *p = make_uint4(word[0], word[1], word[2], word[3]);
-                        }
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    if ((word[e] & 0x7f80u) == 0x7f80u) { word[e] &= 0xffff0000u; odd = true; }
+                    if ((word[e] & 0x7f800000u) == 0x7f800000u) { word[e] &= 0xffffu; odd = true; }
                 }
-                fence_proxy_async_smem();
+                if (odd) atomicOr(&sm.bad[n_unit & 7], 1ull << behind);
+                if (odd || t >= w.q.len) *p = make_uint4(word[0], word[1], word[2], word[3]);
             }
         }
-        alive = warp_wait(&sm.s_full, j & 1, gave_up);
-        if (!alive) break;
+        fence_proxy_async_smem();
+        return true;
+    }
+
+    // One tile: scores -> probabilities.  `first`: of its unit.
+    __device__ __forceinline__ bool tile(const Walk& w, int j, uint32_t g, uint32_t n_unit, bool warp_live, bool live,
+                                         unsigned long long sees, float unit, float& m_ref, float& l_sum)
+    {
+        const int t0 = (w.tile0 + j) * kTile;
+        const bool ends = t0 + kTile > w.committed();  // some row does not see all of the tile
+        if constexpr (!F4)
+            if (ends && !clean_values(w, t0, g, n_unit)) return false;
+        if (!warp_wait(&sm.s_full[g & 1], (g >> 1) & 1, &sm.gave_up)) return false;
         if (warp_live) {
             tc_fence_after_sync();
-            uint32_t see[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
-            if (ends)
+            const uint32_t t_s = tmem + kColS + (g & 1) * kTile;
+            uint32_t s[2][32];
+            tmem_ld32(t_s + 64 * half, s[0]);
+            tmem_ld32(t_s + 64 * half + 32, s[1]);
+            tmem_ld_wait();
+            if (ends) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    see[c] = w.committed + node >= 0 ? seen_columns(t0 + 32 * c, w.committed, w.len, sees) : 0u;
-            float mx = -INFINITY;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t s[32];
-                tmem_ld32(t_s + 32 * c, s);
-                tmem_ld_wait();
-                if (ends)
+                for (int c = 0; c < 2; ++c) {
+                    const uint32_t see = sees == 0 ? 0u : seen_columns(t0 + 64 * half + 32 * c, w.committed(), w.q.len, sees);
 #pragma unroll
                     for (int x = 0; x < 32; ++x)
-                        if (!((see[c] >> x) & 1)) s[x] = 0xff800000u;
-                float m4[4] = {-INFINITY, -INFINITY, -INFINITY, mx};
+                        if (!((see >> x) & 1)) s[c][x] = 0xff800000u;
+                }
+            }
+            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
 #pragma unroll
                 for (int x = 0; x < 16; ++x)
-                    m4[x & 3] = fmax3(m4[x & 3], __uint_as_float(s[2 * x]), __uint_as_float(s[2 * x + 1]));
-                mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-            }
+                    m4[x & 3] = fmax3(m4[x & 3], __uint_as_float(s[c][2 * x]), __uint_as_float(s[c][2 * x + 1]));
+            float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+            sm.top[g & 1][half][i] = mx;
+            row_barrier();  // also: both threads have their scores, whose columns P takes
+            mx = fmaxf(mx, sm.top[g & 1][half ^ 1][i]);
             if (j == 0) {
                 m_ref = mx;
             } else {
                 const bool need = live && (mx - m_ref) * unit > kRescaleAt;
                 if (__any_sync(0xffffffffu, need)) {
-                    // all MMAs issued before these scores, O's last among them, have completed
+                    if (!warp_wait(&sm.pv_done, (g - 1) & 1, &sm.gave_up)) return false;
+                    tc_fence_after_sync();
                     const float alpha = need ? fast_exp2((m_ref - mx) * unit) : 1.f;
                     if (need) m_ref = mx;
                     l_sum *= alpha;
 #pragma unroll 1
-                    for (int c = 0; c < D / 32; ++c) {
-                        uint32_t o[32];
-                        tmem_ld32(t_o + 32 * c, o);
+                    for (int c = 0; c < D / 32; ++c) {  // this thread's half of the row
+                        uint32_t o[16];
+                        const uint32_t at = tmem + kColO + half * (D / 2) + 16 * c;
+                        tmem_ld16(at, o);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * alpha);
-                        tmem_st32(t_o + 32 * c, o);
+                        for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * alpha);
+                        tmem_st16(at, o);
                     }
                 }
             }
             const float base = m_ref == -INFINITY ? 0.f : m_ref * unit;  // (nothing seen yet)
-            float l4[4] = {0.f, 0.f, 0.f, 0.f};
+            const float2 unit2 = make_float2(unit, unit), base2 = make_float2(-base, -base);
+            float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t s[32], pk[16];
-                tmem_ld32(t_s + 32 * c, s);
-                tmem_ld_wait();
-                if (ends)
-#pragma unroll
-                    for (int x = 0; x < 32; ++x)
-                        if (!((see[c] >> x) & 1)) s[x] = 0xff800000u;
+            for (int c = 0; c < 2; ++c) {
+                uint32_t pk[16];
 #pragma unroll
                 for (int x = 0; x < 16; ++x) {
-                    const float p0 = fast_exp2(fmaf(__uint_as_float(s[2 * x]), unit, -base));
-                    const float p1 = fast_exp2(fmaf(__uint_as_float(s[2 * x + 1]), unit, -base));
-                    l4[2 * (x & 1)] += p0;
-                    l4[2 * (x & 1) + 1] += p1;
-                    pk[x] = F4 ? f16x2(p0, p1) : bf16x2(p0, p1);
+                    float2 p = ffma2(make_float2(__uint_as_float(s[c][2 * x]), __uint_as_float(s[c][2 * x + 1])), unit2, base2);
+                    p.x = fast_exp2(p.x);
+                    p.y = fast_exp2(p.y);
+                    l2[x & 1] = fadd2(l2[x & 1], p);
+                    pk[x] = F4 ? f16x2(p.x, p.y) : bf16x2(p.x, p.y);
                 }
-                tmem_st16(t_s + 16 * c, pk);  // over columns that have been read
+                tmem_st16(t_s + 32 * half + 16 * c, pk);
             }
-            l_sum += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+            l_sum += (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
             tmem_st_wait();
         }
         tc_fence_before_sync();
-        mbar_arrive(&sm.p_full);
+        mbar_arrive(&sm.p_full[g & 1]);
+        return true;
     }
 
-    // ---- the row's result
-    if (alive && w.tiles > 0) alive = warp_wait(&sm.o_full, 0, gave_up);
-    asm volatile("bar.sync 1, 128;" ::: "memory");  // `bad` is complete
-    if (!alive || !warp_live) return;
-    tc_fence_after_sync();
-    const float inv = l_sum == 0.f ? 0.f : 1.f / l_sum;
-    const float base = m_ref == -INFINITY ? 0.f : m_ref * unit;
-    unsigned long long odd = l_sum == 0.f ? 0 : sm.bad & sees;
-    const int32_t* pages = a.kv.page_table + (int64_t)w.r * a.kv.max_pages;
-#pragma unroll
-    for (int c = 0; c < D / 32; ++c) {
-        uint32_t o[32];
-        if (w.tiles > 0) {
-            tmem_ld32(t_o + 32 * c, o);
-            tmem_ld_wait();
+    // The unit's rows: final ones, partial ones of a cut unit, or partial slots.
+    __device__ __forceinline__ void finish(const Walk& w, uint32_t n_unit, bool live, unsigned long long sees, float unit, float m_ref,
+                                           float l_sum)
+    {
+        sm.sum[half][i] = l_sum;
+        row_barrier();
+        l_sum += sm.sum[half ^ 1][i];  // (the same in both threads: two terms)
+        tc_fence_after_sync();
+        const int G = a.Hq / a.Hkv, node = w.node0(a) + i / G;
+        const int64_t row = (int64_t)(w.q.first + node) * a.Hq + w.h * G + i % G;
+        const float inv = l_sum == 0.f ? 0.f : 1.f / l_sum;
+        const float lse = l_sum == 0.f ? -INFINITY : (m_ref == -INFINITY ? 0.f : m_ref * unit * kLn2) + logf(l_sum);
+        const unsigned long long odd = l_sum == 0.f ? 0 : *static_cast<volatile unsigned long long*>(&sm.bad[n_unit & 7]) & sees;
+        const bool whole = w.tiles == w.q.tiles, final_row = a.out != nullptr && whole;
+        float *to = nullptr, *lse_to = nullptr;
+        int spare = 0;  // slots behind this one that hold nothing
+        if (a.out == nullptr) {
+            const long long per = sm.part.per, c0 = w.start / per;
+            const int k = a.n_splits == 1 ? 0 : (int)(blockIdx.x - c0);
+            const int parts = a.n_splits == 1 ? 1 : (int)((w.start + w.q.tiles - 1) / per - c0) + 1;
+            const int64_t slot = row * a.n_slots + a.slot0 + k;
+            to = a.o_part + slot * D;
+            lse_to = a.lse_part + slot;
+            if (k == parts - 1) spare = a.n_splits - parts;
+        } else if (!whole) {
+            const int64_t slot = (int64_t)(2 * blockIdx.x + (w.tile0 == 0 ? 1 : 0)) * kTileRows + i;
+            to = a.o_cut + slot * D;
+            lse_to = a.lse_cut + slot;
+        } else if (a.lse_out != nullptr) {
+            lse_to = a.lse_out + row;
         }
-        float x[32];
+        const int32_t* pages = a.kv.page_table + (int64_t)w.r * a.kv.max_pages;
 #pragma unroll
-        for (int e = 0; e < 32; ++e) x[e] = l_sum == 0.f ? 0.f : __uint_as_float(o[e]) * inv;
-        for (unsigned long long left = odd; left != 0; left &= left - 1) {  // values that were taken out
-            const int t = w.committed + __ffsll(left) - 1, in = t & ((1 << a.kv.page_shift) - 1);
-            const int64_t page = paged_page(a.kv, pages, t >> a.kv.page_shift);
-            if constexpr (F4) {
-                using B = Fp4Block<D>;
-                const uint8_t* b = a.kv.k + (((page * a.Hkv + w.h) << (a.kv.page_shift - 4)) + (in >> 4)) * B::kBytes;
-                const uint32_t sc = *reinterpret_cast<const uint16_t*>(b + B::v_scale(in & 15, c));
-                if ((sc & 0x7fffu) <= 0x7154u) continue;
+        for (int c = 0; c < D / 32; ++c) {  // 16 dimensions at a time
+            const int d0 = half * (D / 2) + 16 * c;
+            uint32_t o[16];
+            tmem_ld16(tmem + kColO + d0, o);
+            tmem_ld_wait();
+            float x[16];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    uint32_t f[4];
-                    e2m1x8_to_f16x2(*reinterpret_cast<const uint32_t*>(b + B::v_byte(in & 15, 32 * c + 8 * e)), f);
+            for (int e = 0; e < 16; ++e) x[e] = l_sum == 0.f ? 0.f : __uint_as_float(o[e]) * inv;
+            for (unsigned long long left = odd; left != 0; left &= left - 1) {  // values that were taken out
+                const int t = w.committed() + __ffsll(left) - 1, in = t & ((1 << a.kv.page_shift) - 1);
+                const int64_t page = paged_page(a.kv, pages, t >> a.kv.page_shift);
+                if constexpr (F4) {
+                    using B = Fp4Block<D>;
+                    const uint8_t* b = a.kv.k + (((page * a.Hkv + w.h) << (a.kv.page_shift - 4)) + (in >> 4)) * B::kBytes;
+                    const uint32_t sc = *reinterpret_cast<const uint16_t*>(b + B::v_scale(in & 15, d0 / 32));
+                    if ((sc & 0x7fffu) <= 0x7154u) continue;
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const uint32_t v = hmul2(f[y], sc * 0x10001u);
-                        x[8 * e + 2 * y] += __half2float(__ushort_as_half((unsigned short)v));
-                        x[8 * e + 2 * y + 1] += __half2float(__ushort_as_half((unsigned short)(v >> 16)));
+                    for (int e = 0; e < 2; ++e) {
+                        uint32_t f[4];
+                        e2m1x8_to_f16x2(*reinterpret_cast<const uint32_t*>(b + B::v_byte(in & 15, d0 + 8 * e)), f);
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            const uint32_t v = hmul2(f[y], sc * 0x10001u);
+                            x[8 * e + 2 * y] += __half2float(__ushort_as_half((unsigned short)v));
+                            x[8 * e + 2 * y + 1] += __half2float(__ushort_as_half((unsigned short)(v >> 16)));
+                        }
                     }
-                }
-            } else {
-                const uint16_t* v = reinterpret_cast<const uint16_t*>(a.kv.v) +
-                                    (((page << a.kv.page_shift) + in) * a.Hkv + w.h) * D + 32 * c;
+                } else {
+                    const uint16_t* v = reinterpret_cast<const uint16_t*>(a.kv.v) +
+                                        (((page << a.kv.page_shift) + in) * a.Hkv + w.h) * D + d0;
 #pragma unroll
-                for (int e = 0; e < 32; ++e)
-                    if ((v[e] & 0x7f80u) == 0x7f80u) x[e] += __uint_as_float((uint32_t)v[e] << 16);
+                    for (int e = 0; e < 16; ++e)
+                        if ((v[e] & 0x7f80u) == 0x7f80u) x[e] += __uint_as_float((uint32_t)v[e] << 16);
+                }
+            }
+            if (!live) continue;
+            if (final_row) {
+                uint4* p = reinterpret_cast<uint4*>(a.out + row * D + d0);
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    p[e] = make_uint4(bf16x2(x[8 * e], x[8 * e + 1]), bf16x2(x[8 * e + 2], x[8 * e + 3]),
+                                      bf16x2(x[8 * e + 4], x[8 * e + 5]), bf16x2(x[8 * e + 6], x[8 * e + 7]));
+            } else {
+                float4* p = reinterpret_cast<float4*>(to + d0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) p[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+                for (int k = 1; k <= spare; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) reinterpret_cast<float4*>(to + k * D + d0)[e] = make_float4(0.f, 0.f, 0.f, 0.f);
             }
         }
-        if (!live) continue;
-        if (a.out != nullptr) {
-            uint4* to = reinterpret_cast<uint4*>(a.out + row * D + 32 * c);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                to[e] = make_uint4(bf16x2(x[8 * e], x[8 * e + 1]), bf16x2(x[8 * e + 2], x[8 * e + 3]),
-                                   bf16x2(x[8 * e + 4], x[8 * e + 5]), bf16x2(x[8 * e + 6], x[8 * e + 7]));
-        } else {
-            float4* to = reinterpret_cast<float4*>(a.o_part + slot * D + 32 * c);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) to[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+        if (live && half == 0 && lse_to != nullptr) {
+            *lse_to = lse;
+            for (int k = 1; k <= spare; ++k) lse_to[k] = -INFINITY;
         }
     }
-    if (!live) return;
-    const float lse = l_sum == 0.f ? -INFINITY : base * kLn2 + logf(l_sum);
-    if (a.out == nullptr) a.lse_part[slot] = lse;
-    else if (a.lse_out != nullptr) a.lse_out[row] = lse;
-}
 
+    __device__ __forceinline__ void run(Walk w)
+    {
+        unsigned long long sees, sees_next = 0;
+        float unit, unit_next = 0.f;
+        uint32_t g = 0, n_unit = 0;
+        prepare(w, true, 0, sees, unit);
+        while (true) {
+            const int rows = w.rows(a);
+            const bool live = i < rows, warp_live = (warp & 3) * 32 < rows;
+            float m_ref = -INFINITY, l_sum = 0.f;
+            for (int j = 0; j < w.tiles; ++j, ++g)
+                if (!tile(w, j, g, n_unit, warp_live, live, sees, unit, m_ref, l_sum)) return;
+            Walk after = w;
+            const bool more = after.next(a, sm.part);
+            if (more) prepare(after, after.r != w.r, n_unit + 1, sees_next, unit_next);
+            if (!warp_wait(&sm.pv_done, (g - 1) & 1, &sm.gave_up)) return;
+            if (warp_live) finish(w, n_unit, live, sees, unit, m_ref, l_sum);
+            if (!more) return;
+            w = after;
+            sees = sees_next;
+            unit = unit_next;
+            ++n_unit;
+        }
+    }
+};
+
+// ---- copies -----------------------------------------------------------------------------------------
 template <int D, bool F4>
 __device__ __forceinline__ void load_role(Smem<D, F4>& sm, const CUtensorMap& tm_k, const CUtensorMap& tm_v, const TreeArgs& a,
-                                          const Work& w, int lane)
+                                          Walk w, int lane)
 {
     using C = Cfg<D, F4>;
-    const int32_t* pages = a.kv.page_table + (int64_t)w.r * a.kv.max_pages;
     const int shift = a.kv.page_shift;
-    const int end = w.len;
-    if constexpr (!F4) {
-        const int box = min(kTile, 1 << shift);  // tokens of a copy; lane b < kTile / box copies the b-th of a tile
-        const int boxes = kTile / box;
-        auto page_of = [&](int j) {
-            const int t = (w.tile0 + j) * kTile + lane * box;
-            return lane < boxes && j < w.tiles && t < end ? paged_page(a.kv, pages, t >> shift) : -1;
-        };
-        int next = page_of(0), seq = 0;
-        bool ok = true;
-        for (int j = 0; j < w.tiles && ok; ++j) {
-            const int page = next;
-            next = page_of(j + 1);
-            const int t = (w.tile0 + j) * kTile + lane * box;
-            const int there = __popc(__ballot_sync(0xffffffffu, page >= 0));
-            const int z = (page << shift) + (t & ((1 << shift) - 1));
+    uint32_t seq = 0;
+    bool ok = true;
+    do {
+        const int32_t* pages = a.kv.page_table + (int64_t)w.r * a.kv.max_pages;
+        if constexpr (!F4) {
+            const int box = min(kTile, 1 << shift);  // tokens of a copy; lane b < kTile / box copies the b-th of a tile
+            const int boxes = kTile / box;
+            auto page_of = [&](int j) {
+                const int t = (w.tile0 + j) * kTile + lane * box;
+                return lane < boxes && j < w.tiles && t < w.q.len ? paged_page(a.kv, pages, t >> shift) : -1;
+            };
+            int ahead = page_of(0);
+            for (int j = 0; j < w.tiles && ok; ++j) {
+                const int page = ahead;
+                ahead = page_of(j + 1);
+                const int t = (w.tile0 + j) * kTile + lane * box;
+                const int there = __popc(__ballot_sync(0xffffffffu, page >= 0));
+                const int z = (page << shift) + (t & ((1 << shift) - 1));
 #pragma unroll
-            for (int x = 0; x < 2 * C::kHalves; ++x, ++seq) {
-                const int s = seq % C::kSlots;
-                if (seq >= C::kSlots) ok = warp_wait(&sm.empty[s], ((seq / C::kSlots) - 1) & 1, &sm.gave_up);
-                if (!ok) break;
-                if (lane == 0) mbar_arrive_expect_tx(&sm.full[s], there * box * 128);
-                __syncwarp();
-                if (page >= 0)
-                    tma_load_3d(sm.slot[s] + lane * box * 128, x < C::kHalves ? &tm_k : &tm_v, 64 * (x % C::kHalves), w.h, z,
-                                &sm.full[s]);
-            }
-        }
-        if (*static_cast<volatile int*>(&sm.gave_up))  // the copies in flight end before the CTA leaves (each wait again has a limit)
-            for (int x = max(0, seq - C::kSlots); x < seq; ++x) {
-                int never = 0;
-                mbar_wait(&sm.full[x % C::kSlots], (x / C::kSlots) & 1, &never);
-            }
-    } else {
-        using B = Fp4Block<D>;
-        // units: keys of tokens 0 .. 63 of a tile, of 64 .. 127, then the values; lane 2 b + c copies block b's codes
-        // (c = 0) or scales (c = 1)
-        const int b = lane >> 1, c = lane & 1;
-        const int64_t page_bytes = ((int64_t)a.Hkv << (shift - 4)) * B::kBytes;
-        const uint8_t* pool = a.kv.k + ((int64_t)w.h << (shift - 4)) * B::kBytes;
-        auto page_of = [&](int j, int half) {
-            const int t = (w.tile0 + j) * kTile + 64 * half + 16 * b;
-            return lane < 2 * C::kUnitBlocks && j < w.tiles && t < end ? paged_page(a.kv, pages, t >> shift) : -1;
-        };
-        int next[2] = {page_of(0, 0), page_of(0, 1)}, seq = 0;
-        bool ok = true;
-        for (int j = 0; j < w.tiles && ok; ++j) {
-            const int page[2] = {next[0], next[1]};
-            next[0] = page_of(j + 1, 0);
-            next[1] = page_of(j + 1, 1);
+                for (int kind = 0; kind < 2; ++kind) {
+                    const uint32_t s = seq % C::kSlots;
+                    if (seq >= C::kSlots) ok = warp_wait(&sm.empty[s], ((seq / C::kSlots) - 1) & 1, &sm.gave_up);
+                    if (!ok) break;
+                    if (lane == 0) mbar_arrive_expect_tx(&sm.full[s], there * box * 128 * C::kHalves);
+                    __syncwarp();
+                    if (page >= 0)
 #pragma unroll
-            for (int x = 0; x < 4; ++x, ++seq) {
-                const int half = x & 1;
-                const bool value = x >= 2;
-                const int u = seq % C::kUnits;
-                if (seq >= C::kUnits) ok = warp_wait(&sm.unit_empty[u], ((seq / C::kUnits) - 1) & 1, &sm.gave_up);
-                if (!ok) break;
-                const int there = __popc(__ballot_sync(0xffffffffu, page[half] >= 0)) / 2;
-                if (lane == 0) mbar_arrive_expect_tx(&sm.unit_full[u], there * C::kPartBytes);
-                __syncwarp();
-                if (page[half] >= 0) {
-                    const int t = (w.tile0 + j) * kTile + 64 * half + 16 * b;
-                    const int block = (t & ((1 << shift) - 1)) >> 4;
-                    const uint8_t* from = pool + page[half] * page_bytes + (int64_t)block * B::kBytes;
-                    from += c == 0 ? (value ? B::kV : 0) : (value ? B::kVScale : B::kKScale);
-                    bulk_load(sm.unit + u * C::kUnitBytes + b * C::kPartBytes + (c == 0 ? 0 : 8 * D), from, c == 0 ? 8 * D : D,
-                              &sm.unit_full[u]);
+                        for (int hv = 0; hv < C::kHalves; ++hv)
+                            tma_load_3d(sm.slot[s] + hv * kHalfBytes + lane * box * 128, kind == 0 ? &tm_k : &tm_v, 64 * hv, w.h, z,
+                                        &sm.full[s]);
+                    ++seq;
+                }
+            }
+        } else {
+            using B = Fp4Block<D>;
+            // units: the key parts of a tile, then its value parts; lane 2 b + c copies block b's codes (c = 0) or scales
+            const int b = lane >> 1, c = lane & 1;
+            const int64_t page_bytes = ((int64_t)a.Hkv << (shift - 4)) * B::kBytes;
+            const uint8_t* pool = a.kv.k + ((int64_t)w.h << (shift - 4)) * B::kBytes;
+            auto page_of = [&](int j) {
+                const int t = (w.tile0 + j) * kTile + 16 * b;
+                return lane < 2 * C::kBlocks && j < w.tiles && t < w.q.len ? paged_page(a.kv, pages, t >> shift) : -1;
+            };
+            int ahead = page_of(0);
+            for (int j = 0; j < w.tiles && ok; ++j) {
+                const int page = ahead;
+                ahead = page_of(j + 1);
+                const int t = (w.tile0 + j) * kTile + 16 * b;
+                const int there = __popc(__ballot_sync(0xffffffffu, page >= 0)) / 2;
+                const uint8_t* from = pool + page * page_bytes + (int64_t)((t & ((1 << shift) - 1)) >> 4) * B::kBytes;
+#pragma unroll
+                for (int kind = 0; kind < 2; ++kind) {
+                    const uint32_t u = seq % C::kUnits;
+                    if (seq >= C::kUnits) ok = warp_wait(&sm.unit_empty[u], ((seq / C::kUnits) - 1) & 1, &sm.gave_up);
+                    if (!ok) break;
+                    if (lane == 0) mbar_arrive_expect_tx(&sm.unit_full[u], there * C::kPartBytes);
+                    __syncwarp();
+                    if (page >= 0) {
+                        const int at = c == 0 ? (kind == 0 ? 0 : B::kV) : (kind == 0 ? B::kKScale : B::kVScale);
+                        bulk_load(sm.unit + u * C::kUnitBytes + b * C::kPartBytes + (c == 0 ? 0 : 8 * D), from + at,
+                                  c == 0 ? 8 * D : D, &sm.unit_full[u]);
+                    }
+                    ++seq;
                 }
             }
         }
-        if (*static_cast<volatile int*>(&sm.gave_up))
-            for (int x = max(0, seq - C::kUnits); x < seq; ++x) {
-                int never = 0;
-                mbar_wait(&sm.unit_full[x % C::kUnits], (x / C::kUnits) & 1, &never);
-            }
+    } while (ok && w.next(a, sm.part));
+    if (*static_cast<volatile int*>(&sm.gave_up)) {
+        // the copies in flight end before the CTA leaves (each wait again has a limit)
+        constexpr uint32_t kRing = F4 ? C::kUnits : C::kSlots;
+        for (uint32_t x = seq > kRing ? seq - kRing : 0; x < seq; ++x) {
+            int never = 0;
+            mbar_wait(F4 ? &sm.unit_full[x % kRing] : &sm.full[x % kRing], (x / kRing) & 1, &never);
+        }
     }
 }
 
+// ---- MMAs -------------------------------------------------------------------------------------------
 template <int D, bool F4>
-__device__ __forceinline__ void mma_role(Smem<D, F4>& sm, const Work& w, uint32_t tmem)
+__device__ __forceinline__ void mma_role(Smem<D, F4>& sm, const TreeArgs& a, Walk w, uint32_t tmem)
 {
     using C = Cfg<D, F4>;
-    constexpr int H = C::kHalves;
     const uint32_t id_qk = F4 ? idesc_f16_f32(128, kTile, false) : idesc_bf16_f32(128, kTile, false);
-    const uint32_t id_pv = F4 ? idesc_f16_f32(128, 64, true) : idesc_bf16_f32(128, 64, true);
-    const uint64_t d_k = smem_desc_sw128(0, 16, 1024), d_n = smem_desc_sw128(0, kSlotBytes, 1024);
+    const uint32_t id_pv = F4 ? idesc_f16_f32(128, D, true) : idesc_bf16_f32(128, D, true);
+    const uint64_t d_k = smem_desc_sw128(0, 16, 1024), d_n = smem_desc_sw128(0, kHalfBytes, 1024);
     const uint32_t hi_k = static_cast<uint32_t>(d_k >> 32), hi_n = static_cast<uint32_t>(d_n >> 32);
-    const uint32_t lo_q = static_cast<uint32_t>(d_k) + (smem_u32(sm.q[0]) >> 4);
     const uint32_t lo_k = static_cast<uint32_t>(d_k) + (smem_u32(sm.slot[0]) >> 4);
     const uint32_t lo_v = static_cast<uint32_t>(d_n) + (smem_u32(sm.slot[0]) >> 4);
     auto desc = [](uint32_t hi, uint32_t lo) { return (static_cast<uint64_t>(hi) << 32) | lo; };
     int* gave_up = &sm.gave_up;
-    auto scores = [&](int j) {
+    uint32_t g = 0, n_unit = 0;
+    auto scores = [&](uint32_t x) {  // of tile x, for the current unit
+        const uint32_t seq = 2 * x, s = seq % C::kSlots;
+        if (!warp_wait(&sm.full[s], (seq / C::kSlots) & 1, gave_up)) return false;
+        tc_fence_after_sync();
+        if (elect_one()) {
+            const uint32_t to = tmem + kColS + (x & 1) * kTile, q = tmem + kColQ + (n_unit & 1) * 64;
+            const uint32_t k = lo_k + ((s * C::kSlotBytes) >> 4);
 #pragma unroll
-        for (int hv = 0; hv < H; ++hv) {
-            const int seq = j * 2 * H + hv, s = seq % C::kSlots;
-            if (!mbar_wait(&sm.full[s], (seq / C::kSlots) & 1, gave_up)) return false;
-            tc_fence_after_sync();
-#pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
-                mma_ss(tmem, desc(hi_k, lo_q + ((hv * kSlotBytes + ks * 32) >> 4)), desc(hi_k, lo_k + ((s * kSlotBytes + ks * 32) >> 4)),
-                       id_qk, hv > 0 || ks > 0);
+            for (int ks = 0; ks < D / 16; ++ks)
+                mma_ts(to, q + 8 * ks, desc(hi_k, k + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4)), id_qk, ks > 0);
+            tc_commit(&sm.s_full[x & 1]);
             tc_commit(&sm.empty[s]);
         }
-        tc_commit(&sm.s_full);
+        __syncwarp();
         return true;
     };
-    bool ok = mbar_wait(&sm.q_full, 0, gave_up) && scores(0);
-    for (int j = 0; j < w.tiles && ok; ++j) {
-        ok = mbar_wait(&sm.p_full, j & 1, gave_up);
-#pragma unroll
-        for (int hv = 0; hv < H && ok; ++hv) {
-            const int seq = j * 2 * H + H + hv, s = seq % C::kSlots;
-            ok = mbar_wait(&sm.full[s], (seq / C::kSlots) & 1, gave_up);
-            if (!ok) break;
+    while (true) {
+        if (!warp_wait(&sm.q_full[n_unit & 1], (n_unit >> 1) & 1, gave_up)) return;
+        if (!scores(g)) return;
+        for (int j = 0; j < w.tiles; ++j, ++g) {
+            if (j + 1 < w.tiles && !scores(g + 1)) return;
+            const uint32_t seq = 2 * g + 1, s = seq % C::kSlots;
+            if (!warp_wait(&sm.p_full[g & 1], (g >> 1) & 1, gave_up)) return;
+            if (!warp_wait(&sm.full[s], (seq / C::kSlots) & 1, gave_up)) return;
             tc_fence_after_sync();
+            if (elect_one()) {
+                const uint32_t p = tmem + kColS + (g & 1) * kTile, v = lo_v + ((s * C::kSlotBytes) >> 4);
 #pragma unroll
-            for (int ks = 0; ks < kTile / 16; ++ks)
-                mma_ts(tmem + kTile + 64 * hv, tmem + 8 * ks, desc(hi_n, lo_v + ((s * kSlotBytes + ks * 2048) >> 4)), id_pv,
-                       j > 0 || ks > 0);
-            tc_commit(&sm.empty[s]);
+                for (int ks = 0; ks < kTile / 16; ++ks)
+                    mma_ts(tmem + kColO, p + 8 * ks, desc(hi_n, v + ((ks * 2048) >> 4)), id_pv, j > 0 || ks > 0);
+                tc_commit(&sm.pv_done);
+                tc_commit(&sm.empty[s]);
+            }
+            __syncwarp();
         }
-        if (!ok) break;
-        if (j + 1 < w.tiles) ok = scores(j + 1);
-        else tc_commit(&sm.o_full);
+        if (!w.next(a, sm.part)) return;
+        ++n_unit;
     }
 }
 
-// Codes of one block (a warp) of every unit -> f16 operand rows in the slots.
+// ---- 4 bits: codes of every fourth block of a tile (a warp) -> f16 operand rows ------------------------
 template <int D>
-__device__ __forceinline__ void widen_role(Smem<D, true>& sm, const Work& w, int block, int lane)
+__device__ __forceinline__ void widen_role(Smem<D, true>& sm, const TreeArgs& a, Walk w, int warp, int lane)
 {
     using C = Cfg<D, true>;
-    constexpr int H = C::kHalves, J = D / 32;
+    constexpr int J = D / 32;
     int* gave_up = &sm.gave_up;
-    int unit = 0, seq = 0;
-    bool ok = true;
-    for (int j = 0; j < w.tiles && ok; ++j) {
-        const int t0 = (w.tile0 + j) * kTile;
-        const bool ends = t0 + kTile > w.committed;
-#pragma unroll 1
-        for (int kind = 0; kind < 2 && ok; ++kind, seq += H) {
-            uint8_t* to[H];
+    uint32_t seq = 0, n_unit = 0;
+    do {
+        for (int j = 0; j < w.tiles; ++j) {
+            const int t0 = (w.tile0 + j) * kTile;
+            const bool ends = t0 + kTile > w.committed();
 #pragma unroll
-            for (int hv = 0; hv < H; ++hv) {
-                const int s = (seq + hv) % C::kSlots;
-                to[hv] = sm.slot[s];
-                if (seq + hv >= C::kSlots) ok = ok && warp_wait(&sm.empty[s], (((seq + hv) / C::kSlots) - 1) & 1, gave_up);
-            }
+            for (int kind = 0; kind < 2; ++kind, ++seq) {
+                const uint32_t s = seq % C::kSlots, u = seq % C::kUnits;
+                if (seq >= C::kSlots && !warp_wait(&sm.empty[s], ((seq / C::kSlots) - 1) & 1, gave_up)) return;
+                if (!warp_wait(&sm.unit_full[u], (seq / C::kUnits) & 1, gave_up)) return;
+                uint8_t* to = sm.slot[s];
 #pragma unroll 1
-            for (int half = 0; half < 2 && ok; ++half, ++unit) {
-                ok = warp_wait(&sm.unit_full[unit % C::kUnits], (unit / C::kUnits) & 1, gave_up);
-                if (!ok) break;
-                const uint8_t* from = sm.unit + (unit % C::kUnits) * C::kUnitBytes + block * C::kPartBytes;
-                const int row0 = 64 * half + 16 * block;
+                for (int block = warp; block < C::kBlocks; block += kWidenWarps) {
+                const uint8_t* from = sm.unit + u * C::kUnitBytes + block * C::kPartBytes;
+                const int row0 = 16 * block;
                 if (kind == 0) {
-                    // Keys: the D / 8 bytes of (token, c) are dimensions 32 g + 8 c .. + 7 for each group g.  Eight lanes that
-                    // go to memory together have tokens x and x ^ 5: their loads and their swizzled stores both fall on
+                    // Keys: the D / 8 bytes of (token, c) are dimensions 32 x + 8 c .. + 7 for each group x.  Eight lanes that
+                    // go to memory together have tokens y and y ^ 5: their loads and their swizzled stores both fall on
                     // eight different 16-byte pieces of the banks.
 #pragma unroll
                     for (int it = 0; it < 2; ++it) {
@@ -608,11 +843,11 @@ __device__ __forceinline__ void widen_role(Smem<D, true>& sm, const Work& w, int
                         }
                         const int row = row0 + t;
 #pragma unroll
-                        for (int g = 0; g < J; ++g) {
+                        for (int x = 0; x < J; ++x) {
                             uint32_t f[4];
-                            e2m1x8_to_f16x2(code[g], f);
-                            const uint32_t s2 = __byte_perm(sc[g >> 1], 0, (g & 1) ? 0x3232 : 0x1010);
-                            *reinterpret_cast<uint4*>(to[g >> 1] + row * 128 + (((4 * (g & 1) + c) ^ (row & 7)) << 4)) =
+                            e2m1x8_to_f16x2(code[x], f);
+                            const uint32_t s2 = __byte_perm(sc[x >> 1], 0, (x & 1) ? 0x3232 : 0x1010);
+                            *reinterpret_cast<uint4*>(to + (x >> 1) * kHalfBytes + row * 128 + (((4 * (x & 1) + c) ^ (row & 7)) << 4)) =
                                 make_uint4(hmul2(f[0], s2), hmul2(f[1], s2), hmul2(f[2], s2), hmul2(f[3], s2));
                         }
                     }
@@ -631,16 +866,16 @@ __device__ __forceinline__ void widen_role(Smem<D, true>& sm, const Work& w, int
                             const uint2 y = *reinterpret_cast<const uint2*>(at);
                             code[0] = y.x; code[1] = y.y;
                         }
-                        uint32_t sc = *reinterpret_cast<const uint32_t*>(from + 8 * D + 2 * ((x * (D / 8) / 32) * 16 + 2 * p));
+                        const uint32_t sc = *reinterpret_cast<const uint32_t*>(from + 8 * D + 2 * ((x * (D / 8) / 32) * 16 + 2 * p));
 #pragma unroll
                         for (int tok = 0; tok < 2; ++tok) {
-                            const int row = row0 + 2 * p + tok, t = t0 + row;
+                            const int row = row0 + 2 * p + tok, behind = t0 + row - w.committed();
                             uint32_t s1 = tok == 0 ? sc & 0xffffu : sc >> 16;
-                            if (ends && t >= w.committed) {
-                                if (t >= w.len) {
+                            if (ends && behind >= 0) {
+                                if (behind >= w.q.nodes) {  // behind the context
                                     s1 = 0;
                                 } else if ((s1 & 0x7fffu) > 0x7154u) {  // above what appends write, infinities and NaN included
-                                    atomicOr(&sm.bad, 1ull << (t - w.committed));
+                                    atomicOr(&sm.bad[n_unit & 7], 1ull << behind);
                                     s1 = 0;
                                 }
                             }
@@ -654,30 +889,31 @@ __device__ __forceinline__ void widen_role(Smem<D, true>& sm, const Work& w, int
                             }
                             if constexpr (W == 2) {
                                 // (lanes of the other half store their pieces the other way round: different banks)
-                                const int first = x >> 2, piece = 2 * (x & 3);
-                                uint8_t* base = (first ? to[H - 1] : to[0]) + row * 128;
-                                *reinterpret_cast<uint4*>(base + (((piece + first) ^ (row & 7)) << 4)) = first ? v[W - 1] : v[0];
-                                *reinterpret_cast<uint4*>(base + (((piece + 1 - first) ^ (row & 7)) << 4)) = first ? v[0] : v[W - 1];
+                                const int other = x >> 2, piece = 2 * (x & 3);
+                                uint8_t* base = to + other * kHalfBytes + row * 128;
+                                *reinterpret_cast<uint4*>(base + (((piece + other) ^ (row & 7)) << 4)) = other ? v[W - 1] : v[0];
+                                *reinterpret_cast<uint4*>(base + (((piece + 1 - other) ^ (row & 7)) << 4)) = other ? v[0] : v[W - 1];
                             } else {
-                                *reinterpret_cast<uint4*>(to[0] + row * 128 + ((x ^ (row & 7)) << 4)) = v[0];
+                                *reinterpret_cast<uint4*>(to + row * 128 + ((x ^ (row & 7)) << 4)) = v[0];
                             }
                         }
                     }
                 }
+                }
+                fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&sm.unit_empty[unit % C::kUnits]);
+                if (lane == 0) {
+                    mbar_arrive(&sm.unit_empty[u]);
+                    mbar_arrive(&sm.full[s]);
+                }
             }
-            if (!ok) break;
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0)
-                for (int hv = 0; hv < H; ++hv) mbar_arrive(&sm.full[(seq + hv) % C::kSlots]);
         }
-    }
+        ++n_unit;
+    } while (w.next(a, sm.part));
 }
 
 template <int D, bool F4>
-__global__ void __launch_bounds__(Cfg<D, F4>::kThreads, 2)
+__global__ void __launch_bounds__(Cfg<D, F4>::kThreads, 1)
 tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const TreeArgs a)
 {
     using C = Cfg<D, F4>;
@@ -689,51 +925,94 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         if (tid == 0) atomicMin(a.kv.status, (int)MOSKA_ERR_CUDA);
         return;
     }
-    const Work w = work_of(a);
-    if (w.rows <= 0) return;
-    if (tid == 0) {
+    if (warp < kLoadWarp) {
+        find_part(a, blockIdx.x, gridDim.x, sm.part);
+    } else if (warp == kLoadWarp && lane == 0) {
         for (int s = 0; s < C::kSlots; ++s) {
-            mbar_init(&sm.full[s], F4 ? 4 : 1);  // 4 bits: one arrival per widening warp
+            mbar_init(&sm.full[s], F4 ? kWidenWarps : 1);
             mbar_init(&sm.empty[s], 1);
         }
-        if constexpr (F4)
-            for (int u = 0; u < C::kUnits; ++u) {
-                mbar_init(&sm.unit_full[u], 1);
-                mbar_init(&sm.unit_empty[u], 4);
-            }
-        mbar_init(&sm.q_full, 128);
-        mbar_init(&sm.s_full, 1);
-        mbar_init(&sm.p_full, 128);
-        mbar_init(&sm.o_full, 1);
-        sm.bad = 0;
+        for (int u = 0; u < C::kUnits; ++u) {
+            mbar_init(&sm.unit_full[u], 1);
+            mbar_init(&sm.unit_empty[u], kWidenWarps);
+        }
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(&sm.q_full[x], kSoftmaxThreads);
+            mbar_init(&sm.s_full[x], 1);
+            mbar_init(&sm.p_full[x], kSoftmaxThreads);
+        }
+        mbar_init(&sm.pv_done, 1);
+        for (int x = 0; x < 8; ++x) sm.bad[x] = 0;
         sm.gave_up = 0;
         fence_mbar_init();
         fence_proxy_async_smem();
-    }
-    if (warp == kMmaWarp) {
-        tmem_alloc(&sm.tmem_base, 256);
+    } else if (warp == kMmaWarp) {
+        tmem_alloc(&sm.tmem_base, 512);
         tmem_relinquish();
     }
+    __syncwarp();
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = sm.tmem_base;
 
-    if (warp < 4) {
-        softmax_role<D, F4>(sm, a, w, tmem, warp, lane);
-    } else if (warp == kLoadWarp) {
-        load_role<D, F4>(sm, tm_k, tm_v, a, w, lane);
-    } else if (warp == kMmaWarp) {
-        if (lane == 0 && w.tiles > 0) mma_role<D, F4>(sm, w, tmem);
-        __syncwarp();
-    } else {
-        if constexpr (F4) widen_role<D>(sm, w, warp - kWidenWarp0, lane);
+    Walk w;
+    if (w.begin(a, sm.part)) {
+        if (warp < kLoadWarp) {
+            Softmax<D, F4>{sm, a, tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16), warp, warp >> 2, (warp & 3) * 32 + lane}.run(w);
+        } else if (warp == kLoadWarp) {
+            load_role<D, F4>(sm, tm_k, tm_v, a, w, lane);
+        } else if (warp == kMmaWarp) {
+            mma_role<D, F4>(sm, a, w, tmem);
+        } else {
+            if constexpr (F4) widen_role<D>(sm, a, w, warp - kWidenWarp0, lane);
+        }
     }
-
+    __syncwarp();
     tc_fence_before_sync();
     __syncthreads();
-    if (warp == kMmaWarp) tmem_dealloc(tmem, 256);
+    if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
     if (tid == 0 && sm.gave_up) atomicMin(a.kv.status, (int)MOSKA_ERR_TIMEOUT);
+}
+
+// Joins the partial rows of a unit that cuts divide: CTA x looks at the cut before part x + 1; the first cut of a unit's has it.
+template <int D>
+__global__ void __launch_bounds__(kSoftmaxThreads) tree_join_kernel(const TreeArgs a, int ctas)
+{
+    __shared__ Part part;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x + 1;
+    find_part(a, cta, ctas, part);
+    __syncthreads();
+    Walk w;
+    wait_for_results();
+    if (!w.begin(a, part) || w.tile0 == 0) return;
+    const int c0 = (int)(w.start / part.per), c1 = (int)((w.start + w.q.tiles - 1) / part.per);
+    if (cta != c0 + 1) return;
+    const int G = a.Hq / a.Hkv, rows = w.rows(a);
+    constexpr int W = D / 32;  // dimensions a lane
+    for (int i = warp; i < rows; i += kSoftmaxThreads / 32) {
+        auto slot = [&](int c) { return (int64_t)(2 * c + (c == c0 ? 1 : 0)) * kTileRows + i; };
+        float top = -INFINITY;
+        for (int c = c0 + lane; c <= c1; c += 32) top = max_or_nan(top, a.lse_cut[slot(c)]);
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) top = max_or_nan(top, __shfl_xor_sync(0xffffffffu, top, off));
+        const float base = top == -INFINITY ? 0.f : top;  // (all parts empty: every weight is 0)
+        float total = 0.f, acc[W] = {};
+#pragma unroll 4
+        for (int c = c0; c <= c1; ++c) {
+            const float* o = a.o_cut + slot(c) * D + W * lane;
+            const float weight = __expf(a.lse_cut[slot(c)] - base);
+            total += weight;
+#pragma unroll
+            for (int e = 0; e < W; ++e) acc[e] = fmaf(weight, o[e], acc[e]);
+        }
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+        const int64_t row = (int64_t)(w.q.first + w.node0(a) + i / G) * a.Hq + w.h * G + i % G;
+#pragma unroll
+        for (int e = 0; e < W; e += 2)
+            *reinterpret_cast<uint32_t*>(a.out + row * D + W * lane + e) = bf16x2(acc[e] * inv, acc[e + 1] * inv);
+        if (lane == 0 && a.lse_out != nullptr) a.lse_out[row] = top == -INFINITY ? -INFINITY : top + logf(total);
+    }
 }
 
 // ---- host side ------------------------------------------------------------------------------------
@@ -778,36 +1057,45 @@ int make_page_map(CUtensorMap* tm, const void* pool, const PagedView& kv, int Hk
 
 }  // namespace
 
-int default_tree_splits(bool, int n_requests, int nodes, int G, int Hkv, int, int max_len)
+int default_tree_splits(int n_requests, int nodes, int G, int Hkv, int max_len)
 {
-    // as many CTAs as there are places, two tiles at least
-    const long long row_tiles = (nodes + kTileRows / G - 1) / (kTileRows / G);
-    long long s = 296 / (n_requests * Hkv * row_tiles);
-    const long long cap = ((long long)max_len + 2 * kTile - 1) / (2 * kTile);
-    if (s > cap) s = cap;
+    // slots for the parts that equal contexts are cut into: the CTAs that share a unit's tiles, and one more
+    const long long row_tiles = (nodes + kTileRows / G - 1) / (kTileRows / G), units = (long long)n_requests * Hkv * row_tiles;
+    const long long tiles = ((long long)max_len + kTile - 1) / kTile;
+    long long s = (kMaxCtas + units - 1) / units + 1;
+    if (s > tiles) s = tiles;
     return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
 }
 
+size_t tree_cut_bytes(int D) { return (size_t)kMaxCtas * 2 * kTileRows * (D + 1) * sizeof(float); }
+
 int launch_tree_attn(const uint16_t* q, const PagedView& kv, bool fp4, const TreeRows& tree, float* o_part, float* lse_part,
-                     int slot0, int n_slots, uint16_t* out, float* lse_out, float scale, const moska_shape* s,
+                     int slot0, int n_slots, uint16_t* out, float* lse_out, void* ws, float scale, const moska_shape* s,
                      cudaStream_t st)
 {
     if (tree.n_rows == 0) return MOSKA_OK;
     const int G = s->Hq / s->Hkv, per_tile = kTileRows / G, row_tiles = (tree.max_nodes + per_tile - 1) / per_tile;
-    const long long grid = (long long)tree.n_requests * s->Hkv * s->n_unique_splits * row_tiles;
-    if (grid > 0x7fffffffLL) return fail(MOSKA_ERR_UNSUPPORTED, "tree attention grid too large");
     if (((long long)kv.n_pages << kv.page_shift) > 0x7fffffffLL)
         return fail(MOSKA_ERR_UNSUPPORTED, "a pool of more than 2^31 tokens");
-    const TreeArgs a{q, kv, tree, o_part, lse_part, out, lse_out, scale, s->Hq, s->Hkv, s->n_unique_splits, slot0, n_slots,
-                     row_tiles, per_tile};
+    TreeArgs a{q, kv, tree, o_part, lse_part, out, lse_out, nullptr, nullptr, scale, s->Hq, s->Hkv, s->n_unique_splits, slot0,
+               n_slots, row_tiles, per_tile};
+    if (ws != nullptr) {
+        a.o_cut = static_cast<float*>(ws);
+        a.lse_cut = a.o_cut + (size_t)kMaxCtas * 2 * kTileRows * s->D;
+    }
     CUtensorMap tm_k{}, tm_v{};
     if (!fp4) {
         MOSKA_TRY_STATUS(make_page_map(&tm_k, kv.k, kv, s->Hkv, s->D));
         MOSKA_TRY_STATUS(make_page_map(&tm_v, kv.v, kv, s->Hkv, s->D));
     }
+    int dev = 0, n_sms = 0;
+    MOSKA_CUDA_TRY(cudaGetDevice(&dev));
+    MOSKA_CUDA_TRY(cudaDeviceGetAttribute(&n_sms, cudaDevAttrMultiProcessorCount, dev));
+    // a multiple of the row tiles: trees of one size are cut alike in each
+    const int ctas = (n_sms < kMaxCtas ? n_sms : kMaxCtas) / row_tiles * row_tiles;
     auto go = [&](auto kernel, int threads, int smem) {
         MOSKA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-        kernel<<<(unsigned)grid, threads, smem, st>>>(tm_k, tm_v, a);
+        kernel<<<(unsigned)ctas, threads, smem, st>>>(tm_k, tm_v, a);
         MOSKA_LAUNCH_CHECK("tree_attn_kernel");
         return (int)MOSKA_OK;
     };
@@ -818,8 +1106,20 @@ int launch_tree_attn(const uint16_t* q, const PagedView& kv, bool fp4, const Tre
     };
     const std::integral_constant<int, 128> d128;
     const std::integral_constant<int, 64> d64;
-    if (s->D == 128) return fp4 ? form(d128, std::true_type{}) : form(d128, std::false_type{});
-    return fp4 ? form(d64, std::true_type{}) : form(d64, std::false_type{});
+    if (s->D == 128) MOSKA_TRY_STATUS(fp4 ? form(d128, std::true_type{}) : form(d128, std::false_type{}));
+    else MOSKA_TRY_STATUS(fp4 ? form(d64, std::true_type{}) : form(d64, std::false_type{}));
+    if (out == nullptr || s->n_unique_splits == 1 || ctas < 2) return MOSKA_OK;
+    cudaLaunchConfig_t config{};
+    config.gridDim = dim3((unsigned)(ctas - 1));
+    config.blockDim = dim3(kSoftmaxThreads);
+    config.stream = st;
+    cudaLaunchAttribute early{};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    config.attrs = &early;
+    config.numAttrs = 1;
+    MOSKA_CUDA_TRY(cudaLaunchKernelEx(&config, s->D == 128 ? tree_join_kernel<128> : tree_join_kernel<64>, a, ctas));
+    return MOSKA_OK;
 }
 
 }  // namespace moska

@@ -20,8 +20,7 @@ class MoskaLayer:
         self.device = torch.device(device)
         self.dense = dense
         if n_unique_splits is None and paged_fmt is not None and q_len * (Hq // Hkv) > 16:  # trees alone
-            n_unique_splits = M.default_tree_splits({"bf16": M.KV_BF16, "fp4": M.KV_FP4}[paged_fmt], B // q_len, q_len, Hq, Hkv,
-                                                    D, max(1, max_unique_len))
+            n_unique_splits = M.default_tree_splits(B // q_len, q_len, Hq, Hkv, max(1, max_unique_len))
         elif n_unique_splits is None and paged_fmt is not None:
             n_unique_splits = M.default_paged_splits({"bf16": M.KV_BF16, "fp4": M.KV_FP4}[paged_fmt],
                                                      B // max(1, q_len), Hkv, D, max(1, max_unique_len))

@@ -29,12 +29,14 @@ class TreeAttention:
 
     def __init__(self, B, Hq, Hkv, D, max_len, n_requests, max_nodes, fmt="bf16", n_unique_splits=None, device="cuda"):
         """B counts batch rows (nodes of n_requests trees of at most max_nodes, and padding rows behind them);
-        max_len: longest context, the nodes included."""
+        max_len: longest context, the nodes included.  n_unique_splits: parts that a context may be cut into."""
+        if fmt not in FORMATS:
+            raise ValueError(f"fmt = {fmt!r} is not one of {sorted(FORMATS)}")
         if not 1 <= max_nodes <= MAX_NODES:
             raise ValueError(f"max_nodes = {max_nodes}, 1..{MAX_NODES} are possible")
         self.fmt, self.n_requests, self.max_nodes = fmt, n_requests, max_nodes
         if n_unique_splits is None:
-            n_unique_splits = M.default_tree_splits(FORMATS[fmt], n_requests, max_nodes, Hq, Hkv, D, max(1, max_len))
+            n_unique_splits = 64 if max_len > 128 else 1  # (a cut is a multiple of 128 tokens)
         self.shape = M.shape(B, Hq, Hkv, D, 1, 128, 1, n_unique_splits=n_unique_splits, q_len=max_nodes)
         self.scale = 1.0 / math.sqrt(D)
         self.out = torch.empty(B, Hq, D, dtype=torch.bfloat16, device=device)

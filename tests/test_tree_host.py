@@ -116,12 +116,11 @@ def test_sizes_and_splits(M):
     assert M.tree_attn_workspace_bytes(s) >= 35 * 8 * 3 * 129 * 4
     s.n_unique_splits = 1
     assert M.tree_attn_workspace_bytes(s) == 0
-    for fmt in (0, 1):
-        assert M.default_tree_splits(fmt, 1, 8, 32, 8, 128, 100000) > 1
-        assert M.default_tree_splits(fmt, 1, 8, 32, 8, 128, 8) == 1
-        assert M.default_tree_splits(fmt, 1000, 64, 64, 8, 128, 32768) >= 1
-        assert M.default_tree_splits(fmt, 0, 8, 32, 8, 128, 8) == 1
-        assert M.default_tree_splits(fmt, 1, 64, 32, 8, 64, 1 << 30) <= 64
+    assert M.default_tree_splits(1, 8, 32, 8, 100000) > 1
+    assert M.default_tree_splits(1, 8, 32, 8, 8) == 1
+    assert M.default_tree_splits(1000, 64, 64, 8, 32768) >= 1
+    assert M.default_tree_splits(0, 8, 32, 8, 8) == M.default_tree_splits(1, 8, 72, 8, 8) == 1
+    assert M.default_tree_splits(1, 64, 4, 1, 1 << 30) <= 64
 
 
 def test_python_checks(M):
