@@ -2,19 +2,23 @@
 //
 // The T G query rows of a request's KV head (T nodes, G heads each) share one context.  Work comes in units: up to 128 of
 // these rows (whole nodes) and the context in tiles of 128 tokens:
-//   S = Q K^T          tcgen05.mma, Q in tensor memory, K in shared memory: 128 x 128 scores in tensor memory
-//   P = exp2(S - m)    two threads per row: TMEM -> registers -> 16 bits, back over the columns of S
+//   S = Q K^T          tcgen05.mma, Q in tensor memory, K in shared memory: 128 x 64 scores (half a tile) in tensor memory
+//   P = exp2(S - m)    a thread per row: TMEM -> registers -> 16 bits, back over the columns of S
 //   O += P V           tcgen05.mma, P from TMEM, V from shared memory
-// Scores have two buffers, so that the next tile's product runs under this tile's softmax; Q has two, so that the next
-// unit's first product runs under this unit's end.  TMEM: O, S, S, Q, Q = 512 columns.
+// Two groups of softmax warps take turns at the halves: while one group's exponentials keep the special function units busy
+// (512 cycles a half), the other reads its scores and finds its maximum.  Scores have four buffers, so that products run ahead.  A third
+// group stages the next unit's queries and writes the last unit's rows.  TMEM: O 128, S 4 x 64, Q 2 x 64 = 512 columns.
 //
-// One CTA per SM.  All tiles of all units, row tiles slowest, then requests, then heads, form one line that is cut into equal
-// parts, one per CTA, whatever the lengths: a CTA walks the units in its part.  A unit that a cut divides leaves partial
-// rows, which a second kernel joins.  (Row tiles slowest: with trees of one size the CTAs of the row tiles walk the same
-// contexts at the same time, and all but the first find them in L2.)
+// One CTA per SM.  For each row tile (first 128 rows of every request, second 128, ..) the tiles of all its units, request after
+// request and head after head, form a line.  Lines get CTAs by their lengths and are cut into equal parts, one per CTA,
+// whatever the contexts' lengths: a CTA walks the units in its part.  A unit that a cut divides leaves partial rows, which a
+// second kernel joins.  (With trees of one size the lines are alike and their CTAs walk the same contexts at the same time, so
+// that all but the first find them in L2; cut as one line, each fetched them from memory: 24 requests of 60 nodes
+// read 3.45 GB instead of 0.9.)
 //
-// Warps 0-7: softmax (thread i and i + 128: row i % 128 = TMEM lane, columns 0-63 and 64-127).  Warp 8: copies.  Warp 9: MMAs.
-// 4-bit pages: warps 10-13 widen.  Operands lie in a ring of slots, a K or a V tile each, as halves of 64 dimensions in rows of
+// Warps 0-3 and 4-7: softmax of the first and second halves of tiles (thread i: row i % 128 = TMEM lane).  Warps 8-11: queries and results.
+// Warp 12: copies.  Warps 13 and 14: MMAs of Q K^T and of P V (one warp for both left the tensor cores idle while it
+// waited: 2800 cycles a tile, XXXX).  4-bit pages: warps 15-18 widen.  Operands lie in a ring of slots, a K or a V tile each, as halves of 64 dimensions in rows of
 // 128 bytes with the 128-byte swizzle.
 //   bf16: one TMA box of min(page_size, 128) tokens a page and half.
 //   4 bits: bulk copies of the key parts or the value parts (codes, then scales) of the tile's 16-token blocks into a ring of
@@ -30,6 +34,7 @@
 
 #include <cfloat>
 #include <mutex>
+#include <type_traits>
 
 #include "sm100.cuh"
 #include "tree.cuh"
@@ -39,10 +44,11 @@ namespace {
 using namespace sm100;
 
 constexpr int kTile = 128;      // tokens of a tile
+constexpr int kStep = 64;       // tokens whose scores are computed at once
 constexpr int kTileRows = 128;  // query rows of a unit
 constexpr int kHalfBytes = kTile * 64 * 2;
 constexpr int kSoftmaxThreads = 256;
-constexpr int kLoadWarp = 8, kMmaWarp = 9, kWidenWarp0 = 10, kWidenWarps = 4;
+constexpr int kRowWarp0 = 8, kLoadWarp = 12, kScoreWarp = 13, kValueWarp = 14, kWidenWarp0 = 15, kWidenWarps = 4;
 constexpr int kMaxRowTiles = 4;  // 64 nodes of up to 8 heads
 constexpr int kMaxCtas = 148;    // parts of the line of tiles
 constexpr uint32_t kColO = 0, kColS = 128, kColQ = 384;  // tensor-memory columns
@@ -52,7 +58,7 @@ constexpr float kRescaleAt = 8.f;  // log2 units that a row's maximum may grow b
 template <int D, bool F4>
 struct Cfg {
     static constexpr int kHalves = D / 64;
-    static constexpr int kThreads = F4 ? 448 : 320;
+    static constexpr int kThreads = F4 ? 608 : 480;
     static constexpr int kSlotBytes = kHalves * kHalfBytes;
     static constexpr int kSlots = F4 ? (D == 128 ? 4 : 8) : (D == 128 ? 6 : 12);
     static constexpr int kBlocks = kTile / kBlockTokens;  // 16-token blocks of a unit of codes
@@ -61,13 +67,19 @@ struct Cfg {
     static constexpr int kUnits = F4 ? (D == 128 ? 8 : 16) : 1;
 };
 
-// A CTA's part of the line of tiles.
+// A CTA's part of the line of its row tile.
 struct Part {
     long long p0, p1, per;  // tiles p0 .. p1 - 1; `per` in a full part
     long long start;        // first tile of the unit that p0 is in: (row tile, request, head)
     int rt, r, h;
+    int cta0, ctas;         // CTAs of the line
     int longest[kSoftmaxThreads / 32];
     long long tiles[kMaxRowTiles][kSoftmaxThreads / 32];  // of each warp's requests
+};
+
+// What the softmax needs of a unit.
+struct UnitInfo {
+    int committed, len, tile0, tiles, rows, more;
 };
 
 template <int D, bool F4>
@@ -75,12 +87,15 @@ struct Smem {
     using C = Cfg<D, F4>;
     uint8_t slot[C::kSlots][C::kSlotBytes];
     uint8_t unit[F4 ? C::kUnits * C::kUnitBytes : 16];
-    float top[2][2][kTileRows];  // row maxima of the two column halves; alternate tiles
-    float sum[2][kTileRows];     // row sums of the halves at a unit's end; 4 bits: largest query elements at its start
+    float ref[2][kTileRows];         // the reference of a row's probabilities after a half of each softmax group
+    float2 stat[2][2][kTileRows];    // (reference, sum) of a unit's rows by each group; units take turns
+    UnitInfo info[2];                // units take turns
+    unsigned long long sees[2][kTileRows];
+    float row_unit[2][kTileRows];
     TreeSmem tree;
     uint64_t full[C::kSlots], empty[C::kSlots];
     uint64_t unit_full[C::kUnits], unit_empty[C::kUnits];
-    uint64_t q_full[2], s_full[2], p_full[2], pv_done;
+    uint64_t q_full[2], s_full[4], p_full[4], stat_full[2], ref_full[2][4], pv_done[4], o_full, o_free;
     unsigned long long bad[8];  // tree tokens with values that are not finite; units take turns
     Part part;
     uint32_t tmem_base;
@@ -194,6 +209,22 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int* g
 }
 
 __device__ __forceinline__ void softmax_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+// Of the third group; true if all of its threads say so.  (No thread leaves on its own: the others would wait for it.)
+__device__ __forceinline__ bool row_barrier(bool ok = true)
+{
+    uint32_t all;
+    asm volatile(
+        "{\n"
+        ".reg .pred p, q;\n"
+        "setp.ne.u32 p, %1, 0;\n"
+        "barrier.cta.red.and.pred q, 2, 128, p;\n"
+        "selp.u32 %0, 1, 0, q;\n"
+        "}\n"
+        : "=r"(all)
+        : "r"(ok ? 1u : 0u)
+        : "memory");
+    return all != 0;
+}
 
 // True in one lane of the calling warp (converged).  With it, and loops that the whole warp runs, descriptors stay in
 // uniform registers: under `lane == 0` an MMA took about 90 cycles to issue.
@@ -260,43 +291,61 @@ __device__ __forceinline__ void find_part(const TreeArgs& a, int cta, int ctas, 
     longest = __reduce_max_sync(0xffffffffu, longest);
     if (lane == 0) part.longest[warp] = longest;
     softmax_barrier();
-    long long total = 0;
-    for (int k = 0; k < a.row_tiles; ++k)
-        for (int x = 0; x < kWarps; ++x) total += part.tiles[k][x];
+    long long line[kMaxRowTiles] = {}, total = 0;
+#pragma unroll
+    for (int k = 0; k < kMaxRowTiles; ++k) {
+        if (k >= a.row_tiles) continue;
+        for (int x = 0; x < kWarps; ++x) line[k] += part.tiles[k][x];
+        total += line[k];
+    }
     for (int x = 0; x < kWarps; ++x) longest = max(longest, part.longest[x]);
-    total *= a.Hkv;
+    // CTAs of the lines: by their lengths, one at least; the first line, the longest, gets what is over
+    int rt = 0, cta0 = 0, n = ctas;
+    long long mine_all = line[0];
+#pragma unroll
+    for (int k = kMaxRowTiles - 1; k > 0; --k) {
+        if (line[k] == 0 || rt != 0) continue;
+        const int c = max(1, (int)(ctas * line[k] / total));
+        n -= c;
+        if (cta >= n) {
+            rt = k;
+            cta0 = n;
+            n = c;
+            mine_all = line[k];
+        }
+    }
+    const long long tiles = mine_all * a.Hkv;
     // equal parts; no unit in more of them than there may be
-    long long per = (total + ctas - 1) / ctas;
+    long long per = (tiles + n - 1) / n;
     if (a.n_splits > 1) per = max(per, (long long)(longest + a.n_splits - 2) / (a.n_splits - 1));
     per = max(1ll, per);
-    const long long p0 = cta * per, p1 = min(total, p0 + per);
+    const long long p0 = (cta - cta0) * per, p1 = min(tiles, p0 + per);
     if (i == 0) {
         part.p0 = p0;
         part.p1 = p1;
         part.per = per;
+        part.rt = rt;
+        part.cta0 = cta0;
+        part.ctas = n;
     }
-    long long before = 0;  // tiles of the row tiles before k
+    long long at = 0;
 #pragma unroll
     for (int k = 0; k < kMaxRowTiles; ++k) {
-        if (k >= a.row_tiles) continue;
-        long long ahead = 0;
-        for (int x = 0; x < warp; ++x) ahead += part.tiles[k][x];
-        long long at = before + (ahead + upto[k] - mine[k]) * a.Hkv;
-        if (p0 < p1 && p0 >= at && p0 < at + mine[k] * a.Hkv) {  // one thread: the part begins in its stretch
-            for (int r = r0; r < r1; ++r) {
-                const Request q = request_of(a, r);
-                if (q.row_tiles <= k) continue;
-                if (p0 < at + (long long)q.tiles * a.Hkv) {
-                    part.rt = k;
-                    part.r = r;
-                    part.h = (int)((p0 - at) / q.tiles);
-                    part.start = at + (long long)part.h * q.tiles;
-                    break;
-                }
-                at += (long long)q.tiles * a.Hkv;
+        if (k != rt) continue;
+        for (int x = 0; x < warp; ++x) at += part.tiles[k][x];
+        at = (at + upto[k] - mine[k]) * a.Hkv;
+        if (p0 >= p1 || p0 < at || p0 >= at + mine[k] * a.Hkv) continue;
+        for (int r = r0; r < r1; ++r) {  // one thread: the part begins in its stretch
+            const Request q = request_of(a, r);
+            if (q.row_tiles <= k) continue;
+            if (p0 < at + (long long)q.tiles * a.Hkv) {
+                part.r = r;
+                part.h = (int)((p0 - at) / q.tiles);
+                part.start = at + (long long)part.h * q.tiles;
+                break;
             }
+            at += (long long)q.tiles * a.Hkv;
         }
-        for (int x = 0; x < kWarps; ++x) before += part.tiles[k][x] * a.Hkv;
     }
 }
 
@@ -328,10 +377,7 @@ struct Walk {
         if (++h == a.Hkv) {
             h = 0;
             do {
-                if (++r == a.tree.n_requests) {
-                    r = 0;
-                    if (++rt == a.row_tiles) return false;
-                }
+                if (++r == a.tree.n_requests) return false;
                 q = request_of(a, r);
             } while (q.row_tiles <= rt);
         }
@@ -352,12 +398,12 @@ struct Walk {
     }
 };
 
-// Columns 32 c .. 32 c + 31 of a tile that begins at token t0: those that a row sees.
-__device__ __forceinline__ uint32_t seen_columns(int t, int committed, int len, unsigned long long sees)
+// Tokens t .. t + 31: bits of those that a row sees.
+__device__ __forceinline__ uint32_t seen_tokens(int t, int committed, int len, unsigned long long sees)
 {
     if (t + 32 <= committed) return 0xffffffffu;
     uint32_t bits;
-    const int behind = t - committed;  // first column's place behind the committed tokens
+    const int behind = t - committed;  // the first one's place behind the committed tokens
     if (behind >= 0) {
         bits = behind < 64 ? (uint32_t)(sees >> behind) : 0u;
     } else {
@@ -367,205 +413,232 @@ __device__ __forceinline__ uint32_t seen_columns(int t, int committed, int len, 
 }
 
 // ---- softmax ----------------------------------------------------------------------------------------
+// Values of half a tile behind the context, and those of drafted tokens that are not finite, become 0 (bf16): two threads per
+// token row.
+template <int D>
+__device__ __forceinline__ bool clean_values(Smem<D, false>& sm, const UnitInfo& u, int t0, uint32_t g, int group, uint32_t n_unit, int i)
+{
+    using C = Cfg<D, false>;
+    const uint32_t seq = 2 * g + 1;
+    if (!warp_wait(&sm.full[seq % C::kSlots], (seq / C::kSlots) & 1, &sm.gave_up)) return false;
+    const int token = i & (kStep - 1), t = t0 + token, behind = t - u.committed;
+    if (behind >= 0) {
+        // 16-byte pieces: of a half of the dimensions (D = 128), every second one (D = 64)
+        uint8_t* at = sm.slot[seq % C::kSlots] + (C::kHalves == 2 ? (i >> 6) * kHalfBytes : 0) + (group * kStep + token) * 128;
+#pragma unroll 1
+        for (int x = C::kHalves == 2 ? 0 : i >> 6; x < 8; x += C::kHalves == 2 ? 1 : 2) {
+            uint4* p = reinterpret_cast<uint4*>(at + (((x + i) & 7) << 4));
+            const uint4 v = t < u.len ? *p : make_uint4(0, 0, 0, 0);
+            uint32_t word[4] = {v.x, v.y, v.z, v.w};
+            bool odd = false;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if ((word[e] & 0x7f80u) == 0x7f80u) { word[e] &= 0xffff0000u; odd = true; }
+                if ((word[e] & 0x7f800000u) == 0x7f800000u) { word[e] &= 0xffffu; odd = true; }
+            }
+            if (odd) atomicOr(&sm.bad[n_unit & 7], 1ull << behind);
+            if (odd || t >= u.len) *p = make_uint4(word[0], word[1], word[2], word[3]);
+        }
+    }
+    fence_proxy_async_smem();
+    return true;
+}
+
+// Scores of one half of every tile -> probabilities.  A row's reference m passes from group to group; it moves when a
+// half's maximum passes it by 2^8, and whoever moves it rescales O.  Each group keeps its own sum, relative to the reference
+// that it saw last.
 template <int D, bool F4>
-struct Softmax {
-    using C = Cfg<D, F4>;
+__device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int group, int warp, int i)
+{
+    int* gave_up = &sm.gave_up;
+    uint32_t g = 0;
+    for (uint32_t n_unit = 0;; ++n_unit) {
+        if (!warp_wait(&sm.q_full[n_unit & 1], (n_unit >> 1) & 1, gave_up)) return;
+        const UnitInfo u = sm.info[n_unit & 1];
+        const unsigned long long sees = sm.sees[n_unit & 1][i];
+        const float unit = sm.row_unit[n_unit & 1][i];  // log2 units of one score
+        const bool live = i < u.rows, warp_live = (warp & 3) * 32 < u.rows;
+        float m = -INFINITY, l = 0.f;
+        for (int j = 0; j < u.tiles; ++j, ++g) {
+            const uint32_t step = 2 * g + group;
+            const int t0 = (u.tile0 + j) * kTile + kStep * group;
+            const bool ends = t0 + kStep > u.committed;  // some row does not see all of the half
+            if constexpr (!F4)
+                if (ends && !clean_values<D>(sm, u, t0, g, group, n_unit, i)) return;
+            if (!warp_wait(&sm.s_full[step & 3], (step >> 2) & 1, gave_up)) return;
+            tc_fence_after_sync();
+            const uint32_t t_s = tmem + kColS + (step & 3) * kStep;
+            uint32_t s[2][32];
+            float mx = -INFINITY;
+            if (warp_live) {
+                tmem_ld32(t_s, s[0]);
+                tmem_ld32(t_s + 32, s[1]);
+                tmem_ld_wait();
+                if (ends)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const uint32_t see = sees == 0 ? 0u : seen_tokens(t0 + 32 * c, u.committed, u.len, sees);
+#pragma unroll
+                        for (int x = 0; x < 32; ++x)
+                            if (!((see >> x) & 1)) s[c][x] = 0xff800000u;
+                    }
+                float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int x = 0; x < 16; ++x)
+                        m4[x & 3] = fmax3(m4[x & 3], __uint_as_float(s[c][2 * x]), __uint_as_float(s[c][2 * x + 1]));
+                mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+            }
+            // the reference: the other group's, of the half before
+            if (step > 0 && !warp_wait(&sm.ref_full[group ^ 1][warp & 3], ((step - 1) >> 1) & 1, gave_up)) return;
+            const bool first = j == 0 && group == 0;
+            const float before = first ? mx : sm.ref[group ^ 1][i];
+            const bool need = !first && live && (mx - before) * unit > kRescaleAt;
+            const float now = need ? mx : before;
+            sm.ref[group][i] = now;
+            mbar_arrive(&sm.ref_full[group][warp & 3]);
+            if (warp_live) {
+                if (__any_sync(0xffffffffu, need)) {
+                    // the last product has left O (its barrier's turn before, step - 5, is over: these scores came behind it)
+                    if (!warp_wait(&sm.pv_done[(step - 1) & 3], ((step - 1) >> 2) & 1, gave_up)) return;
+                    tc_fence_after_sync();
+                    const float alpha = need ? fast_exp2((before - now) * unit) : 1.f;
+#pragma unroll 1
+                    for (int c = 0; c < D / 16; ++c) {
+                        uint32_t o[16];
+                        tmem_ld16(tmem + kColO + 16 * c, o);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * alpha);
+                        tmem_st16(tmem + kColO + 16 * c, o);
+                    }
+                }
+                if (now != m) l *= fast_exp2((m - now) * unit);
+                m = now;
+                const float base = m == -INFINITY ? 0.f : m * unit;  // (nothing seen yet)
+                const float2 unit2 = make_float2(unit, unit), base2 = make_float2(-base, -base);
+                float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        float2 p = ffma2(make_float2(__uint_as_float(s[c][2 * x]), __uint_as_float(s[c][2 * x + 1])), unit2, base2);
+                        p.x = fast_exp2(p.x);
+                        p.y = fast_exp2(p.y);
+                        l2[x & 1] = fadd2(l2[x & 1], p);
+                        pk[x] = F4 ? f16x2(p.x, p.y) : bf16x2(p.x, p.y);
+                    }
+                    tmem_st16(t_s + 16 * c, pk);
+                }
+                l += (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
+                tmem_st_wait();
+            }
+            tc_fence_before_sync();
+            mbar_arrive(&sm.p_full[step & 3]);
+        }
+        sm.stat[n_unit & 1][group][i] = make_float2(m, l);
+        mbar_arrive(&sm.stat_full[n_unit & 1]);
+        if (!u.more) return;
+    }
+}
+
+// ---- queries and results ----------------------------------------------------------------------------
+template <int D, bool F4>
+struct Rows {
     Smem<D, F4>& sm;
     const TreeArgs& a;
     const uint32_t tmem;  // with this warp's lanes
-    const int warp, half, i;
+    const int i;          // row
 
-    // the two threads of the rows of a warp
-    __device__ __forceinline__ void row_barrier() const { asm volatile("bar.sync %0, 64;" ::"r"(2 + (warp & 3)) : "memory"); }
-
-    // The row of the next unit: what it sees, and its query into tensor memory.  In 4-bit pages queries are f16 times a
-    // power of two that brings the row's largest element into [1, 2) (exact down to 2^-17 of it, within 2^-25 of it below);
-    // `unit`: log2 units of one score.
-    __device__ __forceinline__ void prepare(const Walk& w, bool new_request, uint32_t n_unit, unsigned long long& sees, float& unit)
+    // A unit's rows: what they see, and their queries into tensor memory.  In 4-bit pages queries are f16 times a
+    // power of two that brings the row's largest element into [1, 2) (exact down to 2^-17 of it, within 2^-25 of it below).
+    __device__ __forceinline__ void prepare(const Walk& w, bool new_request, bool more, uint32_t n_unit)
     {
-        softmax_barrier();  // all have left the unit before the last: its `bad`, and the ancestors, may go
-        if (threadIdx.x == 0) sm.bad[(n_unit - 2) & 7] = 0;
         if (new_request) {
-            if (threadIdx.x < MOSKA_TREE_MAX_NODES) {
-                const int x = threadIdx.x;
-                tree_ancestors(sm.tree, x, x < w.q.nodes ? tree_parent(a.tree, w.q.first, x, a.kv.status) : -1,
-                               [] { asm volatile("bar.sync 7, 64;" ::: "memory"); });
-            }
-            softmax_barrier();
+            row_barrier();
+            if (i < MOSKA_TREE_MAX_NODES)
+                tree_ancestors(sm.tree, i, i < w.q.nodes ? tree_parent(a.tree, w.q.first, i, a.kv.status) : -1,
+                               [] { asm volatile("bar.sync 3, 64;" ::: "memory"); });
+            row_barrier();
         }
-        const int G = a.Hq / a.Hkv, node = w.node0(a) + i / G, committed = w.committed();
-        const bool live = i < w.rows(a);
-        sees = live && committed + node >= 0 ? sm.tree.bits[node] : 0;
+        const int G = a.Hq / a.Hkv, node = w.node0(a) + i / G, committed = w.committed(), rows = w.rows(a);
+        const bool live = i < rows;
+        unsigned long long sees = live && committed + node >= 0 ? sm.tree.bits[node] : 0;
         if (committed < 0) sees &= ~0ull << min(63, -committed);  // nodes without a token
-        constexpr int kWords = D / 4;  // of half a row
-        uint32_t x[kWords];
-        const uint4* from = reinterpret_cast<const uint4*>(a.q + ((int64_t)(w.q.first + node) * a.Hq + w.h * G + i % G) * D) +
-                            half * (kWords / 4);
+        sm.sees[n_unit & 1][i] = sees;
+        if (i == 0) sm.info[n_unit & 1] = UnitInfo{committed, w.q.len, w.tile0, w.tiles, rows, more};
+        float unit = a.scale * kLog2e;
+        const uint4* from = reinterpret_cast<const uint4*>(a.q + ((int64_t)(w.q.first + node) * a.Hq + w.h * G + i % G) * D);
+        auto load = [&](int c, uint32_t (&x)[32]) {  // dimensions 64 c .. 64 c + 63
 #pragma unroll
-        for (int e = 0; e < kWords / 4; ++e) {
-            const uint4 v = live ? __ldg(from + e) : make_uint4(0, 0, 0, 0);
-            x[4 * e] = v.x;
-            x[4 * e + 1] = v.y;
-            x[4 * e + 2] = v.z;
-            x[4 * e + 3] = v.w;
-        }
+            for (int e = 0; e < 8; ++e) {
+                const uint4 v = live ? __ldg(from + 8 * c + e) : make_uint4(0, 0, 0, 0);
+                x[4 * e] = v.x;
+                x[4 * e + 1] = v.y;
+                x[4 * e + 2] = v.z;
+                x[4 * e + 3] = v.w;
+            }
+        };
+        float down = 1.f;
         if constexpr (F4) {
             float top = 0.f;
+#pragma unroll 1
+            for (int c = 0; c < D / 64; ++c) {
+                uint32_t x[32];
+                load(c, x);
 #pragma unroll
-            for (int e = 0; e < kWords; ++e)
-                top = fmax3(top, fabsf(__uint_as_float(x[e] << 16)), fabsf(__uint_as_float(x[e] & 0xffff0000u)));
-            sm.top[0][half][i] = top;  // (free: between two units)
-            row_barrier();
-            top = fmaxf(top, sm.top[0][half ^ 1][i]);
-            row_barrier();
+                for (int e = 0; e < 32; ++e)
+                    top = fmax3(top, fabsf(__uint_as_float(x[e] << 16)), fabsf(__uint_as_float(x[e] & 0xffff0000u)));
+            }
             const int e2 = min(max((int)(__float_as_uint(top) >> 23), 2), 252) - 127;
-            const float down = __uint_as_float((uint32_t)(127 - e2) << 23), up = __uint_as_float((uint32_t)(127 + e2) << 23);
+            down = __uint_as_float((uint32_t)(127 - e2) << 23);
+            const float up = __uint_as_float((uint32_t)(127 + e2) << 23);
             // (neither 0 nor infinite: the -inf of a hidden token, or a score of 0, times that would be NaN)
             unit = fminf(fmaxf(a.scale * up * kLog2e, FLT_MIN), FLT_MAX);
-#pragma unroll
-            for (int e = 0; e < kWords; ++e)
-                x[e] = f16x2(__uint_as_float(x[e] << 16) * down, __uint_as_float(x[e] & 0xffff0000u) * down);
-        } else {
-            unit = a.scale * kLog2e;
         }
-        const uint32_t to = tmem + kColQ + (n_unit & 1) * 64 + half * kWords;
-        if constexpr (kWords == 32) tmem_st32(to, x);
-        else tmem_st16(to, x);
+        sm.row_unit[n_unit & 1][i] = unit;
+#pragma unroll 1
+        for (int c = 0; c < D / 64; ++c) {
+            uint32_t x[32];
+            load(c, x);
+            if constexpr (F4)
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    x[e] = f16x2(__uint_as_float(x[e] << 16) * down, __uint_as_float(x[e] & 0xffff0000u) * down);
+            tmem_st32(tmem + kColQ + (n_unit & 1) * 64 + 32 * c, x);
+        }
         tmem_st_wait();
         tc_fence_before_sync();
         mbar_arrive(&sm.q_full[n_unit & 1]);
     }
 
-    // Values of tile g behind the context, and those of drafted tokens that are not finite, become 0 (bf16): token row i, this
-    // thread's half of it.
-    __device__ __forceinline__ bool clean_values(const Walk& w, int t0, uint32_t g, uint32_t n_unit)
-    {
-        const uint32_t seq = 2 * g + 1;
-        if (!warp_wait(&sm.full[seq % C::kSlots], (seq / C::kSlots) & 1, &sm.gave_up)) return false;
-        const int t = t0 + i, behind = t - w.committed();
-        if (behind >= 0) {
-            constexpr int kPieces = C::kHalves * 4;  // 16-byte pieces of half a row
-            uint8_t* at = sm.slot[seq % C::kSlots] + (C::kHalves == 2 ? half * kHalfBytes : 0) + i * 128;
-            const int first = C::kHalves == 2 ? 0 : 4 * half;
-#pragma unroll 1
-            for (int x = 0; x < kPieces; ++x) {
-                uint4* p = reinterpret_cast<uint4*>(at + (((first + x + i) & 7) << 4));
-                const uint4 v = t < w.q.len ? *p : make_uint4(0, 0, 0, 0);
-                uint32_t word[4] = {v.x, v.y, v.z, v.w};
-                bool odd = false;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if ((word[e] & 0x7f80u) == 0x7f80u) { word[e] &= 0xffff0000u; odd = true; }
-                    if ((word[e] & 0x7f800000u) == 0x7f800000u) { word[e] &= 0xffffu; odd = true; }
-                }
-                if (odd) atomicOr(&sm.bad[n_unit & 7], 1ull << behind);
-                if (odd || t >= w.q.len) *p = make_uint4(word[0], word[1], word[2], word[3]);
-            }
-        }
-        fence_proxy_async_smem();
-        return true;
-    }
-
-    // One tile: scores -> probabilities.  `first`: of its unit.
-    __device__ __forceinline__ bool tile(const Walk& w, int j, uint32_t g, uint32_t n_unit, bool warp_live, bool live,
-                                         unsigned long long sees, float unit, float& m_ref, float& l_sum)
-    {
-        const int t0 = (w.tile0 + j) * kTile;
-        const bool ends = t0 + kTile > w.committed();  // some row does not see all of the tile
-        if constexpr (!F4)
-            if (ends && !clean_values(w, t0, g, n_unit)) return false;
-        if (!warp_wait(&sm.s_full[g & 1], (g >> 1) & 1, &sm.gave_up)) return false;
-        if (warp_live) {
-            tc_fence_after_sync();
-            const uint32_t t_s = tmem + kColS + (g & 1) * kTile;
-            uint32_t s[2][32];
-            tmem_ld32(t_s + 64 * half, s[0]);
-            tmem_ld32(t_s + 64 * half + 32, s[1]);
-            tmem_ld_wait();
-            if (ends) {
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const uint32_t see = sees == 0 ? 0u : seen_columns(t0 + 64 * half + 32 * c, w.committed(), w.q.len, sees);
-#pragma unroll
-                    for (int x = 0; x < 32; ++x)
-                        if (!((see >> x) & 1)) s[c][x] = 0xff800000u;
-                }
-            }
-            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int x = 0; x < 16; ++x)
-                    m4[x & 3] = fmax3(m4[x & 3], __uint_as_float(s[c][2 * x]), __uint_as_float(s[c][2 * x + 1]));
-            float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-            sm.top[g & 1][half][i] = mx;
-            row_barrier();  // also: both threads have their scores, whose columns P takes
-            mx = fmaxf(mx, sm.top[g & 1][half ^ 1][i]);
-            if (j == 0) {
-                m_ref = mx;
-            } else {
-                const bool need = live && (mx - m_ref) * unit > kRescaleAt;
-                if (__any_sync(0xffffffffu, need)) {
-                    if (!warp_wait(&sm.pv_done, (g - 1) & 1, &sm.gave_up)) return false;
-                    tc_fence_after_sync();
-                    const float alpha = need ? fast_exp2((m_ref - mx) * unit) : 1.f;
-                    if (need) m_ref = mx;
-                    l_sum *= alpha;
-#pragma unroll 1
-                    for (int c = 0; c < D / 32; ++c) {  // this thread's half of the row
-                        uint32_t o[16];
-                        const uint32_t at = tmem + kColO + half * (D / 2) + 16 * c;
-                        tmem_ld16(at, o);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * alpha);
-                        tmem_st16(at, o);
-                    }
-                }
-            }
-            const float base = m_ref == -INFINITY ? 0.f : m_ref * unit;  // (nothing seen yet)
-            const float2 unit2 = make_float2(unit, unit), base2 = make_float2(-base, -base);
-            float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t pk[16];
-#pragma unroll
-                for (int x = 0; x < 16; ++x) {
-                    float2 p = ffma2(make_float2(__uint_as_float(s[c][2 * x]), __uint_as_float(s[c][2 * x + 1])), unit2, base2);
-                    p.x = fast_exp2(p.x);
-                    p.y = fast_exp2(p.y);
-                    l2[x & 1] = fadd2(l2[x & 1], p);
-                    pk[x] = F4 ? f16x2(p.x, p.y) : bf16x2(p.x, p.y);
-                }
-                tmem_st16(t_s + 32 * half + 16 * c, pk);
-            }
-            l_sum += (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
-            tmem_st_wait();
-        }
-        tc_fence_before_sync();
-        mbar_arrive(&sm.p_full[g & 1]);
-        return true;
-    }
-
     // The unit's rows: final ones, partial ones of a cut unit, or partial slots.
-    __device__ __forceinline__ void finish(const Walk& w, uint32_t n_unit, bool live, unsigned long long sees, float unit, float m_ref,
-                                           float l_sum)
+    __device__ __forceinline__ bool finish(const Walk& w, uint32_t n_unit)
     {
-        sm.sum[half][i] = l_sum;
-        row_barrier();
-        l_sum += sm.sum[half ^ 1][i];  // (the same in both threads: two terms)
+        if (!row_barrier(warp_wait(&sm.stat_full[n_unit & 1], (n_unit >> 1) & 1, &sm.gave_up) &&
+                         warp_wait(&sm.o_full, n_unit & 1, &sm.gave_up)))
+            return false;
         tc_fence_after_sync();
+        // the second group has the row's reference; the other's sum is brought to it
+        const float unit = sm.row_unit[n_unit & 1][i];
+        const float2 own = sm.stat[n_unit & 1][1][i], others = sm.stat[n_unit & 1][0][i];
+        const float m = own.x;
+        const float l = own.y + (others.x == m ? others.y : others.y * fast_exp2((others.x - m) * unit));
         const int G = a.Hq / a.Hkv, node = w.node0(a) + i / G;
+        const bool live = i < w.rows(a);
+        const unsigned long long bad = *static_cast<volatile unsigned long long*>(&sm.bad[n_unit & 7]);
+        const unsigned long long odd = l == 0.f ? 0 : bad & sm.sees[n_unit & 1][i];
         const int64_t row = (int64_t)(w.q.first + node) * a.Hq + w.h * G + i % G;
-        const float inv = l_sum == 0.f ? 0.f : 1.f / l_sum;
-        const float lse = l_sum == 0.f ? -INFINITY : (m_ref == -INFINITY ? 0.f : m_ref * unit * kLn2) + logf(l_sum);
-        const unsigned long long odd = l_sum == 0.f ? 0 : *static_cast<volatile unsigned long long*>(&sm.bad[n_unit & 7]) & sees;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float lse = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m * unit * kLn2) + logf(l);
         const bool whole = w.tiles == w.q.tiles, final_row = a.out != nullptr && whole;
         float *to = nullptr, *lse_to = nullptr;
         int spare = 0;  // slots behind this one that hold nothing
         if (a.out == nullptr) {
             const long long per = sm.part.per, c0 = w.start / per;
-            const int k = a.n_splits == 1 ? 0 : (int)(blockIdx.x - c0);
+            const int k = a.n_splits == 1 ? 0 : (int)(blockIdx.x - sm.part.cta0 - c0);
             const int parts = a.n_splits == 1 ? 1 : (int)((w.start + w.q.tiles - 1) / per - c0) + 1;
             const int64_t slot = row * a.n_slots + a.slot0 + k;
             to = a.o_part + slot * D;
@@ -579,27 +652,30 @@ struct Softmax {
             lse_to = a.lse_out + row;
         }
         const int32_t* pages = a.kv.page_table + (int64_t)w.r * a.kv.max_pages;
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c) {  // 16 dimensions at a time
-            const int d0 = half * (D / 2) + 16 * c;
-            uint32_t o[16];
-            tmem_ld16(tmem + kColO + d0, o);
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+            uint32_t o[32];
+            tmem_ld32(tmem + kColO + 32 * c, o);
             tmem_ld_wait();
-            float x[16];
+            if (c == D / 32 - 1) {  // O may be written again
+                tc_fence_before_sync();
+                mbar_arrive(&sm.o_free);
+            }
+            float x[32];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] = l_sum == 0.f ? 0.f : __uint_as_float(o[e]) * inv;
+            for (int e = 0; e < 32; ++e) x[e] = l == 0.f ? 0.f : __uint_as_float(o[e]) * inv;
             for (unsigned long long left = odd; left != 0; left &= left - 1) {  // values that were taken out
                 const int t = w.committed() + __ffsll(left) - 1, in = t & ((1 << a.kv.page_shift) - 1);
                 const int64_t page = paged_page(a.kv, pages, t >> a.kv.page_shift);
                 if constexpr (F4) {
                     using B = Fp4Block<D>;
                     const uint8_t* b = a.kv.k + (((page * a.Hkv + w.h) << (a.kv.page_shift - 4)) + (in >> 4)) * B::kBytes;
-                    const uint32_t sc = *reinterpret_cast<const uint16_t*>(b + B::v_scale(in & 15, d0 / 32));
+                    const uint32_t sc = *reinterpret_cast<const uint16_t*>(b + B::v_scale(in & 15, c));
                     if ((sc & 0x7fffu) <= 0x7154u) continue;
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
+                    for (int e = 0; e < 4; ++e) {
                         uint32_t f[4];
-                        e2m1x8_to_f16x2(*reinterpret_cast<const uint32_t*>(b + B::v_byte(in & 15, d0 + 8 * e)), f);
+                        e2m1x8_to_f16x2(*reinterpret_cast<const uint32_t*>(b + B::v_byte(in & 15, 32 * c + 8 * e)), f);
 #pragma unroll
                         for (int y = 0; y < 4; ++y) {
                             const uint32_t v = hmul2(f[y], sc * 0x10001u);
@@ -609,56 +685,54 @@ struct Softmax {
                     }
                 } else {
                     const uint16_t* v = reinterpret_cast<const uint16_t*>(a.kv.v) +
-                                        (((page << a.kv.page_shift) + in) * a.Hkv + w.h) * D + d0;
+                                        (((page << a.kv.page_shift) + in) * a.Hkv + w.h) * D + 32 * c;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
+                    for (int e = 0; e < 32; ++e)
                         if ((v[e] & 0x7f80u) == 0x7f80u) x[e] += __uint_as_float((uint32_t)v[e] << 16);
                 }
             }
             if (!live) continue;
             if (final_row) {
-                uint4* p = reinterpret_cast<uint4*>(a.out + row * D + d0);
+                uint4* p = reinterpret_cast<uint4*>(a.out + row * D + 32 * c);
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
+                for (int e = 0; e < 4; ++e)
                     p[e] = make_uint4(bf16x2(x[8 * e], x[8 * e + 1]), bf16x2(x[8 * e + 2], x[8 * e + 3]),
                                       bf16x2(x[8 * e + 4], x[8 * e + 5]), bf16x2(x[8 * e + 6], x[8 * e + 7]));
             } else {
-                float4* p = reinterpret_cast<float4*>(to + d0);
+                float4* p = reinterpret_cast<float4*>(to + 32 * c);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) p[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+                for (int e = 0; e < 8; ++e) p[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
                 for (int k = 1; k <= spare; ++k)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) reinterpret_cast<float4*>(to + k * D + d0)[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int e = 0; e < 8; ++e)
+                        reinterpret_cast<float4*>(to + k * D + 32 * c)[e] = make_float4(0.f, 0.f, 0.f, 0.f);
             }
         }
-        if (live && half == 0 && lse_to != nullptr) {
+        if (live && lse_to != nullptr) {
             *lse_to = lse;
             for (int k = 1; k <= spare; ++k) lse_to[k] = -INFINITY;
         }
+        row_barrier();  // all have read `bad`
+        if (i == 0) sm.bad[n_unit & 7] = 0;
+        return true;
     }
 
+    // One unit is prepared ahead of the one that is finished.
     __device__ __forceinline__ void run(Walk w)
     {
-        unsigned long long sees, sees_next = 0;
-        float unit, unit_next = 0.f;
-        uint32_t g = 0, n_unit = 0;
-        prepare(w, true, 0, sees, unit);
-        while (true) {
-            const int rows = w.rows(a);
-            const bool live = i < rows, warp_live = (warp & 3) * 32 < rows;
-            float m_ref = -INFINITY, l_sum = 0.f;
-            for (int j = 0; j < w.tiles; ++j, ++g)
-                if (!tile(w, j, g, n_unit, warp_live, live, sees, unit, m_ref, l_sum)) return;
-            Walk after = w;
-            const bool more = after.next(a, sm.part);
-            if (more) prepare(after, after.r != w.r, n_unit + 1, sees_next, unit_next);
-            if (!warp_wait(&sm.pv_done, (g - 1) & 1, &sm.gave_up)) return;
-            if (warp_live) finish(w, n_unit, live, sees, unit, m_ref, l_sum);
-            if (!more) return;
+        Walk after = w;
+        bool more = after.next(a, sm.part);
+        prepare(w, true, more, 0);
+        for (uint32_t n_unit = 0;; ++n_unit) {
+            Walk then = after;
+            const bool go_on = more;
+            if (go_on) {
+                more = then.next(a, sm.part);
+                prepare(after, after.r != w.r, more, n_unit + 1);
+            }
+            if (!finish(w, n_unit) || !go_on) return;
             w = after;
-            sees = sees_next;
-            unit = unit_next;
-            ++n_unit;
+            after = then;
         }
     }
 };
@@ -748,56 +822,73 @@ __device__ __forceinline__ void load_role(Smem<D, F4>& sm, const CUtensorMap& tm
 }
 
 // ---- MMAs -------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint64_t descriptor(uint32_t hi, uint32_t lo) { return (static_cast<uint64_t>(hi) << 32) | lo; }
+
+// Scores of step after step, into the buffer of the step four before, when its probabilities have been used.
 template <int D, bool F4>
-__device__ __forceinline__ void mma_role(Smem<D, F4>& sm, const TreeArgs& a, Walk w, uint32_t tmem)
+__device__ __forceinline__ void score_role(Smem<D, F4>& sm, uint32_t tmem)
 {
     using C = Cfg<D, F4>;
-    const uint32_t id_qk = F4 ? idesc_f16_f32(128, kTile, false) : idesc_bf16_f32(128, kTile, false);
-    const uint32_t id_pv = F4 ? idesc_f16_f32(128, D, true) : idesc_bf16_f32(128, D, true);
-    const uint64_t d_k = smem_desc_sw128(0, 16, 1024), d_n = smem_desc_sw128(0, kHalfBytes, 1024);
-    const uint32_t hi_k = static_cast<uint32_t>(d_k >> 32), hi_n = static_cast<uint32_t>(d_n >> 32);
-    const uint32_t lo_k = static_cast<uint32_t>(d_k) + (smem_u32(sm.slot[0]) >> 4);
-    const uint32_t lo_v = static_cast<uint32_t>(d_n) + (smem_u32(sm.slot[0]) >> 4);
-    auto desc = [](uint32_t hi, uint32_t lo) { return (static_cast<uint64_t>(hi) << 32) | lo; };
+    const uint32_t id = F4 ? idesc_f16_f32(128, kStep, false) : idesc_bf16_f32(128, kStep, false);
+    const uint64_t d = smem_desc_sw128(0, 16, 1024);
+    const uint32_t hi = static_cast<uint32_t>(d >> 32), lo = static_cast<uint32_t>(d) + (smem_u32(sm.slot[0]) >> 4);
     int* gave_up = &sm.gave_up;
-    uint32_t g = 0, n_unit = 0;
-    auto scores = [&](uint32_t x) {  // of tile x, for the current unit
-        const uint32_t seq = 2 * x, s = seq % C::kSlots;
-        if (!warp_wait(&sm.full[s], (seq / C::kSlots) & 1, gave_up)) return false;
-        tc_fence_after_sync();
-        if (elect_one()) {
-            const uint32_t to = tmem + kColS + (x & 1) * kTile, q = tmem + kColQ + (n_unit & 1) * 64;
-            const uint32_t k = lo_k + ((s * C::kSlotBytes) >> 4);
-#pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks)
-                mma_ts(to, q + 8 * ks, desc(hi_k, k + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4)), id_qk, ks > 0);
-            tc_commit(&sm.s_full[x & 1]);
-            tc_commit(&sm.empty[s]);
-        }
-        __syncwarp();
-        return true;
-    };
-    while (true) {
+    uint32_t step = 0;
+    for (uint32_t n_unit = 0;; ++n_unit) {
         if (!warp_wait(&sm.q_full[n_unit & 1], (n_unit >> 1) & 1, gave_up)) return;
-        if (!scores(g)) return;
-        for (int j = 0; j < w.tiles; ++j, ++g) {
-            if (j + 1 < w.tiles && !scores(g + 1)) return;
-            const uint32_t seq = 2 * g + 1, s = seq % C::kSlots;
-            if (!warp_wait(&sm.p_full[g & 1], (g >> 1) & 1, gave_up)) return;
-            if (!warp_wait(&sm.full[s], (seq / C::kSlots) & 1, gave_up)) return;
+        const int steps = 2 * sm.info[n_unit & 1].tiles, more = sm.info[n_unit & 1].more;
+        const uint32_t q = tmem + kColQ + (n_unit & 1) * 64;
+        for (int j = 0; j < steps; ++j, ++step) {
+            const uint32_t seq = step & ~1u, s = seq % C::kSlots, half = step & 1;  // (tile step / 2: slots 2 (step / 2) and the next)
+            if (step >= 4 && !warp_wait(&sm.pv_done[step & 3], ((step >> 2) - 1) & 1, gave_up)) return;
+            if (half == 0 && !warp_wait(&sm.full[s], (seq / C::kSlots) & 1, gave_up)) return;
             tc_fence_after_sync();
             if (elect_one()) {
-                const uint32_t p = tmem + kColS + (g & 1) * kTile, v = lo_v + ((s * C::kSlotBytes) >> 4);
+                const uint32_t to = tmem + kColS + (step & 3) * kStep;
+                const uint32_t k = lo + ((s * C::kSlotBytes + half * kStep * 128) >> 4);
 #pragma unroll
-                for (int ks = 0; ks < kTile / 16; ++ks)
-                    mma_ts(tmem + kColO, p + 8 * ks, desc(hi_n, v + ((ks * 2048) >> 4)), id_pv, j > 0 || ks > 0);
-                tc_commit(&sm.pv_done);
-                tc_commit(&sm.empty[s]);
+                for (int ks = 0; ks < D / 16; ++ks)
+                    mma_ts(to, q + 8 * ks, descriptor(hi, k + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4)), id, ks > 0);
+                tc_commit(&sm.s_full[step & 3]);
+                if (half == 1) tc_commit(&sm.empty[s]);
             }
             __syncwarp();
         }
-        if (!w.next(a, sm.part)) return;
-        ++n_unit;
+        if (!more) return;
+    }
+}
+
+template <int D, bool F4>
+__device__ __forceinline__ void value_role(Smem<D, F4>& sm, uint32_t tmem)
+{
+    using C = Cfg<D, F4>;
+    const uint32_t id = F4 ? idesc_f16_f32(128, D, true) : idesc_bf16_f32(128, D, true);
+    const uint64_t d = smem_desc_sw128(0, kHalfBytes, 1024);
+    const uint32_t hi = static_cast<uint32_t>(d >> 32), lo = static_cast<uint32_t>(d) + (smem_u32(sm.slot[0]) >> 4);
+    int* gave_up = &sm.gave_up;
+    uint32_t step = 0;
+    for (uint32_t n_unit = 0;; ++n_unit) {
+        if (!warp_wait(&sm.q_full[n_unit & 1], (n_unit >> 1) & 1, gave_up)) return;
+        const int steps = 2 * sm.info[n_unit & 1].tiles, more = sm.info[n_unit & 1].more;
+        for (int j = 0; j < steps; ++j, ++step) {
+            const uint32_t seq = step | 1u, s = seq % C::kSlots, half = step & 1;
+            if (!warp_wait(&sm.p_full[step & 3], (step >> 2) & 1, gave_up)) return;
+            if (half == 0 && !warp_wait(&sm.full[s], (seq / C::kSlots) & 1, gave_up)) return;
+            // (a unit's first product overwrites O, which the rows of the unit before have to have left)
+            if (j == 0 && n_unit > 0 && !warp_wait(&sm.o_free, (n_unit - 1) & 1, gave_up)) return;
+            tc_fence_after_sync();
+            if (elect_one()) {
+                const uint32_t p = tmem + kColS + (step & 3) * kStep, v = lo + ((s * C::kSlotBytes + half * kStep * 128) >> 4);
+#pragma unroll
+                for (int ks = 0; ks < kStep / 16; ++ks)
+                    mma_ts(tmem + kColO, p + 8 * ks, descriptor(hi, v + ((ks * 2048) >> 4)), id, j > 0 || ks > 0);
+                tc_commit(&sm.pv_done[step & 3]);
+                if (half == 1) tc_commit(&sm.empty[s]);
+                if (j + 1 == steps) tc_commit(&sm.o_full);
+            }
+            __syncwarp();
+        }
+        if (!more) return;
     }
 }
 
@@ -819,7 +910,7 @@ __device__ __forceinline__ void widen_role(Smem<D, true>& sm, const TreeArgs& a,
                 if (seq >= C::kSlots && !warp_wait(&sm.empty[s], ((seq / C::kSlots) - 1) & 1, gave_up)) return;
                 if (!warp_wait(&sm.unit_full[u], (seq / C::kUnits) & 1, gave_up)) return;
                 uint8_t* to = sm.slot[s];
-#pragma unroll 1
+#pragma unroll
                 for (int block = warp; block < C::kBlocks; block += kWidenWarps) {
                 const uint8_t* from = sm.unit + u * C::kUnitBytes + block * C::kPartBytes;
                 const int row0 = 16 * block;
@@ -925,7 +1016,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         if (tid == 0) atomicMin(a.kv.status, (int)MOSKA_ERR_CUDA);
         return;
     }
-    if (warp < kLoadWarp) {
+    if (warp < kRowWarp0) {
         find_part(a, blockIdx.x, gridDim.x, sm.part);
     } else if (warp == kLoadWarp && lane == 0) {
         for (int s = 0; s < C::kSlots; ++s) {
@@ -937,16 +1028,22 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             mbar_init(&sm.unit_empty[u], kWidenWarps);
         }
         for (int x = 0; x < 2; ++x) {
-            mbar_init(&sm.q_full[x], kSoftmaxThreads);
-            mbar_init(&sm.s_full[x], 1);
-            mbar_init(&sm.p_full[x], kSoftmaxThreads);
+            mbar_init(&sm.q_full[x], kTileRows);
+            mbar_init(&sm.stat_full[x], kSoftmaxThreads);
+            for (int y = 0; y < 4; ++y) mbar_init(&sm.ref_full[x][y], 32);
         }
-        mbar_init(&sm.pv_done, 1);
+        for (int x = 0; x < 4; ++x) {
+            mbar_init(&sm.s_full[x], 1);
+            mbar_init(&sm.p_full[x], kTileRows);
+            mbar_init(&sm.pv_done[x], 1);
+        }
+        mbar_init(&sm.o_full, 1);
+        mbar_init(&sm.o_free, kTileRows);
         for (int x = 0; x < 8; ++x) sm.bad[x] = 0;
         sm.gave_up = 0;
         fence_mbar_init();
         fence_proxy_async_smem();
-    } else if (warp == kMmaWarp) {
+    } else if (warp == kScoreWarp) {
         tmem_alloc(&sm.tmem_base, 512);
         tmem_relinquish();
     }
@@ -958,12 +1055,18 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
 
     Walk w;
     if (w.begin(a, sm.part)) {
-        if (warp < kLoadWarp) {
-            Softmax<D, F4>{sm, a, tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16), warp, warp >> 2, (warp & 3) * 32 + lane}.run(w);
+        const uint32_t lanes = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+        const int row = (warp & 3) * 32 + lane;
+        if (warp < kRowWarp0) {
+            softmax_role<D, F4>(sm, lanes, warp >> 2, warp, row);
+        } else if (warp < kLoadWarp) {
+            Rows<D, F4>{sm, a, lanes, row}.run(w);
         } else if (warp == kLoadWarp) {
             load_role<D, F4>(sm, tm_k, tm_v, a, w, lane);
-        } else if (warp == kMmaWarp) {
-            mma_role<D, F4>(sm, a, w, tmem);
+        } else if (warp == kScoreWarp) {
+            score_role<D, F4>(sm, tmem);
+        } else if (warp == kValueWarp) {
+            value_role<D, F4>(sm, tmem);
         } else {
             if constexpr (F4) widen_role<D>(sm, a, w, warp - kWidenWarp0, lane);
         }
@@ -971,47 +1074,75 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     __syncwarp();
     tc_fence_before_sync();
     __syncthreads();
-    if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
+    if (warp == kScoreWarp) tmem_dealloc(tmem, 512);
     if (tid == 0 && sm.gave_up) atomicMin(a.kv.status, (int)MOSKA_ERR_TIMEOUT);
 }
 
-// Joins the partial rows of a unit that cuts divide: CTA x looks at the cut before part x + 1; the first cut of a unit's has it.
+// Joins the partial rows of a unit that cuts divide: kJoinCtas CTAs look at the cut before part 1, as many at the one before part 2,
+// ..; a unit's first cut has it, and its CTAs have 16 rows each, two a warp.
+constexpr int kJoinCtas = 8;
 template <int D>
 __global__ void __launch_bounds__(kSoftmaxThreads) tree_join_kernel(const TreeArgs a, int ctas)
 {
     __shared__ Part part;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x + 1;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x / kJoinCtas + 1;
     find_part(a, cta, ctas, part);
     __syncthreads();
     Walk w;
     wait_for_results();
     if (!w.begin(a, part) || w.tile0 == 0) return;
-    const int c0 = (int)(w.start / part.per), c1 = (int)((w.start + w.q.tiles - 1) / part.per);
+    const int c0 = part.cta0 + (int)(w.start / part.per), c1 = part.cta0 + (int)((w.start + w.q.tiles - 1) / part.per);
     if (cta != c0 + 1) return;
     const int G = a.Hq / a.Hkv, rows = w.rows(a);
     constexpr int W = D / 32;  // dimensions a lane
-    for (int i = warp; i < rows; i += kSoftmaxThreads / 32) {
-        auto slot = [&](int c) { return (int64_t)(2 * c + (c == c0 ? 1 : 0)) * kTileRows + i; };
-        float top = -INFINITY;
-        for (int c = c0 + lane; c <= c1; c += 32) top = max_or_nan(top, a.lse_cut[slot(c)]);
+    using Vec = typename std::conditional<W == 4, float4, float2>::type;
+    const int i0 = (blockIdx.x % kJoinCtas) * (kTileRows / kJoinCtas) + warp;  // and i0 + 8
+    auto slot = [&](int c, int x) { return (int64_t)(2 * c + (c == c0 ? 1 : 0)) * kTileRows + i0 + 8 * x; };
+    if (i0 >= rows) return;
+    float top[2] = {-INFINITY, -INFINITY};
+    for (int c = c0 + lane; c <= c1; c += 32)
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) top = max_or_nan(top, __shfl_xor_sync(0xffffffffu, top, off));
-        const float base = top == -INFINITY ? 0.f : top;  // (all parts empty: every weight is 0)
-        float total = 0.f, acc[W] = {};
-#pragma unroll 4
-        for (int c = c0; c <= c1; ++c) {
-            const float* o = a.o_cut + slot(c) * D + W * lane;
-            const float weight = __expf(a.lse_cut[slot(c)] - base);
-            total += weight;
+        for (int x = 0; x < 2; ++x)
+            if (i0 + 8 * x < rows) top[x] = max_or_nan(top[x], a.lse_cut[slot(c, x)]);
 #pragma unroll
-            for (int e = 0; e < W; ++e) acc[e] = fmaf(weight, o[e], acc[e]);
-        }
-        const float inv = total == 0.f ? 0.f : 1.f / total;
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) top[x] = max_or_nan(top[x], __shfl_xor_sync(0xffffffffu, top[x], off));
+    float total[2] = {}, acc[2][W] = {};
+    constexpr int kAtOnce = 4;
+    for (int c = c0; c <= c1; c += kAtOnce) {
+        Vec o[kAtOnce][2];
+        float weight[kAtOnce][2];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                if (c + u > c1 || i0 + 8 * x >= rows) continue;
+                weight[u][x] = a.lse_cut[slot(c + u, x)];
+                o[u][x] = *reinterpret_cast<const Vec*>(a.o_cut + slot(c + u, x) * D + W * lane);
+            }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                if (c + u > c1 || i0 + 8 * x >= rows) continue;
+                // (all parts empty: every weight is 0)
+                const float y = __expf(weight[u][x] - (top[x] == -INFINITY ? 0.f : top[x]));
+                total[x] += y;
+#pragma unroll
+                for (int e = 0; e < W; ++e) acc[x][e] = fmaf(y, reinterpret_cast<const float*>(&o[u][x])[e], acc[x][e]);
+            }
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const int i = i0 + 8 * x;
+        if (i >= rows) continue;
+        const float inv = total[x] == 0.f ? 0.f : 1.f / total[x];
         const int64_t row = (int64_t)(w.q.first + w.node0(a) + i / G) * a.Hq + w.h * G + i % G;
 #pragma unroll
         for (int e = 0; e < W; e += 2)
-            *reinterpret_cast<uint32_t*>(a.out + row * D + W * lane + e) = bf16x2(acc[e] * inv, acc[e + 1] * inv);
-        if (lane == 0 && a.lse_out != nullptr) a.lse_out[row] = top == -INFINITY ? -INFINITY : top + logf(total);
+            *reinterpret_cast<uint32_t*>(a.out + row * D + W * lane + e) = bf16x2(acc[x][e] * inv, acc[x][e + 1] * inv);
+        if (lane == 0 && a.lse_out != nullptr) a.lse_out[row] = top[x] == -INFINITY ? -INFINITY : top[x] + logf(total[x]);
     }
 }
 
@@ -1110,7 +1241,7 @@ int launch_tree_attn(const uint16_t* q, const PagedView& kv, bool fp4, const Tre
     else MOSKA_TRY_STATUS(fp4 ? form(d64, std::true_type{}) : form(d64, std::false_type{}));
     if (out == nullptr || s->n_unique_splits == 1 || ctas < 2) return MOSKA_OK;
     cudaLaunchConfig_t config{};
-    config.gridDim = dim3((unsigned)(ctas - 1));
+    config.gridDim = dim3((unsigned)(kJoinCtas * (ctas - 1)));
     config.blockDim = dim3(kSoftmaxThreads);
     config.stream = st;
     cudaLaunchAttribute early{};
