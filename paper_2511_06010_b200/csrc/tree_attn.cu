@@ -5,8 +5,8 @@
 //   S = Q K^T          tcgen05.mma, Q in tensor memory, K in shared memory: 128 x 64 scores (half a tile) in tensor memory
 //   P = exp2(S - m)    a thread per row: TMEM -> registers -> 16 bits, back over the columns of S
 //   O += P V           tcgen05.mma, P from TMEM, V from shared memory
-// Two groups of softmax warps take turns at the halves: while one group's exponentials keep the special function units busy
-// (512 cycles a half), the other reads its scores and finds its maximum.  Scores have four buffers, so that products run ahead.  A third
+// Groups of softmax warps take turns at the halves: while one group's exponentials keep the special function units busy
+// (512 cycles a half), the others read their scores and find their maxima.  Scores have four buffers, so that products run ahead.  A third
 // group stages the next unit's queries and writes the last unit's rows.  TMEM: O 128, S 4 x 64, Q 2 x 64 = 512 columns.
 //
 // One CTA per SM.  For each row tile (first 128 rows of every request, second 128, ..) the tiles of all its units, request after
@@ -16,14 +16,13 @@
 // that all but the first find them in L2; cut as one line, each fetched them from memory: 24 requests of 60 nodes
 // read 3.45 GB instead of 0.9.)
 //
-// Warps 0-3 and 4-7: softmax of the first and second halves of tiles (thread i: row i % 128 = TMEM lane).  Warps 8-11: queries and results.
-// Warp 12: copies.  Warps 13 and 14: MMAs of Q K^T and of P V (one warp for both left the tensor cores idle while it
-// waited: 2800 cycles a tile, XXXX).  4-bit pages: warps 15-18 widen.  Operands lie in a ring of slots, a K or a V tile each, as halves of 64 dimensions in rows of
+// Warps, in this order: groups of four for the softmax (thread i: row i % 128 = TMEM lane), four for queries and results, one for
+// copies, one for the MMAs of Q K^T and one for those of P V (one warp for both left the tensor cores idle while it waited).  4-bit
+// pages: eight that widen.  Operands lie in a ring of slots, a K or a V tile each, as halves of 64 dimensions in rows of
 // 128 bytes with the 128-byte swizzle.
 //   bf16: one TMA box of min(page_size, 128) tokens a page and half.
-//   4 bits: bulk copies of the key parts or the value parts (codes, then scales) of the tile's 16-token blocks into a ring of
-//   their own; a warp widens every fourth to f16 operands, code times scale (half a step: 2^-11).  Queries are f16 too,
-//   scaled by a power of two per row.
+//   4 bits: a bulk copy a page into a ring of tiles of codes, which are widened to f16 operands, code times scale (half a
+//   step: 2^-11).  Queries are f16 too, scaled by a power of two per row.
 //
 // What a node sees: committed tokens, and of the last T tokens those whose bit is set in its 64-bit word of ancestors.
 // Only tiles that reach past the committed tokens look at it.  0 times NaN is NaN, so values of such tiles that are
@@ -47,8 +46,7 @@ constexpr int kTile = 128;      // tokens of a tile
 constexpr int kStep = 64;       // tokens whose scores are computed at once
 constexpr int kTileRows = 128;  // query rows of a unit
 constexpr int kHalfBytes = kTile * 64 * 2;
-constexpr int kSoftmaxThreads = 256;
-constexpr int kRowWarp0 = 8, kLoadWarp = 12, kScoreWarp = 13, kValueWarp = 14, kWidenWarp0 = 15, kWidenWarps = 4;
+constexpr int kFindThreads = 256;  // of those that find a CTA's part
 constexpr int kMaxRowTiles = 4;  // 64 nodes of up to 8 heads
 constexpr int kMaxCtas = 148;    // parts of the line of tiles
 constexpr uint32_t kColO = 0, kColS = 128, kColQ = 384;  // tensor-memory columns
@@ -58,13 +56,20 @@ constexpr float kRescaleAt = 8.f;  // log2 units that a row's maximum may grow b
 template <int D, bool F4>
 struct Cfg {
     static constexpr int kHalves = D / 64;
-    static constexpr int kThreads = F4 ? 608 : 480;
+    static constexpr int kGroups = 2;  // of softmax warps
+    static constexpr int kRowWarp0 = 4 * kGroups, kLoadWarp = kRowWarp0 + 4, kScoreWarp = kLoadWarp + 1, kValueWarp = kLoadWarp + 2,
+                         kWidenWarp0 = kLoadWarp + 4, kWidenWarps = 8;
+    static constexpr int kThreads = 32 * (F4 ? kWidenWarp0 + kWidenWarps : kWidenWarp0);
+    // Registers of a thread: at the launch, and of the groups of four warps after it.
+    static constexpr int kLaunchRegs = F4 ? 80 : 128;
+    static constexpr int kSoftmaxRegs = F4 ? 112 : 152, kRowRegs = F4 ? 112 : 128, kIssueRegs = F4 ? 40 : 80, kWidenRegs = 48;
+    static_assert(128 * (kGroups * kSoftmaxRegs + kRowRegs + kIssueRegs + (F4 ? 2 * kWidenRegs : 0)) <= kThreads * kLaunchRegs,
+                  "setmaxnreg: more than the CTA was launched with would be waited for without end");
     static constexpr int kSlotBytes = kHalves * kHalfBytes;
     static constexpr int kSlots = F4 ? (D == 128 ? 4 : 8) : (D == 128 ? 6 : 12);
-    static constexpr int kBlocks = kTile / kBlockTokens;  // 16-token blocks of a unit of codes
-    static constexpr int kPartBytes = 9 * D;              // codes and scales of a block's keys, or of its values
-    static constexpr int kUnitBytes = kBlocks * kPartBytes;
-    static constexpr int kUnits = F4 ? (D == 128 ? 8 : 16) : 1;
+    static constexpr int kBlocks = kTile / kBlockTokens;  // 16-token blocks of a tile
+    static constexpr int kCodeBytes = kBlocks * fp4_block_bytes(D);
+    static constexpr int kCodeSlots = F4 ? (D == 128 ? 4 : 8) : 1;
 };
 
 // A CTA's part of the line of its row tile.
@@ -72,9 +77,10 @@ struct Part {
     long long p0, p1, per;  // tiles p0 .. p1 - 1; `per` in a full part
     long long start;        // first tile of the unit that p0 is in: (row tile, request, head)
     int rt, r, h;
-    int cta0, ctas;         // CTAs of the line
-    int longest[kSoftmaxThreads / 32];
-    long long tiles[kMaxRowTiles][kSoftmaxThreads / 32];  // of each warp's requests
+    int cta0;               // the line's first CTA
+    int cost;               // of a unit, in tiles
+    int longest[kFindThreads / 32];
+    long long sums[kMaxRowTiles][kFindThreads / 32];  // of each warp's requests
 };
 
 // What the softmax needs of a unit.
@@ -86,16 +92,16 @@ template <int D, bool F4>
 struct Smem {
     using C = Cfg<D, F4>;
     uint8_t slot[C::kSlots][C::kSlotBytes];
-    uint8_t unit[F4 ? C::kUnits * C::kUnitBytes : 16];
-    float ref[2][kTileRows];         // the reference of a row's probabilities after a half of each softmax group
-    float2 stat[2][2][kTileRows];    // (reference, sum) of a unit's rows by each group; units take turns
+    uint8_t code[F4 ? C::kCodeSlots * C::kCodeBytes : 16];
+    float ref[C::kGroups][kTileRows];       // the reference of a row's probabilities after a step of each softmax group
+    float2 stat[2][C::kGroups][kTileRows];  // (reference, sum) of a unit's rows by each group; units take turns
     UnitInfo info[2];                // units take turns
     unsigned long long sees[2][kTileRows];
     float row_unit[2][kTileRows];
     TreeSmem tree;
     uint64_t full[C::kSlots], empty[C::kSlots];
-    uint64_t unit_full[C::kUnits], unit_empty[C::kUnits];
-    uint64_t q_full[2], s_full[4], p_full[4], stat_full[2], ref_full[2][4], pv_done[4], o_full, o_free;
+    uint64_t code_full[C::kCodeSlots], code_empty[C::kCodeSlots];
+    uint64_t q_full[2], s_full[4], p_full[4], stat_full[2], ref_full[C::kGroups][4], pv_done[4], o_full, o_free;
     unsigned long long bad[8];  // tree tokens with values that are not finite; units take turns
     Part part;
     uint32_t tmem_base;
@@ -208,7 +214,7 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int* g
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, gave_up));
 }
 
-__device__ __forceinline__ void softmax_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+__device__ __forceinline__ void find_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 // Of the third group; true if all of its threads say so.  (No thread leaves on its own: the others would wait for it.)
 __device__ __forceinline__ bool row_barrier(bool ok = true)
 {
@@ -246,6 +252,15 @@ __device__ __forceinline__ bool elect_one()
 struct Request {
     int first, nodes, len, tiles, row_tiles;
 };
+// On the line a unit is longer than its tiles by what its beginning and its end cost, in tiles; where parts are short
+// (few tiles in all, or latency counts) by nothing.
+constexpr int kUnitCost = 2, kShortPart = 16;
+// Tiles and units of a stretch of requests in one number.
+constexpr int kUnitBit = 40;
+__device__ __forceinline__ long long places(long long packed, int cost)
+{
+    return (packed & ((1ll << kUnitBit) - 1)) + (packed >> kUnitBit) * cost;
+}
 
 __device__ __forceinline__ Request request_of(const TreeArgs& a, int r)
 {
@@ -259,15 +274,15 @@ __device__ __forceinline__ Request request_of(const TreeArgs& a, int r)
     return q;
 }
 
-// Finds part `cta` of `ctas`: for kSoftmaxThreads threads, in shared memory that all of the CTA may read after its next
-// barrier (p0 >= p1: nothing).  Each thread counts a stretch of requests; the tiles before a warp, a lane and a request are
+// Finds part `cta` of `ctas`: for kFindThreads threads, in shared memory that all of the CTA may read after its next
+// barrier (p0 >= p1: nothing).  Each thread counts a stretch of requests; what is before a warp, a lane and a request is
 // then added up.
 __device__ __forceinline__ void find_part(const TreeArgs& a, int cta, int ctas, Part& part)
 {
-    constexpr int kWarps = kSoftmaxThreads / 32;
+    constexpr int kWarps = kFindThreads / 32;
     const int i = threadIdx.x, warp = i >> 5, lane = i & 31, R = a.tree.n_requests;
-    const int stretch = (R + kSoftmaxThreads - 1) / kSoftmaxThreads;
-    const int r0 = min((long long)R, (long long)i * stretch), r1 = min(R, r0 + stretch);
+    const int stretch = (R + kFindThreads - 1) / kFindThreads;
+    const int r0 = (int)min((long long)R, (long long)i * stretch), r1 = min(R, r0 + stretch);
     long long mine[kMaxRowTiles] = {}, upto[kMaxRowTiles] = {};
     int longest = 0;
     for (int r = r0; r < r1; ++r) {
@@ -275,7 +290,7 @@ __device__ __forceinline__ void find_part(const TreeArgs& a, int cta, int ctas, 
         if (q.row_tiles > 0) longest = max(longest, q.tiles);
 #pragma unroll
         for (int k = 0; k < kMaxRowTiles; ++k)
-            if (k < q.row_tiles) mine[k] += q.tiles;
+            if (k < q.row_tiles) mine[k] += q.tiles + (1ll << kUnitBit);
     }
 #pragma unroll
     for (int k = 0; k < kMaxRowTiles; ++k) {
@@ -286,26 +301,30 @@ __device__ __forceinline__ void find_part(const TreeArgs& a, int cta, int ctas, 
             const long long y = __shfl_up_sync(0xffffffffu, upto[k], off);
             if (lane >= off) upto[k] += y;
         }
-        if (lane == 31) part.tiles[k][warp] = upto[k];
+        if (lane == 31) part.sums[k][warp] = upto[k];
     }
     longest = __reduce_max_sync(0xffffffffu, longest);
     if (lane == 0) part.longest[warp] = longest;
-    softmax_barrier();
+    find_barrier();
     long long line[kMaxRowTiles] = {}, total = 0;
 #pragma unroll
     for (int k = 0; k < kMaxRowTiles; ++k) {
         if (k >= a.row_tiles) continue;
-        for (int x = 0; x < kWarps; ++x) line[k] += part.tiles[k][x];
-        total += line[k];
+        for (int x = 0; x < kWarps; ++x) line[k] += part.sums[k][x];
+        total += places(line[k], 0);
     }
     for (int x = 0; x < kWarps; ++x) longest = max(longest, part.longest[x]);
+    const int cost = total * a.Hkv >= (long long)ctas * kShortPart ? kUnitCost : 0;
+    total = 0;
+#pragma unroll
+    for (int k = 0; k < kMaxRowTiles; ++k) total += places(line[k], cost);
     // CTAs of the lines: by their lengths, one at least; the first line, the longest, gets what is over
     int rt = 0, cta0 = 0, n = ctas;
     long long mine_all = line[0];
 #pragma unroll
     for (int k = kMaxRowTiles - 1; k > 0; --k) {
         if (line[k] == 0 || rt != 0) continue;
-        const int c = max(1, (int)(ctas * line[k] / total));
+        const int c = max(1, (int)(ctas * places(line[k], cost) / total));
         n -= c;
         if (cta >= n) {
             rt = k;
@@ -314,37 +333,38 @@ __device__ __forceinline__ void find_part(const TreeArgs& a, int cta, int ctas, 
             mine_all = line[k];
         }
     }
-    const long long tiles = mine_all * a.Hkv;
-    // equal parts; no unit in more of them than there may be
-    long long per = (tiles + n - 1) / n;
-    if (a.n_splits > 1) per = max(per, (long long)(longest + a.n_splits - 2) / (a.n_splits - 1));
-    per = max(1ll, per);
-    const long long p0 = (cta - cta0) * per, p1 = min(tiles, p0 + per);
+    const long long all = places(mine_all, cost) * a.Hkv;
+    // equal parts, in each at least one tile of a unit that begins in it; no unit in more of them than there may be
+    long long per = (all + n - 1) / n;
+    if (a.n_splits > 1) per = max(per, (long long)(longest + cost + a.n_splits - 2) / (a.n_splits - 1));
+    per = max((long long)cost + 1, per);
+    const long long p0 = (cta - cta0) * per, p1 = min(all, p0 + per);
     if (i == 0) {
         part.p0 = p0;
         part.p1 = p1;
         part.per = per;
+        part.cost = cost;
         part.rt = rt;
         part.cta0 = cta0;
-        part.ctas = n;
     }
     long long at = 0;
 #pragma unroll
     for (int k = 0; k < kMaxRowTiles; ++k) {
         if (k != rt) continue;
-        for (int x = 0; x < warp; ++x) at += part.tiles[k][x];
-        at = (at + upto[k] - mine[k]) * a.Hkv;
-        if (p0 >= p1 || p0 < at || p0 >= at + mine[k] * a.Hkv) continue;
+        for (int x = 0; x < warp; ++x) at += part.sums[k][x];
+        at = places(at + upto[k] - mine[k], cost) * a.Hkv;
+        if (p0 >= p1 || p0 < at || p0 >= at + places(mine[k], cost) * a.Hkv) continue;
         for (int r = r0; r < r1; ++r) {  // one thread: the part begins in its stretch
             const Request q = request_of(a, r);
             if (q.row_tiles <= k) continue;
-            if (p0 < at + (long long)q.tiles * a.Hkv) {
+            const long long long_is = q.tiles + cost;
+            if (p0 < at + long_is * a.Hkv) {
                 part.r = r;
-                part.h = (int)((p0 - at) / q.tiles);
-                part.start = at + (long long)part.h * q.tiles;
+                part.h = (int)((p0 - at) / long_is);
+                part.start = at + part.h * long_is;
                 break;
             }
-            at += (long long)q.tiles * a.Hkv;
+            at += long_is * a.Hkv;
         }
     }
 }
@@ -362,17 +382,23 @@ struct Walk {
     {
         return min(a.nodes_per_tile, q.nodes - node0(a)) * (a.Hq / a.Hkv);
     }
-    __device__ __forceinline__ void cut(const TreeArgs& a, const Part& p)
+    // first and last CTA that has tiles of the unit (from the line's first)
+    __device__ __forceinline__ int first_cta(const Part& p) const { return (int)((start + p.cost) / p.per); }
+    __device__ __forceinline__ int last_cta(const Part& p) const { return (int)((start + p.cost + q.tiles - 1) / p.per); }
+    // false if none of its tiles is in this part
+    __device__ __forceinline__ bool cut(const TreeArgs& a, const Part& p)
     {
         tile0 = 0;
         tiles = q.tiles;
-        if (a.n_splits == 1) return;  // units are not divided: the part in which one begins takes it
-        tile0 = (int)(max(p.p0, start) - start);
-        tiles = (int)(min(p.p1, start + q.tiles) - start) - tile0;
+        if (a.n_splits == 1) return true;  // units are not divided: the part in which one begins takes it
+        const long long first = start + p.cost;  // place of its first tile
+        tile0 = (int)max(0ll, p.p0 - first);
+        tiles = (int)(min(p.p1, first + q.tiles) - first) - tile0;
+        return tiles > 0;
     }
     __device__ __forceinline__ bool next(const TreeArgs& a, const Part& p)
     {
-        start += q.tiles;
+        start += q.tiles + p.cost;
         if (start >= p.p1) return false;
         if (++h == a.Hkv) {
             h = 0;
@@ -381,8 +407,7 @@ struct Walk {
                 q = request_of(a, r);
             } while (q.row_tiles <= rt);
         }
-        cut(a, p);
-        return true;
+        return cut(a, p);
     }
     // the first one; false if there is none
     __device__ __forceinline__ bool begin(const TreeArgs& a, const Part& p)
@@ -393,8 +418,8 @@ struct Walk {
         h = p.h;
         start = p.start;
         q = request_of(a, r);
-        cut(a, p);
-        return a.n_splits > 1 || start >= p.p0 || next(a, p);
+        if (a.n_splits == 1 && start < p.p0) return next(a, p);
+        return cut(a, p);
     }
 };
 
@@ -416,15 +441,15 @@ __device__ __forceinline__ uint32_t seen_tokens(int t, int committed, int len, u
 // Values of half a tile behind the context, and those of drafted tokens that are not finite, become 0 (bf16): two threads per
 // token row.
 template <int D>
-__device__ __forceinline__ bool clean_values(Smem<D, false>& sm, const UnitInfo& u, int t0, uint32_t g, int group, uint32_t n_unit, int i)
+__device__ __forceinline__ bool clean_values(Smem<D, false>& sm, const UnitInfo& u, int t0, uint32_t step, uint32_t n_unit, int i)
 {
     using C = Cfg<D, false>;
-    const uint32_t seq = 2 * g + 1;
+    const uint32_t seq = step | 1u;
     if (!warp_wait(&sm.full[seq % C::kSlots], (seq / C::kSlots) & 1, &sm.gave_up)) return false;
     const int token = i & (kStep - 1), t = t0 + token, behind = t - u.committed;
     if (behind >= 0) {
         // 16-byte pieces: of a half of the dimensions (D = 128), every second one (D = 64)
-        uint8_t* at = sm.slot[seq % C::kSlots] + (C::kHalves == 2 ? (i >> 6) * kHalfBytes : 0) + (group * kStep + token) * 128;
+        uint8_t* at = sm.slot[seq % C::kSlots] + (C::kHalves == 2 ? (i >> 6) * kHalfBytes : 0) + ((step & 1) * kStep + token) * 128;
 #pragma unroll 1
         for (int x = C::kHalves == 2 ? 0 : i >> 6; x < 8; x += C::kHalves == 2 ? 1 : 2) {
             uint4* p = reinterpret_cast<uint4*>(at + (((x + i) & 7) << 4));
@@ -444,14 +469,18 @@ __device__ __forceinline__ bool clean_values(Smem<D, false>& sm, const UnitInfo&
     return true;
 }
 
-// Scores of one half of every tile -> probabilities.  A row's reference m passes from group to group; it moves when a
-// half's maximum passes it by 2^8, and whoever moves it rescales O.  Each group keeps its own sum, relative to the reference
+// Scores of every kGroups-th step (half a tile) -> probabilities.  A row's reference m passes from step to step; it moves when a
+// step's maximum passes it by 2^8, and whoever moves it rescales O.  Each group keeps its own sum, relative to the reference
 // that it saw last.
 template <int D, bool F4>
 __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int group, int warp, int i)
 {
+    constexpr int kGroups = Cfg<D, F4>::kGroups;
     int* gave_up = &sm.gave_up;
-    uint32_t g = 0;
+    const int before_me = group == 0 ? kGroups - 1 : group - 1;  // the group of the step before
+    uint32_t mine = group;             // this group's next step, and how many it had
+    uint32_t turn = 0;
+    uint32_t unit0 = 0;                // first step of the unit
     for (uint32_t n_unit = 0;; ++n_unit) {
         if (!warp_wait(&sm.q_full[n_unit & 1], (n_unit >> 1) & 1, gave_up)) return;
         const UnitInfo u = sm.info[n_unit & 1];
@@ -459,49 +488,53 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
         const float unit = sm.row_unit[n_unit & 1][i];  // log2 units of one score
         const bool live = i < u.rows, warp_live = (warp & 3) * 32 < u.rows;
         float m = -INFINITY, l = 0.f;
-        for (int j = 0; j < u.tiles; ++j, ++g) {
-            const uint32_t step = 2 * g + group;
-            const int t0 = (u.tile0 + j) * kTile + kStep * group;
-            const bool ends = t0 + kStep > u.committed;  // some row does not see all of the half
+        const uint32_t end = unit0 + 2 * u.tiles;
+        for (; mine < end; mine += kGroups, ++turn) {
+            const int t0 = u.tile0 * kTile + (int)(mine - unit0) * kStep;
+            const bool ends = t0 + kStep > u.committed;  // some row does not see all of it
             if constexpr (!F4)
-                if (ends && !clean_values<D>(sm, u, t0, g, group, n_unit, i)) return;
-            if (!warp_wait(&sm.s_full[step & 3], (step >> 2) & 1, gave_up)) return;
+                if (ends && !clean_values<D>(sm, u, t0, mine, n_unit, i)) return;
+            if (!warp_wait(&sm.s_full[mine & 3], (mine >> 2) & 1, gave_up)) return;
             tc_fence_after_sync();
-            const uint32_t t_s = tmem + kColS + (step & 3) * kStep;
+            const uint32_t t_s = tmem + kColS + (mine & 3) * kStep;
             uint32_t s[2][32];
             float mx = -INFINITY;
+            auto hide = [&](int c) {
+                const uint32_t see = sees == 0 ? 0u : seen_tokens(t0 + 32 * c, u.committed, u.len, sees);
+#pragma unroll
+                for (int x = 0; x < 32; ++x)
+                    if (!((see >> x) & 1)) s[c][x] = 0xff800000u;
+            };
             if (warp_live) {
-                tmem_ld32(t_s, s[0]);
-                tmem_ld32(t_s + 32, s[1]);
-                tmem_ld_wait();
-                if (ends)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const uint32_t see = sees == 0 ? 0u : seen_tokens(t0 + 32 * c, u.committed, u.len, sees);
-#pragma unroll
-                        for (int x = 0; x < 32; ++x)
-                            if (!((see >> x) & 1)) s[c][x] = 0xff800000u;
-                    }
                 float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                tmem_ld32(t_s, s[0]);
+                if constexpr (!F4) tmem_ld32(t_s + 32, s[1]);
+                tmem_ld_wait();
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
+                for (int c = 0; c < 2; ++c) {
+                    if constexpr (F4)
+                        if (c == 1) {
+                            tmem_ld32(t_s + 32, s[1]);
+                            tmem_ld_wait();
+                        }
+                    if (ends) hide(c);
 #pragma unroll
                     for (int x = 0; x < 16; ++x)
                         m4[x & 3] = fmax3(m4[x & 3], __uint_as_float(s[c][2 * x]), __uint_as_float(s[c][2 * x + 1]));
+                }
                 mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
             }
-            // the reference: the other group's, of the half before
-            if (step > 0 && !warp_wait(&sm.ref_full[group ^ 1][warp & 3], ((step - 1) >> 1) & 1, gave_up)) return;
-            const bool first = j == 0 && group == 0;
-            const float before = first ? mx : sm.ref[group ^ 1][i];
-            const bool need = !first && live && (mx - before) * unit > kRescaleAt;
+            // the reference of the step before
+            if (mine > 0 && !warp_wait(&sm.ref_full[before_me][warp & 3], (group == 0 ? turn - 1 : turn) & 1, gave_up)) return;
+            const float before = mine == unit0 ? mx : sm.ref[before_me][i];
+            const bool need = mine != unit0 && live && (mx - before) * unit > kRescaleAt;
             const float now = need ? mx : before;
             sm.ref[group][i] = now;
             mbar_arrive(&sm.ref_full[group][warp & 3]);
             if (warp_live) {
                 if (__any_sync(0xffffffffu, need)) {
-                    // the last product has left O (its barrier's turn before, step - 5, is over: these scores came behind it)
-                    if (!warp_wait(&sm.pv_done[(step - 1) & 3], ((step - 1) >> 2) & 1, gave_up)) return;
+                    // the last product has left O (its barrier's turn before, four steps back, is over: these scores came behind it)
+                    if (!warp_wait(&sm.pv_done[(mine - 1) & 3], ((mine - 1) >> 2) & 1, gave_up)) return;
                     tc_fence_after_sync();
                     const float alpha = need ? fast_exp2((before - now) * unit) : 1.f;
 #pragma unroll 1
@@ -521,6 +554,11 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
                 float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
+                    if constexpr (F4) {  // (80 registers do not hold them)
+                        tmem_ld32(t_s + 32 * c, s[c]);
+                        tmem_ld_wait();
+                        if (ends) hide(c);
+                    }
                     uint32_t pk[16];
 #pragma unroll
                     for (int x = 0; x < 16; ++x) {
@@ -530,14 +568,15 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
                         l2[x & 1] = fadd2(l2[x & 1], p);
                         pk[x] = F4 ? f16x2(p.x, p.y) : bf16x2(p.x, p.y);
                     }
-                    tmem_st16(t_s + 16 * c, pk);
+                    tmem_st16(t_s + 16 * c, pk);  // over columns that have been read
                 }
                 l += (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
                 tmem_st_wait();
             }
             tc_fence_before_sync();
-            mbar_arrive(&sm.p_full[step & 3]);
+            mbar_arrive(&sm.p_full[mine & 3]);
         }
+        unit0 = end;
         sm.stat[n_unit & 1][group][i] = make_float2(m, l);
         mbar_arrive(&sm.stat_full[n_unit & 1]);
         if (!u.more) return;
@@ -547,6 +586,7 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
 // ---- queries and results ----------------------------------------------------------------------------
 template <int D, bool F4>
 struct Rows {
+    using C = Cfg<D, F4>;
     Smem<D, F4>& sm;
     const TreeArgs& a;
     const uint32_t tmem;  // with this warp's lanes
@@ -614,104 +654,130 @@ struct Rows {
         mbar_arrive(&sm.q_full[n_unit & 1]);
     }
 
-    // The unit's rows: final ones, partial ones of a cut unit, or partial slots.
-    __device__ __forceinline__ bool finish(const Walk& w, uint32_t n_unit)
+    // Adds the values that were taken out of the operands to a row that sees them, 0 or not: whatever is added to is not finite
+    // then.  Rare, and out of the way of what is not.
+    __device__ __noinline__ static void put_back(const TreeArgs& a, const int32_t* pages, int h, int committed, unsigned long long odd,
+                                                 void* to, bool is_bf16)
     {
-        if (!row_barrier(warp_wait(&sm.stat_full[n_unit & 1], (n_unit >> 1) & 1, &sm.gave_up) &&
-                         warp_wait(&sm.o_full, n_unit & 1, &sm.gave_up)))
-            return false;
-        tc_fence_after_sync();
-        // the second group has the row's reference; the other's sum is brought to it
+#pragma unroll 1
+        for (unsigned long long left = odd; left != 0; left &= left - 1) {
+            const int t = committed + __ffsll(left) - 1, in = t & ((1 << a.kv.page_shift) - 1);
+            const int64_t page = paged_page(a.kv, pages, t >> a.kv.page_shift);
+#pragma unroll 1
+            for (int d = 0; d < D; ++d) {
+                float v;
+                if constexpr (F4) {
+                    using B = Fp4Block<D>;
+                    const uint8_t* b = a.kv.k + (((page * a.Hkv + h) << (a.kv.page_shift - 4)) + (in >> 4)) * B::kBytes;
+                    const uint16_t sc = *reinterpret_cast<const uint16_t*>(b + B::v_scale(in & 15, d / 32));
+                    if ((sc & 0x7fffu) <= 0x7154u) continue;
+                    uint32_t f[4];
+                    e2m1x8_to_f16x2(b[B::v_byte(in & 15, d & ~7) + (d & 7) / 2], f);
+                    const uint32_t x = hmul2(f[0], sc * 0x10001u);
+                    v = __half2float(__ushort_as_half((unsigned short)((d & 1) ? x >> 16 : x)));
+                } else {
+                    const uint16_t x = reinterpret_cast<const uint16_t*>(a.kv.v)[(((page << a.kv.page_shift) + in) * a.Hkv + h) * D + d];
+                    if ((x & 0x7f80u) != 0x7f80u) continue;
+                    v = __uint_as_float((uint32_t)x << 16);
+                }
+                if (is_bf16) {
+                    __nv_bfloat16* o = static_cast<__nv_bfloat16*>(to) + d;
+                    *o = __float2bfloat16_rn(__bfloat162float(*o) + v);
+                } else {
+                    static_cast<float*>(to)[d] += v;
+                }
+            }
+        }
+    }
+
+    // The unit's rows: final ones, partial ones of a cut unit, or partial slots.
+    __device__ __forceinline__ bool finish(const Walk& w, uint32_t n_unit, uint32_t last)
+    {
+        bool ok = warp_wait(&sm.stat_full[n_unit & 1], (n_unit >> 1) & 1, &sm.gave_up);
+        // the group of the last step has the row's reference; the others' sums are brought to it
         const float unit = sm.row_unit[n_unit & 1][i];
-        const float2 own = sm.stat[n_unit & 1][1][i], others = sm.stat[n_unit & 1][0][i];
-        const float m = own.x;
-        const float l = own.y + (others.x == m ? others.y : others.y * fast_exp2((others.x - m) * unit));
+        const float m = sm.stat[n_unit & 1][last % C::kGroups][i].x;
+        float l = 0.f;
+#pragma unroll
+        for (int x = 0; x < C::kGroups; ++x) {
+            const float2 part = sm.stat[n_unit & 1][x][i];
+            l += part.x == m ? part.y : part.y * fast_exp2((part.x - m) * unit);
+        }
         const int G = a.Hq / a.Hkv, node = w.node0(a) + i / G;
         const bool live = i < w.rows(a);
-        const unsigned long long bad = *static_cast<volatile unsigned long long*>(&sm.bad[n_unit & 7]);
-        const unsigned long long odd = l == 0.f ? 0 : bad & sm.sees[n_unit & 1][i];
         const int64_t row = (int64_t)(w.q.first + node) * a.Hq + w.h * G + i % G;
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const float lse = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m * unit * kLn2) + logf(l);
-        const bool whole = w.tiles == w.q.tiles, final_row = a.out != nullptr && whole;
+        const bool final_row = a.out != nullptr && w.tiles == w.q.tiles;  // (the same for all rows)
+        ok = ok && warp_wait(&sm.o_full, n_unit & 1, &sm.gave_up);
+        if (!row_barrier(ok)) return false;
+        tc_fence_after_sync();
         float *to = nullptr, *lse_to = nullptr;
-        int spare = 0;  // slots behind this one that hold nothing
-        if (a.out == nullptr) {
-            const long long per = sm.part.per, c0 = w.start / per;
-            const int k = a.n_splits == 1 ? 0 : (int)(blockIdx.x - sm.part.cta0 - c0);
-            const int parts = a.n_splits == 1 ? 1 : (int)((w.start + w.q.tiles - 1) / per - c0) + 1;
-            const int64_t slot = row * a.n_slots + a.slot0 + k;
-            to = a.o_part + slot * D;
-            lse_to = a.lse_part + slot;
-            if (k == parts - 1) spare = a.n_splits - parts;
-        } else if (!whole) {
-            const int64_t slot = (int64_t)(2 * blockIdx.x + (w.tile0 == 0 ? 1 : 0)) * kTileRows + i;
-            to = a.o_cut + slot * D;
-            lse_to = a.lse_cut + slot;
-        } else if (a.lse_out != nullptr) {
-            lse_to = a.lse_out + row;
-        }
-        const int32_t* pages = a.kv.page_table + (int64_t)w.r * a.kv.max_pages;
-#pragma unroll 1
-        for (int c = 0; c < D / 32; ++c) {
-            uint32_t o[32];
-            tmem_ld32(tmem + kColO + 32 * c, o);
-            tmem_ld_wait();
-            if (c == D / 32 - 1) {  // O may be written again
-                tc_fence_before_sync();
-                mbar_arrive(&sm.o_free);
+        if (final_row) {
+            uint32_t y[D / 2];
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t o[32];
+                tmem_ld32(tmem + kColO + 32 * c, o);
+                tmem_ld_wait();
+                // (a row that has seen nothing: its O is 0 or was never written)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    y[16 * c + e] = l == 0.f ? 0u : bf16x2(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
             }
-            float x[32];
+            tc_fence_before_sync();
+            mbar_arrive(&sm.o_free);  // O may be written again
+            if (live)
 #pragma unroll
-            for (int e = 0; e < 32; ++e) x[e] = l == 0.f ? 0.f : __uint_as_float(o[e]) * inv;
-            for (unsigned long long left = odd; left != 0; left &= left - 1) {  // values that were taken out
-                const int t = w.committed() + __ffsll(left) - 1, in = t & ((1 << a.kv.page_shift) - 1);
-                const int64_t page = paged_page(a.kv, pages, t >> a.kv.page_shift);
-                if constexpr (F4) {
-                    using B = Fp4Block<D>;
-                    const uint8_t* b = a.kv.k + (((page * a.Hkv + w.h) << (a.kv.page_shift - 4)) + (in >> 4)) * B::kBytes;
-                    const uint32_t sc = *reinterpret_cast<const uint16_t*>(b + B::v_scale(in & 15, c));
-                    if ((sc & 0x7fffu) <= 0x7154u) continue;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        uint32_t f[4];
-                        e2m1x8_to_f16x2(*reinterpret_cast<const uint32_t*>(b + B::v_byte(in & 15, 32 * c + 8 * e)), f);
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) {
-                            const uint32_t v = hmul2(f[y], sc * 0x10001u);
-                            x[8 * e + 2 * y] += __half2float(__ushort_as_half((unsigned short)v));
-                            x[8 * e + 2 * y + 1] += __half2float(__ushort_as_half((unsigned short)(v >> 16)));
-                        }
-                    }
-                } else {
-                    const uint16_t* v = reinterpret_cast<const uint16_t*>(a.kv.v) +
-                                        (((page << a.kv.page_shift) + in) * a.Hkv + w.h) * D + 32 * c;
-#pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if ((v[e] & 0x7f80u) == 0x7f80u) x[e] += __uint_as_float((uint32_t)v[e] << 16);
-                }
-            }
-            if (!live) continue;
-            if (final_row) {
-                uint4* p = reinterpret_cast<uint4*>(a.out + row * D + 32 * c);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    p[e] = make_uint4(bf16x2(x[8 * e], x[8 * e + 1]), bf16x2(x[8 * e + 2], x[8 * e + 3]),
-                                      bf16x2(x[8 * e + 4], x[8 * e + 5]), bf16x2(x[8 * e + 6], x[8 * e + 7]));
+                for (int e = 0; e < D / 8; ++e)
+                    reinterpret_cast<uint4*>(a.out + row * D)[e] = make_uint4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
+            if (a.lse_out != nullptr) lse_to = a.lse_out + row;
+        } else {
+            int spare = 0;  // slots behind this one that hold nothing
+            if (a.out == nullptr) {
+                const int c0 = w.first_cta(sm.part);
+                const int k = a.n_splits == 1 ? 0 : (int)blockIdx.x - sm.part.cta0 - c0;
+                const int parts = a.n_splits == 1 ? 1 : w.last_cta(sm.part) - c0 + 1;
+                const int64_t slot = row * a.n_slots + a.slot0 + k;
+                to = a.o_part + slot * D;
+                lse_to = a.lse_part + slot;
+                if (k == parts - 1) spare = a.n_splits - parts;
             } else {
+                const int64_t slot = (int64_t)(2 * blockIdx.x + (w.tile0 == 0 ? 1 : 0)) * kTileRows + i;
+                to = a.o_cut + slot * D;
+                lse_to = a.lse_cut + slot;
+            }
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t o[32];
+                tmem_ld32(tmem + kColO + 32 * c, o);
+                tmem_ld_wait();
                 float4* p = reinterpret_cast<float4*>(to + 32 * c);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) p[e] = make_float4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
-                for (int k = 1; k <= spare; ++k)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        reinterpret_cast<float4*>(to + k * D + 32 * c)[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int e = 0; e < 8; ++e) {
+                    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (l != 0.f)
+                        x = make_float4(__uint_as_float(o[4 * e]) * inv, __uint_as_float(o[4 * e + 1]) * inv,
+                                        __uint_as_float(o[4 * e + 2]) * inv, __uint_as_float(o[4 * e + 3]) * inv);
+                    if (live) p[e] = x;
+                }
             }
+            tc_fence_before_sync();
+            mbar_arrive(&sm.o_free);
+            if (live)
+#pragma unroll 1
+                for (int k = 1; k <= spare; ++k) {
+                    lse_to[k] = -INFINITY;
+#pragma unroll 1
+                    for (int d = 0; d < D; d += 4) *reinterpret_cast<float4*>(to + k * D + d) = make_float4(0.f, 0.f, 0.f, 0.f);
+                }
         }
-        if (live && lse_to != nullptr) {
-            *lse_to = lse;
-            for (int k = 1; k <= spare; ++k) lse_to[k] = -INFINITY;
-        }
+        if (live && lse_to != nullptr) *lse_to = lse;
+        const unsigned long long odd =
+            l == 0.f ? 0 : *static_cast<volatile unsigned long long*>(&sm.bad[n_unit & 7]) & sm.sees[n_unit & 1][i];
+        if (live && odd != 0)
+            put_back(a, a.kv.page_table + (int64_t)w.r * a.kv.max_pages, w.h, w.committed(), odd,
+                     final_row ? static_cast<void*>(a.out + row * D) : to, final_row);
         row_barrier();  // all have read `bad`
         if (i == 0) sm.bad[n_unit & 7] = 0;
         return true;
@@ -723,6 +789,7 @@ struct Rows {
         Walk after = w;
         bool more = after.next(a, sm.part);
         prepare(w, true, more, 0);
+        uint32_t steps = 0;
         for (uint32_t n_unit = 0;; ++n_unit) {
             Walk then = after;
             const bool go_on = more;
@@ -730,7 +797,8 @@ struct Rows {
                 more = then.next(a, sm.part);
                 prepare(after, after.r != w.r, more, n_unit + 1);
             }
-            if (!finish(w, n_unit) || !go_on) return;
+            steps += 2 * w.tiles;
+            if (!finish(w, n_unit, steps - 1) || !go_on) return;
             w = after;
             after = then;
         }
@@ -779,44 +847,40 @@ __device__ __forceinline__ void load_role(Smem<D, F4>& sm, const CUtensorMap& tm
             }
         } else {
             using B = Fp4Block<D>;
-            // units: the key parts of a tile, then its value parts; lane 2 b + c copies block b's codes (c = 0) or scales
-            const int b = lane >> 1, c = lane & 1;
+            // A page's blocks of a head are neighbours: one copy of min(page_size, 128) tokens, up to the context's last block.
+            // (Copies of key and value parts, block by block, kept the tensor cores waiting: a copy costs its warp about 60 cycles.)
+            const int box = min(kTile, 1 << shift), boxes = kTile / box;
             const int64_t page_bytes = ((int64_t)a.Hkv << (shift - 4)) * B::kBytes;
             const uint8_t* pool = a.kv.k + ((int64_t)w.h << (shift - 4)) * B::kBytes;
             auto page_of = [&](int j) {
-                const int t = (w.tile0 + j) * kTile + 16 * b;
-                return lane < 2 * C::kBlocks && j < w.tiles && t < w.q.len ? paged_page(a.kv, pages, t >> shift) : -1;
+                const int t = (w.tile0 + j) * kTile + lane * box;
+                return lane < boxes && j < w.tiles && t < w.q.len ? paged_page(a.kv, pages, t >> shift) : -1;
             };
             int ahead = page_of(0);
-            for (int j = 0; j < w.tiles && ok; ++j) {
+            for (int j = 0; j < w.tiles; ++j) {
                 const int page = ahead;
                 ahead = page_of(j + 1);
-                const int t = (w.tile0 + j) * kTile + 16 * b;
-                const int there = __popc(__ballot_sync(0xffffffffu, page >= 0)) / 2;
-                const uint8_t* from = pool + page * page_bytes + (int64_t)((t & ((1 << shift) - 1)) >> 4) * B::kBytes;
-#pragma unroll
-                for (int kind = 0; kind < 2; ++kind) {
-                    const uint32_t u = seq % C::kUnits;
-                    if (seq >= C::kUnits) ok = warp_wait(&sm.unit_empty[u], ((seq / C::kUnits) - 1) & 1, &sm.gave_up);
-                    if (!ok) break;
-                    if (lane == 0) mbar_arrive_expect_tx(&sm.unit_full[u], there * C::kPartBytes);
-                    __syncwarp();
-                    if (page >= 0) {
-                        const int at = c == 0 ? (kind == 0 ? 0 : B::kV) : (kind == 0 ? B::kKScale : B::kVScale);
-                        bulk_load(sm.unit + u * C::kUnitBytes + b * C::kPartBytes + (c == 0 ? 0 : 8 * D), from + at,
-                                  c == 0 ? 8 * D : D, &sm.unit_full[u]);
-                    }
-                    ++seq;
-                }
+                const int t0 = (w.tile0 + j) * kTile, t = t0 + lane * box;
+                const uint32_t s = seq % C::kCodeSlots;
+                if (seq >= C::kCodeSlots) ok = warp_wait(&sm.code_empty[s], ((seq / C::kCodeSlots) - 1) & 1, &sm.gave_up);
+                if (!ok) break;
+                const int there = (min(kTile, w.q.len - t0) + 15) >> 4;  // blocks (0: an empty context)
+                if (lane == 0) mbar_arrive_expect_tx(&sm.code_full[s], max(0, there) * B::kBytes);
+                __syncwarp();
+                if (page >= 0)
+                    bulk_load(sm.code + s * C::kCodeBytes + lane * (box >> 4) * B::kBytes,
+                              pool + page * page_bytes + (int64_t)((t & ((1 << shift) - 1)) >> 4) * B::kBytes,
+                              min(box >> 4, there - lane * (box >> 4)) * B::kBytes, &sm.code_full[s]);
+                ++seq;
             }
         }
     } while (ok && w.next(a, sm.part));
     if (*static_cast<volatile int*>(&sm.gave_up)) {
         // the copies in flight end before the CTA leaves (each wait again has a limit)
-        constexpr uint32_t kRing = F4 ? C::kUnits : C::kSlots;
+        constexpr uint32_t kRing = F4 ? C::kCodeSlots : C::kSlots;
         for (uint32_t x = seq > kRing ? seq - kRing : 0; x < seq; ++x) {
             int never = 0;
-            mbar_wait(F4 ? &sm.unit_full[x % kRing] : &sm.full[x % kRing], (x / kRing) & 1, &never);
+            mbar_wait(F4 ? &sm.code_full[x % kRing] : &sm.full[x % kRing], (x / kRing) & 1, &never);
         }
     }
 }
@@ -892,111 +956,117 @@ __device__ __forceinline__ void value_role(Smem<D, F4>& sm, uint32_t tmem)
     }
 }
 
-// ---- 4 bits: codes of every fourth block of a tile (a warp) -> f16 operand rows ------------------------
+// ---- 4 bits: codes -> f16 operand rows ----------------------------------------------------------------
+// Keys of two blocks.  The D / 8 bytes of (token, c) are dimensions 32 x + 8 c .. + 7 for each group x.  Eight lanes that
+// go to memory together have tokens y and y ^ 5: their loads and their swizzled stores both fall on eight different
+// 16-byte pieces of the banks.
+template <int D>
+__device__ __forceinline__ void widen_keys(const uint8_t* code_tile, uint8_t* to, int block0, int lane)
+{
+    using B = Fp4Block<D>;
+    constexpr int J = D / 32;
+    const int l = lane & 7, c = l & 3, qd = lane >> 3, token = (l >> 2) ? (qd ^ 5) : qd;
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+        const int block = block0 + (it >> 1), t = 8 * (it & 1) + token, row = 16 * block + t;
+        const uint8_t* from = code_tile + block * B::kBytes;
+        uint32_t code[J], sc[J / 2];
+        if constexpr (J == 4) {
+            const uint4 x = *reinterpret_cast<const uint4*>(from + t * (D / 2) + c * (D / 8));
+            code[0] = x.x; code[1] = x.y; code[2] = x.z; code[3] = x.w;
+            const uint2 y = *reinterpret_cast<const uint2*>(from + B::k_scale(t, 0));
+            sc[0] = y.x; sc[1] = y.y;
+        } else {
+            const uint2 x = *reinterpret_cast<const uint2*>(from + t * (D / 2) + c * (D / 8));
+            code[0] = x.x; code[1] = x.y;
+            sc[0] = *reinterpret_cast<const uint32_t*>(from + B::k_scale(t, 0));
+        }
+#pragma unroll
+        for (int x = 0; x < J; ++x) {
+            uint32_t f[4];
+            e2m1x8_to_f16x2(code[x], f);
+            const uint32_t s2 = __byte_perm(sc[x >> 1], 0, (x & 1) ? 0x3232 : 0x1010);
+            *reinterpret_cast<uint4*>(to + (x >> 1) * kHalfBytes + row * 128 + (((4 * (x & 1) + c) ^ (row & 7)) << 4)) =
+                make_uint4(hmul2(f[0], s2), hmul2(f[1], s2), hmul2(f[2], s2), hmul2(f[3], s2));
+        }
+    }
+}
+
+// Values of two blocks.  Chunk x (D / 8 dimensions) of a pair of tokens: first token's bytes, then the second's.  In a tile that
+// reaches past the committed tokens (`ends`; `behind`: its first token's place behind them) values behind the context are 0, and those
+// with a scale above what appends write, infinities and NaN included, are taken out.
+template <int D>
+__device__ __forceinline__ void widen_values(const uint8_t* code_tile, uint8_t* to, int block0, int lane, bool ends, int behind, int nodes,
+                                             unsigned long long* bad)
+{
+    using B = Fp4Block<D>;
+    constexpr int W = D / 64;  // words of a token's chunk
+    const int x = lane & 7, other = x >> 2;
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+        const int block = block0 + (it >> 1), p = 4 * (it & 1) + (lane >> 3);
+        const uint8_t* from = code_tile + block * B::kBytes;
+        const uint8_t* at = from + B::kV + p * D + (x ^ B::v_swap(p)) * (D / 8);
+        uint32_t code[2 * W];
+        if constexpr (W == 2) {
+            const uint4 y = *reinterpret_cast<const uint4*>(at);
+            // (lanes of the other half of the dimensions store their pieces the other way round: different banks)
+            code[0] = other ? y.y : y.x; code[1] = other ? y.x : y.y;
+            code[2] = other ? y.w : y.z; code[3] = other ? y.z : y.w;
+        } else {
+            const uint2 y = *reinterpret_cast<const uint2*>(at);
+            code[0] = y.x; code[1] = y.y;
+        }
+        const uint32_t sc = *reinterpret_cast<const uint32_t*>(from + B::v_scale(2 * p, x * (D / 8) / 32));
+#pragma unroll
+        for (int tok = 0; tok < 2; ++tok) {
+            const int row = 16 * block + 2 * p + tok;
+            uint32_t s2 = __byte_perm(sc, 0, tok ? 0x3232 : 0x1010);
+            if (ends && behind + row >= 0) {
+                if (behind + row >= nodes) {
+                    s2 = 0;
+                } else if ((s2 & 0x7fffu) > 0x7154u) {
+                    atomicOr(bad, 1ull << (behind + row));
+                    s2 = 0;
+                }
+            }
+            uint8_t* base = to + (W == 2 ? other * kHalfBytes : 0) + row * 128;
+#pragma unroll
+            for (int y = 0; y < W; ++y) {
+                uint32_t f[4];
+                e2m1x8_to_f16x2(code[tok * W + y], f);
+                const int piece = W == 2 ? 2 * (x & 3) + (y ^ other) : x;
+                *reinterpret_cast<uint4*>(base + ((piece ^ (row & 7)) << 4)) =
+                    make_uint4(hmul2(f[0], s2), hmul2(f[1], s2), hmul2(f[2], s2), hmul2(f[3], s2));
+            }
+        }
+    }
+}
+
+// Four warps widen keys and four values, two blocks each.
 template <int D>
 __device__ __forceinline__ void widen_role(Smem<D, true>& sm, const TreeArgs& a, Walk w, int warp, int lane)
 {
     using C = Cfg<D, true>;
-    constexpr int J = D / 32;
+    static_assert(C::kWidenWarps == C::kBlocks, "two blocks a warp, of keys or of values");
     int* gave_up = &sm.gave_up;
-    uint32_t seq = 0, n_unit = 0;
+    const bool values = warp >= 4;
+    const int block0 = 2 * (warp & 3);
+    uint32_t tile = 0, n_unit = 0;
     do {
-        for (int j = 0; j < w.tiles; ++j) {
-            const int t0 = (w.tile0 + j) * kTile;
-            const bool ends = t0 + kTile > w.committed();
-#pragma unroll
-            for (int kind = 0; kind < 2; ++kind, ++seq) {
-                const uint32_t s = seq % C::kSlots, u = seq % C::kUnits;
-                if (seq >= C::kSlots && !warp_wait(&sm.empty[s], ((seq / C::kSlots) - 1) & 1, gave_up)) return;
-                if (!warp_wait(&sm.unit_full[u], (seq / C::kUnits) & 1, gave_up)) return;
-                uint8_t* to = sm.slot[s];
-#pragma unroll
-                for (int block = warp; block < C::kBlocks; block += kWidenWarps) {
-                const uint8_t* from = sm.unit + u * C::kUnitBytes + block * C::kPartBytes;
-                const int row0 = 16 * block;
-                if (kind == 0) {
-                    // Keys: the D / 8 bytes of (token, c) are dimensions 32 x + 8 c .. + 7 for each group x.  Eight lanes that
-                    // go to memory together have tokens y and y ^ 5: their loads and their swizzled stores both fall on
-                    // eight different 16-byte pieces of the banks.
-#pragma unroll
-                    for (int it = 0; it < 2; ++it) {
-                        const int l = lane & 7, c = l & 3, qd = lane >> 3, t = 8 * it + ((l >> 2) ? (qd ^ 5) : qd);
-                        uint32_t code[J], sc[J / 2];
-                        if constexpr (J == 4) {
-                            const uint4 x = *reinterpret_cast<const uint4*>(from + t * (D / 2) + c * (D / 8));
-                            code[0] = x.x; code[1] = x.y; code[2] = x.z; code[3] = x.w;
-                            const uint2 y = *reinterpret_cast<const uint2*>(from + 8 * D + 2 * t * J);
-                            sc[0] = y.x; sc[1] = y.y;
-                        } else {
-                            const uint2 x = *reinterpret_cast<const uint2*>(from + t * (D / 2) + c * (D / 8));
-                            code[0] = x.x; code[1] = x.y;
-                            sc[0] = *reinterpret_cast<const uint32_t*>(from + 8 * D + 2 * t * J);
-                        }
-                        const int row = row0 + t;
-#pragma unroll
-                        for (int x = 0; x < J; ++x) {
-                            uint32_t f[4];
-                            e2m1x8_to_f16x2(code[x], f);
-                            const uint32_t s2 = __byte_perm(sc[x >> 1], 0, (x & 1) ? 0x3232 : 0x1010);
-                            *reinterpret_cast<uint4*>(to + (x >> 1) * kHalfBytes + row * 128 + (((4 * (x & 1) + c) ^ (row & 7)) << 4)) =
-                                make_uint4(hmul2(f[0], s2), hmul2(f[1], s2), hmul2(f[2], s2), hmul2(f[3], s2));
-                        }
-                    }
-                } else {
-                    // Values: chunk x (D / 8 dimensions) of a pair of tokens, first token's bytes, then the second's
-#pragma unroll
-                    for (int it = 0; it < 2; ++it) {
-                        const int x = lane & 7, p = 4 * it + (lane >> 3);
-                        constexpr int W = D / 64;  // words of a token's chunk
-                        uint32_t code[2 * W];
-                        const uint8_t* at = from + p * D + (x ^ Fp4Block<D>::v_swap(p)) * (D / 8);
-                        if constexpr (W == 2) {
-                            const uint4 y = *reinterpret_cast<const uint4*>(at);
-                            code[0] = y.x; code[1] = y.y; code[2] = y.z; code[3] = y.w;
-                        } else {
-                            const uint2 y = *reinterpret_cast<const uint2*>(at);
-                            code[0] = y.x; code[1] = y.y;
-                        }
-                        const uint32_t sc = *reinterpret_cast<const uint32_t*>(from + 8 * D + 2 * ((x * (D / 8) / 32) * 16 + 2 * p));
-#pragma unroll
-                        for (int tok = 0; tok < 2; ++tok) {
-                            const int row = row0 + 2 * p + tok, behind = t0 + row - w.committed();
-                            uint32_t s1 = tok == 0 ? sc & 0xffffu : sc >> 16;
-                            if (ends && behind >= 0) {
-                                if (behind >= w.q.nodes) {  // behind the context
-                                    s1 = 0;
-                                } else if ((s1 & 0x7fffu) > 0x7154u) {  // above what appends write, infinities and NaN included
-                                    atomicOr(&sm.bad[n_unit & 7], 1ull << behind);
-                                    s1 = 0;
-                                }
-                            }
-                            const uint32_t s2 = s1 * 0x10001u;
-                            uint4 v[W];
-#pragma unroll
-                            for (int y = 0; y < W; ++y) {
-                                uint32_t f[4];
-                                e2m1x8_to_f16x2(code[tok * W + y], f);
-                                v[y] = make_uint4(hmul2(f[0], s2), hmul2(f[1], s2), hmul2(f[2], s2), hmul2(f[3], s2));
-                            }
-                            if constexpr (W == 2) {
-                                // (lanes of the other half store their pieces the other way round: different banks)
-                                const int other = x >> 2, piece = 2 * (x & 3);
-                                uint8_t* base = to + other * kHalfBytes + row * 128;
-                                *reinterpret_cast<uint4*>(base + (((piece + other) ^ (row & 7)) << 4)) = other ? v[W - 1] : v[0];
-                                *reinterpret_cast<uint4*>(base + (((piece + 1 - other) ^ (row & 7)) << 4)) = other ? v[0] : v[W - 1];
-                            } else {
-                                *reinterpret_cast<uint4*>(to + row * 128 + ((x ^ (row & 7)) << 4)) = v[0];
-                            }
-                        }
-                    }
-                }
-                }
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(&sm.unit_empty[u]);
-                    mbar_arrive(&sm.full[s]);
-                }
+        for (int j = 0; j < w.tiles; ++j, ++tile) {
+            const int behind = (w.tile0 + j) * kTile - w.committed();
+            const uint32_t seq = 2 * tile + values, s = seq % C::kSlots, c = tile % C::kCodeSlots;
+            if (!warp_wait(&sm.code_full[c], (tile / C::kCodeSlots) & 1, gave_up)) return;
+            if (seq >= C::kSlots && !warp_wait(&sm.empty[s], ((seq / C::kSlots) - 1) & 1, gave_up)) return;
+            const uint8_t* from = sm.code + c * C::kCodeBytes;
+            if (values) widen_values<D>(from, sm.slot[s], block0, lane, behind + kTile > 0, behind, w.q.nodes, &sm.bad[n_unit & 7]);
+            else widen_keys<D>(from, sm.slot[s], block0, lane);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(&sm.full[s]);
+                mbar_arrive(&sm.code_empty[c]);
             }
         }
         ++n_unit;
@@ -1016,22 +1086,23 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         if (tid == 0) atomicMin(a.kv.status, (int)MOSKA_ERR_CUDA);
         return;
     }
-    if (warp < kRowWarp0) {
+    if (tid < kFindThreads) {
         find_part(a, blockIdx.x, gridDim.x, sm.part);
-    } else if (warp == kLoadWarp && lane == 0) {
+    } else if (warp == C::kLoadWarp && lane == 0) {
         for (int s = 0; s < C::kSlots; ++s) {
-            mbar_init(&sm.full[s], F4 ? kWidenWarps : 1);
+            mbar_init(&sm.full[s], F4 ? C::kWidenWarps / 2 : 1);
             mbar_init(&sm.empty[s], 1);
         }
-        for (int u = 0; u < C::kUnits; ++u) {
-            mbar_init(&sm.unit_full[u], 1);
-            mbar_init(&sm.unit_empty[u], kWidenWarps);
+        for (int x = 0; x < C::kCodeSlots; ++x) {
+            mbar_init(&sm.code_full[x], 1);
+            mbar_init(&sm.code_empty[x], C::kWidenWarps);
         }
         for (int x = 0; x < 2; ++x) {
             mbar_init(&sm.q_full[x], kTileRows);
-            mbar_init(&sm.stat_full[x], kSoftmaxThreads);
-            for (int y = 0; y < 4; ++y) mbar_init(&sm.ref_full[x][y], 32);
+            mbar_init(&sm.stat_full[x], C::kGroups * kTileRows);
         }
+        for (int x = 0; x < C::kGroups; ++x)
+            for (int y = 0; y < 4; ++y) mbar_init(&sm.ref_full[x][y], 32);
         for (int x = 0; x < 4; ++x) {
             mbar_init(&sm.s_full[x], 1);
             mbar_init(&sm.p_full[x], kTileRows);
@@ -1043,7 +1114,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         sm.gave_up = 0;
         fence_mbar_init();
         fence_proxy_async_smem();
-    } else if (warp == kScoreWarp) {
+    } else if (warp == C::kScoreWarp) {
         tmem_alloc(&sm.tmem_base, 512);
         tmem_relinquish();
     }
@@ -1057,24 +1128,28 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     if (w.begin(a, sm.part)) {
         const uint32_t lanes = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
         const int row = (warp & 3) * 32 + lane;
-        if (warp < kRowWarp0) {
+        if (warp < C::kRowWarp0) {
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kSoftmaxRegs));
             softmax_role<D, F4>(sm, lanes, warp >> 2, warp, row);
-        } else if (warp < kLoadWarp) {
+        } else if (warp < C::kLoadWarp) {
+            if constexpr (C::kRowRegs > C::kLaunchRegs) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRowRegs));
             Rows<D, F4>{sm, a, lanes, row}.run(w);
-        } else if (warp == kLoadWarp) {
-            load_role<D, F4>(sm, tm_k, tm_v, a, w, lane);
-        } else if (warp == kScoreWarp) {
-            score_role<D, F4>(sm, tmem);
-        } else if (warp == kValueWarp) {
-            value_role<D, F4>(sm, tmem);
+        } else if (warp < C::kWidenWarp0) {
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kIssueRegs));
+            if (warp == C::kLoadWarp) load_role<D, F4>(sm, tm_k, tm_v, a, w, lane);
+            else if (warp == C::kScoreWarp) score_role<D, F4>(sm, tmem);
+            else if (warp == C::kValueWarp) value_role<D, F4>(sm, tmem);
         } else {
-            if constexpr (F4) widen_role<D>(sm, a, w, warp - kWidenWarp0, lane);
+            if constexpr (F4) {
+                asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kWidenRegs));
+                widen_role<D>(sm, a, w, warp - C::kWidenWarp0, lane);
+            }
         }
     }
     __syncwarp();
     tc_fence_before_sync();
     __syncthreads();
-    if (warp == kScoreWarp) tmem_dealloc(tmem, 512);
+    if (warp == C::kScoreWarp) tmem_dealloc(tmem, 512);
     if (tid == 0 && sm.gave_up) atomicMin(a.kv.status, (int)MOSKA_ERR_TIMEOUT);
 }
 
@@ -1082,7 +1157,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
 // ..; a unit's first cut has it, and its CTAs have 16 rows each, two a warp.
 constexpr int kJoinCtas = 8;
 template <int D>
-__global__ void __launch_bounds__(kSoftmaxThreads) tree_join_kernel(const TreeArgs a, int ctas)
+__global__ void __launch_bounds__(kFindThreads) tree_join_kernel(const TreeArgs a, int ctas)
 {
     __shared__ Part part;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x / kJoinCtas + 1;
@@ -1091,7 +1166,7 @@ __global__ void __launch_bounds__(kSoftmaxThreads) tree_join_kernel(const TreeAr
     Walk w;
     wait_for_results();
     if (!w.begin(a, part) || w.tile0 == 0) return;
-    const int c0 = part.cta0 + (int)(w.start / part.per), c1 = part.cta0 + (int)((w.start + w.q.tiles - 1) / part.per);
+    const int c0 = part.cta0 + w.first_cta(part), c1 = part.cta0 + w.last_cta(part);
     if (cta != c0 + 1) return;
     const int G = a.Hq / a.Hkv, rows = w.rows(a);
     constexpr int W = D / 32;  // dimensions a lane
@@ -1208,6 +1283,7 @@ int launch_tree_attn(const uint16_t* q, const PagedView& kv, bool fp4, const Tre
     const int G = s->Hq / s->Hkv, per_tile = kTileRows / G, row_tiles = (tree.max_nodes + per_tile - 1) / per_tile;
     if (((long long)kv.n_pages << kv.page_shift) > 0x7fffffffLL)
         return fail(MOSKA_ERR_UNSUPPORTED, "a pool of more than 2^31 tokens");
+    if (tree.n_requests >= 1 << (62 - kUnitBit)) return fail(MOSKA_ERR_UNSUPPORTED, "%d requests", tree.n_requests);
     TreeArgs a{q, kv, tree, o_part, lse_part, out, lse_out, nullptr, nullptr, scale, s->Hq, s->Hkv, s->n_unique_splits, slot0,
                n_slots, row_tiles, per_tile};
     if (ws != nullptr) {
@@ -1242,7 +1318,7 @@ int launch_tree_attn(const uint16_t* q, const PagedView& kv, bool fp4, const Tre
     if (out == nullptr || s->n_unique_splits == 1 || ctas < 2) return MOSKA_OK;
     cudaLaunchConfig_t config{};
     config.gridDim = dim3((unsigned)(kJoinCtas * (ctas - 1)));
-    config.blockDim = dim3(kSoftmaxThreads);
+    config.blockDim = dim3(kFindThreads);
     config.stream = st;
     cudaLaunchAttribute early{};
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
