@@ -51,6 +51,7 @@ constexpr int kMaxRowTiles = 4;  // 64 nodes of up to 8 heads
 constexpr int kMaxCtas = 148;    // parts of the line of tiles
 constexpr uint32_t kColO = 0, kColS = 128, kColQ = 384;  // tensor-memory columns
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kStagePitch = 144;  // 128 bytes and 16: a row's pieces and a piece's rows both fall on different banks
 constexpr float kRescaleAt = 8.f;  // log2 units that a row's maximum may grow before its sums are rescaled
 
 template <int D, bool F4>
@@ -62,21 +63,26 @@ struct Cfg {
     static constexpr int kThreads = 32 * (F4 ? kWidenWarp0 + kWidenWarps : kWidenWarp0);
     // Registers of a thread: at the launch, and of the groups of four warps after it.
     static constexpr int kLaunchRegs = F4 ? 80 : 128;
-    static constexpr int kSoftmaxRegs = F4 ? 112 : 152, kRowRegs = F4 ? 112 : 128, kIssueRegs = F4 ? 40 : 80, kWidenRegs = 48;
+    static constexpr int kSoftmaxRegs = F4 ? 112 : 152, kRowRegs = F4 ? 96 : 128, kIssueRegs = F4 ? 40 : 80, kWidenRegs = 56;
     static_assert(128 * (kGroups * kSoftmaxRegs + kRowRegs + kIssueRegs + (F4 ? 2 * kWidenRegs : 0)) <= kThreads * kLaunchRegs,
                   "setmaxnreg: more than the CTA was launched with would be waited for without end");
     static constexpr int kSlotBytes = kHalves * kHalfBytes;
     static constexpr int kSlots = F4 ? (D == 128 ? 4 : 8) : (D == 128 ? 6 : 12);
     static constexpr int kBlocks = kTile / kBlockTokens;  // 16-token blocks of a tile
     static constexpr int kCodeBytes = kBlocks * fp4_block_bytes(D);
-    static constexpr int kCodeSlots = F4 ? (D == 128 ? 4 : 8) : 1;
+    static constexpr int kCodeSlots = F4 ? (D == 128 ? 3 : 6) : 1;
 };
 
+// Tiles of request r's context (an empty one counts as one, so that its rows are written) and its row tiles.
+struct Request {
+    int first, nodes, len, tiles, row_tiles;
+};
 // A CTA's part of the line of its row tile.
 struct Part {
     long long p0, p1, per;  // tiles p0 .. p1 - 1; `per` in a full part
     long long start;        // first tile of the unit that p0 is in: (row tile, request, head)
     int rt, r, h;
+    Request q;
     int cta0;               // the line's first CTA
     int cost;               // of a unit, in tiles
     int longest[kFindThreads / 32];
@@ -98,6 +104,8 @@ struct Smem {
     UnitInfo info[2];                // units take turns
     unsigned long long sees[2][kTileRows];
     float row_unit[2][kTileRows];
+    uint8_t stage[4][32][kStagePitch];  // pieces of 128 bytes of each warp's rows, on their way to and from global memory
+    void* row_to[4][32];                // where the rows of a unit go
     TreeSmem tree;
     uint64_t full[C::kSlots], empty[C::kSlots];
     uint64_t code_full[C::kCodeSlots], code_empty[C::kCodeSlots];
@@ -248,15 +256,16 @@ __device__ __forceinline__ bool elect_one()
 }
 
 // ---- the line of tiles ------------------------------------------------------------------------------
-// Tiles of request r's context (an empty one counts as one, so that its rows are written) and its row tiles.
-struct Request {
-    int first, nodes, len, tiles, row_tiles;
-};
 // On the line a unit is longer than its tiles by what its beginning and its end cost, in tiles; where parts are short
 // (few tiles in all, or latency counts) by nothing.
 constexpr int kUnitCost = 2, kShortPart = 16;
 // Tiles and units of a stretch of requests in one number.
 constexpr int kUnitBit = 40;
+// (64-bit divisions are long: 32 bits where they do)
+__device__ __forceinline__ long long divide(long long a, long long b)
+{
+    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
 __device__ __forceinline__ long long places(long long packed, int cost)
 {
     return (packed & ((1ll << kUnitBit) - 1)) + (packed >> kUnitBit) * cost;
@@ -324,7 +333,7 @@ __device__ __forceinline__ void find_part(const TreeArgs& a, int cta, int ctas, 
 #pragma unroll
     for (int k = kMaxRowTiles - 1; k > 0; --k) {
         if (line[k] == 0 || rt != 0) continue;
-        const int c = max(1, (int)(ctas * places(line[k], cost) / total));
+        const int c = max(1, (int)divide(ctas * places(line[k], cost), total));
         n -= c;
         if (cta >= n) {
             rt = k;
@@ -335,8 +344,8 @@ __device__ __forceinline__ void find_part(const TreeArgs& a, int cta, int ctas, 
     }
     const long long all = places(mine_all, cost) * a.Hkv;
     // equal parts, in each at least one tile of a unit that begins in it; no unit in more of them than there may be
-    long long per = (all + n - 1) / n;
-    if (a.n_splits > 1) per = max(per, (long long)(longest + cost + a.n_splits - 2) / (a.n_splits - 1));
+    long long per = divide(all + n - 1, n);
+    if (a.n_splits > 1) per = max(per, (long long)((longest + cost + a.n_splits - 2) / (a.n_splits - 1)));
     per = max((long long)cost + 1, per);
     const long long p0 = (cta - cta0) * per, p1 = min(all, p0 + per);
     if (i == 0) {
@@ -360,7 +369,8 @@ __device__ __forceinline__ void find_part(const TreeArgs& a, int cta, int ctas, 
             const long long long_is = q.tiles + cost;
             if (p0 < at + long_is * a.Hkv) {
                 part.r = r;
-                part.h = (int)((p0 - at) / long_is);
+                part.q = q;
+                part.h = (int)divide(p0 - at, long_is);
                 part.start = at + part.h * long_is;
                 break;
             }
@@ -383,8 +393,8 @@ struct Walk {
         return min(a.nodes_per_tile, q.nodes - node0(a)) * (a.Hq / a.Hkv);
     }
     // first and last CTA that has tiles of the unit (from the line's first)
-    __device__ __forceinline__ int first_cta(const Part& p) const { return (int)((start + p.cost) / p.per); }
-    __device__ __forceinline__ int last_cta(const Part& p) const { return (int)((start + p.cost + q.tiles - 1) / p.per); }
+    __device__ __forceinline__ int first_cta(const Part& p) const { return (int)divide(start + p.cost, p.per); }
+    __device__ __forceinline__ int last_cta(const Part& p) const { return (int)divide(start + p.cost + q.tiles - 1, p.per); }
     // false if none of its tiles is in this part
     __device__ __forceinline__ bool cut(const TreeArgs& a, const Part& p)
     {
@@ -417,7 +427,7 @@ struct Walk {
         r = p.r;
         h = p.h;
         start = p.start;
-        q = request_of(a, r);
+        q = p.q;
         if (a.n_splits == 1 && start < p.p0) return next(a, p);
         return cut(a, p);
     }
@@ -450,19 +460,25 @@ __device__ __forceinline__ bool clean_values(Smem<D, false>& sm, const UnitInfo&
     if (behind >= 0) {
         // 16-byte pieces: of a half of the dimensions (D = 128), every second one (D = 64)
         uint8_t* at = sm.slot[seq % C::kSlots] + (C::kHalves == 2 ? (i >> 6) * kHalfBytes : 0) + ((step & 1) * kStep + token) * 128;
-#pragma unroll 1
+#pragma unroll 4
         for (int x = C::kHalves == 2 ? 0 : i >> 6; x < 8; x += C::kHalves == 2 ? 1 : 2) {
             uint4* p = reinterpret_cast<uint4*>(at + (((x + i) & 7) << 4));
-            const uint4 v = t < u.len ? *p : make_uint4(0, 0, 0, 0);
+            if (t >= u.len) {
+                *p = make_uint4(0, 0, 0, 0);
+                continue;
+            }
+            const uint4 v = *p;
+            const uint32_t m = 0x7fff7fffu;
+            const uint32_t top = __vmaxu2(__vmaxu2(v.x & m, v.y & m), __vmaxu2(v.z & m, v.w & m));
+            if (__vmaxu2(top, 0x7f7f7f7fu) == 0x7f7f7f7fu) continue;  // all below an infinity
             uint32_t word[4] = {v.x, v.y, v.z, v.w};
-            bool odd = false;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                if ((word[e] & 0x7f80u) == 0x7f80u) { word[e] &= 0xffff0000u; odd = true; }
-                if ((word[e] & 0x7f800000u) == 0x7f800000u) { word[e] &= 0xffffu; odd = true; }
+                if ((word[e] & 0x7f80u) == 0x7f80u) word[e] &= 0xffff0000u;
+                if ((word[e] & 0x7f800000u) == 0x7f800000u) word[e] &= 0xffffu;
             }
-            if (odd) atomicOr(&sm.bad[n_unit & 7], 1ull << behind);
-            if (odd || t >= u.len) *p = make_uint4(word[0], word[1], word[2], word[3]);
+            atomicOr(&sm.bad[n_unit & 7], 1ull << behind);
+            *p = make_uint4(word[0], word[1], word[2], word[3]);
         }
     }
     fence_proxy_async_smem();
@@ -476,6 +492,10 @@ template <int D, bool F4>
 __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int group, int warp, int i)
 {
     constexpr int kGroups = Cfg<D, F4>::kGroups;
+    // 4 bits: scores are read twice, 32 at a time, and loops are rolled.  The roles' code shares the instruction caches, and the
+    // widening takes its part (64 scores at once and all unrolled: 32 requests of 64 nodes 514 us, so 409; bf16 24 of 60 nodes
+    // 465 us so, 490 rolled).
+    constexpr int kKeep = F4 ? 0 : 1;
     int* gave_up = &sm.gave_up;
     const int before_me = group == 0 ? kGroups - 1 : group - 1;  // the group of the step before
     uint32_t mine = group;             // this group's next step, and how many it had
@@ -497,30 +517,42 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
             if (!warp_wait(&sm.s_full[mine & 3], (mine >> 2) & 1, gave_up)) return;
             tc_fence_after_sync();
             const uint32_t t_s = tmem + kColS + (mine & 3) * kStep;
-            uint32_t s[2][32];
-            float mx = -INFINITY;
-            auto hide = [&](int c) {
-                const uint32_t see = sees == 0 ? 0u : seen_tokens(t0 + 32 * c, u.committed, u.len, sees);
+            if (ends && warp_live) {  // scores of what the row does not see, in place
+#pragma unroll 1
+                for (int c = 0; c < kStep / 16; ++c) {
+                    const uint32_t see = sees == 0 ? 0u : seen_tokens(t0 + 16 * c, u.committed, u.len, sees);
+                    uint32_t x[16];
+                    tmem_ld16(t_s + 16 * c, x);
+                    tmem_ld_wait();
 #pragma unroll
-                for (int x = 0; x < 32; ++x)
-                    if (!((see >> x) & 1)) s[c][x] = 0xff800000u;
-            };
+                    for (int e = 0; e < 16; ++e)
+                        if (!((see >> e) & 1)) x[e] = 0xff800000u;
+                    tmem_st16(t_s + 16 * c, x);
+                }
+                tmem_st_wait();
+            }
+            float mx = -INFINITY;
+            uint32_t s[1 + kKeep][32];
             if (warp_live) {
                 float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                tmem_ld32(t_s, s[0]);
-                if constexpr (!F4) tmem_ld32(t_s + 32, s[1]);
-                tmem_ld_wait();
+                auto most = [&](const uint32_t (&x)[32]) {
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    if constexpr (F4)
-                        if (c == 1) {
-                            tmem_ld32(t_s + 32, s[1]);
-                            tmem_ld_wait();
-                        }
-                    if (ends) hide(c);
-#pragma unroll
-                    for (int x = 0; x < 16; ++x)
-                        m4[x & 3] = fmax3(m4[x & 3], __uint_as_float(s[c][2 * x]), __uint_as_float(s[c][2 * x + 1]));
+                    for (int e = 0; e < 16; ++e)
+                        m4[e & 3] = fmax3(m4[e & 3], __uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1]));
+                };
+                if constexpr (kKeep) {
+                    tmem_ld32(t_s, s[0]);
+                    tmem_ld32(t_s + 32, s[kKeep]);
+                    tmem_ld_wait();
+                    most(s[0]);
+                    most(s[kKeep]);
+                } else {
+#pragma unroll 1
+                    for (int c = 0; c < 2; ++c) {
+                        tmem_ld32(t_s + 32 * c, s[0]);
+                        tmem_ld_wait();
+                        most(s[0]);
+                    }
                 }
                 mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
             }
@@ -552,23 +584,28 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
                 const float base = m == -INFINITY ? 0.f : m * unit;  // (nothing seen yet)
                 const float2 unit2 = make_float2(unit, unit), base2 = make_float2(-base, -base);
                 float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    if constexpr (F4) {  // (80 registers do not hold them)
-                        tmem_ld32(t_s + 32 * c, s[c]);
-                        tmem_ld_wait();
-                        if (ends) hide(c);
-                    }
+                auto exponentials = [&](const uint32_t (&x)[32], int c) {
                     uint32_t pk[16];
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        float2 p = ffma2(make_float2(__uint_as_float(s[c][2 * x]), __uint_as_float(s[c][2 * x + 1])), unit2, base2);
+                    for (int e = 0; e < 16; ++e) {
+                        float2 p = ffma2(make_float2(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), unit2, base2);
                         p.x = fast_exp2(p.x);
                         p.y = fast_exp2(p.y);
-                        l2[x & 1] = fadd2(l2[x & 1], p);
-                        pk[x] = F4 ? f16x2(p.x, p.y) : bf16x2(p.x, p.y);
+                        l2[e & 1] = fadd2(l2[e & 1], p);
+                        pk[e] = F4 ? f16x2(p.x, p.y) : bf16x2(p.x, p.y);
                     }
                     tmem_st16(t_s + 16 * c, pk);  // over columns that have been read
+                };
+                if constexpr (kKeep) {
+                    exponentials(s[0], 0);
+                    exponentials(s[kKeep], 1);
+                } else {
+#pragma unroll 1
+                    for (int c = 0; c < 2; ++c) {
+                        tmem_ld32(t_s + 32 * c, s[0]);
+                        tmem_ld_wait();
+                        exponentials(s[0], c);
+                    }
                 }
                 l += (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
                 tmem_st_wait();
@@ -591,6 +628,26 @@ struct Rows {
     const TreeArgs& a;
     const uint32_t tmem;  // with this warp's lanes
     const int i;          // row
+    const int warp = i >> 5, lane = i & 31;
+
+    // 128 bytes of every row of the warp, from its lane's registers to where the row goes (row_to), at `offset`: eight lanes a
+    // row (rows of the warp's lanes one by one: 3600 cycles a unit).
+    __device__ __forceinline__ void store_pieces(const uint32_t (&x)[32], int offset)
+    {
+        uint8_t(*stage)[kStagePitch] = sm.stage[warp];
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            *reinterpret_cast<uint4*>(&stage[lane][16 * e]) = make_uint4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int row = 4 * e + (lane >> 3);
+            uint8_t* to = static_cast<uint8_t*>(sm.row_to[warp][row]);
+            if (to != nullptr)
+                *reinterpret_cast<uint4*>(to + offset + 16 * (lane & 7)) = *reinterpret_cast<const uint4*>(&stage[row][16 * (lane & 7)]);
+        }
+    }
 
     // A unit's rows: what they see, and their queries into tensor memory.  In 4-bit pages queries are f16 times a
     // power of two that brings the row's largest element into [1, 2) (exact down to 2^-17 of it, within 2^-25 of it below).
@@ -609,44 +666,72 @@ struct Rows {
         if (committed < 0) sees &= ~0ull << min(63, -committed);  // nodes without a token
         sm.sees[n_unit & 1][i] = sees;
         if (i == 0) sm.info[n_unit & 1] = UnitInfo{committed, w.q.len, w.tile0, w.tiles, rows, more};
-        float unit = a.scale * kLog2e;
-        const uint4* from = reinterpret_cast<const uint4*>(a.q + ((int64_t)(w.q.first + node) * a.Hq + w.h * G + i % G) * D);
-        auto load = [&](int c, uint32_t (&x)[32]) {  // dimensions 64 c .. 64 c + 63
+        // Rows come in pieces of 64 dimensions: eight lanes a row, by way of shared memory (a lane that reads its own row touches
+        // another line in each of 16 loads).
+        const int64_t at = live ? ((int64_t)(w.q.first + node) * a.Hq + w.h * G + i % G) * D : -1;
+        auto load = [&](int c, uint4 (&v)[8]) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const uint4 v = live ? __ldg(from + 8 * c + e) : make_uint4(0, 0, 0, 0);
-                x[4 * e] = v.x;
-                x[4 * e + 1] = v.y;
-                x[4 * e + 2] = v.z;
-                x[4 * e + 3] = v.w;
+                const int64_t from = __shfl_sync(0xffffffffu, at, 4 * e + (lane >> 3));
+                v[e] = from >= 0 ? __ldg(reinterpret_cast<const uint4*>(a.q + from + 64 * c + 8 * (lane & 7))) : make_uint4(0, 0, 0, 0);
             }
         };
-        float down = 1.f;
+        float down[8];  // of the rows of this lane's pieces
         if constexpr (F4) {
-            float top = 0.f;
+            float top[8] = {};
 #pragma unroll 1
             for (int c = 0; c < D / 64; ++c) {
-                uint32_t x[32];
-                load(c, x);
+                uint4 v[8];
+                load(c, v);
 #pragma unroll
-                for (int e = 0; e < 32; ++e)
-                    top = fmax3(top, fabsf(__uint_as_float(x[e] << 16)), fabsf(__uint_as_float(x[e] & 0xffff0000u)));
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t word[4] = {v[e].x, v[e].y, v[e].z, v[e].w};
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+                        top[e] = fmax3(top[e], fabsf(__uint_as_float(word[y] << 16)), fabsf(__uint_as_float(word[y] & 0xffff0000u)));
+                }
             }
-            const int e2 = min(max((int)(__float_as_uint(top) >> 23), 2), 252) - 127;
-            down = __uint_as_float((uint32_t)(127 - e2) << 23);
-            const float up = __uint_as_float((uint32_t)(127 + e2) << 23);
-            // (neither 0 nor infinite: the -inf of a hidden token, or a score of 0, times that would be NaN)
-            unit = fminf(fmaxf(a.scale * up * kLog2e, FLT_MIN), FLT_MAX);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+#pragma unroll
+                for (int off = 1; off < 8; off <<= 1) top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], off));
+                const int e2 = min(max((int)(__float_as_uint(top[e]) >> 23), 2), 252) - 127;
+                down[e] = __uint_as_float((uint32_t)(127 - e2) << 23);
+                // (neither 0 nor infinite: the -inf of a hidden token, or a score of 0, times that would be NaN)
+                if ((lane & 7) == 0)
+                    sm.row_unit[n_unit & 1][warp * 32 + 4 * e + (lane >> 3)] =
+                        fminf(fmaxf(a.scale * __uint_as_float((uint32_t)(127 + e2) << 23) * kLog2e, FLT_MIN), FLT_MAX);
+            }
+        } else {
+            sm.row_unit[n_unit & 1][i] = a.scale * kLog2e;
         }
-        sm.row_unit[n_unit & 1][i] = unit;
+        uint8_t(*stage)[kStagePitch] = sm.stage[warp];
 #pragma unroll 1
         for (int c = 0; c < D / 64; ++c) {
-            uint32_t x[32];
-            load(c, x);
-            if constexpr (F4)
+            uint4 v[8];
+            load(c, v);
+            __syncwarp();
 #pragma unroll
-                for (int e = 0; e < 32; ++e)
-                    x[e] = f16x2(__uint_as_float(x[e] << 16) * down, __uint_as_float(x[e] & 0xffff0000u) * down);
+            for (int e = 0; e < 8; ++e) {
+                if constexpr (F4) {
+                    uint32_t word[4] = {v[e].x, v[e].y, v[e].z, v[e].w};
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+                        word[y] = f16x2(__uint_as_float(word[y] << 16) * down[e], __uint_as_float(word[y] & 0xffff0000u) * down[e]);
+                    v[e] = make_uint4(word[0], word[1], word[2], word[3]);
+                }
+                *reinterpret_cast<uint4*>(&stage[4 * e + (lane >> 3)][16 * (lane & 7)]) = v[e];
+            }
+            __syncwarp();
+            uint32_t x[32];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint4 y = *reinterpret_cast<const uint4*>(&stage[lane][16 * e]);
+                x[4 * e] = y.x;
+                x[4 * e + 1] = y.y;
+                x[4 * e + 2] = y.z;
+                x[4 * e + 3] = y.w;
+            }
             tmem_st32(tmem + kColQ + (n_unit & 1) * 64 + 32 * c, x);
         }
         tmem_st_wait();
@@ -656,8 +741,8 @@ struct Rows {
 
     // Adds the values that were taken out of the operands to a row that sees them, 0 or not: whatever is added to is not finite
     // then.  Rare, and out of the way of what is not.
-    __device__ __noinline__ static void put_back(const TreeArgs& a, const int32_t* pages, int h, int committed, unsigned long long odd,
-                                                 void* to, bool is_bf16)
+    __device__ __forceinline__ void put_back(const int32_t* pages, int h, int committed, unsigned long long odd, void* to,
+                                             bool is_bf16) const
     {
 #pragma unroll 1
         for (unsigned long long left = odd; left != 0; left &= left - 1) {
@@ -709,12 +794,28 @@ struct Rows {
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const float lse = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m * unit * kLn2) + logf(l);
         const bool final_row = a.out != nullptr && w.tiles == w.q.tiles;  // (the same for all rows)
+        void* to = a.out + row * D;
+        float* lse_to = a.lse_out != nullptr ? a.lse_out + row : nullptr;
+        int spare = 0;  // slots behind this one that hold nothing
+        if (!final_row && a.out == nullptr) {
+            const int c0 = w.first_cta(sm.part);
+            const int k = a.n_splits == 1 ? 0 : (int)blockIdx.x - sm.part.cta0 - c0;
+            const int parts = a.n_splits == 1 ? 1 : w.last_cta(sm.part) - c0 + 1;
+            const int64_t slot = row * a.n_slots + a.slot0 + k;
+            to = a.o_part + slot * D;
+            lse_to = a.lse_part + slot;
+            if (k == parts - 1) spare = a.n_splits - parts;
+        } else if (!final_row) {
+            const int64_t slot = (int64_t)(2 * blockIdx.x + (w.tile0 == 0 ? 1 : 0)) * kTileRows + i;
+            to = a.o_cut + slot * D;
+            lse_to = a.lse_cut + slot;
+        }
+        sm.row_to[warp][lane] = live ? to : nullptr;
         ok = ok && warp_wait(&sm.o_full, n_unit & 1, &sm.gave_up);
         if (!row_barrier(ok)) return false;
         tc_fence_after_sync();
-        float *to = nullptr, *lse_to = nullptr;
         if (final_row) {
-            uint32_t y[D / 2];
+            uint32_t y[D / 64][32];
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
                 uint32_t o[32];
@@ -723,44 +824,22 @@ struct Rows {
                 // (a row that has seen nothing: its O is 0 or was never written)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    y[16 * c + e] = l == 0.f ? 0u : bf16x2(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
+                    y[c >> 1][16 * (c & 1) + e] =
+                        l == 0.f ? 0u : bf16x2(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv);
             }
             tc_fence_before_sync();
             mbar_arrive(&sm.o_free);  // O may be written again
-            if (live)
 #pragma unroll
-                for (int e = 0; e < D / 8; ++e)
-                    reinterpret_cast<uint4*>(a.out + row * D)[e] = make_uint4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
-            if (a.lse_out != nullptr) lse_to = a.lse_out + row;
+            for (int c = 0; c < D / 64; ++c) store_pieces(y[c], 128 * c);
         } else {
-            int spare = 0;  // slots behind this one that hold nothing
-            if (a.out == nullptr) {
-                const int c0 = w.first_cta(sm.part);
-                const int k = a.n_splits == 1 ? 0 : (int)blockIdx.x - sm.part.cta0 - c0;
-                const int parts = a.n_splits == 1 ? 1 : w.last_cta(sm.part) - c0 + 1;
-                const int64_t slot = row * a.n_slots + a.slot0 + k;
-                to = a.o_part + slot * D;
-                lse_to = a.lse_part + slot;
-                if (k == parts - 1) spare = a.n_splits - parts;
-            } else {
-                const int64_t slot = (int64_t)(2 * blockIdx.x + (w.tile0 == 0 ? 1 : 0)) * kTileRows + i;
-                to = a.o_cut + slot * D;
-                lse_to = a.lse_cut + slot;
-            }
 #pragma unroll 1
             for (int c = 0; c < D / 32; ++c) {
                 uint32_t o[32];
                 tmem_ld32(tmem + kColO + 32 * c, o);
                 tmem_ld_wait();
-                float4* p = reinterpret_cast<float4*>(to + 32 * c);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (l != 0.f)
-                        x = make_float4(__uint_as_float(o[4 * e]) * inv, __uint_as_float(o[4 * e + 1]) * inv,
-                                        __uint_as_float(o[4 * e + 2]) * inv, __uint_as_float(o[4 * e + 3]) * inv);
-                    if (live) p[e] = x;
-                }
+                for (int e = 0; e < 32; ++e) o[e] = l == 0.f ? 0u : __float_as_uint(__uint_as_float(o[e]) * inv);
+                store_pieces(o, 128 * c);
             }
             tc_fence_before_sync();
             mbar_arrive(&sm.o_free);
@@ -769,15 +848,16 @@ struct Rows {
                 for (int k = 1; k <= spare; ++k) {
                     lse_to[k] = -INFINITY;
 #pragma unroll 1
-                    for (int d = 0; d < D; d += 4) *reinterpret_cast<float4*>(to + k * D + d) = make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int d = 0; d < D; d += 4)
+                        *reinterpret_cast<float4*>(static_cast<float*>(to) + k * D + d) = make_float4(0.f, 0.f, 0.f, 0.f);
                 }
         }
+        __syncwarp();
         if (live && lse_to != nullptr) *lse_to = lse;
         const unsigned long long odd =
             l == 0.f ? 0 : *static_cast<volatile unsigned long long*>(&sm.bad[n_unit & 7]) & sm.sees[n_unit & 1][i];
         if (live && odd != 0)
-            put_back(a, a.kv.page_table + (int64_t)w.r * a.kv.max_pages, w.h, w.committed(), odd,
-                     final_row ? static_cast<void*>(a.out + row * D) : to, final_row);
+            put_back(a.kv.page_table + (int64_t)w.r * a.kv.max_pages, w.h, w.committed(), odd, to, final_row);
         row_barrier();  // all have read `bad`
         if (i == 0) sm.bad[n_unit & 7] = 0;
         return true;
@@ -966,7 +1046,7 @@ __device__ __forceinline__ void widen_keys(const uint8_t* code_tile, uint8_t* to
     using B = Fp4Block<D>;
     constexpr int J = D / 32;
     const int l = lane & 7, c = l & 3, qd = lane >> 3, token = (l >> 2) ? (qd ^ 5) : qd;
-#pragma unroll
+#pragma unroll 2
     for (int it = 0; it < 4; ++it) {
         const int block = block0 + (it >> 1), t = 8 * (it & 1) + token, row = 16 * block + t;
         const uint8_t* from = code_tile + block * B::kBytes;
@@ -1002,7 +1082,7 @@ __device__ __forceinline__ void widen_values(const uint8_t* code_tile, uint8_t* 
     using B = Fp4Block<D>;
     constexpr int W = D / 64;  // words of a token's chunk
     const int x = lane & 7, other = x >> 2;
-#pragma unroll
+#pragma unroll 2
     for (int it = 0; it < 4; ++it) {
         const int block = block0 + (it >> 1), p = 4 * (it & 1) + (lane >> 3);
         const uint8_t* from = code_tile + block * B::kBytes;
