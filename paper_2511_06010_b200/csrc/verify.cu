@@ -17,7 +17,7 @@ namespace moska {
 namespace {
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;  // the portable size
 constexpr int kNodes = MOSKA_TREE_MAX_NODES;
 
@@ -45,9 +45,15 @@ struct VerifySmem {
     double warp_sum[kWarps];
     double cta_sum[2][kMaxCluster];  // of all CTAs of the cluster; passes alternate
     int path[kNodes];
+    int range[2];
 };
 
 __device__ __forceinline__ float positive(float x) { return x > 0.f ? x : 0.f; }  // (NaN: 0)
+
+template <int N>
+struct Values {
+    float x[N];
+};
 
 // A row of probabilities from its first element on: 16-byte pieces of kVec elements that lie on 16-byte boundaries; element v
 // of the row is element v + shift of the pieces.
@@ -61,42 +67,52 @@ struct Row {
         if constexpr (sizeof(T) == 4) return __ldg(reinterpret_cast<const float*>(p) + v);
         else return __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(p) + v) << 16);
     }
-    // elements v .. v + kVec - 1, those outside [0, V) as 0; `whole`: v + this row's shift is a multiple of kVec
-    __device__ __forceinline__ void load(int v, int V, bool whole, float (&x)[kVec]) const
+    static __device__ __forceinline__ Values<kVec> values(const uint4& w)
     {
-        if (whole && v >= 0 && v + kVec <= V) {
-            const uint4 w = __ldg(reinterpret_cast<const uint4*>(p + v));
-            const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+        Values<kVec> y;
+        const uint32_t word[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (sizeof(T) == 4) {
-                    x[i] = __uint_as_float(word[i]);
-                } else {
-                    x[2 * i] = __uint_as_float(word[i] << 16);
-                    x[2 * i + 1] = __uint_as_float(word[i] & 0xffff0000u);
-                }
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                y.x[i] = __uint_as_float(word[i]);
+            } else {
+                y.x[2 * i] = __uint_as_float(word[i] << 16);
+                y.x[2 * i + 1] = __uint_as_float(word[i] & 0xffff0000u);
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) x[i] = v + i >= 0 && v + i < V ? at(v + i) : 0.f;
         }
+        return y;
+    }
+    // elements v .. v + kVec - 1, those outside [0, V) as 0; `whole`: v + this row's shift is a multiple of kVec
+    __device__ __forceinline__ Values<kVec> load(int v, int V, bool whole) const
+    {
+        if (whole && v >= 0 && v + kVec <= V) return values(__ldg(reinterpret_cast<const uint4*>(p + v)));
+        Values<kVec> y;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) y.x[i] = v + i >= 0 && v + i < V ? at(v + i) : 0.f;
+        return y;
     }
 };
 
-// What is left of p after `failed` tests.
-__device__ __forceinline__ double left_of(float p, float q, int failed, const double* inv)
+// What is left of p after `failed` tests, of N elements at once.
+template <int N>
+__device__ __forceinline__ void left_of(const float (&p)[N], const float (&q)[N], int failed, const double* inv, double (&r)[N])
 {
-    double r = positive(p);
-    const double qd = positive(q);
+#pragma unroll
+    for (int e = 0; e < N; ++e) r[e] = positive(p[e]);
+    if (failed == 0) return;
+    double minus_q[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) minus_q[e] = -(double)positive(q[e]);
+#pragma unroll 1
     for (int i = 0; i < failed; ++i) {
-        r = (i == 0 ? r : r * inv[i]) - qd;
-        r = r > 0.0 ? r : 0.0;
+        const double f = inv[i];  // (1 at first)
+#pragma unroll
+        for (int e = 0; e < N; ++e) r[e] = fmax(fma(r[e], f, minus_q[e]), 0.0);
     }
-    return r;
 }
 
 template <class T, bool kDraft>
-__global__ void __launch_bounds__(kThreads) verify_kernel(const VerifyArgs a)
+__global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyArgs a)
 {
     __shared__ VerifySmem sm;
     const cg::cluster_group cluster = cg::this_cluster();
@@ -140,36 +156,67 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const VerifyArgs a)
         piece1 = min(c1, piece0 + per_warp);
     };
     // elements of piece i: what is left of them after `failed` tests
-    auto left = [&](int i, double (&x)[kVec]) {
-        const int v = i * kVec - shift;
-        float p[kVec], q[kVec];
-        target_row(cur).load(v, V, true, p);
+    auto left_of_piece = [&](int i, const Values<kVec>& p, const Values<kVec>& q, double (&x)[kVec]) {
         if constexpr (kDraft) {
-            if (failed > 0) draft_row(cur).load(v, V, q_whole, q);
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) x[e] = left_of(p[e], q[e], failed, sm.inv);
+            left_of(p.x, q.x, failed, sm.inv, x);
         } else {
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) x[e] = positive(p[e]);
+            for (int e = 0; e < kVec; ++e) x[e] = positive(p.x[e]);
             for (int f = 0; f < failed; ++f) {
-                const int at = sm.removed[f] - v;
+                const int at = sm.removed[f] - (i * kVec - shift);
 #pragma unroll
                 for (int e = 0; e < kVec; ++e)
                     if (e == at) x[e] = 0.0;
             }
         }
     };
-    auto sum_pass = [&] {
-        split();
+    auto left = [&](int i, double (&x)[kVec]) {
+        Values<kVec> p, q;
+        p = target_row(cur).load(i * kVec - shift, V, true);
+        if constexpr (kDraft)
+            if (failed > 0) q = draft_row(cur).load(i * kVec - shift, V, q_whole);
+        left_of_piece(i, p, q, x);
+    };
+    // what is left in pieces begin .. end - 1, over the warp
+    auto sum_of = [&](int begin, int end) {
         double s = 0.0;
-        for (int i = piece0 + lane; i < piece1; i += 32) {
+        // Whole pieces, kAhead of a lane's in flight; then the ends of the row (and all of it where the two rows are aligned
+        // differently), one by one.
+        constexpr int kAhead = sizeof(T) == 4 ? 4 : 2;
+        const int whole0 = q_whole ? max(begin, shift > 0 ? 1 : 0) : end, whole1 = q_whole ? min(end, (V + shift) / kVec) : end;
+        const uint4* p = reinterpret_cast<const uint4*>(target_row(cur).p - shift);
+        const uint4* q = kDraft ? reinterpret_cast<const uint4*>(draft_row(cur).p - shift) : nullptr;
+        for (int i0 = whole0; i0 < whole1; i0 += 32 * kAhead) {
+            uint4 pw[kAhead], qw[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int i = i0 + 32 * u + lane;
+                pw[u] = i < whole1 ? __ldg(p + i) : make_uint4(0, 0, 0, 0);
+                if constexpr (kDraft) qw[u] = failed > 0 && i < whole1 ? __ldg(q + i) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                double x[kVec];
+                left_of_piece(i0 + 32 * u + lane, Row<T>::values(pw[u]), Row<T>::values(qw[u]), x);
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) s += x[e];
+            }
+        }
+        auto one = [&](int at) {
             double x[kVec];
-            left(i, x);
+            left(at, x);
 #pragma unroll
             for (int e = 0; e < kVec; ++e) s += x[e];
-        }
+        };
+        for (int at = begin + lane; at < min(end, whole0); at += 32) one(at);
+        for (int at = max(whole0, whole1) + lane; at < end; at += 32) one(at);
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+        return s;
+    };
+    auto sum_pass = [&] {
+        split();
+        const double s = sum_of(piece0, piece1);
         if (lane == 0) sm.warp_sum[warp] = s;
         __syncthreads();
         double mine = 0.0;
@@ -188,7 +235,10 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const VerifyArgs a)
         const int x = sm.token[j];
         double px;
         if constexpr (kDraft) {
-            px = left_of(sm.p[j], sm.q[j], failed, sm.inv);
+            const float p1[1] = {sm.p[j]}, q1[1] = {sm.q[j]};
+            double r1[1];
+            left_of(p1, q1, failed, sm.inv, r1);
+            px = r1[0];
         } else {
             px = sm.p[j];
             for (int f = 0; f < failed; ++f)
@@ -248,16 +298,45 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const VerifyArgs a)
         if (before > goal) break;
     }
     if (cta != rank) return;
-    int at = -1;
-    before = base;
-    for (int w = 0; w < kWarps; ++w) {
-        if (!(sm.warp_sum[w] > 0.0)) continue;
-        at = w;
-        base = before;
-        before += sm.warp_sum[w];
-        if (before > goal) break;
+    // the part in which `sum` (its kWarps parts' sums) passes the goal, and what is before it; the last with anything, should
+    // rounding leave none
+    auto part_of = [&](const double* sum) {
+        int at = -1;
+        double upto = base;
+        for (int w = 0; w < kWarps; ++w) {
+            if (!(sum[w] > 0.0)) continue;
+            at = w;
+            base = upto;
+            upto += sum[w];
+            if (upto > goal) break;
+        }
+        return at;
+    };
+    int at = part_of(sm.warp_sum);
+    if (lane == 0 && warp == at) {
+        sm.range[0] = piece0;
+        sm.range[1] = piece1;
     }
-    if (at != warp) return;
+    __syncthreads();
+    // that warp's pieces among all warps once more, until one load does for what is left (one warp alone would go through them
+    // for as long as a pass takes)
+    int begin = sm.range[0], end = sm.range[1];
+    while (end - begin > 32) {
+        const int per = (end - begin + kWarps - 1) / kWarps;
+        piece0 = min(end, begin + warp * per);
+        piece1 = min(end, piece0 + per);
+        const double mine = sum_of(piece0, piece1);
+        __syncthreads();
+        if (lane == 0) sm.warp_sum[warp] = mine;
+        __syncthreads();
+        const int next = part_of(sm.warp_sum);
+        if (next >= 0) at = next;
+        begin = min(end, begin + at * per);
+        end = min(end, begin + per);
+    }
+    if (warp > 0) return;
+    piece0 = begin;
+    piece1 = end;
     int last = -1;
     for (int i0 = piece0; i0 < piece1; i0 += 32) {
         const int i = i0 + lane;
@@ -303,7 +382,7 @@ int launch_verify(const void* target, int64_t target_stride, const void* draft, 
 {
     if (tree.n_requests == 0) return MOSKA_OK;
     int cluster = 1;
-    while (cluster < kMaxCluster && V / cluster > 8192 && (long long)tree.n_requests * cluster < 592) cluster *= 2;
+    while (cluster < kMaxCluster && V / cluster > 2048 && (long long)tree.n_requests * cluster < 400) cluster *= 2;
     const long long grid = (long long)tree.n_requests * cluster;
     if (grid > 0x7fffffffLL) return fail(MOSKA_ERR_UNSUPPORTED, "verification grid too large");
     const VerifyArgs a{target, draft, target_stride, draft_stride, tokens, u_accept, u_next, tree, path, n_path, next_token,
