@@ -39,26 +39,21 @@ __global__ void __launch_bounds__(kThreads) commit_kernel(const CommitArgs a)
     }
     __syncthreads();
     if (tid > 0 && tid < n) good &= source[tid - 1] < x;
-    good = __syncthreads_and(good);
+    const int shift = a.kv.page_shift, in_page = (1 << shift) - 1;
+    const int32_t* pages = a.kv.page_table + (int64_t)r * a.kv.max_pages;
+    if (tid < n && good && committed >= 0) {
+        const int t = committed + tid, f = committed + x;
+        const int pt = __ldg(pages + (t >> shift)), pf = __ldg(pages + (f >> shift));
+        good = (unsigned)pt < (unsigned)a.kv.n_pages && (unsigned)pf < (unsigned)a.kv.n_pages;
+        to[tid] = ((int64_t)pt << shift) + (t & in_page);
+        from[tid] = ((int64_t)pf << shift) + (f & in_page);
+    }
+    good = __syncthreads_and(good);  // (else, or with a page that is not in the pool, nothing is moved)
     if (part == 0 && tid == 0) {
         a.kv_len_out[r] = good && committed >= 0 ? committed + n : len;
         if (!good) atomicMin(a.kv.status, MOSKA_ERR_INVALID_ARG);
     }
     if (!good || committed < 0) return;
-    const int shift = a.kv.page_shift, in_page = (1 << shift) - 1;
-    const int32_t* pages = a.kv.page_table + (int64_t)r * a.kv.max_pages;
-    bool there = true;
-    if (tid < n) {
-        const int t = committed + tid, f = committed + x;
-        const int pt = __ldg(pages + (t >> shift)), pf = __ldg(pages + (f >> shift));
-        there = (unsigned)pt < (unsigned)a.kv.n_pages && (unsigned)pf < (unsigned)a.kv.n_pages;
-        to[tid] = ((int64_t)pt << shift) + (t & in_page);
-        from[tid] = ((int64_t)pf << shift) + (f & in_page);
-    }
-    if (!__syncthreads_and(there)) {  // a page that is not in the pool: nothing is moved
-        if (part == 0 && tid == 0) atomicMin(a.kv.status, MOSKA_ERR_INVALID_ARG);
-        return;
-    }
     int skip = 0;  // rows that are where they belong
     while (skip < n && source[skip] == skip) ++skip;
 

@@ -89,6 +89,12 @@ struct Part {
     long long sums[kMaxRowTiles][kFindThreads / 32];  // of each warp's requests
 };
 
+// A unit that cuts divide, for the kernel that joins its rows: its first node's batch row, its KV head, rows (0: none) and the
+// CTAs of its parts.
+struct __align__(16) CutUnit {
+    int first, h, rows, c0, c1, unused[3];
+};
+
 // What the softmax needs of a unit.
 struct UnitInfo {
     int committed, len, tile0, tiles, rows, more;
@@ -130,6 +136,7 @@ struct TreeArgs {
     float* lse_out;
     float* o_cut;   // partial rows of units that a cut divides [CTA][2][128][D] (final rows only)
     float* lse_cut;
+    CutUnit* cut;   // [CTA]: the unit whose second part is the CTA's first
     float scale;
     int Hq, Hkv, n_splits, slot0, n_slots;
     int row_tiles;       // of the largest tree
@@ -278,7 +285,7 @@ __device__ __forceinline__ Request request_of(const TreeArgs& a, int r)
     q.first = rows.x;
     q.nodes = rows.y;
     q.len = paged_len(a.kv, r);
-    q.tiles = max(1, (q.len + kTile - 1) / kTile);
+    q.tiles = max(1, (int)(((unsigned)q.len + kTile - 1) / kTile));
     q.row_tiles = (q.nodes + a.nodes_per_tile - 1) / a.nodes_per_tile;
     return q;
 }
@@ -436,7 +443,7 @@ struct Walk {
 // Tokens t .. t + 31: bits of those that a row sees.
 __device__ __forceinline__ uint32_t seen_tokens(int t, int committed, int len, unsigned long long sees)
 {
-    if (t + 32 <= committed) return 0xffffffffu;
+    if (t <= committed - 32) return 0xffffffffu;
     uint32_t bits;
     const int behind = t - committed;  // the first one's place behind the committed tokens
     if (behind >= 0) {
@@ -444,7 +451,7 @@ __device__ __forceinline__ uint32_t seen_tokens(int t, int committed, int len, u
     } else {
         bits = (uint32_t)(sees << -behind) | ((1u << -behind) - 1u);
     }
-    return t + 32 <= len ? bits : len > t ? bits & ((1u << (len - t)) - 1u) : 0u;
+    return t <= len - 32 ? bits : len > t ? bits & ((1u << (len - t)) - 1u) : 0u;
 }
 
 // ---- softmax ----------------------------------------------------------------------------------------
@@ -487,7 +494,9 @@ __device__ __forceinline__ bool clean_values(Smem<D, false>& sm, const UnitInfo&
 
 // Scores of every kGroups-th step (half a tile) -> probabilities.  A row's reference m passes from step to step; it moves when a
 // step's maximum passes it by 2^8, and whoever moves it rescales O.  Each group keeps its own sum, relative to the reference
-// that it saw last.
+// that it saw last.  The reference is handed on when half of a step's exponentials are done, which also keeps the groups out of
+// step: handed on before them, both had their exponentials at one time and both waited at another (fp4 32 requests of 64
+// nodes 393 us so, 372 now; bf16 24 of 60 nodes 452 and 437); after all of them it comes too late (414, 465).
 template <int D, bool F4>
 __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int group, int warp, int i)
 {
@@ -511,7 +520,7 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
         const uint32_t end = unit0 + 2 * u.tiles;
         for (; mine < end; mine += kGroups, ++turn) {
             const int t0 = u.tile0 * kTile + (int)(mine - unit0) * kStep;
-            const bool ends = t0 + kStep > u.committed;  // some row does not see all of it
+            const bool ends = t0 > u.committed - kStep;  // some row does not see all of it
             if constexpr (!F4)
                 if (ends && !clean_values<D>(sm, u, t0, mine, n_unit, i)) return;
             if (!warp_wait(&sm.s_full[mine & 3], (mine >> 2) & 1, gave_up)) return;
@@ -562,8 +571,9 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
             const bool need = mine != unit0 && live && (mx - before) * unit > kRescaleAt;
             const float now = need ? mx : before;
             sm.ref[group][i] = now;
-            mbar_arrive(&sm.ref_full[group][warp & 3]);
-            if (warp_live) {
+            if (!warp_live) {
+                mbar_arrive(&sm.ref_full[group][warp & 3]);
+            } else {
                 if (__any_sync(0xffffffffu, need)) {
                     // the last product has left O (its barrier's turn before, four steps back, is over: these scores came behind it)
                     if (!warp_wait(&sm.pv_done[(mine - 1) & 3], ((mine - 1) >> 2) & 1, gave_up)) return;
@@ -598,6 +608,7 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
                 };
                 if constexpr (kKeep) {
                     exponentials(s[0], 0);
+                    mbar_arrive(&sm.ref_full[group][warp & 3]);
                     exponentials(s[kKeep], 1);
                 } else {
 #pragma unroll 1
@@ -605,6 +616,7 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
                         tmem_ld32(t_s + 32 * c, s[0]);
                         tmem_ld_wait();
                         exponentials(s[0], c);
+                        if (c == 0) mbar_arrive(&sm.ref_full[group][warp & 3]);
                     }
                 }
                 l += (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
@@ -1164,6 +1176,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     dependents_may_launch();
     if ((smem_u32(smem_raw) & 1023u) != 0) {  // (operand tiles lie on 1024-byte boundaries)
         if (tid == 0) atomicMin(a.kv.status, (int)MOSKA_ERR_CUDA);
+        if (tid == 0 && a.cut != nullptr) a.cut[blockIdx.x] = CutUnit{};
         return;
     }
     if (tid < kFindThreads) {
@@ -1205,7 +1218,16 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     const uint32_t tmem = sm.tmem_base;
 
     Walk w;
-    if (w.begin(a, sm.part)) {
+    const bool any = w.begin(a, sm.part);
+    if (warp == C::kValueWarp + 1 && lane == 0 && a.cut != nullptr) {
+        CutUnit u{};
+        if (any && w.tile0 > 0) {
+            u = {w.q.first + w.node0(a), w.h, w.rows(a), sm.part.cta0 + w.first_cta(sm.part), sm.part.cta0 + w.last_cta(sm.part), {}};
+            if ((int)blockIdx.x != u.c0 + 1) u.rows = 0;
+        }
+        a.cut[blockIdx.x] = u;
+    }
+    if (any) {
         const uint32_t lanes = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
         const int row = (warp & 3) * 32 + lane;
         if (warp < C::kRowWarp0) {
@@ -1233,22 +1255,16 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     if (tid == 0 && sm.gave_up) atomicMin(a.kv.status, (int)MOSKA_ERR_TIMEOUT);
 }
 
-// Joins the partial rows of a unit that cuts divide: kJoinCtas CTAs look at the cut before part 1, as many at the one before part 2,
-// ..; a unit's first cut has it, and its CTAs have 16 rows each, two a warp.
+// Joins the partial rows of a unit that cuts divide: kJoinCtas CTAs a cut, with 16 rows each, two a warp.  (Where a cut falls is
+// written down: found anew here by all CTAs, each call took 2 to 10 us longer.)
 constexpr int kJoinCtas = 8;
 template <int D>
-__global__ void __launch_bounds__(kFindThreads) tree_join_kernel(const TreeArgs a, int ctas)
+__global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a)
 {
-    __shared__ Part part;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x / kJoinCtas + 1;
-    find_part(a, cta, ctas, part);
-    __syncthreads();
-    Walk w;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     wait_for_results();
-    if (!w.begin(a, part) || w.tile0 == 0) return;
-    const int c0 = part.cta0 + w.first_cta(part), c1 = part.cta0 + w.last_cta(part);
-    if (cta != c0 + 1) return;
-    const int G = a.Hq / a.Hkv, rows = w.rows(a);
+    const CutUnit unit = a.cut[blockIdx.x / kJoinCtas + 1];  // (no unit's second part is the first CTA's)
+    const int G = a.Hq / a.Hkv, rows = unit.rows, c0 = unit.c0, c1 = unit.c1;
     constexpr int W = D / 32;  // dimensions a lane
     using Vec = typename std::conditional<W == 4, float4, float2>::type;
     const int i0 = (blockIdx.x % kJoinCtas) * (kTileRows / kJoinCtas) + warp;  // and i0 + 8
@@ -1293,7 +1309,7 @@ __global__ void __launch_bounds__(kFindThreads) tree_join_kernel(const TreeArgs 
         const int i = i0 + 8 * x;
         if (i >= rows) continue;
         const float inv = total[x] == 0.f ? 0.f : 1.f / total[x];
-        const int64_t row = (int64_t)(w.q.first + w.node0(a) + i / G) * a.Hq + w.h * G + i % G;
+        const int64_t row = (int64_t)(unit.first + i / G) * a.Hq + unit.h * G + i % G;
 #pragma unroll
         for (int e = 0; e < W; e += 2)
             *reinterpret_cast<uint32_t*>(a.out + row * D + W * lane + e) = bf16x2(acc[x][e] * inv, acc[x][e + 1] * inv);
@@ -1353,7 +1369,10 @@ int default_tree_splits(int n_requests, int nodes, int G, int Hkv, int max_len)
     return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
 }
 
-size_t tree_cut_bytes(int D) { return (size_t)kMaxCtas * 2 * kTileRows * (D + 1) * sizeof(float); }
+size_t tree_cut_bytes(int D)
+{
+    return kMaxCtas * (2 * kTileRows * (D + 1) * sizeof(float) + sizeof(CutUnit));
+}
 
 int launch_tree_attn(const uint16_t* q, const PagedView& kv, bool fp4, const TreeRows& tree, float* o_part, float* lse_part,
                      int slot0, int n_slots, uint16_t* out, float* lse_out, void* ws, float scale, const moska_shape* s,
@@ -1364,11 +1383,12 @@ int launch_tree_attn(const uint16_t* q, const PagedView& kv, bool fp4, const Tre
     if (((long long)kv.n_pages << kv.page_shift) > 0x7fffffffLL)
         return fail(MOSKA_ERR_UNSUPPORTED, "a pool of more than 2^31 tokens");
     if (tree.n_requests >= 1 << (62 - kUnitBit)) return fail(MOSKA_ERR_UNSUPPORTED, "%d requests", tree.n_requests);
-    TreeArgs a{q, kv, tree, o_part, lse_part, out, lse_out, nullptr, nullptr, scale, s->Hq, s->Hkv, s->n_unique_splits, slot0,
+    TreeArgs a{q, kv, tree, o_part, lse_part, out, lse_out, nullptr, nullptr, nullptr, scale, s->Hq, s->Hkv, s->n_unique_splits, slot0,
                n_slots, row_tiles, per_tile};
     if (ws != nullptr) {
         a.o_cut = static_cast<float*>(ws);
         a.lse_cut = a.o_cut + (size_t)kMaxCtas * 2 * kTileRows * s->D;
+        a.cut = reinterpret_cast<CutUnit*>(a.lse_cut + kMaxCtas * 2 * kTileRows);
     }
     CUtensorMap tm_k{}, tm_v{};
     if (!fp4) {
@@ -1398,14 +1418,14 @@ int launch_tree_attn(const uint16_t* q, const PagedView& kv, bool fp4, const Tre
     if (out == nullptr || s->n_unique_splits == 1 || ctas < 2) return MOSKA_OK;
     cudaLaunchConfig_t config{};
     config.gridDim = dim3((unsigned)(kJoinCtas * (ctas - 1)));
-    config.blockDim = dim3(kFindThreads);
+    config.blockDim = dim3(256);
     config.stream = st;
     cudaLaunchAttribute early{};
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     early.val.programmaticStreamSerializationAllowed = 1;
     config.attrs = &early;
     config.numAttrs = 1;
-    MOSKA_CUDA_TRY(cudaLaunchKernelEx(&config, s->D == 128 ? tree_join_kernel<128> : tree_join_kernel<64>, a, ctas));
+    MOSKA_CUDA_TRY(cudaLaunchKernelEx(&config, s->D == 128 ? tree_join_kernel<128> : tree_join_kernel<64>, a));
     return MOSKA_OK;
 }
 

@@ -143,8 +143,9 @@ def test_a_page_outside_the_pool_is_reported(fmt):
     table = torch.tensor([[0, 4], [2, -1]], dtype=torch.int32).cuda()
     length = torch.tensor([20, 16], dtype=torch.int32).cuda()
     path = torch.tensor([[0, 5], [0, 3]], dtype=torch.int32).cuda()
-    st.commit(table, length, path, torch.tensor([2, 2], dtype=torch.int32).cuda(), 6)
+    new = st.commit(table, length, path, torch.tensor([2, 2], dtype=torch.int32).cuda(), 6)
     assert M.device_status() == M.ERR_INVALID_ARG
+    assert new.tolist() == [20, 12]  # the first request is left as it was
     for got, want in zip(token_bytes(st), expected(before, table.cpu().numpy(), [20, 16], [6, 6], [[], [0, 3]], [0, 2], 16)):
         assert np.array_equal(got, want)
 
