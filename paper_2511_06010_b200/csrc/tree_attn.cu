@@ -652,13 +652,17 @@ struct Rows {
         for (int e = 0; e < 8; ++e)
             *reinterpret_cast<uint4*>(&stage[lane][16 * e]) = make_uint4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
         __syncwarp();
+        uint8_t* to[8];
+        uint4 v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int row = 4 * e + (lane >> 3);
-            uint8_t* to = static_cast<uint8_t*>(sm.row_to[warp][row]);
-            if (to != nullptr)
-                *reinterpret_cast<uint4*>(to + offset + 16 * (lane & 7)) = *reinterpret_cast<const uint4*>(&stage[row][16 * (lane & 7)]);
+            to[e] = static_cast<uint8_t*>(sm.row_to[warp][row]);
+            v[e] = *reinterpret_cast<const uint4*>(&stage[row][16 * (lane & 7)]);
         }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (to[e] != nullptr) *reinterpret_cast<uint4*>(to[e] + offset + 16 * (lane & 7)) = v[e];
     }
 
     // A unit's rows: what they see, and their queries into tensor memory.  In 4-bit pages queries are f16 times a
