@@ -73,6 +73,16 @@ struct Cfg {
     static constexpr int kCodeSlots = F4 ? (D == 128 ? 3 : 6) : 1;
 };
 
+// Units of few rows have each row P times, in lanes kTileRows / P apart: the i-th has the i-th part of every step's tokens, with a
+// reference, a sum and an O of its own, as if a context were cut into P.  The four warps of a group have a P-th of the
+// scores each then, where one warp of live rows would have had them all (4 bits, 64 requests of 4096 tokens: 32 rows 143 us with
+// P = 4, 152 with 2, 176 without; 64 rows 156 with 2, 183 without.  bf16 waits for memory there: 182, 182, 183 us and 190, 192;
+// it has P = 1 alone).
+template <int P>
+struct Spread {
+    static constexpr int kRows = kTileRows / P, kCols = kStep / P;
+};
+
 // Tiles of request r's context (an empty one counts as one, so that its rows are written) and its row tiles.
 struct Request {
     int first, nodes, len, tiles, row_tiles;
@@ -497,7 +507,7 @@ __device__ __forceinline__ bool clean_values(Smem<D, false>& sm, const UnitInfo&
 // that it saw last.  The reference is handed on when half of a step's exponentials are done, which also keeps the groups out of
 // step: handed on before them, both had their exponentials at one time and both waited at another (fp4 32 requests of 64
 // nodes 393 us so, 372 now; bf16 24 of 60 nodes 452 and 437); after all of them it comes too late (414, 465).
-template <int D, bool F4>
+template <int D, bool F4, int P>
 __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int group, int warp, int i)
 {
     constexpr int kGroups = Cfg<D, F4>::kGroups;
@@ -515,7 +525,7 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
         const UnitInfo u = sm.info[n_unit & 1];
         const unsigned long long sees = sm.sees[n_unit & 1][i];
         const float unit = sm.row_unit[n_unit & 1][i];  // log2 units of one score
-        const bool live = i < u.rows, warp_live = (warp & 3) * 32 < u.rows;
+        const bool live = i % Spread<P>::kRows < u.rows, warp_live = (warp & 3) * 32 % Spread<P>::kRows < u.rows;
         float m = -INFINITY, l = 0.f;
         const uint32_t end = unit0 + 2 * u.tiles;
         for (; mine < end; mine += kGroups, ++turn) {
@@ -526,7 +536,7 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
             if (!warp_wait(&sm.s_full[mine & 3], (mine >> 2) & 1, gave_up)) return;
             tc_fence_after_sync();
             const uint32_t t_s = tmem + kColS + (mine & 3) * kStep;
-            if (ends && warp_live) {  // scores of what the row does not see, in place
+            if (P == 1 && ends && warp_live) {  // scores of what the row does not see, in place
 #pragma unroll 1
                 for (int c = 0; c < kStep / 16; ++c) {
                     const uint32_t see = sees == 0 ? 0u : seen_tokens(t0 + 16 * c, u.committed, u.len, sees);
@@ -542,7 +552,27 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
             }
             float mx = -INFINITY;
             uint32_t s[1 + kKeep][32];
-            if (warp_live) {
+            constexpr int kCols = Spread<P>::kCols;
+            const uint32_t part = i / Spread<P>::kRows;  // (the same for the warp)
+            uint32_t few[kCols];
+            if constexpr (P > 1) {
+                if (warp_live) {
+                    if constexpr (P == 4) tmem_ld16(t_s + kCols * part, few);
+                    else tmem_ld32(t_s + kCols * part, few);
+                    tmem_ld_wait();
+                    if (ends) {
+                        const uint32_t see = sees == 0 ? 0u : seen_tokens(t0 + kCols * part, u.committed, u.len, sees);
+#pragma unroll
+                        for (int e = 0; e < kCols; ++e)
+                            if (!((see >> e) & 1)) few[e] = 0xff800000u;
+                    }
+                    float m2[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                    for (int e = 0; e < kCols / 2; ++e)
+                        m2[e & 1] = fmax3(m2[e & 1], __uint_as_float(few[2 * e]), __uint_as_float(few[2 * e + 1]));
+                    mx = fmaxf(m2[0], m2[1]);
+                }
+            } else if (warp_live) {
                 float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 auto most = [&](const uint32_t (&x)[32]) {
 #pragma unroll
@@ -571,9 +601,8 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
             const bool need = mine != unit0 && live && (mx - before) * unit > kRescaleAt;
             const float now = need ? mx : before;
             sm.ref[group][i] = now;
-            if (!warp_live) {
-                mbar_arrive(&sm.ref_full[group][warp & 3]);
-            } else {
+            if (P > 1 || !warp_live) mbar_arrive(&sm.ref_full[group][warp & 3]);
+            if (warp_live) {
                 if (__any_sync(0xffffffffu, need)) {
                     // the last product has left O (its barrier's turn before, four steps back, is over: these scores came behind it)
                     if (!warp_wait(&sm.pv_done[(mine - 1) & 3], ((mine - 1) >> 2) & 1, gave_up)) return;
@@ -594,19 +623,33 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
                 const float base = m == -INFINITY ? 0.f : m * unit;  // (nothing seen yet)
                 const float2 unit2 = make_float2(unit, unit), base2 = make_float2(-base, -base);
                 float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                auto exponentials = [&](const uint32_t (&x)[32], int c) {
-                    uint32_t pk[16];
+                auto exponentials_of = [&](const auto& x, auto& pk) {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
+                    for (int e = 0; e < (int)(sizeof(pk) / 4); ++e) {
                         float2 p = ffma2(make_float2(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), unit2, base2);
                         p.x = fast_exp2(p.x);
                         p.y = fast_exp2(p.y);
                         l2[e & 1] = fadd2(l2[e & 1], p);
                         pk[e] = F4 ? f16x2(p.x, p.y) : bf16x2(p.x, p.y);
                     }
+                };
+                auto exponentials = [&](const uint32_t (&x)[32], int c) {
+                    uint32_t pk[16];
+                    exponentials_of(x, pk);
                     tmem_st16(t_s + 16 * c, pk);  // over columns that have been read
                 };
-                if constexpr (kKeep) {
+                if constexpr (P > 1) {
+                    uint32_t pk[kCols / 2], none[kCols / 2] = {};
+                    exponentials_of(few, pk);
+#pragma unroll
+                    for (uint32_t c = 1; c < P; ++c) {  // the other parts' tokens
+                        const uint32_t at = t_s + kCols / 2 * ((part + c) % P);
+                        if constexpr (P == 4) tmem_st8(at, none);
+                        else tmem_st16(at, none);
+                    }
+                    if constexpr (P == 4) tmem_st8(t_s + kCols / 2 * part, pk);
+                    else tmem_st16(t_s + kCols / 2 * part, pk);
+                } else if constexpr (kKeep) {
                     exponentials(s[0], 0);
                     mbar_arrive(&sm.ref_full[group][warp & 3]);
                     exponentials(s[kKeep], 1);
@@ -633,7 +676,7 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
 }
 
 // ---- queries and results ----------------------------------------------------------------------------
-template <int D, bool F4>
+template <int D, bool F4, int P>
 struct Rows {
     using C = Cfg<D, F4>;
     Smem<D, F4>& sm;
@@ -641,6 +684,7 @@ struct Rows {
     const uint32_t tmem;  // with this warp's lanes
     const int i;          // row
     const int warp = i >> 5, lane = i & 31;
+    const int ir = i % Spread<P>::kRows;  // row of the unit
 
     // 128 bytes of every row of the warp, from its lane's registers to where the row goes (row_to), at `offset`: eight lanes a
     // row (rows of the warp's lanes one by one: 3600 cycles a unit).
@@ -676,68 +720,41 @@ struct Rows {
                                [] { asm volatile("bar.sync 3, 64;" ::: "memory"); });
             row_barrier();
         }
-        const int G = a.Hq / a.Hkv, node = w.node0(a) + i / G, committed = w.committed(), rows = w.rows(a);
-        const bool live = i < rows;
+        const int G = a.Hq / a.Hkv, node = w.node0(a) + ir / G, committed = w.committed(), rows = w.rows(a);
+        const bool live = ir < rows;
         unsigned long long sees = live && committed + node >= 0 ? sm.tree.bits[node] : 0;
         if (committed < 0) sees &= ~0ull << min(63, -committed);  // nodes without a token
         sm.sees[n_unit & 1][i] = sees;
         if (i == 0) sm.info[n_unit & 1] = UnitInfo{committed, w.q.len, w.tile0, w.tiles, rows, more};
         // Rows come in pieces of 64 dimensions: eight lanes a row, by way of shared memory (a lane that reads its own row touches
         // another line in each of 16 loads).
-        const int64_t at = live ? ((int64_t)(w.q.first + node) * a.Hq + w.h * G + i % G) * D : -1;
+        const int64_t at = live ? ((int64_t)(w.q.first + node) * a.Hq + w.h * G + ir % G) * D : -1;
+        const uint32_t rows_here = __ballot_sync(0xffffffffu, live);
         auto load = [&](int c, uint4 (&v)[8]) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int64_t from = __shfl_sync(0xffffffffu, at, 4 * e + (lane >> 3));
-                v[e] = from >= 0 ? __ldg(reinterpret_cast<const uint4*>(a.q + from + 64 * c + 8 * (lane & 7))) : make_uint4(0, 0, 0, 0);
+                // (a row that is none reads the batch's first one: no branch keeps a load waiting for the one before)
+                const int64_t from = __shfl_sync(0xffffffffu, max(at, (int64_t)0), 4 * e + (lane >> 3));
+                v[e] = __ldg(reinterpret_cast<const uint4*>(a.q + from + 64 * c + 8 * (lane & 7)));
             }
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (!((rows_here >> (4 * e + (lane >> 3))) & 1)) v[e] = make_uint4(0, 0, 0, 0);
         };
-        float down[8];  // of the rows of this lane's pieces
-        if constexpr (F4) {
-            float top[8] = {};
-#pragma unroll 1
-            for (int c = 0; c < D / 64; ++c) {
-                uint4 v[8];
-                load(c, v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t word[4] = {v[e].x, v[e].y, v[e].z, v[e].w};
-#pragma unroll
-                    for (int y = 0; y < 4; ++y)
-                        top[e] = fmax3(top[e], fabsf(__uint_as_float(word[y] << 16)), fabsf(__uint_as_float(word[y] & 0xffff0000u)));
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-#pragma unroll
-                for (int off = 1; off < 8; off <<= 1) top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], off));
-                const int e2 = min(max((int)(__float_as_uint(top[e]) >> 23), 2), 252) - 127;
-                down[e] = __uint_as_float((uint32_t)(127 - e2) << 23);
-                // (neither 0 nor infinite: the -inf of a hidden token, or a score of 0, times that would be NaN)
-                if ((lane & 7) == 0)
-                    sm.row_unit[n_unit & 1][warp * 32 + 4 * e + (lane >> 3)] =
-                        fminf(fmaxf(a.scale * __uint_as_float((uint32_t)(127 + e2) << 23) * kLog2e, FLT_MIN), FLT_MAX);
-            }
-        } else {
-            sm.row_unit[n_unit & 1][i] = a.scale * kLog2e;
-        }
+        // 4 bits: once for the rows' largest elements, then for the operands.  (Rolled, with a row's elements in its lane: the code
+        // is cold when a CTA begins.  Maxima of pieces, joined by shuffles, took 11000 cycles.)
+        if constexpr (!F4) sm.row_unit[n_unit & 1][i] = a.scale * kLog2e;
+        float down = 1.f;
+        uint32_t top = 0;
         uint8_t(*stage)[kStagePitch] = sm.stage[warp];
 #pragma unroll 1
-        for (int c = 0; c < D / 64; ++c) {
+        for (int it = F4 ? 0 : D / 64; it < 2 * (D / 64); ++it) {
+            const int c = it % (D / 64);
             uint4 v[8];
             load(c, v);
             __syncwarp();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if constexpr (F4) {
-                    uint32_t word[4] = {v[e].x, v[e].y, v[e].z, v[e].w};
-#pragma unroll
-                    for (int y = 0; y < 4; ++y)
-                        word[y] = f16x2(__uint_as_float(word[y] << 16) * down[e], __uint_as_float(word[y] & 0xffff0000u) * down[e]);
-                    v[e] = make_uint4(word[0], word[1], word[2], word[3]);
-                }
-                *reinterpret_cast<uint4*>(&stage[4 * e + (lane >> 3)][16 * (lane & 7)]) = v[e];
-            }
+            for (int e = 0; e < 8; ++e) *reinterpret_cast<uint4*>(&stage[4 * e + (lane >> 3)][16 * (lane & 7)]) = v[e];
             __syncwarp();
             uint32_t x[32];
 #pragma unroll
@@ -747,6 +764,23 @@ struct Rows {
                 x[4 * e + 1] = y.y;
                 x[4 * e + 2] = y.z;
                 x[4 * e + 3] = y.w;
+            }
+            if constexpr (F4) {
+                if (it < D / 64) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) top = __vmaxu2(top, x[e] & 0x7fff7fffu);
+                    if (it + 1 == D / 64) {
+                        const int e2 = min(max((int)(max(top >> 16, top & 0xffffu) >> 7), 2), 252) - 127;
+                        down = __uint_as_float((uint32_t)(127 - e2) << 23);
+                        // (neither 0 nor infinite: the -inf of a hidden token, or a score of 0, times that would be NaN)
+                        sm.row_unit[n_unit & 1][i] =
+                            fminf(fmaxf(a.scale * __uint_as_float((uint32_t)(127 + e2) << 23) * kLog2e, FLT_MIN), FLT_MAX);
+                    }
+                    continue;
+                }
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    x[e] = f16x2(__uint_as_float(x[e] << 16) * down, __uint_as_float(x[e] & 0xffff0000u) * down);
             }
             tmem_st32(tmem + kColQ + (n_unit & 1) * 64 + 32 * c, x);
         }
@@ -797,17 +831,23 @@ struct Rows {
         bool ok = warp_wait(&sm.stat_full[n_unit & 1], (n_unit >> 1) & 1, &sm.gave_up);
         // the group of the last step has the row's reference; the others' sums are brought to it
         const float unit = sm.row_unit[n_unit & 1][i];
-        const float m = sm.stat[n_unit & 1][last % C::kGroups][i].x;
+        const float mine = sm.stat[n_unit & 1][last % C::kGroups][i].x;
+        float m = mine;
+#pragma unroll
+        for (int p = 0; p < (P > 1 ? P : 0); ++p) m = fmaxf(m, sm.stat[n_unit & 1][last % C::kGroups][ir + p * Spread<P>::kRows].x);
         float l = 0.f;
 #pragma unroll
-        for (int x = 0; x < C::kGroups; ++x) {
-            const float2 part = sm.stat[n_unit & 1][x][i];
-            l += part.x == m ? part.y : part.y * fast_exp2((part.x - m) * unit);
-        }
-        const int G = a.Hq / a.Hkv, node = w.node0(a) + i / G;
+        for (int x = 0; x < C::kGroups; ++x)
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const float2 part = sm.stat[n_unit & 1][x][ir + p * Spread<P>::kRows];
+                l += part.x == m ? part.y : part.y * fast_exp2((part.x - m) * unit);
+            }
+        const int G = a.Hq / a.Hkv, node = w.node0(a) + ir / G;
         const bool live = i < w.rows(a);
-        const int64_t row = (int64_t)(w.q.first + node) * a.Hq + w.h * G + i % G;
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const int64_t row = (int64_t)(w.q.first + node) * a.Hq + w.h * G + ir % G;
+        float inv = l == 0.f ? 0.f : 1.f / l;
+        if (P > 1 && mine != m) inv *= fast_exp2((mine - m) * unit);  // (0 for a part that has seen nothing)
         const float lse = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m * unit * kLn2) + logf(l);
         const bool final_row = a.out != nullptr && w.tiles == w.q.tiles;  // (the same for all rows)
         void* to = a.out + row * D;
@@ -830,7 +870,54 @@ struct Rows {
         ok = ok && warp_wait(&sm.o_full, n_unit & 1, &sm.gave_up);
         if (!row_barrier(ok)) return false;
         tc_fence_after_sync();
-        if (final_row) {
+        if constexpr (P > 1) {
+            // the sum of the parts, by way of shared memory: thread x has dimensions 8 (x % 4) .. of row x / 4 (P = 4), or 16 of row x / 2
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t o[32];
+                tmem_ld32(tmem + kColO + 32 * c, o);
+                tmem_ld_wait();
+                if (c + 1 == D / 32) {
+                    tc_fence_before_sync();
+                    mbar_arrive(&sm.o_free);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float y[4];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) y[x] = inv == 0.f ? 0.f : __uint_as_float(o[4 * e + x]) * inv;
+                    *reinterpret_cast<float4*>(&sm.stage[warp][lane][16 * e]) = make_float4(y[0], y[1], y[2], y[3]);
+                }
+                row_barrier();
+                constexpr int kLanes = kTileRows / Spread<P>::kRows, kDims = 32 / kLanes;  // threads of a row, dimensions of each
+                const int r = i / kLanes, d0 = (i % kLanes) * kDims;
+                float y[kDims] = {};
+#pragma unroll
+                for (int p = 0; p < P; ++p)
+#pragma unroll
+                    for (int x = 0; x < kDims; x += 4) {
+                        const int from = r + p * Spread<P>::kRows;
+                        const float4 v = *reinterpret_cast<const float4*>(&sm.stage[from >> 5][from & 31][4 * (d0 + x)]);
+                        y[x] += v.x; y[x + 1] += v.y; y[x + 2] += v.z; y[x + 3] += v.w;
+                    }
+                uint8_t* row_to = static_cast<uint8_t*>(sm.row_to[r >> 5][r & 31]);
+                if (row_to != nullptr) {
+#pragma unroll
+                    for (int x = 0; x < kDims; x += 8) {
+                        if (final_row) {
+                            *reinterpret_cast<uint4*>(row_to + 2 * (32 * c + d0 + x)) =
+                                make_uint4(bf16x2(y[x], y[x + 1]), bf16x2(y[x + 2], y[x + 3]), bf16x2(y[x + 4], y[x + 5]),
+                                           bf16x2(y[x + 6], y[x + 7]));
+                        } else {
+                            float4* to4 = reinterpret_cast<float4*>(row_to + 4 * (32 * c + d0 + x));
+                            to4[0] = make_float4(y[x], y[x + 1], y[x + 2], y[x + 3]);
+                            to4[1] = make_float4(y[x + 4], y[x + 5], y[x + 6], y[x + 7]);
+                        }
+                    }
+                }
+                row_barrier();
+            }
+        } else if (final_row) {
             uint32_t y[D / 64][32];
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
@@ -859,15 +946,15 @@ struct Rows {
             }
             tc_fence_before_sync();
             mbar_arrive(&sm.o_free);
-            if (live)
-#pragma unroll 1
-                for (int k = 1; k <= spare; ++k) {
-                    lse_to[k] = -INFINITY;
-#pragma unroll 1
-                    for (int d = 0; d < D; d += 4)
-                        *reinterpret_cast<float4*>(static_cast<float*>(to) + k * D + d) = make_float4(0.f, 0.f, 0.f, 0.f);
-                }
         }
+        if (live)
+#pragma unroll 1
+            for (int k = 1; k <= spare; ++k) {
+                lse_to[k] = -INFINITY;
+#pragma unroll 1
+                for (int d = 0; d < D; d += 4)
+                    *reinterpret_cast<float4*>(static_cast<float*>(to) + k * D + d) = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
         __syncwarp();
         if (live && lse_to != nullptr) *lse_to = lse;
         const unsigned long long odd =
@@ -1089,10 +1176,13 @@ __device__ __forceinline__ void widen_keys(const uint8_t* code_tile, uint8_t* to
 }
 
 // Values of two blocks.  Chunk x (D / 8 dimensions) of a pair of tokens: first token's bytes, then the second's.  In a tile that
-// reaches past the committed tokens (`ends`; `behind`: its first token's place behind them) values behind the context are 0, and those
+// reaches past the committed tokens (kEnds; `behind`: its first token's place behind them) values behind the context are 0, and those
 // with a scale above what appends write, infinities and NaN included, are taken out.
-template <int D>
-__device__ __forceinline__ void widen_values(const uint8_t* code_tile, uint8_t* to, int block0, int lane, bool ends, int behind, int nodes,
+// (A form of its own for the others: a branch at each token keeps loads and stores waiting, 1590 cycles a tile where it takes 1200.
+// But not with P = 1: softmax warps need the issue slots and the room for code there, 32 requests of 64 nodes 394 us with two
+// forms, 375 with one.)
+template <int D, bool kEnds>
+__device__ __forceinline__ void widen_values(const uint8_t* code_tile, uint8_t* to, int block0, int lane, int behind, int nodes,
                                              unsigned long long* bad)
 {
     using B = Fp4Block<D>;
@@ -1118,7 +1208,7 @@ __device__ __forceinline__ void widen_values(const uint8_t* code_tile, uint8_t* 
         for (int tok = 0; tok < 2; ++tok) {
             const int row = 16 * block + 2 * p + tok;
             uint32_t s2 = __byte_perm(sc, 0, tok ? 0x3232 : 0x1010);
-            if (ends && behind + row >= 0) {
+            if (kEnds && behind + row >= 0) {
                 if (behind + row >= nodes) {
                     s2 = 0;
                 } else if ((s2 & 0x7fffu) > 0x7154u) {
@@ -1140,7 +1230,7 @@ __device__ __forceinline__ void widen_values(const uint8_t* code_tile, uint8_t* 
 }
 
 // Four warps widen keys and four values, two blocks each.
-template <int D>
+template <int D, int P>
 __device__ __forceinline__ void widen_role(Smem<D, true>& sm, const TreeArgs& a, Walk w, int warp, int lane)
 {
     using C = Cfg<D, true>;
@@ -1156,8 +1246,9 @@ __device__ __forceinline__ void widen_role(Smem<D, true>& sm, const TreeArgs& a,
             if (!warp_wait(&sm.code_full[c], (tile / C::kCodeSlots) & 1, gave_up)) return;
             if (seq >= C::kSlots && !warp_wait(&sm.empty[s], ((seq / C::kSlots) - 1) & 1, gave_up)) return;
             const uint8_t* from = sm.code + c * C::kCodeBytes;
-            if (values) widen_values<D>(from, sm.slot[s], block0, lane, behind + kTile > 0, behind, w.q.nodes, &sm.bad[n_unit & 7]);
-            else widen_keys<D>(from, sm.slot[s], block0, lane);
+            if (!values) widen_keys<D>(from, sm.slot[s], block0, lane);
+            else if (P > 1 && behind + kTile <= 0) widen_values<D, false>(from, sm.slot[s], block0, lane, behind, w.q.nodes, nullptr);
+            else widen_values<D, true>(from, sm.slot[s], block0, lane, behind, w.q.nodes, &sm.bad[n_unit & 7]);
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) {
@@ -1169,7 +1260,7 @@ __device__ __forceinline__ void widen_role(Smem<D, true>& sm, const TreeArgs& a,
     } while (w.next(a, sm.part));
 }
 
-template <int D, bool F4>
+template <int D, bool F4, int P>
 __global__ void __launch_bounds__(Cfg<D, F4>::kThreads, 1)
 tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const TreeArgs a)
 {
@@ -1236,10 +1327,10 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         const int row = (warp & 3) * 32 + lane;
         if (warp < C::kRowWarp0) {
             asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kSoftmaxRegs));
-            softmax_role<D, F4>(sm, lanes, warp >> 2, warp, row);
+            softmax_role<D, F4, P>(sm, lanes, warp >> 2, warp, row);
         } else if (warp < C::kLoadWarp) {
             if constexpr (C::kRowRegs > C::kLaunchRegs) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kRowRegs));
-            Rows<D, F4>{sm, a, lanes, row}.run(w);
+            Rows<D, F4, P>{sm, a, lanes, row}.run(w);
         } else if (warp < C::kWidenWarp0) {
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kIssueRegs));
             if (warp == C::kLoadWarp) load_role<D, F4>(sm, tm_k, tm_v, a, w, lane);
@@ -1248,7 +1339,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         } else {
             if constexpr (F4) {
                 asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kWidenRegs));
-                widen_role<D>(sm, a, w, warp - C::kWidenWarp0, lane);
+                widen_role<D, P>(sm, a, w, warp - C::kWidenWarp0, lane);
             }
         }
     }
@@ -1410,10 +1501,14 @@ int launch_tree_attn(const uint16_t* q, const PagedView& kv, bool fp4, const Tre
         MOSKA_LAUNCH_CHECK("tree_attn_kernel");
         return (int)MOSKA_OK;
     };
+    const int rows = tree.max_nodes * G;  // of the largest unit, if there is one row tile
     auto form = [&](auto d, auto f4) {
         constexpr int D = decltype(d)::value;
         constexpr bool F4 = decltype(f4)::value;
-        return go(tree_attn_kernel<D, F4>, Cfg<D, F4>::kThreads, (int)sizeof(Smem<D, F4>));
+        auto kernel = tree_attn_kernel<D, F4, 1>;
+        if constexpr (F4)
+            kernel = rows <= Spread<4>::kRows ? tree_attn_kernel<D, F4, 4> : rows <= Spread<2>::kRows ? tree_attn_kernel<D, F4, 2> : kernel;
+        return go(kernel, Cfg<D, F4>::kThreads, (int)sizeof(Smem<D, F4>));
     };
     const std::integral_constant<int, 128> d128;
     const std::integral_constant<int, 64> d64;

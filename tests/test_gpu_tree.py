@@ -128,11 +128,12 @@ def test_ragged_trees_and_padding_rows(fmt, splits, D):
 
 @pytest.mark.parametrize("fmt", ["bf16", "fp4"])
 @pytest.mark.parametrize("D", [64, 128])
-def test_what_a_node_does_not_see_has_no_influence(fmt, D):
+@pytest.mark.parametrize("G", [4, 1])
+def test_what_a_node_does_not_see_has_no_influence(fmt, D, G):
     """Infinities and NaN in the keys and values of nodes: rows that do not see them are as without them, bit for
     bit; the others are not finite."""
     lens, nodes = [200, 131], [40, 40]
-    c = case(fmt, D, 8, 2, 16, lens, nodes, seed=3)
+    c = case(fmt, D, 2 * G, 2, 16, lens, nodes, seed=3)
     out, lse = (x.clone() for x in c["attention"](c["q"].cuda(), c["store"], c["table"], c["length"], c["up"]))
     check(c, out, lse)
     Hkv, bad = 2, {7: float("nan"), 21: float("inf"), 39: -float("inf")}
@@ -146,23 +147,24 @@ def test_what_a_node_does_not_see_has_no_influence(fmt, D):
     out2, lse2 = c["attention"](c["q"].cuda(), c["store"], c["table"], c["length"], c["up"])
     keep = torch.from_numpy(~touched.reshape(-1)).cuda()
     assert torch.equal(out2[keep], out[keep]) and torch.equal(lse2[keep], lse[keep])
-    assert torch.equal(out2[:, :4], out[:, :4])  # the other head's rows
+    assert torch.equal(out2[:, :G], out[:, :G])  # the other head's rows
     spoilt = slice(5, 6) if fmt == "bf16" else slice(0, 32)  # in 4 bits all that shares the scale
-    assert not torch.isfinite(out2[~keep][:, 4:, spoilt]).any()
-    rest = out2[~keep][:, 4:].clone()
+    assert not torch.isfinite(out2[~keep][:, G:, spoilt]).any()
+    rest = out2[~keep][:, G:].clone()
     rest[..., spoilt] = 0
     assert torch.isfinite(rest).all()
     k[7, 0] = float("nan")  # a key: every score of that node
     c["store"].append(None, k, v, c["table"], c["length"], q_len=40)
     out3, _ = c["attention"](c["q"].cuda(), c["store"], c["table"], c["length"], c["up"])
     sees = torch.from_numpy(TR.ancestors(c["parents"][:40])[:, 7]).cuda()
-    assert torch.isnan(out3[:40][sees][:, :4]).all() and torch.equal(out3[:40][~sees][:, :4], out[:40][~sees][:, :4])
+    assert torch.isnan(out3[:40][sees][:, :G]).all() and torch.equal(out3[:40][~sees][:, :G], out[:40][~sees][:, :G])
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "fp4"])
-def test_large_scores(fmt):
+@pytest.mark.parametrize("nodes", [17, 14, 5])
+def test_large_scores(fmt, nodes):
     """Scores of hundreds: probabilities that underflow, a maximum that moves by more than any of them."""
-    c = case(fmt, 128, 8, 2, 64, [900, 401], [17, 17], seed=9, scale=24.0)
+    c = case(fmt, 128, 8, 2, 64, [900, 401], [nodes, nodes], seed=9, scale=24.0)
     out, lse = c["attention"](c["q"].cuda(), c["store"], c["table"], c["length"], c["up"])
     check(c, out, lse)
 
