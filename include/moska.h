@@ -107,11 +107,11 @@ const char* moska_last_error(void);
 /* Waits for the current device to finish, stores the sticky device-side status word in
  * *status_host (host pointer) and clears it.  0 means no kernel of the library raised anything.
  * MOSKA_ERR_TIMEOUT: a CTA of the tensor-core Shared KV Attention kernel, or a warp of the 4-bit
- * paged attention, gave up on one of its bounded waits (TMA, MMA or bulk-copy completion).
+ * paged attention or tree attention, gave up on one of its bounded waits (TMA, MMA or bulk-copy completion).
  * MOSKA_ERR_INVALID_ARG: a grouping call (either entry point) met a chunk index outside [0, C) or
  * a (request, KV head) list that is not strictly ascending, shared attention met an entry of
- * seg_entries outside [0, B*Hkv*k), or a call on a paged store met a page index, a length or a
- * position that is out of range.  In every
+ * seg_entries outside [0, B*Hkv*k), a call on a paged store met a page index, a length or a
+ * position that is out of range, or one on trees a parent, a row range or a path that is none.  In every
  * case the outputs of the steps since the last read are not valid.  MOSKA_ERR_CORRUPT (debug
  * build only): guard words of the workspace were overwritten or a work list would have overflowed.
  * The most negative code raised since the last read is the one reported. */
@@ -618,8 +618,13 @@ int moska_decode_step_paged(const uint16_t* q, const float* summaries, const voi
  *   ws       moska_tree_attn_workspace_bytes(shape) bytes (20 MB for D = 128), 256-byte aligned; calls that
  *            share it must not overlap.  Not read or written (may be NULL) with n_unique_splits = 1.
  * shape: B, Hq, Hkv, D, q_len and n_unique_splits are read: a context is cut into at most that many parts, as the
- * work of all contexts is shared among the SMs; 64 lets any batch be shared evenly, and costs no more than 2.  What a node does not see has no influence on it,
- * infinities and NaN included.  Scores, softmax and row sums are fp32.
+ * work of all contexts is shared among the SMs; 64 lets any batch be shared evenly, and costs no more than 2.  What a
+ * node does not see has no influence on it, infinities and NaN included.  Scores, softmax statistics, row sums and results
+ * are held in fp32.  In 16 bits: bf16 pages, the probabilities (bf16, half a step 2^-8 of each); 4-bit pages, the
+ * probabilities (f16, 2^-11), a key and a value as scale * code (f16, 2^-11; lse_out is off by a few 1e-6 for it) and the
+ * queries times a power of two per row (f16, exact down to 2^-17 of the row's largest element).  out is rounded once more.
+ * A part of a context of more than about 400 million tokens would pass the limit of a wait (2 s): MOSKA_ERR_TIMEOUT in the
+ * device status word, and results that are not valid; cut it (n_unique_splits).
  */
 int moska_tree_attn(const uint16_t* q, const moska_paged_kv* kv, const int32_t* parents, const int32_t* row_start,
                     int32_t n_requests, uint16_t* out, float* lse_out, float softmax_scale, const moska_shape* shape,
@@ -656,7 +661,7 @@ int moska_decode_step_tree(const uint16_t* q, const float* summaries, const void
  * At the end next_token is the first v with P(0) + .. + P(v) > u_next[r] sum(P) and P(v) > 0 (the last v with
  * P(v) > 0 if there is none, -1 if P is 0 everywhere).  P, Z and the sums are held in 64 bits.
  *   target_probs  [B][V] of prob_type, row i (elements i target_stride ..) behind node i; entries that are
- *                 not > 0 (NaN included) count as 0
+ *                 not > 0 (NaN included) count as 0, none is infinite
  *   draft_probs   the same, with draft_stride; row i is what the children of node i were drawn from.
  *                 May be NULL
  *   tokens        int32 [B]; a node whose token is not in [0, V) is not tried

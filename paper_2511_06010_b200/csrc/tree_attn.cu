@@ -5,9 +5,20 @@
 //   S = Q K^T          tcgen05.mma, Q in tensor memory, K in shared memory: 128 x 64 scores (half a tile) in tensor memory
 //   P = exp2(S - m)    a thread per row: TMEM -> registers -> 16 bits, back over the columns of S
 //   O += P V           tcgen05.mma, P from TMEM, V from shared memory
-// Groups of softmax warps take turns at the halves: while one group's exponentials keep the special function units busy
-// (512 cycles a half), the others read their scores and find their maxima.  Scores have four buffers, so that products run ahead.  A third
-// group stages the next unit's queries and writes the last unit's rows.  TMEM: O 128, S 4 x 64, Q 2 x 64 = 512 columns.
+// Two groups of softmax warps take turns at the halves: while one has the special function units (512 cycles of exponentials a
+// half), the other reads its scores, finds their maxima and stores.  Scores have four buffers, so that products run ahead.  A
+// third group stages the next unit's queries and writes the last unit's rows.  TMEM: O 128, S 4 x 64, Q 2 x 64 = 512 columns.
+//
+// What bounds it.  A tile of 128 rows and 128 tokens is 1024 cycles of MMA (D = 128), as many of exponentials, and in 4 bits
+// some 1300 cycles of shared memory (operands written, and read by the MMAs).  A half takes a group about 1900 cycles from
+// scores to probabilities, of which 900 are exponentials that the other group's slow down, so a tile takes 1900 cycles instead of
+// 1024 (bf16, 24 requests of 60 nodes and 1K-16K tokens: 0.43 ms, 0.95 PFLOP/s, tensor pipe 53 % busy).  Up to 64 rows bf16
+// waits for memory (64 requests of 16 nodes and 4096 tokens: 188 us, 5.7 TB/s).  4 bits, 32 requests of 64 nodes and 1K-8K tokens:
+// 365 us.  One request of 8 nodes and 1000 tokens: 17 us, of which 3.7 find the part, 1.3 bring the queries, 3 are the tile,
+// 1.2 its rows, and the rest the two launches.
+// Not kept: a third softmax group (bf16 471 us for 437: registers), products of 128 tokens (one MMA warp waits for the other's
+// operands), the next scores read between a step's exponentials (468 for 434), part of the exponentials as polynomials (all
+// of them left out saves 10 %), sixteen warps that widen (144 for 142).
 //
 // One CTA per SM.  For each row tile (first 128 rows of every request, second 128, ..) the tiles of all its units, request after
 // request and head after head, form a line.  Lines get CTAs by their lengths and are cut into equal parts, one per CTA,
