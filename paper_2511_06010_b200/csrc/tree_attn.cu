@@ -313,24 +313,25 @@ __device__ __forceinline__ Request request_of(const TreeArgs& a, int r)
 
 // Finds part `cta` of `ctas`: for kFindThreads threads, in shared memory that all of the CTA may read after its next
 // barrier (p0 >= p1: nothing).  Each thread counts a stretch of requests; what is before a warp, a lane and a request is
-// then added up.
+// then added up.  kTiles: row tiles of the largest tree at most.
+template <int kTiles>
 __device__ __forceinline__ void find_part(const TreeArgs& a, int cta, int ctas, Part& part)
 {
     constexpr int kWarps = kFindThreads / 32;
     const int i = threadIdx.x, warp = i >> 5, lane = i & 31, R = a.tree.n_requests;
     const int stretch = (R + kFindThreads - 1) / kFindThreads;
     const int r0 = (int)min((long long)R, (long long)i * stretch), r1 = min(R, r0 + stretch);
-    long long mine[kMaxRowTiles] = {}, upto[kMaxRowTiles] = {};
+    long long mine[kTiles] = {}, upto[kTiles] = {};
     int longest = 0;
     for (int r = r0; r < r1; ++r) {
         const Request q = request_of(a, r);
         if (q.row_tiles > 0) longest = max(longest, q.tiles);
 #pragma unroll
-        for (int k = 0; k < kMaxRowTiles; ++k)
+        for (int k = 0; k < kTiles; ++k)
             if (k < q.row_tiles) mine[k] += q.tiles + (1ll << kUnitBit);
     }
 #pragma unroll
-    for (int k = 0; k < kMaxRowTiles; ++k) {
+    for (int k = 0; k < kTiles; ++k) {
         if (k >= a.row_tiles) continue;
         upto[k] = mine[k];
 #pragma unroll
@@ -343,9 +344,9 @@ __device__ __forceinline__ void find_part(const TreeArgs& a, int cta, int ctas, 
     longest = __reduce_max_sync(0xffffffffu, longest);
     if (lane == 0) part.longest[warp] = longest;
     find_barrier();
-    long long line[kMaxRowTiles] = {}, total = 0;
+    long long line[kTiles] = {}, total = 0;
 #pragma unroll
-    for (int k = 0; k < kMaxRowTiles; ++k) {
+    for (int k = 0; k < kTiles; ++k) {
         if (k >= a.row_tiles) continue;
         for (int x = 0; x < kWarps; ++x) line[k] += part.sums[k][x];
         total += places(line[k], 0);
@@ -354,12 +355,12 @@ __device__ __forceinline__ void find_part(const TreeArgs& a, int cta, int ctas, 
     const int cost = total * a.Hkv >= (long long)ctas * kShortPart ? kUnitCost : 0;
     total = 0;
 #pragma unroll
-    for (int k = 0; k < kMaxRowTiles; ++k) total += places(line[k], cost);
+    for (int k = 0; k < kTiles; ++k) total += places(line[k], cost);
     // CTAs of the lines: by their lengths, one at least; the first line, the longest, gets what is over
     int rt = 0, cta0 = 0, n = ctas;
     long long mine_all = line[0];
 #pragma unroll
-    for (int k = kMaxRowTiles - 1; k > 0; --k) {
+    for (int k = kTiles - 1; k > 0; --k) {
         if (line[k] == 0 || rt != 0) continue;
         const int c = max(1, (int)divide(ctas * places(line[k], cost), total));
         n -= c;
@@ -386,7 +387,7 @@ __device__ __forceinline__ void find_part(const TreeArgs& a, int cta, int ctas, 
     }
     long long at = 0;
 #pragma unroll
-    for (int k = 0; k < kMaxRowTiles; ++k) {
+    for (int k = 0; k < kTiles; ++k) {
         if (k != rt) continue;
         for (int x = 0; x < warp; ++x) at += part.sums[k][x];
         at = places(at + upto[k] - mine[k], cost) * a.Hkv;
@@ -1286,7 +1287,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         return;
     }
     if (tid < kFindThreads) {
-        find_part(a, blockIdx.x, gridDim.x, sm.part);
+        find_part<(P > 1 ? 1 : kMaxRowTiles)>(a, blockIdx.x, gridDim.x, sm.part);
     } else if (warp == C::kLoadWarp && lane == 0) {
         for (int s = 0; s < C::kSlots; ++s) {
             mbar_init(&sm.full[s], F4 ? C::kWidenWarps / 2 : 1);
