@@ -617,6 +617,7 @@ int moska_decode_step_paged(const uint16_t* q, const float* summaries, const voi
  *   lse_out  float [B][Hq]      may be NULL; -inf for such a row
  *   ws       moska_tree_attn_workspace_bytes(shape) bytes (20 MB for D = 128), 256-byte aligned; calls that
  *            share it must not overlap.  Not read or written (may be NULL) with n_unique_splits = 1.
+ * out, lse_out and ws may not overlap one another or what is read: the call is refused.
  * shape: B, Hq, Hkv, D, q_len and n_unique_splits are read: a context is cut into at most that many parts, as the
  * work of all contexts is shared among the SMs; 64 lets any batch be shared evenly, and costs no more than 2.  What a
  * node does not see has no influence on it, infinities and NaN included.  Scores, softmax statistics, row sums and results

@@ -1301,6 +1301,23 @@ int moska_tree_attn(const uint16_t* q, const moska_paged_kv* kv, const int32_t* 
     const size_t need = moska_tree_attn_workspace_bytes(shape);
     if (need > 0 && (ws == nullptr || !aligned(ws, 256) || ws_bytes < need))
         return fail(MOSKA_ERR_WORKSPACE, "workspace missing, misaligned or smaller than %zu bytes", need);
+    auto extent = [](const char* name, const void* p, size_t bytes) {
+        return Extent{name, reinterpret_cast<uintptr_t>(p), p == nullptr ? 0 : bytes};
+    };
+    const size_t rows = (size_t)shape->B * shape->Hq, requests = (size_t)n_requests * 4;
+    moska_shape heads = *shape;
+    heads.q_len = 0;
+    Extent pool[2];
+    pool_extents(kv, &heads, pool);
+    const Extent to[3] = {extent("out", out, rows * shape->D * 2), extent("lse_out", lse_out, rows * 4),
+                          extent("ws", need > 0 ? ws : nullptr, need)};
+    const Extent from[7] = {extent("q", q, rows * shape->D * 2), extent("parents", parents, (size_t)shape->B * 4),
+                            extent("row_start", row_start, requests + 4), extent("kv_len", kv->kv_len, requests),
+                            extent("page_table", kv->page_table, requests * kv->max_pages), pool[0], pool[1]};
+    for (int i = 0; i < 3; ++i) {
+        for (int j = 0; j < i; ++j) MOSKA_TRY(check_apart(to[j], to[i]));
+        for (const Extent& f : from) MOSKA_TRY(check_apart(to[i], f));
+    }
     MOSKA_TRY(check_device());
     MOSKA_TRY(status_word(&view.status));
     const bool fp4 = kv->format == MOSKA_KV_FP4;

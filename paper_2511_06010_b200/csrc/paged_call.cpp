@@ -488,7 +488,8 @@ PyObject* py_commit(PyObject*, PyObject* const* a, Py_ssize_t n_args)
         if (n * nodes > INT32_MAX) refuse("too many nodes");
         const auto result = [&] { return at::empty({n}, at::TensorOptions().dtype(at::kInt).device(s.device)); };
         if (n > 0) {
-            const moska_shape shape = shape_of(n * nodes, s.Hkv, s.Hkv, s.D, nodes);
+            // (with row_start the rows themselves are not at hand)
+            const moska_shape shape = shape_of(first == nullptr ? n * nodes : INT32_MAX, s.Hkv, s.Hkv, s.D, nodes);
             const OnDevice on(s.device, a[8]);
             if (tp == nullptr) {
                 to = result();

@@ -56,13 +56,14 @@ def test_long_parts(fmt, D, Hq, nodes):
 
 @pytest.mark.parametrize("fmt", ["bf16", "fp4"])
 @pytest.mark.parametrize("splits", [1, 2, 5, 64])
-def test_slots_of_the_layer(fmt, splits):
+@pytest.mark.parametrize("T,Hq", [(20, 16), (7, 8), (1, 2)])
+def test_slots_of_the_layer(fmt, splits, T, Hq):
     """The layer's partial slots for any number of them, long and short contexts in one batch."""
     from paper_2511_06010_b200.engine import MoskaLayer
 
-    lens, T = [2000, 30, 0, 700], 20
-    c = case(fmt, 128, 16, 2, 64, lens, [T] * 4, seed=7)
-    layer = MoskaLayer(c["rows"], 16, 2, 128, 1, 128, 1, max(lens), q_len=T, paged_fmt=fmt, n_unique_splits=splits)
+    lens = [2000, 30, 0, 700]
+    c = case(fmt, 128, Hq, 2, 64, lens, [T] * 4, seed=7)
+    layer = MoskaLayer(c["rows"], Hq, 2, 128, 1, 128, 1, max(lens), q_len=T, paged_fmt=fmt, n_unique_splits=splits)
     layer.o_part.fill_(float("nan"))
     layer.lse_part.fill_(float("nan"))
     layer.unique_paged(c["q"].cuda(), c["store"], c["table"], c["length"], parents=c["up"])
@@ -142,3 +143,20 @@ def test_contexts_of_millions_of_tokens(fmt, length):
         mass = (p / p.sum(-1, keepdims=True)) @ np.abs(vv[sees[i], 0])
         assert (np.abs(lse[i].double().cpu().numpy() - l) <= l_tol + part / 128 * 2.0 ** -24 + 2.0 ** -20).all()
         assert (np.abs(R.to_f64(out[i]) - o) <= 2 * o_tol + part / 16 * 2.0 ** -23 * mass).all()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp4"])
+@pytest.mark.parametrize("splits", [1, 3])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("most", [1, 8, 16])
+def test_small_ragged_trees(fmt, splits, D, most):
+    """Trees of few rows, ragged, without nodes or a context, or with a context shorter than the tree."""
+    from paper_2511_06010_b200 import binding as M
+
+    lens = [40, 0, 700, 5, 64, 257]
+    nodes = [min(most, x) for x in (3, 6, most, 9, 0, 5)]
+    c = case(fmt, D, 8, 2, 32, lens, nodes, seed=5, pad=4, splits=splits, max_nodes=most)
+    out, lse = run(c, row_start=c["start"])
+    check(c, out, lse)
+    assert torch.isnan(out[-4:]).all() and torch.isnan(lse[-4:]).all()
+    assert M.device_status() == 0

@@ -199,3 +199,13 @@ def test_the_reference_attention_of_a_chain_is_the_paged_reference():
         assert all(np.array_equal(x, y) for x, y in zip(a, b))
     assert TR.visible(np.array([-1, 0, 0, 2]), 3) == [[], [0], [1], [1, 2]]
     assert TR.visible(np.array([-1, 0]), 0) == [[], []]
+
+
+def test_overlaps_of_tree_attention(M):
+    """Results and workspace apart from one another and from what is read (bytes of the batch: q and out 65536, lse 1024)."""
+    apart = dict(q=FAR[4], out=FAR[5], lse=FAR[6], parents=FAR[7])
+    for over, text in (
+            (dict(out=FAR[4] + 65536 - 16), "out"), (dict(lse=FAR[5] + 65536 - 4), "lse_out"), (dict(lse=FAR[4] + 4), "lse_out"),
+            (dict(lse=FAR[7] + 124), "parents"), (dict(out=FAR[0] + 16), "k_pages"), (dict(lse=FAR[1]), "v_pages"),
+            (dict(lse=FAR[3] + 12), "kv_len"), (dict(out=FAR[2] + 48), "page_table"), (dict(row_start=FAR[6] + 1020), "row_start")):
+        refused(M, -1, attn(M, **{**apart, **over}), text)
