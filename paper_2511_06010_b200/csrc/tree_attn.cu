@@ -32,8 +32,10 @@
 // pages: eight that widen.  Operands lie in a ring of slots, a K or a V tile each, as halves of 64 dimensions in rows of
 // 128 bytes with the 128-byte swizzle.
 //   bf16: one TMA box of min(page_size, 128) tokens a page and half.
-//   4 bits: a bulk copy a page into a ring of tiles of codes, which are widened to f16 operands, code times scale (half a
-//   step: 2^-11).  Queries are f16 too, scaled by a power of two per row.
+//   4 bits: a bulk copy a page into a ring of tiles of codes, which are widened to f16 operands, code times scale (values: half a
+//   step, 2^-11).  A key's product has 13 bits at most: what f16 cannot hold of it is a second operand, so that scores are
+//   exact but for their sums (without it lse was off by 2e-6 relative in contexts of 4096 tokens, 1e-5 in short ones).
+//   Queries are f16 too, scaled by a power of two per row.
 //
 // What a node sees: committed tokens, and of the last T tokens those whose bit is set in its 64-bit word of ancestors.
 // Only tiles that reach past the committed tokens look at it.  0 times NaN is NaN, so values of such tiles that are
@@ -81,7 +83,7 @@ struct Cfg {
     static constexpr int kSlots = F4 ? (D == 128 ? 4 : 8) : (D == 128 ? 6 : 12);
     static constexpr int kBlocks = kTile / kBlockTokens;  // 16-token blocks of a tile
     static constexpr int kCodeBytes = kBlocks * fp4_block_bytes(D);
-    static constexpr int kCodeSlots = F4 ? (D == 128 ? 3 : 6) : 1;
+    static constexpr int kCodeSlots = F4 ? (D == 128 ? 2 : 6) : 1;
 };
 
 // Units of few rows have each row P times, in lanes kTileRows / P apart: the i-th has the i-th part of every step's tokens, with a
@@ -125,6 +127,7 @@ template <int D, bool F4>
 struct Smem {
     using C = Cfg<D, F4>;
     uint8_t slot[C::kSlots][C::kSlotBytes];
+    uint8_t rest[F4 ? C::kSlotBytes : 1024];  // what the keys' rounding to f16 left of one tile
     uint8_t code[F4 ? C::kCodeSlots * C::kCodeBytes : 16];
     float ref[C::kGroups][kTileRows];       // the reference of a row's probabilities after a step of each softmax group
     float2 stat[2][C::kGroups][kTileRows];  // (reference, sum) of a unit's rows by each group; units take turns
@@ -136,7 +139,7 @@ struct Smem {
     TreeSmem tree;
     uint64_t full[C::kSlots], empty[C::kSlots];
     uint64_t code_full[C::kCodeSlots], code_empty[C::kCodeSlots];
-    uint64_t q_full[2], s_full[4], p_full[4], stat_full[2], ref_full[C::kGroups][4], pv_done[4], o_full, o_free;
+    uint64_t q_full[2], s_full[4], p_full[4], stat_full[2], ref_full[C::kGroups][4], pv_done[4], o_full, o_free, rest_empty;
     unsigned long long bad[8];  // tree tokens with values that are not finite; units take turns
     Part part;
     uint32_t tmem_base;
@@ -225,6 +228,15 @@ __device__ __forceinline__ uint32_t bf16x2(float lo, float hi)
 __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b)
 {
     const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// a b - c, rounded once
+__device__ __forceinline__ uint32_t hfms2(uint32_t a, uint32_t b, uint32_t c)
+{
+    const uint32_t minus = c ^ 0x80008000u;
+    const __half2 v = __hfma2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b),
+                              *reinterpret_cast<const __half2*>(&minus));
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
@@ -1091,6 +1103,7 @@ __device__ __forceinline__ void score_role(Smem<D, F4>& sm, uint32_t tmem)
     const uint32_t id = F4 ? idesc_f16_f32(128, kStep, false) : idesc_bf16_f32(128, kStep, false);
     const uint64_t d = smem_desc_sw128(0, 16, 1024);
     const uint32_t hi = static_cast<uint32_t>(d >> 32), lo = static_cast<uint32_t>(d) + (smem_u32(sm.slot[0]) >> 4);
+    const uint32_t rest = static_cast<uint32_t>(d) + (smem_u32(sm.rest) >> 4);
     int* gave_up = &sm.gave_up;
     uint32_t step = 0;
     for (uint32_t n_unit = 0;; ++n_unit) {
@@ -1108,6 +1121,13 @@ __device__ __forceinline__ void score_role(Smem<D, F4>& sm, uint32_t tmem)
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks)
                     mma_ts(to, q + 8 * ks, descriptor(hi, k + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4)), id, ks > 0);
+                if constexpr (F4) {
+                    const uint32_t r = rest + ((half * kStep * 128) >> 4);
+#pragma unroll
+                    for (int ks = 0; ks < D / 16; ++ks)
+                        mma_ts(to, q + 8 * ks, descriptor(hi, r + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4)), id, true);
+                    if (half == 1) tc_commit(&sm.rest_empty);
+                }
                 tc_commit(&sm.s_full[step & 3]);
                 if (half == 1) tc_commit(&sm.empty[s]);
             }
@@ -1156,7 +1176,7 @@ __device__ __forceinline__ void value_role(Smem<D, F4>& sm, uint32_t tmem)
 // go to memory together have tokens y and y ^ 5: their loads and their swizzled stores both fall on eight different
 // 16-byte pieces of the banks.
 template <int D>
-__device__ __forceinline__ void widen_keys(const uint8_t* code_tile, uint8_t* to, int block0, int lane)
+__device__ __forceinline__ void widen_keys(const uint8_t* code_tile, uint8_t* to, uint8_t* rest, int block0, int lane)
 {
     using B = Fp4Block<D>;
     constexpr int J = D / 32;
@@ -1181,8 +1201,15 @@ __device__ __forceinline__ void widen_keys(const uint8_t* code_tile, uint8_t* to
             uint32_t f[4];
             e2m1x8_to_f16x2(code[x], f);
             const uint32_t s2 = __byte_perm(sc[x >> 1], 0, (x & 1) ? 0x3232 : 0x1010);
-            *reinterpret_cast<uint4*>(to + (x >> 1) * kHalfBytes + row * 128 + (((4 * (x & 1) + c) ^ (row & 7)) << 4)) =
-                make_uint4(hmul2(f[0], s2), hmul2(f[1], s2), hmul2(f[2], s2), hmul2(f[3], s2));
+            const int at = (x >> 1) * kHalfBytes + row * 128 + (((4 * (x & 1) + c) ^ (row & 7)) << 4);
+            uint32_t y[4], left[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                y[e] = hmul2(f[e], s2);
+                left[e] = hfms2(f[e], s2, y[e]);
+            }
+            *reinterpret_cast<uint4*>(to + at) = make_uint4(y[0], y[1], y[2], y[3]);
+            *reinterpret_cast<uint4*>(rest + at) = make_uint4(left[0], left[1], left[2], left[3]);
         }
     }
 }
@@ -1257,8 +1284,9 @@ __device__ __forceinline__ void widen_role(Smem<D, true>& sm, const TreeArgs& a,
             const uint32_t seq = 2 * tile + values, s = seq % C::kSlots, c = tile % C::kCodeSlots;
             if (!warp_wait(&sm.code_full[c], (tile / C::kCodeSlots) & 1, gave_up)) return;
             if (seq >= C::kSlots && !warp_wait(&sm.empty[s], ((seq / C::kSlots) - 1) & 1, gave_up)) return;
+            if (!values && tile > 0 && !warp_wait(&sm.rest_empty, (tile - 1) & 1, gave_up)) return;
             const uint8_t* from = sm.code + c * C::kCodeBytes;
-            if (!values) widen_keys<D>(from, sm.slot[s], block0, lane);
+            if (!values) widen_keys<D>(from, sm.slot[s], sm.rest, block0, lane);
             else if (P > 1 && behind + kTile <= 0) widen_values<D, false>(from, sm.slot[s], block0, lane, behind, w.q.nodes, nullptr);
             else widen_values<D, true>(from, sm.slot[s], block0, lane, behind, w.q.nodes, &sm.bad[n_unit & 7]);
             fence_proxy_async_smem();
@@ -1309,6 +1337,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             mbar_init(&sm.pv_done[x], 1);
         }
         mbar_init(&sm.o_full, 1);
+        mbar_init(&sm.rest_empty, 1);
         mbar_init(&sm.o_free, kTileRows);
         for (int x = 0; x < 8; ++x) sm.bad[x] = 0;
         sm.gave_up = 0;
