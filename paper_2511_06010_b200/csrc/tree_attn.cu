@@ -72,12 +72,12 @@ struct Cfg {
     static constexpr int kHalves = D / 64;
     static constexpr int kGroups = 2;  // of softmax warps
     static constexpr int kRowWarp0 = 4 * kGroups, kLoadWarp = kRowWarp0 + 4, kScoreWarp = kLoadWarp + 1, kValueWarp = kLoadWarp + 2,
-                         kWidenWarp0 = kLoadWarp + 4, kWidenWarps = 8;
+                         kWidenWarp0 = kLoadWarp + 4, kKeyWarps = 8, kValueWarps = 4, kWidenWarps = kKeyWarps + kValueWarps;
     static constexpr int kThreads = 32 * (F4 ? kWidenWarp0 + kWidenWarps : kWidenWarp0);
     // Registers of a thread: at the launch, and of the groups of four warps after it.
-    static constexpr int kLaunchRegs = F4 ? 80 : 128;
-    static constexpr int kSoftmaxRegs = F4 ? 112 : 152, kRowRegs = F4 ? 96 : 128, kIssueRegs = F4 ? 40 : 80, kWidenRegs = 56;
-    static_assert(128 * (kGroups * kSoftmaxRegs + kRowRegs + kIssueRegs + (F4 ? 2 * kWidenRegs : 0)) <= kThreads * kLaunchRegs,
+    static constexpr int kLaunchRegs = F4 ? 72 : 128;
+    static constexpr int kSoftmaxRegs = F4 ? 112 : 152, kRowRegs = F4 ? 96 : 128, kIssueRegs = F4 ? 40 : 80, kWidenRegs = 48;
+    static_assert(128 * (kGroups * kSoftmaxRegs + kRowRegs + kIssueRegs + (F4 ? kWidenWarps / 4 * kWidenRegs : 0)) <= kThreads * kLaunchRegs,
                   "setmaxnreg: more than the CTA was launched with would be waited for without end");
     static constexpr int kSlotBytes = kHalves * kHalfBytes;
     static constexpr int kSlots = F4 ? (D == 128 ? 4 : 8) : (D == 128 ? 6 : 12);
@@ -139,7 +139,7 @@ struct Smem {
     TreeSmem tree;
     uint64_t full[C::kSlots], empty[C::kSlots];
     uint64_t code_full[C::kCodeSlots], code_empty[C::kCodeSlots];
-    uint64_t q_full[2], s_full[4], p_full[4], stat_full[2], ref_full[C::kGroups][4], pv_done[4], o_full, o_free, rest_empty;
+    uint64_t q_full[2], s_full[4], p_full[4], stat_full[2], ref_full[C::kGroups][4], pv_done[4], o_full, o_free, rest_empty[2], key_full[C::kSlots][2];  // (halves of a tile of keys)
     unsigned long long bad[8];  // tree tokens with values that are not finite; units take turns
     Part part;
     uint32_t tmem_base;
@@ -1113,7 +1113,11 @@ __device__ __forceinline__ void score_role(Smem<D, F4>& sm, uint32_t tmem)
         for (int j = 0; j < steps; ++j, ++step) {
             const uint32_t seq = step & ~1u, s = seq % C::kSlots, half = step & 1;  // (tile step / 2: slots 2 (step / 2) and the next)
             if (step >= 4 && !warp_wait(&sm.pv_done[step & 3], ((step >> 2) - 1) & 1, gave_up)) return;
-            if (half == 0 && !warp_wait(&sm.full[s], (seq / C::kSlots) & 1, gave_up)) return;
+            if constexpr (F4) {
+                if (!warp_wait(&sm.key_full[s][half], (seq / C::kSlots) & 1, gave_up)) return;
+            } else {
+                if (half == 0 && !warp_wait(&sm.full[s], (seq / C::kSlots) & 1, gave_up)) return;
+            }
             tc_fence_after_sync();
             if (elect_one()) {
                 const uint32_t to = tmem + kColS + (step & 3) * kStep;
@@ -1126,7 +1130,7 @@ __device__ __forceinline__ void score_role(Smem<D, F4>& sm, uint32_t tmem)
 #pragma unroll
                     for (int ks = 0; ks < D / 16; ++ks)
                         mma_ts(to, q + 8 * ks, descriptor(hi, r + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4)), id, true);
-                    if (half == 1) tc_commit(&sm.rest_empty);
+                    tc_commit(&sm.rest_empty[half]);
                 }
                 tc_commit(&sm.s_full[step & 3]);
                 if (half == 1) tc_commit(&sm.empty[s]);
@@ -1172,18 +1176,18 @@ __device__ __forceinline__ void value_role(Smem<D, F4>& sm, uint32_t tmem)
 }
 
 // ---- 4 bits: codes -> f16 operand rows ----------------------------------------------------------------
-// Keys of two blocks.  The D / 8 bytes of (token, c) are dimensions 32 x + 8 c .. + 7 for each group x.  Eight lanes that
+// Keys of a block.  The D / 8 bytes of (token, c) are dimensions 32 x + 8 c .. + 7 for each group x.  Eight lanes that
 // go to memory together have tokens y and y ^ 5: their loads and their swizzled stores both fall on eight different
 // 16-byte pieces of the banks.
 template <int D>
-__device__ __forceinline__ void widen_keys(const uint8_t* code_tile, uint8_t* to, uint8_t* rest, int block0, int lane)
+__device__ __forceinline__ void widen_keys(const uint8_t* code_tile, uint8_t* to, uint8_t* rest, int block, int lane)
 {
     using B = Fp4Block<D>;
     constexpr int J = D / 32;
     const int l = lane & 7, c = l & 3, qd = lane >> 3, token = (l >> 2) ? (qd ^ 5) : qd;
-#pragma unroll 2
-    for (int it = 0; it < 4; ++it) {
-        const int block = block0 + (it >> 1), t = 8 * (it & 1) + token, row = 16 * block + t;
+#pragma unroll
+    for (int it = 0; it < 2; ++it) {
+        const int t = 8 * it + token, row = 16 * block + t;
         const uint8_t* from = code_tile + block * B::kBytes;
         uint32_t code[J], sc[J / 2];
         if constexpr (J == 4) {
@@ -1268,15 +1272,16 @@ __device__ __forceinline__ void widen_values(const uint8_t* code_tile, uint8_t* 
     }
 }
 
-// Four warps widen keys and four values, two blocks each.
+// Eight warps widen a block of keys each, four two blocks of values.  (The remainders of a tile have one buffer: the next tile's keys wait
+// for this one's product, by halves.  With four warps for keys and whole tiles 64 requests of 8 nodes took 224 us, 32 of 64 nodes 568.)
 template <int D, int P>
 __device__ __forceinline__ void widen_role(Smem<D, true>& sm, const TreeArgs& a, Walk w, int warp, int lane)
 {
     using C = Cfg<D, true>;
-    static_assert(C::kWidenWarps == C::kBlocks, "two blocks a warp, of keys or of values");
+    static_assert(C::kKeyWarps == C::kBlocks && 2 * C::kValueWarps == C::kBlocks, "a block of keys or two of values");
     int* gave_up = &sm.gave_up;
-    const bool values = warp >= 4;
-    const int block0 = 2 * (warp & 3);
+    const bool values = warp >= C::kKeyWarps;
+    const int block0 = values ? 2 * (warp - C::kKeyWarps) : warp, half = warp / (C::kKeyWarps / 2);  // (of keys)
     uint32_t tile = 0, n_unit = 0;
     do {
         for (int j = 0; j < w.tiles; ++j, ++tile) {
@@ -1284,7 +1289,7 @@ __device__ __forceinline__ void widen_role(Smem<D, true>& sm, const TreeArgs& a,
             const uint32_t seq = 2 * tile + values, s = seq % C::kSlots, c = tile % C::kCodeSlots;
             if (!warp_wait(&sm.code_full[c], (tile / C::kCodeSlots) & 1, gave_up)) return;
             if (seq >= C::kSlots && !warp_wait(&sm.empty[s], ((seq / C::kSlots) - 1) & 1, gave_up)) return;
-            if (!values && tile > 0 && !warp_wait(&sm.rest_empty, (tile - 1) & 1, gave_up)) return;
+            if (!values && tile > 0 && !warp_wait(&sm.rest_empty[half], (tile - 1) & 1, gave_up)) return;
             const uint8_t* from = sm.code + c * C::kCodeBytes;
             if (!values) widen_keys<D>(from, sm.slot[s], sm.rest, block0, lane);
             else if (P > 1 && behind + kTile <= 0) widen_values<D, false>(from, sm.slot[s], block0, lane, behind, w.q.nodes, nullptr);
@@ -1292,7 +1297,7 @@ __device__ __forceinline__ void widen_role(Smem<D, true>& sm, const TreeArgs& a,
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) {
-                mbar_arrive(&sm.full[s]);
+                mbar_arrive(values ? &sm.full[s] : &sm.key_full[s][half]);
                 mbar_arrive(&sm.code_empty[c]);
             }
         }
@@ -1318,7 +1323,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         find_part<(P > 1 ? 1 : kMaxRowTiles)>(a, blockIdx.x, gridDim.x, sm.part);
     } else if (warp == C::kLoadWarp && lane == 0) {
         for (int s = 0; s < C::kSlots; ++s) {
-            mbar_init(&sm.full[s], F4 ? C::kWidenWarps / 2 : 1);
+            mbar_init(&sm.full[s], F4 ? C::kValueWarps : 1);
             mbar_init(&sm.empty[s], 1);
         }
         for (int x = 0; x < C::kCodeSlots; ++x) {
@@ -1337,7 +1342,10 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             mbar_init(&sm.pv_done[x], 1);
         }
         mbar_init(&sm.o_full, 1);
-        mbar_init(&sm.rest_empty, 1);
+        for (int x = 0; x < 2; ++x) {
+            mbar_init(&sm.rest_empty[x], 1);
+            for (int s = 0; s < C::kSlots; ++s) mbar_init(&sm.key_full[s][x], C::kKeyWarps / 2);
+        }
         mbar_init(&sm.o_free, kTileRows);
         for (int x = 0; x < 8; ++x) sm.bad[x] = 0;
         sm.gave_up = 0;

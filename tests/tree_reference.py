@@ -36,9 +36,10 @@ def visible(parents, length):
 def attend(q, k, v, scale, fmt):
     """q [Hq][D], k and v [tokens][Hkv][D] of the tokens that a node sees -> out, lse and the bounds of both.
 
-    Roundings of paged_reference.attend, and in the 4-bit format those of operands in f16: a key, code times scale,
-    half a step, 2^-11 of it, or 2^-25 below f16's normal range; a query element, exact down to 2^-17 of the row's largest and
-    within 2^-25 of that below.  They change a score by at most scale times the sums below, and the probabilities by that."""
+    Roundings of paged_reference.attend, and in the 4-bit format those of operands in f16: a key is exact, as a product and what
+    its rounding left, down to 2^-25 for each; a query element is exact down to 2^-17 of the row's largest and within 2^-25
+    of that below; a value is half a step off, 2^-11.  They change a score by at most scale times the sums below, and the
+    probabilities by that."""
     out, lse, tol, lse_tol = R.attend(q, k, v, scale, fmt)
     if fmt == "bf16" or len(k) == 0:
         return out, lse, tol, lse_tol
@@ -46,12 +47,12 @@ def attend(q, k, v, scale, fmt):
     kk, vv = (np.repeat(x, q.shape[0] // Hkv, axis=1) for x in (k, v))
     aq, ak = np.abs(q), np.abs(kk)
     top = aq.max(-1)
-    more = 2.0 ** -11 * np.einsum("hd,thd->th", aq, ak) + 2.0 ** -25 * aq.sum(-1) + 2.0 ** -25 * top * ak.sum(-1)
+    more = 2.0 ** -24 * aq.sum(-1) + 2.0 ** -25 * top * ak.sum(-1)
     more = 1.01 * scale * more.max(0)
     s = np.einsum("hd,thd->ht", q, kk) * scale
     p = np.exp(s - s.max(-1, keepdims=True))
     mass = np.einsum("ht,thd->hd", p / p.sum(-1, keepdims=True), np.abs(vv))
-    return out, lse, tol + (1 + 2.0 ** -7) * np.expm1(2 * more)[:, None] * mass, lse_tol + more
+    return out, lse, tol + ((1 + 2.0 ** -7) * np.expm1(2 * more)[:, None] + 2.0 ** -11) * mass, lse_tol + more
 
 
 def verify(target, draft, tokens, parents, u_accept, u_next):
