@@ -10,15 +10,15 @@
 // third group stages the next unit's queries and writes the last unit's rows.  TMEM: O 128, S 4 x 64, Q 2 x 64 = 512 columns.
 //
 // What bounds it.  A tile of 128 rows and 128 tokens is 1024 cycles of MMA (D = 128), as many of exponentials, and in 4 bits
-// some 1300 cycles of shared memory (operands written, and read by the MMAs).  A half takes a group about 1900 cycles from
+// some 1800 cycles of shared memory (operands written, and read by the MMAs) and 512 more of MMA.  A half takes a group about 1900 cycles from
 // scores to probabilities, of which 900 are exponentials that the other group's slow down, so a tile takes 1900 cycles instead of
 // 1024 (bf16, 24 requests of 60 nodes and 1K-16K tokens: 0.43 ms, 0.95 PFLOP/s, tensor pipe 53 % busy).  Up to 64 rows bf16
 // waits for memory (64 requests of 16 nodes and 4096 tokens: 188 us, 5.7 TB/s).  4 bits, 32 requests of 64 nodes and 1K-8K tokens:
-// 365 us.  One request of 8 nodes and 1000 tokens: 17 us, of which 3.7 find the part, 1.3 bring the queries, 3 are the tile,
+// 463 us, a tile's keys wait for the product before (their remainders have one buffer).  One request of 8 nodes and 1000 tokens: 17 us, of which 3.7 find the part, 1.3 bring the queries, 3 are the tile,
 // 1.2 its rows, and the rest the two launches.
 // Not kept: a third softmax group (bf16 471 us for 437: registers), products of 128 tokens (one MMA warp waits for the other's
 // operands), the next scores read between a step's exponentials (468 for 434), part of the exponentials as polynomials (all
-// of them left out saves 10 %), sixteen warps that widen (144 for 142).
+// of them left out saves 10 %).
 //
 // One CTA per SM.  For each row tile (first 128 rows of every request, second 128, ..) the tiles of all its units, request after
 // request and head after head, form a line.  Lines get CTAs by their lengths and are cut into equal parts, one per CTA,
@@ -29,7 +29,7 @@
 //
 // Warps, in this order: groups of four for the softmax (thread i: row i % 128 = TMEM lane), four for queries and results, one for
 // copies, one for the MMAs of Q K^T and one for those of P V (one warp for both left the tensor cores idle while it waited).  4-bit
-// pages: eight that widen.  Operands lie in a ring of slots, a K or a V tile each, as halves of 64 dimensions in rows of
+// pages: twelve that widen.  Operands lie in a ring of slots, a K or a V tile each, as halves of 64 dimensions in rows of
 // 128 bytes with the 128-byte swizzle.
 //   bf16: one TMA box of min(page_size, 128) tokens a page and half.
 //   4 bits: a bulk copy a page into a ring of tiles of codes, which are widened to f16 operands, code times scale (values: half a
@@ -88,8 +88,8 @@ struct Cfg {
 
 // Units of few rows have each row P times, in lanes kTileRows / P apart: the i-th has the i-th part of every step's tokens, with a
 // reference, a sum and an O of its own, as if a context were cut into P.  The four warps of a group have a P-th of the
-// scores each then, where one warp of live rows would have had them all (4 bits, 64 requests of 4096 tokens: 32 rows 143 us with
-// P = 4, 152 with 2, 176 without; 64 rows 156 with 2, 183 without.  bf16 waits for memory there: 182, 182, 183 us and 190, 192;
+// scores each then, where one warp of live rows would have had them all (4 bits, 64 requests of 4096 tokens, before keys had
+// remainders: 32 rows 143 us with P = 4, 152 with 2, 176 without; 64 rows 156 with 2, 183 without.  bf16 waits for memory there: 182, 182, 183 us and 190, 192;
 // it has P = 1 alone).
 template <int P>
 struct Spread {
@@ -1122,16 +1122,16 @@ __device__ __forceinline__ void score_role(Smem<D, F4>& sm, uint32_t tmem)
             if (elect_one()) {
                 const uint32_t to = tmem + kColS + (step & 3) * kStep;
                 const uint32_t k = lo + ((s * C::kSlotBytes + half * kStep * 128) >> 4);
-#pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks)
-                    mma_ts(to, q + 8 * ks, descriptor(hi, k + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4)), id, ks > 0);
-                if constexpr (F4) {
+                if constexpr (F4) {  // the remainders first: their buffer is wanted
                     const uint32_t r = rest + ((half * kStep * 128) >> 4);
 #pragma unroll
                     for (int ks = 0; ks < D / 16; ++ks)
-                        mma_ts(to, q + 8 * ks, descriptor(hi, r + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4)), id, true);
+                        mma_ts(to, q + 8 * ks, descriptor(hi, r + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4)), id, ks > 0);
                     tc_commit(&sm.rest_empty[half]);
                 }
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks)
+                    mma_ts(to, q + 8 * ks, descriptor(hi, k + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4)), id, F4 || ks > 0);
                 tc_commit(&sm.s_full[step & 3]);
                 if (half == 1) tc_commit(&sm.empty[s]);
             }

@@ -38,7 +38,7 @@ def attend(q, k, v, scale, fmt):
 
     Roundings of paged_reference.attend, and in the 4-bit format those of operands in f16: a key is exact, as a product and what
     its rounding left, down to 2^-25 for each; a query element is exact down to 2^-17 of the row's largest and within 2^-25
-    of that below; a value is half a step off, 2^-11.  They change a score by at most scale times the sums below, and the
+    of that below.  They change a score by at most scale times the sums below, and the
     probabilities by that."""
     out, lse, tol, lse_tol = R.attend(q, k, v, scale, fmt)
     if fmt == "bf16" or len(k) == 0:
@@ -52,7 +52,7 @@ def attend(q, k, v, scale, fmt):
     s = np.einsum("hd,thd->ht", q, kk) * scale
     p = np.exp(s - s.max(-1, keepdims=True))
     mass = np.einsum("ht,thd->hd", p / p.sum(-1, keepdims=True), np.abs(vv))
-    return out, lse, tol + ((1 + 2.0 ** -7) * np.expm1(2 * more)[:, None] + 2.0 ** -11) * mass, lse_tol + more
+    return out, lse, tol + (1 + 2.0 ** -7) * np.expm1(2 * more)[:, None] * mass, lse_tol + more
 
 
 def verify(target, draft, tokens, parents, u_accept, u_next):
