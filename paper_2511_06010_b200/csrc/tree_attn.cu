@@ -14,8 +14,8 @@
 // scores to probabilities, of which 900 are exponentials that the other group's slow down, so a tile takes 1900 cycles instead of
 // 1024 (bf16, 24 requests of 60 nodes and 1K-16K tokens: 0.43 ms, 0.95 PFLOP/s, tensor pipe 53 % busy).  Up to 64 rows bf16
 // waits for memory (64 requests of 16 nodes and 4096 tokens: 188 us, 5.7 TB/s).  4 bits, 32 requests of 64 nodes and 1K-8K tokens:
-// 463 us, a tile's keys wait for the product before (their remainders have one buffer).  One request of 8 nodes and 1000 tokens: 17 us, of which 3.7 find the part, 1.3 bring the queries, 3 are the tile,
-// 1.2 its rows, and the rest the two launches.
+// 463 us, a tile's keys wait for the product before (their remainders have one buffer).  One request of 8 nodes and 1000 tokens:
+// 17 us, of which 3.7 find the part, 1.3 bring the queries, 3 are the tile, 1.2 its rows, and the rest the two launches.
 // Not kept: a third softmax group (bf16 471 us for 437: registers), products of 128 tokens (one MMA warp waits for the other's
 // operands), the next scores read between a step's exponentials (468 for 434), part of the exponentials as polynomials (all
 // of them left out saves 10 %).
@@ -89,8 +89,8 @@ struct Cfg {
 // Units of few rows have each row P times, in lanes kTileRows / P apart: the i-th has the i-th part of every step's tokens, with a
 // reference, a sum and an O of its own, as if a context were cut into P.  The four warps of a group have a P-th of the
 // scores each then, where one warp of live rows would have had them all (4 bits, 64 requests of 4096 tokens, before keys had
-// remainders: 32 rows 143 us with P = 4, 152 with 2, 176 without; 64 rows 156 with 2, 183 without.  bf16 waits for memory there: 182, 182, 183 us and 190, 192;
-// it has P = 1 alone).
+// remainders: 32 rows 143 us with P = 4, 152 with 2, 176 without; 64 rows 156 with 2, 183 without.  bf16 waits for memory
+// there, 182, 182, 183 us and 190, 192; it has P = 1 alone).
 template <int P>
 struct Spread {
     static constexpr int kRows = kTileRows / P, kCols = kStep / P;
@@ -139,7 +139,8 @@ struct Smem {
     TreeSmem tree;
     uint64_t full[C::kSlots], empty[C::kSlots];
     uint64_t code_full[C::kCodeSlots], code_empty[C::kCodeSlots];
-    uint64_t q_full[2], s_full[4], p_full[4], stat_full[2], ref_full[C::kGroups][4], pv_done[4], o_full, o_free, rest_empty[2], key_full[C::kSlots][2];  // (halves of a tile of keys)
+    uint64_t q_full[2], s_full[4], p_full[4], stat_full[2], ref_full[C::kGroups][4], pv_done[4], o_full, o_free;
+    uint64_t rest_empty[2], key_full[C::kSlots][2];  // (4 bits: halves of a tile of keys)
     unsigned long long bad[8];  // tree tokens with values that are not finite; units take turns
     Part part;
     uint32_t tmem_base;
