@@ -622,7 +622,8 @@ int moska_decode_step_paged(const uint16_t* q, const float* summaries, const voi
  * work of all contexts is shared among the SMs; 64 lets any batch be shared evenly, and costs no more than 2.  What a
  * node does not see has no influence on it, infinities and NaN included.  Scores, softmax statistics, row sums and results
  * are held in fp32.  In 16 bits: bf16 pages, the probabilities (bf16, half a step 2^-8 of each); 4-bit pages, the
- * probabilities (f16, 2^-11), a value as scale * code (f16, 2^-11), a key as two f16 numbers that add up to scale * code (within
+ * probabilities (f16, 2^-11; below 2^-21 of the row's largest within 2^-32 of that, so what is smaller counts in the row sum
+ * alone), a value as scale * code (f16, 2^-11), a key as two f16 numbers that add up to scale * code (within
  * 2^-25) and the queries times a power of two per row (f16, exact down to 2^-17 of the row's largest element).  out is
  * rounded once more.
  * A part of a context of more than about 400 million tokens would pass the limit of a wait (2 s): MOSKA_ERR_TIMEOUT in the

@@ -66,6 +66,10 @@ constexpr uint32_t kColO = 0, kColS = 128, kColQ = 384;  // tensor-memory column
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kStagePitch = 144;  // 128 bytes and 16: a row's pieces and a piece's rows both fall on different banks
 constexpr float kRescaleAt = 8.f;  // log2 units that a row's maximum may grow before its sums are rescaled
+// 4 bits: log2 of P at a row's reference, so that P is at most 2^15.  f16 ends in steps of 2^-24: with P = 1 at the reference,
+// many tokens of less than 2^-25 each beside one that holds most of a row's weight (3 % of a row of a million tokens) would
+// count in its sum and not in its result.  So they are held down to 2^-32 of the row's largest, as in moska_unique_attn_paged.
+constexpr float kBelowF16 = 7.f;
 
 template <int D, bool F4>
 struct Cfg {
@@ -645,7 +649,8 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
                 }
                 if (now != m) l *= fast_exp2((m - now) * unit);
                 m = now;
-                const float base = m == -INFINITY ? 0.f : m * unit;  // (nothing seen yet)
+                // (the product rounded before the difference, as lse has it)
+                const float base = m == -INFINITY ? 0.f : __fmul_rn(m, unit) - (F4 ? kBelowF16 : 0.f);  // (nothing seen yet)
                 const float2 unit2 = make_float2(unit, unit), base2 = make_float2(-base, -base);
                 float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                 auto exponentials_of = [&](const auto& x, auto& pk) {
@@ -873,7 +878,8 @@ struct Rows {
         const int64_t row = (int64_t)(w.q.first + node) * a.Hq + w.h * G + ir % G;
         float inv = l == 0.f ? 0.f : 1.f / l;
         if (P > 1 && mine != m) inv *= fast_exp2((mine - m) * unit);  // (0 for a part that has seen nothing)
-        const float lse = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m * unit * kLn2) + logf(l);
+        const float lse = l == 0.f ? -INFINITY : (m == -INFINITY ? 0.f : m * unit * kLn2) + logf(F4 ? l * 0.0078125f : l);
+        static_assert(kBelowF16 == 7.f, "l is 2^7 times the sum relative to the reference");
         const bool final_row = a.out != nullptr && w.tiles == w.q.tiles;  // (the same for all rows)
         void* to = a.out + row * D;
         float* lse_to = a.lse_out != nullptr ? a.lse_out + row : nullptr;
