@@ -623,9 +623,8 @@ int moska_decode_step_paged(const uint16_t* q, const float* summaries, const voi
  * node does not see has no influence on it, infinities and NaN included.  Scores, softmax statistics, row sums and results
  * are held in fp32.  In 16 bits: bf16 pages, the probabilities (bf16, half a step 2^-8 of each); 4-bit pages, the
  * probabilities (f16, 2^-11; below 2^-21 of the row's largest within 2^-32 of that, so what is smaller counts in the row sum
- * alone), a value as scale * code (f16, 2^-11), a key as two f16 numbers that add up to scale * code (within
- * 2^-25) and the queries times a power of two per row (f16, exact down to 2^-17 of the row's largest element).  out is
- * rounded once more.
+ * alone) and a value as scale * code (f16, 2^-11); keys are exact for every finite scale, as two bf16 numbers that add up to
+ * scale * code, and so are the queries.  out is rounded once more.
  * A part of a context of more than about 400 million tokens would pass the limit of a wait (2 s): MOSKA_ERR_TIMEOUT in the
  * device status word, and results that are not valid; cut it (n_unique_splits).
  */

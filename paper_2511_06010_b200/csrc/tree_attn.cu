@@ -32,10 +32,13 @@
 // pages: twelve that widen.  Operands lie in a ring of slots, a K or a V tile each, as halves of 64 dimensions in rows of
 // 128 bytes with the 128-byte swizzle.
 //   bf16: one TMA box of min(page_size, 128) tokens a page and half.
-//   4 bits: a bulk copy a page into a ring of tiles of codes, which are widened to f16 operands, code times scale (values: half a
-//   step, 2^-11).  A key's product has 13 bits at most: what f16 cannot hold of it is a second operand, so that scores are
-//   exact but for their sums (without it lse was off by 2e-6 relative in contexts of 4096 tokens, 1e-5 in short ones).
-//   Queries are f16 too, scaled by a power of two per row.
+//   4 bits: a bulk copy a page into a ring of tiles of codes, which are widened to operands, code times scale.  Values: f16 (half
+//   a step, 2^-11).  Keys: two bf16 operands, code times the scale's upper 6 bits and code times the rest of it, exact
+//   for every finite scale, and bf16 queries as they are, so that scores are exact but for their sums.  (With a key as one
+//   f16 operand lse was off by 2e-6 relative in contexts of 4096 tokens, 1e-5 in short ones; two f16 ones, the product and
+//   what is left of it, are 14 instructions less for 8 codes, 205 us for 64 requests of 8 nodes instead of 214 and 511 for 32
+//   of 64 instead of 558, but give inf - inf above a scale of 10912 and steps of 2^-24.)  Rows of queries are scaled
+//   by a power of two.
 //
 // What a node sees: committed tokens, and of the last T tokens those whose bit is set in its 64-bit word of ancestors.
 // Only tiles that reach past the committed tokens look at it.  0 times NaN is NaN, so values of such tiles that are
@@ -131,7 +134,7 @@ template <int D, bool F4>
 struct Smem {
     using C = Cfg<D, F4>;
     uint8_t slot[C::kSlots][C::kSlotBytes];
-    uint8_t rest[F4 ? C::kSlotBytes : 1024];  // what the keys' rounding to f16 left of one tile
+    uint8_t rest[F4 ? C::kSlotBytes : 1024];  // one tile's second operand of keys
     uint8_t code[F4 ? C::kCodeSlots * C::kCodeBytes : 16];
     float ref[C::kGroups][kTileRows];       // the reference of a row's probabilities after a step of each softmax group
     float2 stat[2][C::kGroups][kTileRows];  // (reference, sum) of a unit's rows by each group; units take turns
@@ -236,12 +239,9 @@ __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b)
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// a b - c, rounded once
-__device__ __forceinline__ uint32_t hfms2(uint32_t a, uint32_t b, uint32_t c)
+__device__ __forceinline__ uint32_t bmul2(uint32_t a, uint32_t b)
 {
-    const uint32_t minus = c ^ 0x80008000u;
-    const __half2 v = __hfma2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b),
-                              *reinterpret_cast<const __half2*>(&minus));
+    const __nv_bfloat162 v = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
@@ -739,8 +739,8 @@ struct Rows {
             if (to[e] != nullptr) *reinterpret_cast<uint4*>(to[e] + offset + 16 * (lane & 7)) = v[e];
     }
 
-    // A unit's rows: what they see, and their queries into tensor memory.  In 4-bit pages queries are f16 times a
-    // power of two that brings the row's largest element into [1, 2) (exact down to 2^-17 of it, within 2^-25 of it below).
+    // A unit's rows: what they see, and their queries into tensor memory.  With 4-bit pages times a power of two that brings
+    // the row's largest element into [2^16, 2^17): scores stay finite, keys being up to 6 * 65504 2^-16.
     __device__ __forceinline__ void prepare(const Walk& w, bool new_request, bool more, uint32_t n_unit)
     {
         if (new_request) {
@@ -800,17 +800,26 @@ struct Rows {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) top = __vmaxu2(top, x[e] & 0x7fff7fffu);
                     if (it + 1 == D / 64) {
-                        const int e2 = min(max((int)(max(top >> 16, top & 0xffffu) >> 7), 2), 252) - 127;
-                        down = __uint_as_float((uint32_t)(127 - e2) << 23);
+                        const int e2 = min(max((int)(max(top >> 16, top & 0xffffu) >> 7), 17), 252) - 127;
+                        down = __uint_as_float((uint32_t)(127 + 16 - e2) << 23);
                         // (neither 0 nor infinite: the -inf of a hidden token, or a score of 0, times that would be NaN)
                         sm.row_unit[n_unit & 1][i] =
                             fminf(fmaxf(a.scale * __uint_as_float((uint32_t)(127 + e2) << 23) * kLog2e, FLT_MIN), FLT_MAX);
                     }
                     continue;
                 }
+                // dimensions e and e + 4 of eight together, as in the keys' operands
+                auto lower = [&](uint32_t y) { return __uint_as_float(y << 16) * down; };
+                auto upper = [&](uint32_t y) { return __uint_as_float(y & 0xffff0000u) * down; };
 #pragma unroll
-                for (int e = 0; e < 32; ++e)
-                    x[e] = f16x2(__uint_as_float(x[e] << 16) * down, __uint_as_float(x[e] & 0xffff0000u) * down);
+                for (int e = 0; e < 32; e += 4) {
+                    const uint32_t y[4] = {x[e], x[e + 1], x[e + 2], x[e + 3]};
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        x[e + 2 * u] = bf16x2(lower(y[u]), lower(y[u + 2]));  // (exact)
+                        x[e + 2 * u + 1] = bf16x2(upper(y[u]), upper(y[u + 2]));
+                    }
+                }
             }
             tmem_st32(tmem + kColQ + (n_unit & 1) * 64 + 32 * c, x);
         }
@@ -1107,7 +1116,7 @@ template <int D, bool F4>
 __device__ __forceinline__ void score_role(Smem<D, F4>& sm, uint32_t tmem)
 {
     using C = Cfg<D, F4>;
-    const uint32_t id = F4 ? idesc_f16_f32(128, kStep, false) : idesc_bf16_f32(128, kStep, false);
+    const uint32_t id = idesc_bf16_f32(128, kStep, false);
     const uint64_t d = smem_desc_sw128(0, 16, 1024);
     const uint32_t hi = static_cast<uint32_t>(d >> 32), lo = static_cast<uint32_t>(d) + (smem_u32(sm.slot[0]) >> 4);
     const uint32_t rest = static_cast<uint32_t>(d) + (smem_u32(sm.rest) >> 4);
@@ -1129,7 +1138,7 @@ __device__ __forceinline__ void score_role(Smem<D, F4>& sm, uint32_t tmem)
             if (elect_one()) {
                 const uint32_t to = tmem + kColS + (step & 3) * kStep;
                 const uint32_t k = lo + ((s * C::kSlotBytes + half * kStep * 128) >> 4);
-                if constexpr (F4) {  // the remainders first: their buffer is wanted
+                if constexpr (F4) {  // the second operand first: its buffer is wanted
                     const uint32_t r = rest + ((half * kStep * 128) >> 4);
 #pragma unroll
                     for (int ks = 0; ks < D / 16; ++ks)
@@ -1182,7 +1191,7 @@ __device__ __forceinline__ void value_role(Smem<D, F4>& sm, uint32_t tmem)
     }
 }
 
-// ---- 4 bits: codes -> f16 operand rows ----------------------------------------------------------------
+// ---- 4 bits: codes -> operand rows --------------------------------------------------------------------
 // Keys of a block.  The D / 8 bytes of (token, c) are dimensions 32 x + 8 c .. + 7 for each group x.  Eight lanes that
 // go to memory together have tokens y and y ^ 5: their loads and their swizzled stores both fall on eight different
 // 16-byte pieces of the banks.
@@ -1209,15 +1218,22 @@ __device__ __forceinline__ void widen_keys(const uint8_t* code_tile, uint8_t* to
         }
 #pragma unroll
         for (int x = 0; x < J; ++x) {
-            uint32_t f[4];
-            e2m1x8_to_f16x2(code[x], f);
-            const uint32_t s2 = __byte_perm(sc[x >> 1], 0, (x & 1) ? 0x3232 : 0x1010);
+            // A scale has 11 bits and a code 2: the upper 6 bits of the one times the other are a bf16 number, and so are the lower
+            // 5 times it.  A code's bits (s e e m) in bf16's places are the bf16 number 2^-126 times it, 0.5 a subnormal
+            // one; a scale has 2^110, and the queries the 2^16 that are left.
+            const uint16_t bits = (uint16_t)((x & 1) ? sc[x >> 1] >> 16 : sc[x >> 1]);
+            const float scale = __half2float(__ushort_as_half(bits)) * 0x1p110f;
+            const uint32_t upper = __float_as_uint(scale) & 0xfffc0000u, lower = __float_as_uint(scale - __uint_as_float(upper));
+            const uint32_t upper2 = __byte_perm(upper, 0, 0x3232), lower2 = __byte_perm(lower, 0, 0x3232);
             const int at = (x >> 1) * kHalfBytes + row * 128 + (((4 * (x & 1) + c) ^ (row & 7)) << 4);
             uint32_t y[4], left[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                y[e] = hmul2(f[e], s2);
-                left[e] = hfms2(f[e], s2, y[e]);
+                // dimensions e and e + 4 of the eight: s to bit 15, e e m to bits 8 .. 6 of each half
+                const uint32_t two = (e < 2 ? code[x] : code[x] >> 8) & (e & 1 ? 0x00f000f0u : 0x000f000fu);
+                const uint32_t c2 = two * (e & 1 ? 0x104u : 0x1040u) & 0x81c081c0u;
+                y[e] = bmul2(c2, upper2);
+                left[e] = bmul2(c2, lower2);
             }
             *reinterpret_cast<uint4*>(to + at) = make_uint4(y[0], y[1], y[2], y[3]);
             *reinterpret_cast<uint4*>(rest + at) = make_uint4(left[0], left[1], left[2], left[3]);
@@ -1279,7 +1295,7 @@ __device__ __forceinline__ void widen_values(const uint8_t* code_tile, uint8_t* 
     }
 }
 
-// Eight warps widen a block of keys each, four two blocks of values.  (The remainders of a tile have one buffer: the next tile's keys wait
+// Eight warps widen a block of keys each, four two blocks of values.  (A tile's second operand of keys has one buffer: the next tile's wait
 // for this one's product, by halves.  With four warps for keys and whole tiles 64 requests of 8 nodes took 224 us, 32 of 64 nodes 568.)
 template <int D, int P>
 __device__ __forceinline__ void widen_role(Smem<D, true>& sm, const TreeArgs& a, Walk w, int warp, int lane)

@@ -50,3 +50,58 @@ def test_many_small_probabilities_beside_a_few_large_ones(fmt, D, Hq, T, where):
         got = R.to_f64(out[i])
         assert (np.abs(got - want) <= tol).all(), (i, np.abs(got - want).max(), want, tol)
         assert (np.abs(lse[i].double().cpu().numpy() - (score + np.log(total))) <= 2.0 ** -18 * score + adds * 2.0 ** -24).all()
+
+
+def with_scales(D, page, lens, T, gen, key_scales, value_scales, value_codes=16):
+    """A 4-bit store of random codes whose tokens' scales are drawn from the given ones; tables and lengths.  Value codes are
+    below value_codes or its negatives."""
+    from paper_2511_06010_b200.paged import PagedKvStore
+
+    need = [-(-n // page) for n in lens]
+    table = torch.full((len(lens), max(need)), -1, dtype=torch.int32)
+    for r, n in enumerate(need):
+        table[r, :n] = torch.arange(sum(need[:r]), sum(need[:r]) + n)
+    st = PagedKvStore.empty(sum(need), page, 2, D, "fp4")
+    code = torch.randint(0, 256, st.pages4.shape, generator=gen, dtype=torch.uint8)
+    if value_codes < 16:
+        low = torch.randint(0, value_codes, (2, *st.pages4.shape[:-1], 8 * D), generator=gen, dtype=torch.uint8)
+        sign = torch.randint(0, 2, low.shape, generator=gen, dtype=torch.uint8) * 8
+        code[..., 8 * D:16 * D] = (low[0] + sign[0]) | (low[1] + sign[1]) << 4
+    for at, scales in ((16 * D, key_scales), (17 * D, value_scales)):
+        pick = torch.randint(0, len(scales), (*st.pages4.shape[:-1], D // 2), generator=gen)
+        code[..., at:at + D] = torch.tensor(scales, dtype=torch.float16)[pick].view(torch.uint8).reshape(*st.pages4.shape[:-1], D)
+    st.pages4.copy_(code)
+    return st, table.cuda(), torch.tensor(lens, dtype=torch.int32).cuda()
+
+
+def check(st, table, lens, T, parents, q, attention, out, lse):
+    k64, v64 = R.unpack(st.pages4)
+    for r, n in enumerate(lens):
+        k, v = R.context(k64, v64, table[r].cpu().numpy(), n)
+        sees = TR.visible(parents[r * T:(r + 1) * T], n)
+        for i in range(T):
+            o, l, o_tol, l_tol = R.attend(R.to_f64(q[r * T + i]), k[sees[i]], v[sees[i]], attention.scale, "fp4")
+            assert (np.abs(R.to_f64(out[r * T + i]) - o) <= o_tol).all(), (r, i)
+            assert (np.abs(lse[r * T + i].double().cpu().numpy() - l) <= l_tol).all(), (r, i, lse[r * T + i], l)
+
+
+FORMS = [(64, 8, 7), (128, 8, 5), (128, 8, 13), (64, 2, 40), (128, 16, 20)]  # D, Hq (of 2 KV heads), nodes
+
+
+@pytest.mark.parametrize("D,Hq,T", FORMS)
+@pytest.mark.parametrize("scales,q_scale", [([10912.0, 10920.0, 20000.0, 65504.0], 2.0 ** -17), ([1.0, 30000.0, 2.0 ** -24], 2.0 ** -15),
+                                            ([2.0 ** -24, 3 * 2.0 ** -24, 1000 * 2.0 ** -24, 2.0 ** -14], 2.0 ** 13)])
+@pytest.mark.parametrize("splits", [1, 3])
+def test_key_scales_of_any_size(D, Hq, T, scales, q_scale, splits):
+    """Scales larger than appends write, whose products with a code no f16 number holds, and the smallest there are."""
+    from paper_2511_06010_b200 import binding as M
+    from paper_2511_06010_b200.speculative import TreeAttention
+
+    gen, rng, lens = torch.Generator().manual_seed(D + T), np.random.default_rng(T), [50, 300, 130]
+    st, table, length = with_scales(D, 16, lens, T, gen, scales, [0.5, 1.0, 1.25])
+    parents = np.concatenate([TR.random_tree(rng, T) for _ in lens])
+    q = R.make_bf16((len(lens) * T, Hq, D), gen, q_scale)
+    attention = TreeAttention(len(lens) * T, Hq, 2, D, max(lens), len(lens), T, fmt="fp4", n_unique_splits=splits)
+    out, lse = attention(q.cuda(), st, table, length, torch.from_numpy(parents).cuda())
+    assert M.device_status() == 0
+    check(st, table, lens, T, parents, q, attention, out, lse)
