@@ -623,8 +623,9 @@ int moska_decode_step_paged(const uint16_t* q, const float* summaries, const voi
  * node does not see has no influence on it, infinities and NaN included.  Scores, softmax statistics, row sums and results
  * are held in fp32.  In 16 bits: bf16 pages, the probabilities (bf16, half a step 2^-8 of each); 4-bit pages, the
  * probabilities (f16, 2^-11; below 2^-21 of the row's largest within 2^-32 of that, so what is smaller counts in the row sum
- * alone) and a value as scale * code (f16, 2^-11); keys are exact for every finite scale, as two bf16 numbers that add up to
- * scale * code, and so are the queries.  out is rounded once more.
+ * alone) and a value as scale * code (f16, 2^-11, or 2^-25 absolute below 2^-14; above 65504, which takes a value scale above
+ * the 10912 that append writes at most, it is infinite); keys are exact for every finite scale, as two bf16 numbers that add
+ * up to scale * code, and so are the queries.  out is rounded once more.
  * A part of a context of more than about 400 million tokens would pass the limit of a wait (2 s): MOSKA_ERR_TIMEOUT in the
  * device status word, and results that are not valid; cut it (n_unique_splits).
  */

@@ -124,7 +124,8 @@ __device__ __forceinline__ int paged_page(const PagedView& p, const int32_t* row
 __device__ __forceinline__ void dependents_may_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_results() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// Two E2M1 codes a byte -> two f16 values, exact; the four bytes of w give o[0..3].
+// Two E2M1 codes a byte -> two f16 values, exact; the four bytes of w give o[0..3].  (w is loaded as a word: from a byte loaded
+// alone nvcc 12.9 made code that gave 0.)
 __device__ __forceinline__ void e2m1x8_to_f16x2(uint32_t w, uint32_t (&o)[4])
 {
     asm("{\n"

@@ -105,3 +105,40 @@ def test_key_scales_of_any_size(D, Hq, T, scales, q_scale, splits):
     out, lse = attention(q.cuda(), st, table, length, torch.from_numpy(parents).cuda())
     assert M.device_status() == 0
     check(st, table, lens, T, parents, q, attention, out, lse)
+
+
+@pytest.mark.parametrize("D,Hq,T", FORMS)
+@pytest.mark.parametrize("splits", [1, 3])
+def test_value_scales_above_what_appends_write(D, Hq, T, splits):
+    """Where the product is finite, a value counts with its probability like any other, drafted tokens' too; one that is not
+    spoils its own dimensions of the rows that see it, and nothing else."""
+    from paper_2511_06010_b200 import binding as M
+    from paper_2511_06010_b200.speculative import TreeAttention
+
+    gen, rng, lens = torch.Generator().manual_seed(D + T + 1), np.random.default_rng(T + 1), [50, 300, 130]
+    st, table, length = with_scales(D, 16, lens, T, gen, [0.25, 0.125], [1.0, 10920.0, 20000.0], value_codes=6)  # 3 at most
+    parents = np.concatenate([TR.random_tree(rng, T) for _ in lens])
+    q, up = R.make_bf16((len(lens) * T, Hq, D), gen), torch.from_numpy(parents).cuda()
+    attention = TreeAttention(len(lens) * T, Hq, 2, D, max(lens), len(lens), T, fmt="fp4", n_unique_splits=splits)
+    out, lse = (x.clone() for x in attention(q.cuda(), st, table, length, up))
+    assert M.device_status() == 0
+    check(st, table, lens, T, parents, q, attention, out, lse)
+    j = T // 2  # a node of the second request: its value 120000 in four dimensions of the second head
+    token = lens[1] - T + j
+    pool = st.pages4.cpu().numpy()
+    _, vb, _, vs, _ = R.byte_map(D)
+    block, t = pool[int(table[1, token // 16]), 1, 0], token % 16
+    block[vb[t, :4]] = 0x77
+    block[vs[t, 0]:vs[t, 0] + 2] = np.array([20000.0], dtype=np.float16).view(np.uint8)
+    st.pages4.copy_(torch.from_numpy(pool))
+    out2, lse2 = attention(q.cuda(), st, table, length, up)
+    sees = torch.zeros(len(lens) * T, dtype=torch.bool)
+    sees[T:2 * T] = torch.from_numpy(TR.ancestors(parents[T:2 * T])[:, j])
+    half = Hq // 2
+    assert torch.equal(out2[~sees], out[~sees]) and torch.equal(out2[:, :half], out[:, :half]) and torch.equal(lse2, lse)
+    assert not torch.isfinite(out2[sees][:, half:, :4]).any() and torch.isfinite(out2[sees][:, half:, 4:]).all()
+    k, v = R.context(*R.unpack(st.pages4), table[1].cpu().numpy(), lens[1])
+    seen = TR.visible(parents[T:2 * T], lens[1])
+    for i in np.flatnonzero(sees[T:2 * T].numpy()):
+        o, _, o_tol, _ = R.attend(R.to_f64(q[T + i]), k[seen[i]], v[seen[i]], attention.scale, "fp4")
+        assert (np.abs(R.to_f64(out2[T + i]) - o) <= o_tol)[half:, 4:].all(), i
