@@ -688,8 +688,9 @@ int moska_verify_tree(const void* target_probs, int64_t target_stride, const voi
  *   path        int32 [n_requests][path_stride], strictly ascending within n_path[r], each in [0, T)
  *   n_path      int32 [n_requests], 0 .. min(T, path_stride)
  *   kv_len_out  int32 [n_requests], apart from kv->kv_len
- * A path that is not so, or a page outside the pool, raises MOSKA_ERR_INVALID_ARG in the device status word; the
- * request is left as it was, kv_len_out[r] = kv_len[r].  The same, without an error, for a request with kv_len[r] < T (padding).
+ * A path that is not so, a page outside the pool, a row range outside B or of more than q_len nodes, or a length that is
+ * negative or more than max_pages pages hold, raises MOSKA_ERR_INVALID_ARG in the device status word; the request is left
+ * as it was, kv_len_out[r] = kv_len[r].  The same, without an error, for a request with 0 <= kv_len[r] < T (padding).
  * Nodes' pages belong to one request alone.  shape: B, Hkv, D and q_len are read.
  */
 int moska_kv_commit_paged(const int32_t* path, int32_t path_stride, const int32_t* n_path, const int32_t* row_start,

@@ -27,10 +27,13 @@ __global__ void __launch_bounds__(kThreads) commit_kernel(const CommitArgs a)
     __shared__ int64_t from[MOSKA_TREE_MAX_NODES], to[MOSKA_TREE_MAX_NODES];  // token rows (page * page_size + row)
     __shared__ int source[MOSKA_TREE_MAX_NODES];
     const int r = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x;
-    const int2 rows = tree_rows(a.tree, r, a.kv.status);
-    const int len = paged_len(a.kv, r), committed = len - rows.y;
+    bool good;
+    const int2 rows = tree_rows(a.tree, r, a.kv.status, &good);
+    const int len = __ldg(a.kv.kv_len + r);
+    good &= checked_len(a.kv, len) == len;  // (with rows or a length that are none, the place of the nodes is not known)
+    const int committed = good ? len - rows.y : -1;
     const int given = __ldg(a.n_path + r);
-    bool good = given >= 0 && given <= min(rows.y, a.path_stride);
+    good &= given >= 0 && given <= min(rows.y, a.path_stride);
     const int n = good ? given : 0;
     int x = 0;
     if (tid < n) {
@@ -51,7 +54,7 @@ __global__ void __launch_bounds__(kThreads) commit_kernel(const CommitArgs a)
     }
     good = __syncthreads_and(good);  // (else, or with a page that is not in the pool, nothing is moved)
     if (part == 0 && tid == 0) {
-        a.kv_len_out[r] = good && committed >= 0 ? committed + n : len;
+        a.kv_len_out[r] = good && committed >= 0 ? committed + n : len;  // (`good` of all threads: the path and its pages too)
         if (!good) atomicMin(a.kv.status, MOSKA_ERR_INVALID_ARG);
     }
     if (!good || committed < 0) return;

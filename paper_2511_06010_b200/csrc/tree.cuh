@@ -8,13 +8,16 @@ namespace moska {
 
 static_assert(MOSKA_TREE_MAX_NODES == 64, "a node's ancestors are the bits of a 64-bit word");
 
-// First row and number of nodes of request r (rows outside the batch or more nodes than there may be are reported).
-__device__ __forceinline__ int2 tree_rows(const TreeRows& t, int r, int* status)
+// First row and number of nodes of request r (rows outside the batch or more nodes than there may be are reported, and
+// make *sound false).
+__device__ __forceinline__ int2 tree_rows(const TreeRows& t, int r, int* status, bool* sound = nullptr)
 {
+    if (sound != nullptr) *sound = true;
     if (t.row_start == nullptr) return make_int2(r * t.max_nodes, t.max_nodes);
     const int a = __ldg(t.row_start + r), b = __ldg(t.row_start + r + 1);
     if (a < 0 || b < a || b > t.n_rows || b - a > t.max_nodes) {
         atomicMin(status, MOSKA_ERR_INVALID_ARG);
+        if (sound != nullptr) *sound = false;
         if (a < 0 || b < a || b > t.n_rows) return make_int2(0, 0);
         return make_int2(a, t.max_nodes);
     }
