@@ -151,6 +151,7 @@ struct Smem {
     unsigned long long bad[8];  // tree tokens with values that are not finite; units take turns
     Part part;
     uint32_t tmem_base;
+    uint32_t step;  // that the first softmax group is at
     int gave_up;
 };
 constexpr int kMostSmem = 232448;
@@ -265,6 +266,30 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, int* gave_up)
 {
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, gave_up));
+}
+
+// The same for the end of a unit, whose steps may be many: the limit of a wait begins anew when `step` moves (2^29 tokens in one
+// part take 5 s).
+__device__ __forceinline__ bool unit_wait(uint64_t* bar, uint32_t parity, volatile uint32_t* step, volatile int* gave_up)
+{
+    bool ok = false;
+    uint64_t since = 0;
+    uint32_t seen = 0;
+    for (uint32_t polls = 1; !ok; ++polls) {
+        ok = mbar_try_wait(bar, parity);
+        if (ok || (polls & 1023u) != 0) continue;
+        if (*gave_up) break;
+        const uint64_t now = global_timer_ns();
+        const uint32_t at = *step;
+        if (since == 0 || at != seen) {
+            since = now;
+            seen = at;
+        } else if (now - since > kWaitLimitNs) {
+            *gave_up = 1;
+            break;
+        }
+    }
+    return __all_sync(0xffffffffu, ok);
 }
 
 __device__ __forceinline__ void find_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
@@ -563,6 +588,7 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
             if constexpr (!F4)
                 if (ends && !clean_values<D>(sm, u, t0, mine, n_unit, i)) return;
             if (!warp_wait(&sm.s_full[mine & 3], (mine >> 2) & 1, gave_up)) return;
+            if (group == 0 && i == 0) *static_cast<volatile uint32_t*>(&sm.step) = mine;
             tc_fence_after_sync();
             const uint32_t t_s = tmem + kColS + (mine & 3) * kStep;
             if (P == 1 && ends && warp_live) {  // scores of what the row does not see, in place
@@ -870,7 +896,7 @@ struct Rows {
     // The unit's rows: final ones, partial ones of a cut unit, or partial slots.
     __device__ __forceinline__ bool finish(const Walk& w, uint32_t n_unit, uint32_t last)
     {
-        bool ok = warp_wait(&sm.stat_full[n_unit & 1], (n_unit >> 1) & 1, &sm.gave_up);
+        bool ok = unit_wait(&sm.stat_full[n_unit & 1], (n_unit >> 1) & 1, &sm.step, &sm.gave_up);
         // the group of the last step has the row's reference; the others' sums are brought to it
         const float unit = sm.row_unit[n_unit & 1][i];
         const float mine = sm.stat[n_unit & 1][last % C::kGroups][i].x;
@@ -1423,6 +1449,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         }
         mbar_init(&sm.o_free, kTileRows);
         for (int x = 0; x < 8; ++x) sm.bad[x] = 0;
+        sm.step = 0;
         sm.gave_up = 0;
         fence_mbar_init();
         fence_proxy_async_smem();
