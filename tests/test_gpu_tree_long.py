@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "fp4"])
-@pytest.mark.parametrize("length,splits", [(2 ** 29 + 77, 1)])
+@pytest.mark.parametrize("length,splits", [(2 ** 30, None), (2 ** 29 + 77, 1), (20_000_001, None)])
 def test_contexts_of_hundreds_of_millions_of_tokens(fmt, length, splits):
     """Two pages stand for the two halves of the committed tokens, with values of 2 and of 4 in one of 64 tokens, 0 in the others,
     and keys of 0.  In one part the walk takes seconds.
