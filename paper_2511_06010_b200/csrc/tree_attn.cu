@@ -799,7 +799,7 @@ struct Rows {
         };
         // 4 bits: once for the rows' largest elements, then for the operands.  (Rolled, with a row's elements in its lane: the code
         // is cold when a CTA begins.  Maxima of pieces, joined by shuffles, took 11000 cycles.)
-        if constexpr (!F4) sm.row_unit[n_unit & 1][i] = a.scale * kLog2e;
+        if constexpr (!F4) sm.row_unit[n_unit & 1][i] = fminf(a.scale * kLog2e, FLT_MAX);  // (a score of 0 times an infinity is NaN)
         float down = 1.f;
         uint32_t top = 0;
         uint8_t(*stage)[kStagePitch] = sm.stage[warp];

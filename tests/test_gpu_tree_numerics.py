@@ -142,3 +142,54 @@ def test_value_scales_above_what_appends_write(D, Hq, T, splits):
     for i in np.flatnonzero(sees[T:2 * T].numpy()):
         o, _, o_tol, _ = R.attend(R.to_f64(q[T + i]), k[seen[i]], v[seen[i]], attention.scale, "fp4")
         assert (np.abs(R.to_f64(out2[T + i]) - o) <= o_tol)[half:, 4:].all(), i
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp4"])
+@pytest.mark.parametrize("D,Hq,T", [(128, 4, 5), (64, 8, 16), (128, 2, 24)])
+@pytest.mark.parametrize("scale", [1e-45, 1e-40, 1e-8, 0.125])
+@pytest.mark.parametrize("q_scale", [0.0, 1e-38, 1e-30])
+def test_zero_and_tiny_query_rows_with_small_softmax_scales(fmt, D, Hq, T, scale, q_scale):
+    """A hidden token has weight 0 whatever the row's scores are multiplied with."""
+    from paper_2511_06010_b200.speculative import TreeAttention
+
+    gen, rng, lens = torch.Generator().manual_seed(41), np.random.default_rng(41), [T, 40, 200, 333]
+    k, v = (R.make_bf16((sum(lens), 1, D), gen) for _ in range(2))
+    st, table, length = _filled(fmt, k, v, lens)
+    parents = np.concatenate([TR.random_tree(rng, T) for _ in lens])
+    q = R.make_bf16((len(lens) * T, Hq, D), gen, q_scale)
+    attention = TreeAttention(len(lens) * T, Hq, 1, D, max(lens), len(lens), T, fmt=fmt, n_unique_splits=2)
+    attention.scale = scale
+    out, lse = attention(q.cuda(), st, table, length, torch.from_numpy(parents).cuda())
+    k64, v64, at = _held(k, fmt), _held(v, fmt), 0
+    for r, n in enumerate(lens):
+        sees = TR.visible(parents[r * T:(r + 1) * T], n)
+        for i in range(T):
+            o, l, o_tol, l_tol = R.attend(R.to_f64(q[r * T + i]), k64[at:at + n][sees[i]], v64[at:at + n][sees[i]], scale, fmt)
+            assert (np.abs(R.to_f64(out[r * T + i]) - o) <= o_tol).all(), (r, i)
+            assert (np.abs(lse[r * T + i].double().cpu().numpy() - l) <= l_tol).all(), (r, i)
+        at += n
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp4"])
+@pytest.mark.parametrize("nodes", [3, 24])
+@pytest.mark.parametrize("scale", [64.0, 3e38])
+def test_the_largest_query_rows_and_softmax_scales_on_keys_of_zero(fmt, nodes, scale):
+    """Scores of exactly 0: the mean of the values, however large the row and the softmax scale are."""
+    from paper_2511_06010_b200.speculative import TreeAttention
+
+    lens, D = [nodes, 64, 130], 128
+    gen = torch.Generator().manual_seed(42)
+    v = R.make_bf16((sum(lens), 1, D), gen)
+    st, table, length = _filled(fmt, torch.zeros_like(v), v, lens)
+    q = torch.full((3 * nodes, 4, D), 2.0 ** 126, dtype=torch.bfloat16)
+    attention = TreeAttention(3 * nodes, 4, 1, D, max(lens), 3, nodes, fmt=fmt, n_unique_splits=1)
+    attention.scale = scale
+    out, lse = attention(q.cuda(), st, table, length)  # chains
+    v64, at = _held(v, fmt), 0
+    for r, n in enumerate(lens):
+        for i in range(nodes):
+            m = n - nodes + 1 + i
+            o, l, o_tol, l_tol = R.attend(np.zeros((4, D)), np.zeros((m, 1, D)), v64[at:at + m], 1.0, fmt)
+            row = r * nodes + i
+            assert (np.abs(R.to_f64(out[row]) - o) <= o_tol).all() and (np.abs(lse[row].double().cpu().numpy() - l) <= l_tol).all()
+        at += n
