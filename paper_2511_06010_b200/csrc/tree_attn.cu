@@ -416,7 +416,7 @@ __device__ __forceinline__ void find_part(const TreeArgs& a, int cta, int ctas, 
     const long long all = places(mine_all, cost) * a.Hkv;
     // equal parts, in each at least one tile of a unit that begins in it; no unit in more of them than there may be
     long long per = divide(all + n - 1, n);
-    if (a.n_splits > 1) per = max(per, (long long)((longest + cost + a.n_splits - 2) / (a.n_splits - 1)));
+    if (a.n_splits > 1) per = max(per, divide((long long)longest + cost + a.n_splits - 2, a.n_splits - 1));
     per = max((long long)cost + 1, per);
     const long long p0 = (cta - cta0) * per, p1 = min(all, p0 + per);
     if (i == 0) {
