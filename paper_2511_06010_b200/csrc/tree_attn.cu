@@ -95,9 +95,9 @@ struct Cfg {
 
 // Units of few rows have each row P times, in lanes kTileRows / P apart: the i-th has the i-th part of every step's tokens, with a
 // reference, a sum and an O of its own, as if a context were cut into P.  The four warps of a group have a P-th of the
-// scores each then, where one warp of live rows would have had them all (4 bits, 64 requests of 4096 tokens, before keys had
-// remainders: 32 rows 143 us with P = 4, 152 with 2, 176 without; 64 rows 156 with 2, 183 without.  bf16 waits for memory
-// there, 182, 182, 183 us and 190, 192; it has P = 1 alone).
+// scores each then, where one warp of live rows would have had them all (4 bits, 64 requests of 4096 tokens: 32 rows 214 us with
+// P = 4, 216 with 2, 239 without; with D = 64 74 and 76; 64 rows 232 with 2, 256 without.  bf16 waits for memory there, 182,
+// 182, 183 us and 190, 192; it has P = 1 alone).
 template <int P>
 struct Spread {
     static constexpr int kRows = kTileRows / P, kCols = kStep / P;
@@ -326,9 +326,12 @@ __device__ __forceinline__ bool elect_one()
 }
 
 // ---- the line of tiles ------------------------------------------------------------------------------
-// On the line a unit is longer than its tiles by what its beginning and its end cost, in tiles; where parts are short
-// (few tiles in all, or latency counts) by nothing.
-constexpr int kUnitCost = 2, kShortPart = 16;
+// On the line a unit is longer than its tiles by what its beginning and its end cost, in tiles (bf16 24 requests of 60 nodes 554 us
+// with 0, 545 with 1, 529 with 2, 525 with 4; 4 bits 32 of 64 nodes 597, 578, 571, 580; bf16 100 of 5-33 nodes, D = 64, 75, 76, 76,
+// 78); where parts would be shorter than kShortPart by nothing, as they would be longer for it then (bf16 requests of 8 nodes and
+// 4000 tokens, always counted and from 2, 4, 8 and 16 tiles on: one 20.9, 22.5 us, two 23.3, 23.3, 22.9, 22.6, 22.7, four 28.6, 28.7, 28.7,
+// 29.5, 29.7, eight 39.5, 39.4, 39.5, 39.4, 40.6).
+constexpr int kUnitCost = 2, kShortPart = 4;
 // Tiles and units of a stretch of requests in one number.
 constexpr int kUnitBit = 40;
 // (64-bit divisions are long: 32 bits where they do)
@@ -559,16 +562,19 @@ __device__ __forceinline__ bool clean_values(Smem<D, false>& sm, const UnitInfo&
 // Scores of every kGroups-th step (half a tile) -> probabilities.  A row's reference m passes from step to step; it moves when a
 // step's maximum passes it by 2^8, and whoever moves it rescales O.  Each group keeps its own sum, relative to the reference
 // that it saw last.  The reference is handed on when half of a step's exponentials are done, which also keeps the groups out of
-// step: handed on before them, both had their exponentials at one time and both waited at another (fp4 32 requests of 64
-// nodes 393 us so, 372 now; bf16 24 of 60 nodes 452 and 437); after all of them it comes too late (414, 465).
+// step: handed on before them, both have their exponentials at one time and wait at another, and after all of them it comes too
+// late (bf16 24 requests of 60 nodes 552 us before, 529 halfway, 550 after; 4 bits with D = 64, 100 of 5-33 nodes 88, 86, 94).
+// 4 bits with D = 128 have the reference handed on first: the tensor cores wait for keys there, and halfway costs more than
+// it orders (32 of 64 nodes 529 us before, 581 halfway, 534 after).
 template <int D, bool F4, int P>
 __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int group, int warp, int i)
 {
     constexpr int kGroups = Cfg<D, F4>::kGroups;
     // 4 bits: scores are read twice, 32 at a time, and loops are rolled.  The roles' code shares the instruction caches, and the
-    // widening takes its part (64 scores at once and all unrolled: 32 requests of 64 nodes 514 us, so 409; bf16 24 of 60 nodes
-    // 465 us so, 490 rolled).
+    // widening takes its part (64 scores at once and unrolled: 32 requests of 64 nodes 591 us, rolled 571, with the reference
+    // handed on halfway in both; bf16 24 of 60 nodes 529 us unrolled, 537 rolled).
     constexpr int kKeep = F4 ? 0 : 1;
+    constexpr bool kHandOnFirst = P > 1 || (F4 && D == 128);
     int* gave_up = &sm.gave_up;
     const int before_me = group == 0 ? kGroups - 1 : group - 1;  // the group of the step before
     uint32_t mine = group;             // this group's next step, and how many it had
@@ -656,7 +662,7 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
             const bool need = mine != unit0 && live && (mx - before) * unit > kRescaleAt;
             const float now = need ? mx : before;
             sm.ref[group][i] = now;
-            if (P > 1 || !warp_live) mbar_arrive(&sm.ref_full[group][warp & 3]);
+            if (kHandOnFirst || !warp_live) mbar_arrive(&sm.ref_full[group][warp & 3]);
             if (warp_live) {
                 if (__any_sync(0xffffffffu, need)) {
                     // the last product has left O (its barrier's turn before, four steps back, is over: these scores came behind it)
@@ -706,6 +712,7 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
                     if constexpr (P == 4) tmem_st8(t_s + kCols / 2 * part, pk);
                     else tmem_st16(t_s + kCols / 2 * part, pk);
                 } else if constexpr (kKeep) {
+                    static_assert(!kHandOnFirst, "handed on once");
                     exponentials(s[0], 0);
                     mbar_arrive(&sm.ref_full[group][warp & 3]);
                     exponentials(s[kKeep], 1);
@@ -715,7 +722,7 @@ __device__ __forceinline__ void softmax_role(Smem<D, F4>& sm, uint32_t tmem, int
                         tmem_ld32(t_s + 32 * c, s[0]);
                         tmem_ld_wait();
                         exponentials(s[0], c);
-                        if (c == 0) mbar_arrive(&sm.ref_full[group][warp & 3]);
+                        if (c == 0 && !kHandOnFirst) mbar_arrive(&sm.ref_full[group][warp & 3]);
                     }
                 }
                 l += (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
@@ -1324,9 +1331,8 @@ __device__ __forceinline__ void widen_odd_values(const uint8_t* code_tile, uint8
 
 // Values of two blocks.  In a tile that reaches past the committed tokens (kEnds; `behind`: its first token's place behind them) values behind the context are 0, and those
 // that are not finite are taken out.
-// (A form of its own for the others: a branch at each token keeps loads and stores waiting, 1590 cycles a tile where it takes 1200.
-// But not with P = 1: softmax warps need the issue slots and the room for code there, 32 requests of 64 nodes 394 us with two
-// forms, 375 with one.)
+// (A form of its own for the others: a branch at each token keeps loads and stores waiting, 1590 cycles a tile where it takes 1200;
+// 64 requests of 8 nodes 214 us, 222 with one form; 32 of 64 nodes 524 and 529.)
 template <int D, bool kEnds>
 __device__ __forceinline__ void widen_values(const uint8_t* code_tile, uint8_t* to, int block0, int lane, int behind, int nodes,
                                              unsigned long long* bad)
@@ -1393,7 +1399,7 @@ __device__ __forceinline__ void widen_role(Smem<D, true>& sm, const TreeArgs& a,
             if (!values && tile > 0 && !warp_wait(&sm.rest_empty[half], (tile - 1) & 1, gave_up)) return;
             const uint8_t* from = sm.code + c * C::kCodeBytes;
             if (!values) widen_keys<D>(from, sm.slot[s], sm.rest, block0, lane);
-            else if (P > 1 && behind + kTile <= 0) widen_values<D, false>(from, sm.slot[s], block0, lane, behind, w.q.nodes, nullptr);
+            else if (behind + kTile <= 0) widen_values<D, false>(from, sm.slot[s], block0, lane, behind, w.q.nodes, nullptr);
             else widen_values<D, true>(from, sm.slot[s], block0, lane, behind, w.q.nodes, &sm.bad[n_unit & 7]);
             fence_proxy_async_smem();
             __syncwarp();
