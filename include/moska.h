@@ -667,8 +667,10 @@ int moska_decode_step_tree(const uint16_t* q, const float* summaries, const void
  * P(v) > 0 if there is none, -1 if P is 0 everywhere).  P, Z and the sums are held in 64 bits.
  *   target_probs  [B][V] of prob_type, row i (elements i target_stride ..) behind node i; entries that are
  *                 not > 0 (NaN included) count as 0, none is infinite
- *   draft_probs   the same, with draft_stride; row i is what the children of node i were drawn from.
- *                 May be NULL
+ *   draft_probs   the same, with draft_stride; row i is what the children of node i were drawn from, each on its
+ *                 own from the whole row (with replacement): for siblings that were drawn to be different the walk
+ *                 above does not keep the target's distribution.  May be NULL, for children that were picked
+ *                 without chance (the likeliest ones, for instance)
  *   tokens        int32 [B]; a node whose token is not in [0, V) is not tried
  *   u_accept      float [B], u_next float [n_requests]: in [0, 1)
  *   path          int32 [n_requests][max_nodes]: the accepted nodes, 0 first, then -1

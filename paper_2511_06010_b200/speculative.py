@@ -63,7 +63,9 @@ def verify(target_probs, tokens, parents, u_accept, u_next, draft_probs=None, ro
     """Which drafted tokens the target takes: (path int32 [R][max_nodes], n_path int32 [R], next_token int32 [R]).
 
     target_probs, draft_probs float or bf16 [rows][V] (rows may lie apart): row i is the distribution behind node i; in
-    draft_probs the one that its children were drawn from (None: they were picked, not drawn).  tokens int32 [rows]: a node
+    draft_probs the one that its children were drawn from, each independently of its siblings (for siblings drawn without
+    replacement what is emitted does not follow the target).  None: they were picked without chance, the likeliest ones for
+    instance.  tokens int32 [rows]: a node
     whose token is outside the vocabulary is not tried.  u_accept float [rows] and u_next float [R]: random numbers
     in [0, 1).  path[r]: the accepted nodes, 0 first, then -1.  Rows as in TreeAttention; max_nodes may be left out where
     all requests have as many.  The same inputs always give the same result.  `out`: the three results' tensors."""
