@@ -386,11 +386,15 @@ int launch_verify(const void* target, int64_t target_stride, const void* draft, 
                   int32_t* n_path, int32_t* next_token, int* status, cudaStream_t st)
 {
     if (tree.n_requests == 0) return MOSKA_OK;
-    // CTAs of a request: a pass is a chain of loads, so that more of them make it shorter (one request of 6 nodes and 32000 tokens: 15.3,
-    // 13.0, 10.9, 11.0 us with 1, 2, 4, 8; 64 of 128256: 145, 81, 54, 49), while all have a place (200 of 50257: 29, 23, 31, 42)
-    // and a part is more than a few loads.
+    // CTAs of a request, 1, 2, 4 or 8.  A pass is a chain of loads, so that more of them make it shorter while a part is more than a few
+    // loads (one request of 6 nodes and 32000 tokens: 22.5, 18.4, 14.3, 12.4 us, caches flushed as in what follows).  Without draft
+    // probabilities a request has one pass and a short search, and pays for CTAs that find no place (444 at a time): 5-25 nodes and
+    // 50257 tokens, 100 requests 31, 25, 23, 31 us, 150 33, 26, 33, 41, 300 38, 45, 51, 67.  With them the request with the most
+    // passes takes longest, and others' CTAs fill the gaps: 16 nodes and 128256 tokens, 50 requests 165, 95, 60, 52 us, 99 195, 119,
+    // 85, 81, 200 213, 149, 135, 132.
+    const long long most = draft != nullptr ? 1600 : 400;  // CTAs
     int cluster = 1;
-    while (cluster < kMaxCluster && V / cluster > 2048 && (long long)tree.n_requests * cluster < 400) cluster *= 2;
+    while (cluster < kMaxCluster && V / cluster > 2048 && 2LL * tree.n_requests * cluster <= most) cluster *= 2;
     const long long grid = (long long)tree.n_requests * cluster;
     if (grid > 0x7fffffffLL) return fail(MOSKA_ERR_UNSUPPORTED, "verification grid too large");
     const VerifyArgs a{target, draft, target_stride, draft_stride, tokens, u_accept, u_next, tree, path, n_path, next_token,
