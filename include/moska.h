@@ -646,7 +646,10 @@ int moska_unique_attn_tree(const uint16_t* q, const moska_paged_kv* kv, const in
                            float* lse_part, float softmax_scale, const moska_shape* shape, moska_stream stream);
 
 /* moska_decode_step_paged for trees of shape->q_len nodes each: the shared store is attended to by every
- * node as by a request of its own, the private context as in moska_tree_attn. */
+ * node as by a request of its own, the private context as in moska_tree_attn.  A request with fewer nodes has its rows filled
+ * up with nodes behind them that no other node has above it (parent -1, any token): they are seen by themselves alone, and
+ * moska_kv_commit_paged leaves them behind.  All runs on `stream`, one stage after another: attention of trees takes every SM, and
+ * side_stream is not used. */
 int moska_decode_step_tree(const uint16_t* q, const float* summaries, const void* k_shared,
                            const void* v_shared, const float* k_scale_shared, const float* v_scale_shared,
                            const moska_paged_kv* kv, const int32_t* parents, int32_t* topk_idx, int32_t* seg_offsets,

@@ -1366,9 +1366,14 @@ int moska_decode_step_tree(const uint16_t* q, const float* summaries, const void
     unique.paged = kv;
     unique.parents = parents;
     unique.tree = true;
+    // One stream.  The two-stream schedule is made for private attention in many short CTAs that is bound by HBM; the tree
+    // kernel holds every SM until it ends, so that the shared kernel gets its share of the SMs when it could have all of them (128
+    // chunks, contexts of 4096 tokens, one stream and two: 64 requests of 16 nodes, bf16, routed 453, 444 us, dense 1320, 1588 (1383
+    // with unique_tokens), 32 of 64 nodes dense 2425, 2936 (2495), 8 of 8 nodes routed 165, 180; 4 bits much the same).
+    (void)side_stream;
     return step_with_shared(q, summaries, k_shared, v_shared, k_scale_shared, v_scale_shared, unique, topk_idx, seg_offsets,
                             seg_entries, o_part, lse_part, out, lse_out, softmax_scale, shape, ws, ws_bytes, stream,
-                            side_stream, prof);
+                            nullptr, prof);
 }
 
 int moska_verify_tree(const void* target_probs, int64_t target_stride, const void* draft_probs, int64_t draft_stride,

@@ -178,9 +178,10 @@ class MoskaLayer:
                    unique_tokens=0, sf8=None, parents=None):
         """One decode step with a paged private store (`store`: a paged.PagedKvStore in either format).
         The shared store is bf16, or FP8 when `sf8` is given (k_shared and v_shared are then not read).
-        `parents` int32 [B]: the q_len rows of a request are the nodes of a drafted tree (up to 64)."""
+        `parents` int32 [B]: the q_len rows of a request are the nodes of a drafted tree (up to 64; smaller ones are filled up
+        with nodes of parent -1).  Such a step takes one stream, whatever two_streams says."""
         self.shape.unique_tokens = int(unique_tokens)
-        two_streams = two_streams and self.overlap_routing
+        two_streams = two_streams and self.overlap_routing and parents is None
         if two_streams and self.side_stream is None:
             self.side_stream = torch.cuda.Stream(device=self.device, priority=-1)
         shared = (k_shared, v_shared, None, None) if sf8 is None else (sf8.k8, sf8.v8, sf8.k_scale, sf8.v_scale)

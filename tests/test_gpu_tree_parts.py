@@ -27,3 +27,34 @@ def test_the_same_call_gives_the_same_bits(fmt, D, Hq, nodes):
         c["attention"].out.fill_(7.0)
         out, lse = c["attention"](q, c["store"], c["table"], c["length"], c["up"])
         assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp4"])
+@pytest.mark.parametrize("dense", [False, True])
+def test_a_step_filled_up_with_nodes_that_none_sees(fmt, dense):
+    """Smaller trees in a step of larger ones: a request's rows are what they are without the others' fill, and the step is the
+    same with a second stream."""
+    from paper_2511_06010_b200 import binding as M
+    from tests.test_gpu_tree import _layer_case
+
+    w, c, sh, q, layer = _layer_case(fmt, False, dense)
+    up = c["up"].view(-1, 12).clone()
+    up[:, 7:] = -1  # five nodes of fill
+    parents = up.reshape(-1).contiguous()
+    step = lambda table, length, two: layer.step_paged(q, sh.k_shared, sh.v_shared, c["store"], table, length,  # noqa: E731
+                                                       two_streams=two, parents=parents).clone()
+    out = step(c["table"], c["length"], False)
+    assert torch.equal(step(c["table"], c["length"], True), out)
+    if fmt == "bf16":  # other rows in the places of the fill
+        for r, n in ((0, 256), (1, 40), (3, 333)):
+            for t in range(n - 5, n):
+                page = int(c["table"][r, t // 64])
+                c["store"].k_pages[page, t % 64] = float("inf")
+                c["store"].v_pages[page, t % 64] = float("nan")
+    else:
+        gen = torch.Generator().manual_seed(3)
+        k, v = (100 * torch.randn(20, w.Hkv, w.D, generator=gen).bfloat16().cuda() for _ in range(2))
+        c["store"].append(None, k, v, c["table"], c["length"], q_len=5)
+    again = step(c["table"], c["length"], False)
+    assert torch.equal(again.view(-1, 12, w.Hq, w.D)[:, :7], out.view(-1, 12, w.Hq, w.D)[:, :7])
+    assert M.device_status() == 0
