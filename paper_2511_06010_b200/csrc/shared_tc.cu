@@ -19,14 +19,12 @@
 // copy.  The running maximum is only raised when a row's maximum grew by more than 2^8 (the
 // accumulator rescale is then done in TMEM by the row's owner), which is exact after the final
 // division by the row sum.  TMEM: S_0, S_1, O_0, O_1 of 128 columns each = all 512 columns.
-#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include <mutex>
-
 #include "common.cuh"
 #include "sm100.cuh"
+#include "tensor_map.cuh"
 
 namespace moska {
 namespace {
@@ -116,45 +114,6 @@ struct TcParams {
     float scale;
     int B, Hq, Hkv, C, L, k, shared_slots, n_slots, dense, n_items_dense;
 };
-
-__device__ __forceinline__ float fast_exp2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(y) : "f"(x));
-    return y;
-}
-
-// ---- packed fp32 arithmetic (two lanes per instruction) -------------------------------------------
-__device__ __forceinline__ float2 ffma2(float2 a, float2 b, float2 c)
-{
-    float2 d;
-    asm("{\n"
-        ".reg .b64 ra, rb, rc, rd;\n"
-        "mov.b64 ra, {%2, %3};\n"
-        "mov.b64 rb, {%4, %5};\n"
-        "mov.b64 rc, {%6, %7};\n"
-        "fma.rn.f32x2 rd, ra, rb, rc;\n"
-        "mov.b64 {%0, %1}, rd;\n"
-        "}\n"
-        : "=f"(d.x), "=f"(d.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return d;
-}
-
-__device__ __forceinline__ float2 fadd2(float2 a, float2 b)
-{
-    float2 d;
-    asm("{\n"
-        ".reg .b64 ra, rb, rd;\n"
-        "mov.b64 ra, {%2, %3};\n"
-        "mov.b64 rb, {%4, %5};\n"
-        "add.rn.f32x2 rd, ra, rb;\n"
-        "mov.b64 {%0, %1}, rd;\n"
-        "}\n"
-        : "=f"(d.x), "=f"(d.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return d;
-}
 
 // One 32-byte store (sm_100): p must be 32-byte aligned.
 __device__ __forceinline__ void st_global_v8(float* p, const float* v)
@@ -979,34 +938,11 @@ shared_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
 }
 
 // ---- host side ------------------------------------------------------------------------------------
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
-                                  const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// The driver's tensor-map encoder, looked up through the runtime (no link against libcuda).
-int encoder(EncodeTiledFn* out)
-{
-    static EncodeTiledFn fn = nullptr;
-    static std::mutex mtx;
-    std::lock_guard<std::mutex> lock(mtx);
-    if (fn == nullptr) {
-        void* sym = nullptr;
-        cudaDriverEntryPointQueryResult res;
-        MOSKA_CUDA_TRY(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &res));
-        if (sym == nullptr || res != cudaDriverEntryPointSuccess)
-            return fail(MOSKA_ERR_CUDA, "the driver does not provide cuTensorMapEncodeTiled");
-        fn = reinterpret_cast<EncodeTiledFn>(sym);
-    }
-    *out = fn;
-    return MOSKA_OK;
-}
-
 // [rows][128] bf16 matrix, loaded in boxes of 128 rows x 64 columns with the 128-byte swizzle.
 int make_kv_map(CUtensorMap* tm, const uint16_t* base, long long rows)
 {
     EncodeTiledFn enc = nullptr;
-    MOSKA_TRY_STATUS(encoder(&enc));
+    MOSKA_TRY_STATUS(tensor_map_encoder(&enc));
     const cuuint64_t dims[2] = {(cuuint64_t)kD, (cuuint64_t)rows};
     const cuuint64_t strides[1] = {(cuuint64_t)kD * 2};
     const cuuint32_t box[2] = {64, (cuuint32_t)kKvTile};
@@ -1023,7 +959,7 @@ int make_kv_map(CUtensorMap* tm, const uint16_t* base, long long rows)
 int make_q_map(CUtensorMap* tm, const uint16_t* base, long long rows)
 {
     EncodeTiledFn enc = nullptr;
-    MOSKA_TRY_STATUS(encoder(&enc));
+    MOSKA_TRY_STATUS(tensor_map_encoder(&enc));
     const cuuint64_t dims[2] = {(cuuint64_t)kD, (cuuint64_t)rows};
     const cuuint64_t strides[1] = {(cuuint64_t)kD * 2};
     const cuuint32_t box[2] = {64, 1};
@@ -1046,7 +982,7 @@ namespace {
 int make_code_map(CUtensorMap* tm, const uint8_t* base, long long rows)
 {
     EncodeTiledFn enc = nullptr;
-    MOSKA_TRY_STATUS(encoder(&enc));
+    MOSKA_TRY_STATUS(tensor_map_encoder(&enc));
     const cuuint64_t dims[2] = {(cuuint64_t)kD, (cuuint64_t)rows};
     const cuuint64_t strides[1] = {(cuuint64_t)kD};
     const cuuint32_t box[2] = {(cuuint32_t)kD, (cuuint32_t)kKvTile};

@@ -43,15 +43,14 @@
 // What a node sees: committed tokens, and of the last T tokens those whose bit is set in its 64-bit word of ancestors.
 // Only tiles that reach past the committed tokens look at it.  0 times NaN is NaN, so values of such tiles that are
 // not finite are taken out of the operands (a bit per token remembers), and put into the rows that see them at the end.
-#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include <cfloat>
-#include <mutex>
 #include <type_traits>
 
 #include "sm100.cuh"
+#include "tensor_map.cuh"
 #include "tree.cuh"
 
 namespace moska {
@@ -176,49 +175,10 @@ struct TreeArgs {
     int nodes_per_tile;  // 128 / G
 };
 
-__device__ __forceinline__ float fast_exp2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 __device__ __forceinline__ float fmax3(float a, float b, float c)
 {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
-
-// two fp32 at once
-__device__ __forceinline__ float2 ffma2(float2 a, float2 b, float2 c)
-{
-    float2 d;
-    asm("{\n"
-        ".reg .b64 ra, rb, rc, rd;\n"
-        "mov.b64 ra, {%2, %3};\n"
-        "mov.b64 rb, {%4, %5};\n"
-        "mov.b64 rc, {%6, %7};\n"
-        "fma.rn.f32x2 rd, ra, rb, rc;\n"
-        "mov.b64 {%0, %1}, rd;\n"
-        "}\n"
-        : "=f"(d.x), "=f"(d.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return d;
-}
-
-__device__ __forceinline__ float2 fadd2(float2 a, float2 b)
-{
-    float2 d;
-    asm("{\n"
-        ".reg .b64 ra, rb, rd;\n"
-        "mov.b64 ra, {%2, %3};\n"
-        "mov.b64 rb, {%4, %5};\n"
-        "add.rn.f32x2 rd, ra, rb;\n"
-        "mov.b64 {%0, %1}, rd;\n"
-        "}\n"
-        : "=f"(d.x), "=f"(d.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
 }
 
@@ -1570,33 +1530,11 @@ __global__ void __launch_bounds__(256) tree_join_kernel(const TreeArgs a)
 }
 
 // ---- host side ------------------------------------------------------------------------------------
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// The driver's tensor-map encoder, looked up through the runtime (no link against libcuda).
-int encoder(EncodeTiledFn* out)
-{
-    static EncodeTiledFn fn = nullptr;
-    static std::mutex mtx;
-    std::lock_guard<std::mutex> lock(mtx);
-    if (fn == nullptr) {
-        void* sym = nullptr;
-        cudaDriverEntryPointQueryResult res;
-        MOSKA_CUDA_TRY(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &res));
-        if (sym == nullptr || res != cudaDriverEntryPointSuccess)
-            return fail(MOSKA_ERR_CUDA, "the driver does not provide cuTensorMapEncodeTiled");
-        fn = reinterpret_cast<EncodeTiledFn>(sym);
-    }
-    *out = fn;
-    return MOSKA_OK;
-}
-
 // Pages as [tokens][Hkv][D]: boxes of 64 dimensions of one head, a page's tokens or 128 of them.
 int make_page_map(CUtensorMap* tm, const void* pool, const PagedView& kv, int Hkv, int D)
 {
     EncodeTiledFn enc = nullptr;
-    MOSKA_TRY_STATUS(encoder(&enc));
+    MOSKA_TRY_STATUS(tensor_map_encoder(&enc));
     const int page = 1 << kv.page_shift;
     const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)Hkv, (cuuint64_t)kv.n_pages << kv.page_shift};
     const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)Hkv * D * 2};
