@@ -620,7 +620,8 @@ int moska_decode_step_paged(const uint16_t* q, const float* summaries, const voi
  * out, lse_out and ws may not overlap one another or what is read: the call is refused.
  * shape: B, Hq, Hkv, D, q_len and n_unique_splits are read: a context is cut into at most that many parts, as the
  * work of all contexts is shared among the SMs; 64 lets any batch be shared evenly, and costs no more than 2.  What a
- * node does not see has no influence on it, infinities and NaN included.  Scores, softmax statistics, row sums and results
+ * node does not see has no influence on it, infinities and NaN included; a value that it sees and that is not finite makes that
+ * dimension of its rows not finite.  Scores, softmax statistics, row sums and results
  * are held in fp32.  In 16 bits: bf16 pages, the probabilities (bf16, half a step 2^-8 of each); 4-bit pages, the
  * probabilities (f16, 2^-11; below 2^-21 of the row's largest within 2^-32 of that, so what is smaller counts in the row sum
  * alone) and a value as scale * code (f16, 2^-11, or 2^-25 absolute below 2^-14; above 65504, which takes a value scale above

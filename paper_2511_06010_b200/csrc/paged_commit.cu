@@ -2,7 +2,8 @@
 // context, as bytes.  A path is ascending and starts no earlier than its place (path[j] >= j), so that a row's new
 // place is never the source of a later one: with every thread owning the same bytes of all rows, moving them in
 // order (loads of up to eight rows before their stores) needs no barrier.  Bound by the chain path -> page -> row -> stores: 64
-// requests of 16 nodes 5 us with the call, 512 of 64 nodes in bf16 8.6 us (34 MB read and written), 300 of 33 in 4 bits 10 us.
+// requests of 16 nodes 5 us with the call, 512 of 64 nodes in bf16 9 to 10 us (34 MB read and written), 300 of 33 in 4 bits 11 us
+// (one launch alone).
 #include "tree.cuh"
 
 namespace moska {

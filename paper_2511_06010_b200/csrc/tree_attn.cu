@@ -12,13 +12,15 @@
 // What bounds it.  A tile of 128 rows and 128 tokens is 1024 cycles of MMA (D = 128), as many of exponentials, and in 4 bits
 // some 1800 cycles of shared memory (operands written, and read by the MMAs) and 512 more of MMA.  A half takes a group about 1900 cycles from
 // scores to probabilities, of which 900 are exponentials that the other group's slow down, so a tile takes 1900 cycles instead of
-// 1024 (bf16, 24 requests of 60 nodes and 1K-16K tokens: 0.43 ms, 0.95 PFLOP/s, tensor pipe 53 % busy).  Up to 64 rows bf16
-// waits for memory (64 requests of 16 nodes and 4096 tokens: 188 us, 5.7 TB/s).  4 bits, 32 requests of 64 nodes and 1K-8K tokens:
-// 463 us, a tile's keys wait for the product before (their remainders have one buffer).  One request of 8 nodes and 1000 tokens:
-// 17 us, of which 3.7 find the part, 1.3 bring the queries, 3 are the tile, 1.2 its rows, and the rest the two launches.
-// Not kept: a third softmax group (bf16 471 us for 437: registers), products of 128 tokens (one MMA warp waits for the other's
-// operands), the next scores read between a step's exponentials (468 for 434), part of the exponentials as polynomials (all
-// of them left out saves 10 %).
+// 1024.  Times in long runs, at the clock that the power cap leaves: bf16, 24 requests of 60 nodes and 1K-16K tokens 0.52 ms, 0.79
+// PFLOP/s (one launch alone 0.44 ms, tensor pipe 52 % busy).  Up to 64 rows bf16 waits for memory (64 requests of 16 nodes and
+// 4096 tokens: 202 us, 5.4 TB/s; alone 181).  4 bits, 32 requests of 64 nodes and 1K-8K tokens: 526 us (488), 3300 cycles a tile:
+// its keys wait for the product before (their second operand has one buffer), and issue slots are 63 % full.  One request of
+// 8 nodes and 1000 tokens: 17 us, of which 3.7 find the part, 1.3 bring the queries, 3 are the tile, 1.2 its rows, and the
+// rest the two launches.
+// Not kept (short runs): a third softmax group (bf16 471 us for 437: registers), products of 128 tokens (one MMA warp waits for
+// the other's operands), the next scores read between a step's exponentials (468 for 434), part of the exponentials as
+// polynomials (all of them left out saves 10 %).
 //
 // One CTA per SM.  For each row tile (first 128 rows of every request, second 128, ..) the tiles of all its units, request after
 // request and head after head, form a line.  Lines get CTAs by their lengths and are cut into equal parts, one per CTA,
@@ -1340,7 +1342,8 @@ __device__ __forceinline__ void widen_values(const uint8_t* code_tile, uint8_t* 
 }
 
 // Eight warps widen a block of keys each, four two blocks of values.  (A tile's second operand of keys has one buffer: the next tile's wait
-// for this one's product, by halves.  With four warps for keys and whole tiles 64 requests of 8 nodes took 224 us, 32 of 64 nodes 568.)
+// for this one's product, by halves.  When the second operand was f16, short runs: 64 requests of 8 nodes 180 us, 32 of 64 nodes 461, with
+// four warps for keys and whole tiles 224 and 568.)
 template <int D, int P>
 __device__ __forceinline__ void widen_role(Smem<D, true>& sm, const TreeArgs& a, Walk w, int warp, int lane)
 {

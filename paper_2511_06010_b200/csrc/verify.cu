@@ -9,9 +9,9 @@
 // 100K terms in 32 bits would move that border over many tokens.  Every CTA adds the same numbers in the same
 // order, so that all decide alike, and the results do not change from run to run.
 //
-// What bounds it: chains of dependent passes.  64 requests of 16 nodes and 128256 tokens with draft probabilities: 50 us (memory
+// What bounds it: chains of dependent passes.  64 requests of 16 nodes and 128256 tokens with draft probabilities: 54 us (memory
 // traffic of 66 MB alone 10 us), as long as the request with the most failed tests takes, each 3 to 4 us: four rounds of
-// loads and a barrier of the cluster.  200 requests of 5-25 nodes and 50257 tokens without: 23 us, one of 6 nodes and 32000: 9 us.
+// loads and a barrier of the cluster.  200 requests of 5-25 nodes and 50257 tokens without: 23 us, one of 6 nodes and 32000: 8 us.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 
